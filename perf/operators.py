@@ -133,10 +133,12 @@ def _draw_attention(rng):
         if kind == "step":
             Sq, Sk, causal, lengths = rng.choice([1, 1, 1, 2, 5]), _log_int(rng, 1, 32768), True, True
         else:
-            Sq = _log_int(rng, 1, 3136 if kind == "train" else 12544)
-            Sk = Sq if rng.random() < 0.7 else _log_int(rng, 1, 3136 if kind == "train" else 12544)
+            # (a query that sees one key alone has no gradient: what is trained on has some)
+            lo, hi = (8, 3136) if kind == "train" else (1, 12544)
+            Sq = _log_int(rng, lo, hi)
+            Sk = Sq if rng.random() < 0.7 else _log_int(rng, lo, hi)
             if rng.random() < 0.3:
-                padded, lengths, causal, side = True, False, False, _log_int(rng, 2, 56)
+                padded, lengths, causal, side = True, False, False, _log_int(rng, 3, 56)
                 Sq = Sk = side * side
             fused = Sq == Sk and rng.random() < 0.4
         case = _attention(None, B, Sq, Sk, H, Hkv, D, Dv, dtype, kind == "train", causal, lengths, padded, side, fused)
