@@ -539,3 +539,16 @@ def sconv_tune(x, w, stride=1, pad=0, groups=1, pool=None, relu=False, out=None,
     if rc:
         raise SconvError(rc, "sconv_tune")
     return float(ms.value), sconv_plan_name(desc, pooled)
+
+
+_TOKEN_NAMES = frozenset((
+    "sconv_layernorm_forward", "sconv_layernorm_backward", "sconv_rotary_axes", "sconv_rotary_forward",
+    "sconv_rotary_backward", "sconv_diffattn_forward", "sconv_diffattn_backward", "sconv_diffattn_workspace_size"))
+
+
+def __getattr__(name):
+    """The token operators (tokens.py), loaded with torch by the first program that names one."""
+    if name in _TOKEN_NAMES:
+        from . import tokens
+        return globals().setdefault(name, getattr(tokens, name))
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -1,0 +1,455 @@
+// Differential attention, backward (formulas in sconv_tokens.h, product layout in sconv_diffattn_common.h).
+//
+// The weights are formed again from the saved sums (lse), so nothing of Sq x Sk is ever stored.  The two maps share
+// G = dout V^T, and dv needs one product with A_1 - lam A_2.  Three kernels:
+//   delta   d_1, d_2 of every row, from the saved results.
+//   rows    dq: a wavefront keeps 32 queries and walks the keys, as the forward kernel does; also sum_j A_2 G of every row, from
+//           unrounded weights, for lam's gradient (d_2 itself stems from results that were rounded).
+//   keys    dk, dv: a wavefront keeps 32 keys and walks the queries of every head that shares them, so the sum over heads
+//           and queries has one order and needs no atomics.
+// Weights and dS are rounded to the operands' type for their products; all sums are in 32 bits.
+#include <math.h>
+
+#include <algorithm>
+
+#include "sconv_diffattn_common.h"
+
+namespace sconv {
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896340736f;
+
+// delta[0] = dout . (out + lam second), delta[1] = dout . second; 16 lanes a row.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void attn_delta(AttnArgs a)
+{
+    const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16, all = (int64_t)a.B * a.Sq * a.H;
+    const int lane = threadIdx.x % 16;
+    if (row >= all) return;                            // (whole groups of 16 lanes)
+    const int64_t bi = row / a.H;
+    const int head = (int)(row - bi * a.H), b = (int)(bi / a.Sq), i = (int)(bi - (int64_t)b * a.Sq);
+    const T* g = (const T*)a.dout + row * a.Dv;
+    const T* o = (const T*)a.out_in + row * a.Dv;
+    const T* s = (const T*)a.second_in + row * a.Dv;
+    float first = 0.0f, second = 0.0f;
+    for (int d = lane * V; d < a.Dv; d += 16 * V) {
+        float x[V], y[V], z[V];
+        load_vec<V>(g + d, x);
+        load_vec<V>(o + d, y);
+        load_vec<V>(s + d, z);
+#pragma unroll
+        for (int e = 0; e < V; ++e) { first = fmaf(x[e], y[e], first); second = fmaf(x[e], z[e], second); }
+    }
+    first = lanes_sum<16>(first);
+    second = lanes_sum<16>(second);
+    if (lane == 0) {
+        const int64_t at = ((int64_t)b * a.H + head) * a.Sq + i, half = (int64_t)a.B * a.H * a.Sq;
+        const bool none = a.lse_in[at] == -INFINITY;   // (such a row's dout may be anything)
+        a.delta[at] = none ? 0.0f : fmaf(a.lam[head], second, first);
+        a.delta[half + at] = none ? 0.0f : second;
+    }
+}
+
+// dlam[h] = -sum over requests and queries, in one order.
+__global__ __launch_bounds__(256) void attn_dlam(const float* part, int B, int H, int Sq, float* dlam)
+{
+    __shared__ float t[4];
+    const int h = blockIdx.x;
+    float v = 0.0f;
+    for (int b = 0; b < B; ++b)
+        for (int i = threadIdx.x; i < Sq; i += 256) v += part[((int64_t)b * H + h) * Sq + i];
+    v = lanes_sum<64>(v);
+    if ((threadIdx.x & 63) == 0) t[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x == 0) dlam[h] = 0.0f - ((t[0] + t[1]) + (t[2] + t[3]));
+}
+
+template <typename T, int DT>
+__global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
+{
+    constexpr int NW = 4, TH = 256, BN = 32, DVT = 2 * DT;
+    constexpr int KLD = Tile<T, 2 * DT>::LD, VLD = Tile<T, DVT>::LD, KS = DT / 16, VS = DVT / 16, NT = DT / 32;
+    typedef typename Frag<T>::type frag;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    T* kt = (T*)lds;
+    T* vt = kt + BN * KLD;
+    uint32_t* words = (uint32_t*)(vt + BN * VLD);      // [2]
+
+    const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
+    const int tile = a.row_tiles - 1 - blockIdx.x / bh_all;
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, h = l >> 5;
+    const int mine = tile * 32 * NW + 32 * w + (l & 31), r = min(mine, a.rows - 1), i = r / a.G, g = r - i * a.G;
+    const int head = hk * a.G + g, n = keys_of(a, b);
+    const int64_t stat = ((int64_t)b * a.H + head) * a.Sq + i, half = (int64_t)a.B * a.H * a.Sq;
+    const float lse0 = a.lse_in[stat] * LOG2E, lse1 = a.lse_in[half + stat] * LOG2E;
+    const float d0 = a.delta[stat], d1 = a.delta[half + stat], lam = a.lam[head];
+    const bool none = lse0 == -INFINITY;
+    const int see = limit_of(a, i, n), lim = none ? 0 : see;
+    // (limits of the rows rise; a row that the mask leaves empty only makes its wavefront test every key)
+    const int wmin = __any(none) ? 0 : __builtin_amdgcn_readfirstlane(see), wmax = __builtin_amdgcn_readlane(see, 31);
+    const int k1 = limit_of(a, min(tile * 32 * NW + 32 * NW - 1, a.rows - 1) / a.G, n);
+    const uint8_t* mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+
+    frag qf[2][KS], gf[VS];
+    const T* q = (const T*)a.q + b * a.q_b + i * a.q_s + (int64_t)head * 2 * a.q_h;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[m][s] = global_frag(q + m * a.q_h, 16 * s + 8 * h, a.D, a.vec);
+    const T* go = (const T*)a.dout + (((int64_t)b * a.Sq + i) * a.H + head) * a.Dv;
+#pragma unroll
+    for (int s = 0; s < VS; ++s) gf[s] = global_frag(go, 16 * s + 8 * h, a.Dv, a.vec);
+
+    f32x16 acc[2][NT];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[m][t][e] = 0.0f;
+    float spread = 0.0f;                               // sum_j A_2 G
+
+    const T* kb = (const T*)a.k + b * a.k_b + (int64_t)hk * 2 * a.k_h;
+    const T* vb = (const T*)a.v + b * a.v_b + (int64_t)hk * a.v_h;
+    Stage<T, BN, 2, DT, TH> ks;
+    Stage<T, BN, 1, DVT, TH> vs;
+    uint8_t seen = 1;
+    const auto fetch = [&](int j0) {
+        ks.load(kb, a.k_s, a.k_h, j0, n, a.D, a.vec);
+        vs.load(vb, a.v_s, 0, j0, n, a.Dv, a.vec);
+        if (mask && threadIdx.x < BN) seen = mask[min(j0 + (int)threadIdx.x, n - 1)];
+    };
+    if (k1 > 0) fetch(0);
+    const int kcol = col_lane<T, KLD>();
+    int turn = 0;
+    for (int j0 = 0; j0 < k1; j0 += BN, turn ^= 1) {
+        const bool whole = !mask && j0 + BN <= n;
+        uint32_t* wd = words + turn;
+        if (!whole && threadIdx.x < BN) {
+            const uint64_t there = __ballot(j0 + (int)threadIdx.x < n && seen);
+            if (l == 0) wd[0] = (uint32_t)there;
+        }
+        __syncthreads();
+        ks.store(kt, whole ? nullptr : wd, a.D);
+        vs.store(vt, whole ? nullptr : wd, a.Dv);
+        __syncthreads();
+        if (j0 + BN < k1) fetch(j0 + BN);
+        if (j0 >= wmax) continue;
+        f32x16 s0, s1, gt;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s0[e] = s1[e] = gt[e] = 0.0f;
+        const T* krow = kt + (l & 31) * KLD + 8 * h;
+        const T* vrow = vt + (l & 31) * VLD + 8 * h;
+#pragma unroll
+        for (int t = 0; t < KS; ++t) s0 = mma(s0, row_frag(krow + 16 * t), qf[0][t]);
+#pragma unroll
+        for (int t = 0; t < KS; ++t) s1 = mma(s1, row_frag(krow + DT + 16 * t), qf[1][t]);
+#pragma unroll
+        for (int t = 0; t < VS; ++t) gt = mma(gt, row_frag(vrow + 16 * t), gf[t]);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s0[e] = __builtin_amdgcn_exp2f(fmaf(s0[e], a.scale2, -lse0));
+            s1[e] = __builtin_amdgcn_exp2f(fmaf(s1[e], a.scale2, -lse1));
+        }
+        const uint32_t word = whole ? ~0u : wd[0];
+        if (j0 + 32 > wmin || (mask && word != ~0u)) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int j = 8 * (e >> 2) + 4 * h + (e & 3);
+                const bool ok = j0 + j < lim && (word >> j & 1);
+                s0[e] = ok ? s0[e] : 0.0f;
+                s1[e] = ok ? s1[e] : 0.0f;
+                gt[e] = ok ? gt[e] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            spread = fmaf(s1[e], gt[e], spread);
+            s0[e] *= gt[e] - d0;
+            s1[e] *= -lam * (gt[e] - d1);
+        }
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            frag f0, f1;
+            to_frag(s0, st, f0);
+            to_frag(s1, st, f1);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                acc[0][t] = mma(acc[0][t], col_frag<KLD>(kt + kcol + 16 * st * KLD + 32 * t), f0);
+                acc[1][t] = mma(acc[1][t], col_frag<KLD>(kt + kcol + 16 * st * KLD + DT + 32 * t), f1);
+            }
+        }
+    }
+    spread = half_sum(spread);
+    if (mine >= a.rows) return;
+    if (h == 0) a.dlam_part[stat] = spread;
+    T* dq = (T*)a.dq + (((int64_t)b * a.Sq + i) * a.H + head) * 2 * a.D;
+    const bool v4 = a.ovec && a.D % 4 == 0;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                float x[4];
+#pragma unroll
+                for (int z = 0; z < 4; ++z) x[z] = acc[m][t][e + z] * a.scale;
+                store4(dq + m * a.D, 32 * t + 8 * (e >> 2) + 4 * h, a.D, v4, x);
+            }
+}
+
+// WHAT: 1: dv, 2: dk of the first map, 4: of the second (all three where their sums fit the registers).
+template <typename T, int DT, int WHAT>
+__global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
+{
+    constexpr int NW = 4, TH = 256, BM = 32, DVT = 2 * DT;
+    constexpr int QLD = Tile<T, 2 * DT>::LD, GLD = Tile<T, DVT>::LD, KS = DT / 16, VS = DVT / 16, NT = DT / 32, VT = DVT / 32;
+    constexpr bool DV = WHAT & 1, DK0 = WHAT & 2, DK1 = WHAT & 4, MAP0 = DV || DK0, MAP1 = DV || DK1, NEED_G = DK0 || DK1;
+    typedef typename Frag<T>::type frag;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    T* qt = (T*)lds;
+    T* gt = qt + BM * QLD;
+    float* stats = (float*)(gt + BM * GLD);            // [2][4][32]: lse of both maps (log2), d of both
+    uint32_t* words = (uint32_t*)(stats + 256);        // [2]
+
+    const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
+    const int j0 = (int)(blockIdx.x / bh_all) * 32 * NW;
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, h = l >> 5;
+    const int n = keys_of(a, b), j = j0 + 32 * w + (l & 31), in = min(j, a.Sk - 1);
+    const bool ok = j < n && (!a.mask || a.mask[b * a.mask_b + in]);
+    const bool all_ok = __all(ok);
+    // the first query that sees a key, of this lane's key, the wavefront's and the workgroup's first one; the wavefront's last
+    const int64_t off = (int64_t)a.Sq - n;
+    const int seen_by = a.causal ? (int)std::max<int64_t>(0, j + off) : 0;
+    const int wfirst = __builtin_amdgcn_readfirstlane(seen_by), wlast = __builtin_amdgcn_readlane(seen_by, 31);
+    const int start = a.causal ? (int)std::max<int64_t>(0, j0 + off) / BM * BM : 0;
+
+    frag kf[2][KS], vf[VS];
+    const T* k = (const T*)a.k + b * a.k_b + in * a.k_s + (int64_t)hk * 2 * a.k_h;
+    const T* v = (const T*)a.v + b * a.v_b + in * a.v_s + (int64_t)hk * a.v_h;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        if (MAP0) kf[0][s] = global_frag(k, 16 * s + 8 * h, a.D, a.vec);
+        if (MAP1) kf[1][s] = global_frag(k + a.k_h, 16 * s + 8 * h, a.D, a.vec);
+    }
+    if (NEED_G)
+#pragma unroll
+        for (int s = 0; s < VS; ++s) vf[s] = global_frag(v, 16 * s + 8 * h, a.Dv, a.vec);
+
+    f32x16 dk[2][NT], dv[VT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dk[0][t][e] = dk[1][t][e] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dv[t][e] = 0.0f;
+
+    Stage<T, BM, 2, DT, TH> qs;
+    Stage<T, BM, 1, DVT, TH> gs;
+    float stat = 0.0f, sum = 0.0f;
+    const int64_t half = (int64_t)a.B * a.H * a.Sq;
+    const auto fetch = [&](int g, int i0) {
+        const int head = hk * a.G + g;
+        qs.load((const T*)a.q + b * a.q_b + (int64_t)head * 2 * a.q_h, a.q_s, a.q_h, i0, a.Sq, a.D, a.vec);
+        gs.load((const T*)a.dout + ((int64_t)b * a.Sq * a.H + head) * a.Dv, (int64_t)a.H * a.Dv, 0, i0, a.Sq, a.Dv, a.vec);
+        if (threadIdx.x < 128) {                       // thread: statistic x row
+            const int i = min(i0 + (int)(threadIdx.x & 31), a.Sq - 1), what = threadIdx.x >> 5;
+            const int64_t at = ((int64_t)b * a.H + head) * a.Sq + i;
+            sum = a.lse_in[at];
+            stat = what == 0 ? sum * LOG2E : what == 1 ? a.lse_in[half + at] * LOG2E : a.delta[at + (what == 3 ? half : 0)];
+        }
+    };
+    const bool any = j0 < n && start < a.Sq;
+    if (any) fetch(0, start);
+    const int qcol = col_lane<T, QLD>(), gcol = col_lane<T, GLD>();
+    int turn = 0;
+    for (int g = 0, i0 = start; any && g < a.G; turn ^= 1) {
+        float* st = stats + 128 * turn;
+        if (threadIdx.x < 128) {
+            // a row that is not there, or sees nothing, is cleared: its weights, all 1 then, meet zeros
+            const bool there = i0 + (int)(threadIdx.x & 31) < a.Sq && sum != -INFINITY;
+            st[threadIdx.x] = there ? stat : 0.0f;
+            const uint64_t bits = __ballot(there);
+            if (threadIdx.x == 0) words[turn] = (uint32_t)bits;
+        }
+        __syncthreads();
+        qs.store(qt, words + turn, a.D);
+        gs.store(gt, words + turn, a.Dv);
+        __syncthreads();
+        const int at = i0;
+        const float lam = a.lam[hk * a.G + g];
+        i0 += BM;
+        if (i0 >= a.Sq) { i0 = start; ++g; }
+        if (g < a.G) fetch(g, i0);
+        if (at + BM <= wfirst || j0 + 32 * w >= n) continue;
+        f32x16 s0, s1, gg;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s0[e] = s1[e] = gg[e] = 0.0f;
+        const T* qrow = qt + (l & 31) * QLD + 8 * h;
+        const T* grow = gt + (l & 31) * GLD + 8 * h;
+        if (MAP0)
+#pragma unroll
+            for (int t = 0; t < KS; ++t) s0 = mma(s0, row_frag(qrow + 16 * t), kf[0][t]);
+        if (MAP1)
+#pragma unroll
+            for (int t = 0; t < KS; ++t) s1 = mma(s1, row_frag(qrow + DT + 16 * t), kf[1][t]);
+        if (NEED_G)
+#pragma unroll
+            for (int t = 0; t < VS; ++t) gg = mma(gg, row_frag(grow + 16 * t), vf[t]);
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const f32x4 l0 = *(const f32x4*)(st + 2 * e + 4 * h), l1 = *(const f32x4*)(st + 32 + 2 * e + 4 * h);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                if (MAP0) s0[e + z] = __builtin_amdgcn_exp2f(fmaf(s0[e + z], a.scale2, -l0[z]));
+                if (MAP1) s1[e + z] = __builtin_amdgcn_exp2f(fmaf(s1[e + z], a.scale2, -l1[z]));
+            }
+        }
+        if (!all_ok || at < wlast) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const bool in_sum = ok && at + 8 * (e >> 2) + 4 * h + (e & 3) >= seen_by;
+                s0[e] = in_sum ? s0[e] : 0.0f;
+                s1[e] = in_sum ? s1[e] : 0.0f;
+                gg[e] = in_sum ? gg[e] : 0.0f;
+            }
+        }
+        if (DV) {
+            f32x16 p;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[e] = fmaf(-lam, s1[e], s0[e]);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                frag f;
+                to_frag(p, x, f);
+#pragma unroll
+                for (int t = 0; t < VT; ++t) dv[t] = mma(dv[t], col_frag<GLD>(gt + gcol + 16 * x * GLD + 32 * t), f);
+            }
+        }
+        if (NEED_G) {
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const f32x4 d0 = *(const f32x4*)(st + 64 + 2 * e + 4 * h), d1 = *(const f32x4*)(st + 96 + 2 * e + 4 * h);
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    s0[e + z] *= gg[e + z] - d0[z];
+                    s1[e + z] *= -lam * (gg[e + z] - d1[z]);
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                frag f0, f1;
+                to_frag(s0, x, f0);
+                to_frag(s1, x, f1);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    if (DK0) dk[0][t] = mma(dk[0][t], col_frag<QLD>(qt + qcol + 16 * x * QLD + 32 * t), f0);
+                    if (DK1) dk[1][t] = mma(dk[1][t], col_frag<QLD>(qt + qcol + 16 * x * QLD + DT + 32 * t), f1);
+                }
+            }
+        }
+    }
+    if (j >= a.Sk) return;
+    T* kout = (T*)a.dk + (((int64_t)b * a.Sk + j) * a.Hkv + hk) * 2 * a.D;
+    T* vout = (T*)a.dv + (((int64_t)b * a.Sk + j) * a.Hkv + hk) * a.Dv;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        if (!(m ? DK1 : DK0)) continue;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                float x[4];
+#pragma unroll
+                for (int z = 0; z < 4; ++z) x[z] = dk[m][t][e + z] * a.scale;
+                store4(kout + m * a.D, 32 * t + 8 * (e >> 2) + 4 * h, a.D, a.ovec && a.D % 4 == 0, x);
+            }
+    }
+    if (DV)
+#pragma unroll
+        for (int t = 0; t < VT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const float x[4] = {dv[t][e], dv[t][e + 1], dv[t][e + 2], dv[t][e + 3]};
+                store4(vout, 32 * t + 8 * (e >> 2) + 4 * h, a.Dv, a.ovec && a.Dv % 4 == 0, x);
+            }
+}
+
+template <typename T, int DT, int WHAT>
+int keys_launch(const AttnArgs& a, hipStream_t stream)
+{
+    constexpr size_t lds = 32 * (Tile<T, 2 * DT>::LD + Tile<T, 2 * DT>::LD) * sizeof(T) + 256 * 4 + 8;
+    const int rc = allow_lds(attn_bwd_keys<T, DT, WHAT>, lds);
+    if (rc) return rc;
+    const int64_t grid = (int64_t)((a.Sk + 127) / 128) * a.B * a.Hkv;
+    hipLaunchKernelGGL((attn_bwd_keys<T, DT, WHAT>), dim3((unsigned)grid), dim3(256), lds, stream, a);
+    return launch_status();
+}
+
+template <typename T, int DT>
+int bwd_main(const AttnArgs& a, hipStream_t stream)
+{
+    int rc = SCONV_OK;
+    if (a.Sk > 0) {
+        if constexpr (DT <= 64) rc = keys_launch<T, DT, 7>(a, stream);
+        else {
+            // (the three sums of 128 columns and their operands do not fit a lane's registers together)
+            rc = keys_launch<T, DT, 1>(a, stream);
+            if (!rc) rc = keys_launch<T, DT, 2>(a, stream);
+            if (!rc) rc = keys_launch<T, DT, 4>(a, stream);
+        }
+        if (rc) return rc;
+    }
+    if (a.Sq == 0) return rc;
+    constexpr size_t lds = 32 * (Tile<T, 2 * DT>::LD + Tile<T, 2 * DT>::LD) * sizeof(T) + 8;
+    rc = allow_lds(attn_bwd_rows<T, DT>, lds);
+    if (rc) return rc;
+    hipLaunchKernelGGL((attn_bwd_rows<T, DT>), dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv)), dim3(256), lds, stream, a);
+    return launch_status();
+}
+
+template <typename T>
+int bwd_run(const AttnArgs& a, float* dlam, hipStream_t stream)
+{
+    int rc;
+    if (a.Sq > 0) {
+        const dim3 grid((unsigned)(((int64_t)a.B * a.Sq * a.H + 15) / 16));
+        if (a.Dv % 4 == 0 && aligned_to(a.dout, 16) && aligned_to(a.out_in, 16) && aligned_to(a.second_in, 16)) hipLaunchKernelGGL((attn_delta<T, 4>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((attn_delta<T, 1>), grid, dim3(256), 0, stream, a);
+        rc = launch_status();
+        if (rc) return rc;
+    }
+    const int most = std::max(a.D, (a.Dv + 1) / 2);
+    if (most <= 32) rc = bwd_main<T, 32>(a, stream);
+    else if (most <= 64) rc = bwd_main<T, 64>(a, stream);
+    else rc = bwd_main<T, 128>(a, stream);
+    if (rc) return rc;
+    hipLaunchKernelGGL(attn_dlam, dim3((unsigned)a.H), dim3(256), 0, stream, a.dlam_part, a.B, a.H, a.Sq, dlam);
+    return launch_status();
+}
+
+}  // namespace
+
+size_t diffattn_backward_workspace(const sconv_diffattn_desc_t& d) { return (size_t)d.B * d.H * d.Sq * 3 * sizeof(float); }
+
+int launch_diffattn_backward(const sconv_diffattn_desc_t& d, const void* dout, const void* q, const void* k, const void* v,
+                             const float* lam, const int32_t* lengths, const uint8_t* mask, const void* out,
+                             const void* second, const float* lse, void* dq, void* dk, void* dv, float* dlam, void* ws,
+                             hipStream_t stream)
+{
+    AttnArgs a = attn_args(d, q, k, v, lam, lengths, mask);
+    a.vec = a.vec && aligned_to(dout, 16);
+    a.dout = dout; a.out_in = out; a.second_in = second; a.lse_in = lse;
+    a.dq = dq; a.dk = dk; a.dv = dv;
+    a.ovec = aligned_to(dq, 16) && aligned_to(dk, 16) && aligned_to(dv, 16);
+    a.delta = (float*)ws;
+    a.dlam_part = a.delta + 2 * (int64_t)d.B * d.H * d.Sq;
+    a.row_tiles = (a.rows + 127) / 128;
+    if (d.B == 0) a.Sq = a.Sk = 0;                     // nothing but lam's gradient to clear
+    return d.type == SCONV_BF16 ? bwd_run<bf16>(a, dlam, stream) : bwd_run<float>(a, dlam, stream);
+}
+
+}  // namespace sconv

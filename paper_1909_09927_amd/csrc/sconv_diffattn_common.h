@@ -1,0 +1,209 @@
+// Differential attention: what its kernels share.
+//
+// Layout of the matrix products.  A 32 x 32 product tile takes from each lane 8 elements of a row of A (row l % 32) and 8 of a
+// column of B (column l % 32), both at depths 8 (l / 32) .. + 7 of a 16-deep step (16-bit: one instruction; 32-bit: eight
+// of depth 2, element by element - the depths they pair differ, the sum of products is the same).  Of the result each lane
+// holds column l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4 in registers r = 0..15.
+// So a result can be the next product's B as it stands in its lane: registers 8s..8s+7 are the depths
+//   16 s + 4 (l / 32) + {0, 1, 2, 3, 8, 9, 10, 11}
+// of step s, provided that A's elements come in that order (col_frag below).  Scores are therefore formed transposed - keys down,
+// queries across -: a query's softmax runs inside a lane and its partner, and the weights never leave the registers.
+#pragma once
+
+#include "sconv_tokens_common.h"
+
+namespace sconv {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+struct AttnArgs {
+    const void* q; const void* k; const void* v; const float* lam; const int32_t* len; const uint8_t* mask;
+    void* out; void* second; float* lse;                     // forward: written
+    const void* dout; const void* out_in; const void* second_in; const float* lse_in;   // backward
+    void* dq; void* dk; void* dv;
+    float* part; float* part_ml;                             // forward over several splits: [split][B Hkv][rows]..
+    float* delta; float* dlam_part;                          // backward: [2][B][H][Sq], [B][H][Sq]
+    int B, Sq, Sk, H, Hkv, G, D, Dv, causal, rows;           // rows = Sq * G: of one request and key head, r = i * G + g
+    int splits, split_keys, row_tiles;
+    int vec, ovec;                                           // inputs can be read, outputs written 16 bytes at a time
+    float scale, scale2;                                     // scale2 = scale * log2(e)
+    int64_t q_b, q_s, q_h, k_b, k_s, k_h, v_b, v_s, v_h, mask_b;
+};
+
+template <typename T> struct Frag;
+template <> struct Frag<bf16> { typedef bf16x8 type; };
+template <> struct Frag<float> { typedef f32x8 type; };
+
+__device__ __forceinline__ f32x16 mma(f32x16 c, bf16x8 a, bf16x8 b) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma(f32x16 c, f32x8 a, f32x8 b)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+
+// A tile in LDS: rows of W elements and 16 bytes of padding, so that lanes reading one column chunk of consecutive
+// rows meet different banks.
+template <typename T, int W> struct Tile { static constexpr int E = 16 / sizeof(T), LD = W + E; };
+
+// 8 consecutive elements from an address aligned to 16 bytes.
+__device__ __forceinline__ bf16x8 row_frag(const bf16* p) { return *(const bf16x8*)p; }
+__device__ __forceinline__ f32x8 row_frag(const float* p)
+{
+    const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+    return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+
+// The transposed tile's row fragment: column l % 32 of 32, depths (rows) 4 (l / 32) + {0..3, 8..11}.  p: the tile at its first row
+// and column, plus col_lane().
+template <int LD>
+__device__ __forceinline__ bf16x8 col_frag(const bf16* p)
+{
+    typedef __attribute__((address_space(3))) s16x4 lds4;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 8 * LD));
+    union { s16x4 s[2]; bf16x8 v; } u;
+    u.s[0] = a; u.s[1] = b;
+    return u.v;
+}
+template <int LD>
+__device__ __forceinline__ f32x8 col_frag(const float* p)
+{
+    f32x8 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[i] = p[i * LD]; v[4 + i] = p[(8 + i) * LD]; }
+    return v;
+}
+// Where a lane reads (16 lanes of the transposing read take four rows of 16 columns; lane i has row i / 4, four columns).
+template <typename T, int LD>
+__device__ __forceinline__ int col_lane()
+{
+    const int l = threadIdx.x & 63, h = l >> 5;
+    if constexpr (sizeof(T) == 2) return (4 * h + ((l & 15) >> 2)) * LD + ((l >> 4) & 1) * 16 + (l & 3) * 4;
+    else return 4 * h * LD + (l & 31);
+}
+
+// Registers 8s..8s+7 of a result as the next product's B.
+__device__ __forceinline__ void to_frag(const f32x16& p, int s, bf16x8& f)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = (bf16)p[8 * s + i];
+}
+__device__ __forceinline__ void to_frag(const f32x16& p, int s, f32x8& f)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = p[8 * s + i];
+}
+
+// 16 bytes of elements d.. of a row that has `have` of them.  vec: d and the row are aligned and `have` is whole 16 bytes;
+// where d lies beyond, an address inside is read and the result is to be cleared.
+template <typename T>
+__device__ __forceinline__ u32x4 load16(const T* row, int d, int have, bool vec)
+{
+    constexpr int E = 16 / sizeof(T);
+    if (vec) return *(const u32x4*)(row + (d < have ? d : 0));
+    union { u32x4 u; T e[E]; } r;
+#pragma unroll
+    for (int i = 0; i < E; ++i) r.e[i] = row[d + i < have ? d + i : 0];
+#pragma unroll
+    for (int i = 0; i < E; ++i) if (d + i >= have) r.e[i] = (T)0.0f;
+    return r.u;
+}
+// (the fragment of a row that is read from memory, cleared beyond `have`)
+__device__ __forceinline__ bf16x8 global_frag(const bf16* row, int d, int have, bool vec)
+{
+    union { u32x4 u; bf16x8 v; } r;
+    r.u = load16(row, d, have, vec);
+    if (d >= have) r.u = u32x4{0, 0, 0, 0};
+    return r.v;
+}
+__device__ __forceinline__ f32x8 global_frag(const float* row, int d, int have, bool vec)
+{
+    union { u32x4 u[2]; f32x8 v; } r;
+    r.u[0] = load16(row, d, have, vec);
+    r.u[1] = load16(row, d + 4, have, vec);
+    if (d >= have) r.u[0] = u32x4{0, 0, 0, 0};
+    if (d + 4 >= have) r.u[1] = u32x4{0, 0, 0, 0};
+    return r.v;
+}
+
+// Four neighbouring results of a row (columns d..d+3 of `have`).
+template <typename T>
+__device__ __forceinline__ void store4(T* row, int d, int have, bool vec, const float* v)
+{
+    if (vec) {
+        if (d < have) store_vec<4>(row + d, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (d + i < have) row[d + i] = (T)v[i];
+    }
+}
+
+// The other half of the wavefront's value (lane l +- 32).
+__device__ __forceinline__ float half_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Keys of request b that exist.
+__device__ __forceinline__ int keys_of(const AttnArgs& a, int b) { return a.len ? min(max(a.len[b], 0), a.Sk) : a.Sk; }
+// How many of its n keys query i sees, the mask aside.
+__device__ __forceinline__ int limit_of(const AttnArgs& a, int i, int n)
+{
+    if (!a.causal) return n;
+    const int64_t lim = (int64_t)i + n - a.Sq + 1;
+    return (int)(lim < 0 ? 0 : lim > n ? n : lim);
+}
+
+// ROWS rows of a tile on their way from memory to LDS, through registers, so that the loads of one tile run under the products of
+// the one before.  A row has PARTS rows of W elements of memory beside each other (the two keys of a head).
+template <typename T, int ROWS, int PARTS, int W, int THREADS>
+struct Stage {
+    static constexpr int E = 16 / sizeof(T), PER = PARTS * W / E, N = ROWS * PER / THREADS, LD = Tile<T, PARTS * W>::LD;
+    static_assert(N * THREADS == ROWS * PER, "whole vectors for every thread");
+    u32x4 r[N];
+
+    // row j of the tile: base + (j0 + j) * stride, its part m at + m * part; rows from `rows` on are not there (one that is, is
+    // read instead, and cleared by store).
+    __device__ __forceinline__ void load(const T* base, int64_t stride, int64_t part, int j0, int rows, int have, bool vec)
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int e = n * THREADS + threadIdx.x, row = e / PER, c = e % PER, m = c / (W / E), d = (c % (W / E)) * E;
+            r[n] = load16(base + (int64_t)min(j0 + row, rows - 1) * stride + m * part, d, have, vec);
+        }
+    }
+    // words: a bit for every row that is there (LDS), null: all are
+    __device__ __forceinline__ void store(T* tile, const uint32_t* words, int have) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int e = n * THREADS + threadIdx.x, row = e / PER, c = e % PER, d = (c % (W / E)) * E;
+            const bool there = d < have && (!words || (words[row >> 5] >> (row & 31) & 1));
+            *(u32x4*)(tile + row * LD + c * E) = there ? r[n] : u32x4{0, 0, 0, 0};
+        }
+    }
+};
+
+// The arguments both directions share.
+AttnArgs attn_args(const sconv_diffattn_desc_t& d, const void* q, const void* k, const void* v, const float* lam,
+                   const int32_t* lengths, const uint8_t* mask);
+
+// Sets the dynamic LDS size a kernel may ask for, where it is above the default.
+template <typename K>
+inline int allow_lds(K kern, size_t bytes)
+{
+    if (bytes <= 64 * 1024) return SCONV_OK;
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess
+               ? SCONV_OK : SCONV_ELAUNCH;
+}
+
+}  // namespace sconv
