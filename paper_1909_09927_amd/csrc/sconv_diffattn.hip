@@ -48,28 +48,27 @@ __device__ __forceinline__ void soften(f32x16& s, float scale2, float& top, floa
     l += sum;
 }
 
-template <typename T, int DT, int DVT, int NW, int BN>
-constexpr size_t fwd_lds()
-{
-    return (size_t)BN * (Tile<T, 2 * DT>::LD + Tile<T, DVT>::LD) * sizeof(T) + 2 * (BN / 32) * 4;
-}
 
 template <typename T, int DT, int DVT, int NW, bool FEW>
 struct FwdShape {
-    static constexpr int BN = FEW ? 32 * NW : (sizeof(T) == 2 ? 64 : 32);
+    static constexpr int BN = FEW ? 32 * NW : 32;
     static constexpr int ROWS = FEW ? 32 : 32 * NW;
+    static constexpr int BUFS = FEW ? 1 : 2;           // a wide workgroup writes one tile while it reads the other
+    static constexpr int WAVES = !FEW && sizeof(T) == 2 && DT <= 64 ? 2 : 1;
+    static constexpr int TILE = BN * (Tile<T, 2 * DT>::LD + Tile<T, DVT>::LD);
+    static constexpr size_t LDS = (size_t)BUFS * TILE * sizeof(T) + 3 * (BN / 32) * 4;
 };
 
-template <typename T, int DT, int DVT, int NW, bool FEW>
-__global__ __launch_bounds__(64 * NW) void attn_fwd(AttnArgs a)
+template <typename T, bool VEC, int DT, int DVT, int NW, bool FEW>
+__global__ __launch_bounds__(64 * NW, (FwdShape<T, DT, DVT, NW, FEW>::WAVES)) void attn_fwd(AttnArgs a)
 {
-    constexpr int BN = FwdShape<T, DT, DVT, NW, FEW>::BN, ROWS = FwdShape<T, DT, DVT, NW, FEW>::ROWS;
+    typedef FwdShape<T, DT, DVT, NW, FEW> Shape;
+    constexpr int BN = Shape::BN, ROWS = Shape::ROWS;
     constexpr int KLD = Tile<T, 2 * DT>::LD, VLD = Tile<T, DVT>::LD, KS = DT / 16, NT = DVT / 32, TH = 64 * NW;
     typedef typename Frag<T>::type frag;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    T* kt = (T*)lds;
-    T* vt = kt + BN * KLD;
-    uint32_t* words = (uint32_t*)(vt + BN * VLD);    // [2][BN / 32]
+    T* tiles = (T*)lds;
+    uint32_t* words = (uint32_t*)(tiles + Shape::BUFS * Shape::TILE);    // [3][BN / 32]: of the tile that is read, the next one and the one after
 
     const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
     const int tile = a.row_tiles - 1 - blockIdx.x / bh_all;      // the rows that see most first
@@ -90,7 +89,7 @@ __global__ __launch_bounds__(64 * NW) void attn_fwd(AttnArgs a)
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int s = 0; s < KS; ++s) qf[m][s] = global_frag(q + m * a.q_h, 16 * s + 8 * h, a.D, a.vec);
+        for (int s = 0; s < KS; ++s) qf[m][s] = global_frag<VEC>(q + m * a.q_h, 16 * s + 8 * h, a.D);
 
     f32x16 o[2][NT];
     float top[2], safe[2], sum[2];
@@ -105,30 +104,58 @@ __global__ __launch_bounds__(64 * NW) void attn_fwd(AttnArgs a)
 
     const T* kb = (const T*)a.k + b * a.k_b + (int64_t)hk * 2 * a.k_h;
     const T* vb = (const T*)a.v + b * a.v_b + (int64_t)hk * a.v_h + dv0;
-    Stage<T, BN, 2, DT, TH> ks;
-    Stage<T, BN, 1, DVT, TH> vs;
+    Stage<T, VEC, BN, 2, DT, TH> ks;
+    Stage<T, VEC, BN, 1, DVT, TH> vs;
     uint8_t seen = 1;
     const auto fetch = [&](int j0) {
-        ks.load(kb, a.k_s, a.k_h, j0, n, a.D, a.vec);
-        vs.load(vb, a.v_s, 0, j0, n, dvn, a.vec);
+        ks.load(kb, a.k_s, a.k_h, j0, n, a.D);
+        vs.load(vb, a.v_s, 0, j0, n, dvn);
         if (mask && threadIdx.x < BN) seen = mask[min(j0 + (int)threadIdx.x, n - 1)];
     };
-    if (k0 < k1) fetch(k0);
-    const int vcol = col_lane<T, VLD>();
-    int turn = 0;
-    for (int j0 = k0; j0 < k1; j0 += BN, turn ^= 1) {
-        const bool whole = !mask && j0 + BN <= n;
-        uint32_t* wd = words + turn * (BN / 32);
-        if (!whole && threadIdx.x < BN) {
+    // A tile on its way into LDS: which of its keys are there (words), then the rows.
+    const auto mark = [&](int j0, int slot) {
+        if ((mask || j0 + BN > n) && threadIdx.x < BN) {
             const uint64_t there = __ballot(j0 + (int)threadIdx.x < n && seen);
+            uint32_t* wd = words + slot * (BN / 32);
             if (l == 0) wd[2 * w] = (uint32_t)there;
             if (l == 32) wd[2 * w + 1] = (uint32_t)(there >> 32);
         }
+    };
+    const auto put = [&](int j0, int turn, int slot) {
+        T* kt = tiles + (Shape::BUFS > 1 ? turn : 0) * Shape::TILE;
+        const uint32_t* wd = mask || j0 + BN > n ? words + slot * (BN / 32) : nullptr;
+        ks.store(kt, wd, a.D);
+        vs.store(kt + BN * KLD, wd, dvn);
+    };
+    const int vcol = col_lane<T, VLD>();
+    const auto after = [](int slot) { return slot == 2 ? 0 : slot + 1; };
+    int turn = 0, slot = 0;
+    if (k0 < k1) {
+        fetch(k0);
+        mark(k0, 0);
+        if (Shape::BUFS > 1) {
+            if (mask || k0 + BN > n) __syncthreads();
+            put(k0, 0, 0);
+            if (k0 + BN < k1) { fetch(k0 + BN); mark(k0 + BN, 1); }
+        }
+    }
+    for (int j0 = k0; j0 < k1; j0 += BN, turn ^= 1, slot = after(slot)) {
+        const bool whole = !mask && j0 + BN <= n;
+        const uint32_t* wd = words + slot * (BN / 32);
         __syncthreads();
-        ks.store(kt, whole ? nullptr : wd, a.D);
-        vs.store(vt, whole ? nullptr : wd, dvn);
-        __syncthreads();
-        if (j0 + BN < k1) fetch(j0 + BN);
+        if (Shape::BUFS > 1) {
+            // (this tile is there; the next one's keys were marked before the barrier)
+            if (j0 + BN < k1) {
+                put(j0 + BN, turn ^ 1, after(slot));
+                if (j0 + 2 * BN < k1) fetch(j0 + 2 * BN);
+            }
+        } else {
+            put(j0, 0, slot);
+            __syncthreads();
+            if (j0 + BN < k1) fetch(j0 + BN);
+        }
+        const T* kt = tiles + (Shape::BUFS > 1 ? turn : 0) * Shape::TILE;
+        const T* vt = kt + BN * KLD;
 #pragma unroll
         for (int sub = 0; sub < (FEW ? 1 : BN / 32); ++sub) {
             const int row0 = FEW ? 32 * w : 32 * sub, js = j0 + row0;
@@ -167,6 +194,9 @@ __global__ __launch_bounds__(64 * NW) void attn_fwd(AttnArgs a)
                 }
             }
         }
+        settle();
+        if (Shape::BUFS > 1) { if (j0 + 2 * BN < k1) mark(j0 + 2 * BN, after(after(slot))); }
+        else if (j0 + BN < k1) mark(j0 + BN, after(slot));
     }
 #pragma unroll
     for (int m = 0; m < 2; ++m) sum[m] = half_sum(sum[m]);
@@ -325,10 +355,11 @@ FwdPlan fwd_plan(const sconv_diffattn_desc_t& d, size_t ws_bytes)
     p.chunks = (d.Dv + DVT - 1) / DVT;
     p.splits = 1;
     p.split_keys = d.Sk > 0 ? d.Sk : 1;
-    // keys are split while workgroups do not fill the chip four times over, at 512 keys a part or more
+    // keys are split, at 512 a part or more, where wide workgroups fill half of the chip at most, and until few ones fill it four
+    // times over (requests' lengths differ, and a workgroup without keys ends at once)
     const int64_t base = p.row_tiles * bh * p.chunks;
     if (base == 0) return p;
-    int64_t splits = std::min<int64_t>((1024 + base - 1) / base, (d.Sk + 511) / 512);
+    int64_t splits = std::min<int64_t>(p.few ? (1024 + base - 1) / base : 512 / base, (d.Sk + 511) / 512);
     const int64_t wide = (d.Dv + 3) / 4 * 4, each = bh * rows * (2 * wide + 4) * (int64_t)sizeof(float);
     splits = std::min<int64_t>(splits, (int64_t)(ws_bytes / (size_t)each));
     if (splits > 1) {
@@ -341,13 +372,12 @@ FwdPlan fwd_plan(const sconv_diffattn_desc_t& d, size_t ws_bytes)
     return p;
 }
 
-template <typename T, int DT, int DVT, int NW, bool FEW>
+template <typename T, bool VEC, int DT, int DVT, int NW, bool FEW>
 int fwd_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
 {
-    constexpr int BN = FwdShape<T, DT, DVT, NW, FEW>::BN;
-    constexpr size_t tiles = fwd_lds<T, DT, DVT, NW, BN>(), join = (size_t)(NW * 128 + NW / 2 * 2 * DVT * 32) * 4;
+    constexpr size_t tiles = FwdShape<T, DT, DVT, NW, FEW>::LDS, join = (size_t)(NW * 128 + NW / 2 * 2 * DVT * 32) * 4;
     constexpr size_t lds = FEW && join > tiles ? join : tiles;
-    const auto kern = attn_fwd<T, DT, DVT, NW, FEW>;
+    const auto kern = attn_fwd<T, VEC, DT, DVT, NW, FEW>;
     const int rc = allow_lds(kern, lds);
     if (rc) return rc;
     hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv), (unsigned)p.splits, (unsigned)p.chunks),
@@ -355,20 +385,20 @@ int fwd_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
     return launch_status();
 }
 
-template <typename T>
+template <typename T, bool VEC>
 int fwd_run(AttnArgs& a, const FwdPlan& p, hipStream_t stream)
 {
     const int DT = dim_tile(a.D);
     int rc;
     if (p.few) {
         // (tiles of 128 wide rows in 32 bits do not fit a workgroup's LDS: two wavefronts of 32 keys)
-        if (DT == 32) rc = fwd_launch<T, 32, 64, 4, true>(a, p, stream);
-        else if (DT == 64) rc = fwd_launch<T, 64, 128, sizeof(T) == 2 ? 4 : 2, true>(a, p, stream);
-        else rc = fwd_launch<T, 128, 128, sizeof(T) == 2 ? 4 : 2, true>(a, p, stream);
+        if (DT == 32) rc = fwd_launch<T, VEC, 32, 64, 4, true>(a, p, stream);
+        else if (DT == 64) rc = fwd_launch<T, VEC, 64, 128, sizeof(T) == 2 ? 4 : 2, true>(a, p, stream);
+        else rc = fwd_launch<T, VEC, 128, 128, sizeof(T) == 2 ? 4 : 2, true>(a, p, stream);
     } else {
-        if (DT == 32) rc = fwd_launch<T, 32, 64, 4, false>(a, p, stream);
-        else if (DT == 64) rc = fwd_launch<T, 64, 128, 4, false>(a, p, stream);
-        else rc = fwd_launch<T, 128, 128, 4, false>(a, p, stream);
+        if (DT == 32) rc = fwd_launch<T, VEC, 32, 64, 4, false>(a, p, stream);
+        else if (DT == 64) rc = fwd_launch<T, VEC, 64, 128, 4, false>(a, p, stream);
+        else rc = fwd_launch<T, VEC, 128, 128, 4, false>(a, p, stream);
     }
     if (rc || p.splits == 1) return rc;
     hipLaunchKernelGGL((attn_join<T>), dim3((unsigned)((int64_t)a.B * a.Hkv * a.rows)), dim3(256), 0, stream, a);
@@ -388,10 +418,13 @@ AttnArgs attn_args(const sconv_diffattn_desc_t& d, const void* q, const void* k,
     a.q_b = d.q_b; a.q_s = d.q_s; a.q_h = d.q_h; a.k_b = d.k_b; a.k_s = d.k_s; a.k_h = d.k_h;
     a.v_b = d.v_b; a.v_s = d.v_s; a.v_h = d.v_h; a.mask_b = d.mask_b;
     a.splits = 1;
-    const int E = 16 / type_size(d.type);
-    const int64_t strides = a.q_b | a.q_s | a.q_h | a.k_b | a.k_s | a.k_h | a.v_b | a.v_s | a.v_h | d.D | d.Dv;
-    a.vec = strides % E == 0 && aligned_to(q, 16) && aligned_to(k, 16) && aligned_to(v, 16);
     return a;
+}
+
+bool attn_vector(const AttnArgs& a, int type)
+{
+    const int64_t strides = a.q_b | a.q_s | a.q_h | a.k_b | a.k_s | a.k_h | a.v_b | a.v_s | a.v_h | a.D | a.Dv;
+    return strides % (16 / type_size(type)) == 0 && aligned_to(a.q, 16) && aligned_to(a.k, 16) && aligned_to(a.v, 16);
 }
 
 size_t diffattn_forward_workspace(const sconv_diffattn_desc_t& d)
@@ -412,7 +445,9 @@ int launch_diffattn_forward(const sconv_diffattn_desc_t& d, const void* q, const
     a.splits = p.splits; a.split_keys = p.split_keys; a.row_tiles = p.row_tiles;
     a.part = (float*)ws;
     a.part_ml = (float*)((char*)ws + p.part);
-    return d.type == SCONV_BF16 ? fwd_run<bf16>(a, p, stream) : fwd_run<float>(a, p, stream);
+    const bool vec = attn_vector(a, d.type);
+    if (d.type == SCONV_BF16) return vec ? fwd_run<bf16, true>(a, p, stream) : fwd_run<bf16, false>(a, p, stream);
+    return vec ? fwd_run<float, true>(a, p, stream) : fwd_run<float, false>(a, p, stream);
 }
 
 }  // namespace sconv

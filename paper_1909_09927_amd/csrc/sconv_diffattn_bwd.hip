@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256) void attn_dlam(const float* part, int B, int H
     if (threadIdx.x == 0) dlam[h] = 0.0f - ((t[0] + t[1]) + (t[2] + t[3]));
 }
 
-template <typename T, int DT>
+template <typename T, bool VEC, int DT>
 __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
 {
     constexpr int NW = 4, TH = 256, BN = 32, DVT = 2 * DT;
@@ -96,10 +96,10 @@ __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int s = 0; s < KS; ++s) qf[m][s] = global_frag(q + m * a.q_h, 16 * s + 8 * h, a.D, a.vec);
+        for (int s = 0; s < KS; ++s) qf[m][s] = global_frag<VEC>(q + m * a.q_h, 16 * s + 8 * h, a.D);
     const T* go = (const T*)a.dout + (((int64_t)b * a.Sq + i) * a.H + head) * a.Dv;
 #pragma unroll
-    for (int s = 0; s < VS; ++s) gf[s] = global_frag(go, 16 * s + 8 * h, a.Dv, a.vec);
+    for (int s = 0; s < VS; ++s) gf[s] = global_frag<VEC>(go, 16 * s + 8 * h, a.Dv);
 
     f32x16 acc[2][NT];
 #pragma unroll
@@ -112,12 +112,12 @@ __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
 
     const T* kb = (const T*)a.k + b * a.k_b + (int64_t)hk * 2 * a.k_h;
     const T* vb = (const T*)a.v + b * a.v_b + (int64_t)hk * a.v_h;
-    Stage<T, BN, 2, DT, TH> ks;
-    Stage<T, BN, 1, DVT, TH> vs;
+    Stage<T, VEC, BN, 2, DT, TH> ks;
+    Stage<T, VEC, BN, 1, DVT, TH> vs;
     uint8_t seen = 1;
     const auto fetch = [&](int j0) {
-        ks.load(kb, a.k_s, a.k_h, j0, n, a.D, a.vec);
-        vs.load(vb, a.v_s, 0, j0, n, a.Dv, a.vec);
+        ks.load(kb, a.k_s, a.k_h, j0, n, a.D);
+        vs.load(vb, a.v_s, 0, j0, n, a.Dv);
         if (mask && threadIdx.x < BN) seen = mask[min(j0 + (int)threadIdx.x, n - 1)];
     };
     if (k1 > 0) fetch(0);
@@ -180,6 +180,7 @@ __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
                 acc[1][t] = mma(acc[1][t], col_frag<KLD>(kt + kcol + 16 * st * KLD + DT + 32 * t), f1);
             }
         }
+        settle();
     }
     spread = half_sum(spread);
     if (mine >= a.rows) return;
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
 }
 
 // WHAT: 1: dv, 2: dk of the first map, 4: of the second (all three where their sums fit the registers).
-template <typename T, int DT, int WHAT>
+template <typename T, bool VEC, int DT, int WHAT>
 __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
 {
     constexpr int NW = 4, TH = 256, BM = 32, DVT = 2 * DT;
@@ -230,12 +231,12 @@ __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
     const T* v = (const T*)a.v + b * a.v_b + in * a.v_s + (int64_t)hk * a.v_h;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-        if (MAP0) kf[0][s] = global_frag(k, 16 * s + 8 * h, a.D, a.vec);
-        if (MAP1) kf[1][s] = global_frag(k + a.k_h, 16 * s + 8 * h, a.D, a.vec);
+        if (MAP0) kf[0][s] = global_frag<VEC>(k, 16 * s + 8 * h, a.D);
+        if (MAP1) kf[1][s] = global_frag<VEC>(k + a.k_h, 16 * s + 8 * h, a.D);
     }
     if (NEED_G)
 #pragma unroll
-        for (int s = 0; s < VS; ++s) vf[s] = global_frag(v, 16 * s + 8 * h, a.Dv, a.vec);
+        for (int s = 0; s < VS; ++s) vf[s] = global_frag<VEC>(v, 16 * s + 8 * h, a.Dv);
 
     f32x16 dk[2][NT], dv[VT];
 #pragma unroll
@@ -247,14 +248,14 @@ __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
 #pragma unroll
         for (int e = 0; e < 16; ++e) dv[t][e] = 0.0f;
 
-    Stage<T, BM, 2, DT, TH> qs;
-    Stage<T, BM, 1, DVT, TH> gs;
+    Stage<T, VEC, BM, 2, DT, TH> qs;
+    Stage<T, VEC, BM, 1, DVT, TH> gs;
     float stat = 0.0f, sum = 0.0f;
     const int64_t half = (int64_t)a.B * a.H * a.Sq;
     const auto fetch = [&](int g, int i0) {
         const int head = hk * a.G + g;
-        qs.load((const T*)a.q + b * a.q_b + (int64_t)head * 2 * a.q_h, a.q_s, a.q_h, i0, a.Sq, a.D, a.vec);
-        gs.load((const T*)a.dout + ((int64_t)b * a.Sq * a.H + head) * a.Dv, (int64_t)a.H * a.Dv, 0, i0, a.Sq, a.Dv, a.vec);
+        qs.load((const T*)a.q + b * a.q_b + (int64_t)head * 2 * a.q_h, a.q_s, a.q_h, i0, a.Sq, a.D);
+        gs.load((const T*)a.dout + ((int64_t)b * a.Sq * a.H + head) * a.Dv, (int64_t)a.H * a.Dv, 0, i0, a.Sq, a.Dv);
         if (threadIdx.x < 128) {                       // thread: statistic x row
             const int i = min(i0 + (int)(threadIdx.x & 31), a.Sq - 1), what = threadIdx.x >> 5;
             const int64_t at = ((int64_t)b * a.H + head) * a.Sq + i;
@@ -351,6 +352,7 @@ __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
                 }
             }
         }
+        settle();
     }
     if (j >= a.Sk) return;
     T* kout = (T*)a.dk + (((int64_t)b * a.Sk + j) * a.Hkv + hk) * 2 * a.D;
@@ -378,40 +380,40 @@ __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
             }
 }
 
-template <typename T, int DT, int WHAT>
+template <typename T, bool VEC, int DT, int WHAT>
 int keys_launch(const AttnArgs& a, hipStream_t stream)
 {
     constexpr size_t lds = 32 * (Tile<T, 2 * DT>::LD + Tile<T, 2 * DT>::LD) * sizeof(T) + 256 * 4 + 8;
-    const int rc = allow_lds(attn_bwd_keys<T, DT, WHAT>, lds);
+    const int rc = allow_lds(attn_bwd_keys<T, VEC, DT, WHAT>, lds);
     if (rc) return rc;
     const int64_t grid = (int64_t)((a.Sk + 127) / 128) * a.B * a.Hkv;
-    hipLaunchKernelGGL((attn_bwd_keys<T, DT, WHAT>), dim3((unsigned)grid), dim3(256), lds, stream, a);
+    hipLaunchKernelGGL((attn_bwd_keys<T, VEC, DT, WHAT>), dim3((unsigned)grid), dim3(256), lds, stream, a);
     return launch_status();
 }
 
-template <typename T, int DT>
+template <typename T, bool VEC, int DT>
 int bwd_main(const AttnArgs& a, hipStream_t stream)
 {
     int rc = SCONV_OK;
     if (a.Sk > 0) {
-        if constexpr (DT <= 64) rc = keys_launch<T, DT, 7>(a, stream);
+        if constexpr (DT <= 64) rc = keys_launch<T, VEC, DT, 7>(a, stream);
         else {
             // (the three sums of 128 columns and their operands do not fit a lane's registers together)
-            rc = keys_launch<T, DT, 1>(a, stream);
-            if (!rc) rc = keys_launch<T, DT, 2>(a, stream);
-            if (!rc) rc = keys_launch<T, DT, 4>(a, stream);
+            rc = keys_launch<T, VEC, DT, 1>(a, stream);
+            if (!rc) rc = keys_launch<T, VEC, DT, 2>(a, stream);
+            if (!rc) rc = keys_launch<T, VEC, DT, 4>(a, stream);
         }
         if (rc) return rc;
     }
     if (a.Sq == 0) return rc;
     constexpr size_t lds = 32 * (Tile<T, 2 * DT>::LD + Tile<T, 2 * DT>::LD) * sizeof(T) + 8;
-    rc = allow_lds(attn_bwd_rows<T, DT>, lds);
+    rc = allow_lds(attn_bwd_rows<T, VEC, DT>, lds);
     if (rc) return rc;
-    hipLaunchKernelGGL((attn_bwd_rows<T, DT>), dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv)), dim3(256), lds, stream, a);
+    hipLaunchKernelGGL((attn_bwd_rows<T, VEC, DT>), dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv)), dim3(256), lds, stream, a);
     return launch_status();
 }
 
-template <typename T>
+template <typename T, bool VEC>
 int bwd_run(const AttnArgs& a, float* dlam, hipStream_t stream)
 {
     int rc;
@@ -423,9 +425,9 @@ int bwd_run(const AttnArgs& a, float* dlam, hipStream_t stream)
         if (rc) return rc;
     }
     const int most = std::max(a.D, (a.Dv + 1) / 2);
-    if (most <= 32) rc = bwd_main<T, 32>(a, stream);
-    else if (most <= 64) rc = bwd_main<T, 64>(a, stream);
-    else rc = bwd_main<T, 128>(a, stream);
+    if (most <= 32) rc = bwd_main<T, VEC, 32>(a, stream);
+    else if (most <= 64) rc = bwd_main<T, VEC, 64>(a, stream);
+    else rc = bwd_main<T, VEC, 128>(a, stream);
     if (rc) return rc;
     hipLaunchKernelGGL(attn_dlam, dim3((unsigned)a.H), dim3(256), 0, stream, a.dlam_part, a.B, a.H, a.Sq, dlam);
     return launch_status();
@@ -441,7 +443,7 @@ int launch_diffattn_backward(const sconv_diffattn_desc_t& d, const void* dout, c
                              hipStream_t stream)
 {
     AttnArgs a = attn_args(d, q, k, v, lam, lengths, mask);
-    a.vec = a.vec && aligned_to(dout, 16);
+    const bool vec = attn_vector(a, d.type) && aligned_to(dout, 16);
     a.dout = dout; a.out_in = out; a.second_in = second; a.lse_in = lse;
     a.dq = dq; a.dk = dk; a.dv = dv;
     a.ovec = aligned_to(dq, 16) && aligned_to(dk, 16) && aligned_to(dv, 16);
@@ -449,7 +451,8 @@ int launch_diffattn_backward(const sconv_diffattn_desc_t& d, const void* dout, c
     a.dlam_part = a.delta + 2 * (int64_t)d.B * d.H * d.Sq;
     a.row_tiles = (a.rows + 127) / 128;
     if (d.B == 0) a.Sq = a.Sk = 0;                     // nothing but lam's gradient to clear
-    return d.type == SCONV_BF16 ? bwd_run<bf16>(a, dlam, stream) : bwd_run<float>(a, dlam, stream);
+    if (d.type == SCONV_BF16) return vec ? bwd_run<bf16, true>(a, dlam, stream) : bwd_run<bf16, false>(a, dlam, stream);
+    return vec ? bwd_run<float, true>(a, dlam, stream) : bwd_run<float, false>(a, dlam, stream);
 }
 
 }  // namespace sconv

@@ -26,7 +26,7 @@ struct AttnArgs {
     float* delta; float* dlam_part;                          // backward: [2][B][H][Sq], [B][H][Sq]
     int B, Sq, Sk, H, Hkv, G, D, Dv, causal, rows;           // rows = Sq * G: of one request and key head, r = i * G + g
     int splits, split_keys, row_tiles;
-    int vec, ovec;                                           // inputs can be read, outputs written 16 bytes at a time
+    int ovec;                                                // outputs can be written 16 bytes at a time
     float scale, scale2;                                     // scale2 = scale * log2(e)
     int64_t q_b, q_s, q_h, k_b, k_s, k_h, v_b, v_s, v_h, mask_b;
 };
@@ -41,6 +41,16 @@ __device__ __forceinline__ f32x16 mma(f32x16 c, f32x8 a, f32x8 b)
 #pragma unroll
     for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
     return c;
+}
+
+// Ends a loop's round of products.  The compiler keeps its distance between a product and whoever reads its result, except, seen in
+// 32-bit code, where the first copy of a result stands behind the loop's exit branch: it then read registers a few
+// cycles early.  18 wait states are what the longest product needs.
+__device__ __forceinline__ void settle()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 3");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // A tile in LDS: rows of W elements and 16 bytes of padding, so that lanes reading one column chunk of consecutive
@@ -96,13 +106,13 @@ __device__ __forceinline__ void to_frag(const f32x16& p, int s, f32x8& f)
     for (int i = 0; i < 8; ++i) f[i] = p[8 * s + i];
 }
 
-// 16 bytes of elements d.. of a row that has `have` of them.  vec: d and the row are aligned and `have` is whole 16 bytes;
+// 16 bytes of elements d.. of a row that has `have` of them.  VEC: d and the row are aligned and `have` is whole 16 bytes;
 // where d lies beyond, an address inside is read and the result is to be cleared.
-template <typename T>
-__device__ __forceinline__ u32x4 load16(const T* row, int d, int have, bool vec)
+template <bool VEC, typename T>
+__device__ __forceinline__ u32x4 load16(const T* row, int d, int have)
 {
     constexpr int E = 16 / sizeof(T);
-    if (vec) return *(const u32x4*)(row + (d < have ? d : 0));
+    if constexpr (VEC) return *(const u32x4*)(row + (d < have ? d : 0));
     union { u32x4 u; T e[E]; } r;
 #pragma unroll
     for (int i = 0; i < E; ++i) r.e[i] = row[d + i < have ? d + i : 0];
@@ -111,18 +121,20 @@ __device__ __forceinline__ u32x4 load16(const T* row, int d, int have, bool vec)
     return r.u;
 }
 // (the fragment of a row that is read from memory, cleared beyond `have`)
-__device__ __forceinline__ bf16x8 global_frag(const bf16* row, int d, int have, bool vec)
+template <bool VEC>
+__device__ __forceinline__ bf16x8 global_frag(const bf16* row, int d, int have)
 {
     union { u32x4 u; bf16x8 v; } r;
-    r.u = load16(row, d, have, vec);
+    r.u = load16<VEC>(row, d, have);
     if (d >= have) r.u = u32x4{0, 0, 0, 0};
     return r.v;
 }
-__device__ __forceinline__ f32x8 global_frag(const float* row, int d, int have, bool vec)
+template <bool VEC>
+__device__ __forceinline__ f32x8 global_frag(const float* row, int d, int have)
 {
     union { u32x4 u[2]; f32x8 v; } r;
-    r.u[0] = load16(row, d, have, vec);
-    r.u[1] = load16(row, d + 4, have, vec);
+    r.u[0] = load16<VEC>(row, d, have);
+    r.u[1] = load16<VEC>(row, d + 4, have);
     if (d >= have) r.u[0] = u32x4{0, 0, 0, 0};
     if (d + 4 >= have) r.u[1] = u32x4{0, 0, 0, 0};
     return r.v;
@@ -165,7 +177,7 @@ __device__ __forceinline__ int limit_of(const AttnArgs& a, int i, int n)
 
 // ROWS rows of a tile on their way from memory to LDS, through registers, so that the loads of one tile run under the products of
 // the one before.  A row has PARTS rows of W elements of memory beside each other (the two keys of a head).
-template <typename T, int ROWS, int PARTS, int W, int THREADS>
+template <typename T, bool VEC, int ROWS, int PARTS, int W, int THREADS>
 struct Stage {
     static constexpr int E = 16 / sizeof(T), PER = PARTS * W / E, N = ROWS * PER / THREADS, LD = Tile<T, PARTS * W>::LD;
     static_assert(N * THREADS == ROWS * PER, "whole vectors for every thread");
@@ -173,12 +185,12 @@ struct Stage {
 
     // row j of the tile: base + (j0 + j) * stride, its part m at + m * part; rows from `rows` on are not there (one that is, is
     // read instead, and cleared by store).
-    __device__ __forceinline__ void load(const T* base, int64_t stride, int64_t part, int j0, int rows, int have, bool vec)
+    __device__ __forceinline__ void load(const T* base, int64_t stride, int64_t part, int j0, int rows, int have)
     {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int e = n * THREADS + threadIdx.x, row = e / PER, c = e % PER, m = c / (W / E), d = (c % (W / E)) * E;
-            r[n] = load16(base + (int64_t)min(j0 + row, rows - 1) * stride + m * part, d, have, vec);
+            r[n] = load16<VEC>(base + (int64_t)min(j0 + row, rows - 1) * stride + m * part, d, have);
         }
     }
     // words: a bit for every row that is there (LDS), null: all are
@@ -196,6 +208,9 @@ struct Stage {
 // The arguments both directions share.
 AttnArgs attn_args(const sconv_diffattn_desc_t& d, const void* q, const void* k, const void* v, const float* lam,
                    const int32_t* lengths, const uint8_t* mask);
+
+// Whether q, k and v can be read 16 bytes at a time.
+bool attn_vector(const AttnArgs& a, int type);
 
 // Sets the dynamic LDS size a kernel may ask for, where it is above the default.
 template <typename K>
