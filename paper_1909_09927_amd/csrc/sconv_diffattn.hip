@@ -4,7 +4,7 @@
 // group) pairs, so heads that share keys share their tiles, and a single token's heads fill one tile.  A key tile's values are
 // read once for both maps.
 //   wide   128 rows a workgroup, 32 a wavefront; every wavefront walks all keys of the tile.
-//   few    32 rows a workgroup: its wavefronts take 32 keys each of a tile of 128, and join at the end.
+//   few    up to 32 rows a workgroup: its wavefronts walk keys of their own, and join at the end.
 // Either may split the keys over workgroups, whose parts a second kernel joins in a fixed order.
 // Weights are rounded to the operands' type for their product with the values; the sums they are divided by are of the
 // unrounded ones, in 32 bits.
@@ -49,33 +49,86 @@ __device__ __forceinline__ void soften(f32x16& s, float scale2, float& top, floa
 }
 
 
-template <typename T, int DT, int DVT, int NW, bool FEW>
-struct FwdShape {
-    static constexpr int BN = FEW ? 32 * NW : 32;
-    static constexpr int ROWS = FEW ? 32 : 32 * NW;
-    static constexpr int BUFS = FEW ? 1 : 2;           // a wide workgroup writes one tile while it reads the other
-    static constexpr int WAVES = !FEW && sizeof(T) == 2 && DT <= 64 ? 2 : 1;
+template <typename T, int DT, int DVT>
+struct WideShape {
+    static constexpr int NW = 4, BN = 32, ROWS = 32 * NW;
+    static constexpr int WAVES = sizeof(T) == 2 && DT <= 64 ? 2 : 1;
     static constexpr int TILE = BN * (Tile<T, 2 * DT>::LD + Tile<T, DVT>::LD);
-    static constexpr size_t LDS = (size_t)BUFS * TILE * sizeof(T) + 3 * (BN / 32) * 4;
+    static constexpr size_t LDS = (size_t)2 * TILE * sizeof(T) + 3 * 4;    // (one tile is written while the other is read)
 };
 
-template <typename T, bool VEC, int DT, int DVT, int NW, bool FEW>
-__global__ __launch_bounds__(64 * NW, (FwdShape<T, DT, DVT, NW, FEW>::WAVES)) void attn_fwd(AttnArgs a)
+// A row's part of a call whose keys are split: unweighted sums and statistics, for the joining kernel.
+struct RowPart {
+    float* o; float* ml; int wide;
+    __device__ __forceinline__ RowPart(const AttnArgs& a, int split, int bh, int row)
+    {
+        const int64_t at = ((int64_t)split * a.B * a.Hkv + bh) * a.rows + row;
+        wide = (a.Dv + 3) / 4 * 4;
+        o = a.part + at * 2 * wide;
+        ml = a.part_ml + 4 * at;
+    }
+    __device__ __forceinline__ void stats(const float (&top)[2], const float (&sum)[2]) const { *(f32x4*)ml = f32x4{top[0], sum[0], top[1], sum[1]}; }
+    // (the joining kernel does not read sums of nothing)
+    __device__ __forceinline__ void store(int m, float sum, int dv0, int d, int most, float x, float y, float z, float w) const
+    {
+        if (sum != 0.0f && d < most && dv0 + d < wide) *(f32x4*)(o + m * wide + dv0 + d) = f32x4{x, y, z, w};
+    }
+};
+
+// A row's results: values dv0 .. dv0 + dvn of a head.
+template <typename T>
+struct RowOut {
+    T* out; T* second; int dvn, b, i, head; bool v4, none; float inv0, inv1, lam;
+    __device__ __forceinline__ RowOut(const AttnArgs& a, int b_, int i_, int head_, int dv0, int dvn_, const float (&sum)[2])
+    {
+        b = b_; i = i_; head = head_; dvn = dvn_;
+        const int64_t at = (((int64_t)b * a.Sq + i) * a.H + head) * a.Dv + dv0;
+        out = (T*)a.out + at;
+        second = a.second ? (T*)a.second + at : nullptr;
+        v4 = a.ovec && a.Dv % 4 == 0;
+        none = sum[1] == 0.0f;
+        inv0 = none ? 0.0f : 1.0f / sum[0];
+        inv1 = none ? 0.0f : 1.0f / sum[1];
+        lam = a.lam[head];
+    }
+    __device__ __forceinline__ void store(int d, const float (&o0)[4], const float (&o1)[4]) const
+    {
+        float x[4], y[4];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+            y[z] = o1[z] * inv1;
+            // (a query that sees nothing answers 0, whatever lam is)
+            x[z] = none ? 0.0f : fmaf(-lam, y[z], o0[z] * inv0);
+        }
+        store4(out, d, dvn, v4, x);
+        if (second) store4(second, d, dvn, v4, y);
+    }
+    __device__ __forceinline__ void stats(const AttnArgs& a, const float (&top)[2], const float (&sum)[2]) const
+    {
+        if (!a.lse) return;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+            a.lse[(((int64_t)m * a.B + b) * a.H + head) * a.Sq + i] =
+                sum[m] == 0.0f ? -INFINITY : (top[m] + log2f(sum[m])) * 0.69314718055994530942f;
+    }
+};
+
+template <typename T, bool VEC, int DT, int DVT>
+__global__ __launch_bounds__(256, (WideShape<T, DT, DVT>::WAVES)) void attn_wide(AttnArgs a)
 {
-    typedef FwdShape<T, DT, DVT, NW, FEW> Shape;
-    constexpr int BN = Shape::BN, ROWS = Shape::ROWS;
+    typedef WideShape<T, DT, DVT> Shape;
+    constexpr int NW = Shape::NW, BN = Shape::BN, ROWS = Shape::ROWS;
     constexpr int KLD = Tile<T, 2 * DT>::LD, VLD = Tile<T, DVT>::LD, KS = DT / 16, NT = DVT / 32, TH = 64 * NW;
     typedef typename Frag<T>::type frag;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     T* tiles = (T*)lds;
-    uint32_t* words = (uint32_t*)(tiles + Shape::BUFS * Shape::TILE);    // [3][BN / 32]: of the tile that is read, the next one and the one after
+    uint32_t* words = (uint32_t*)(tiles + 2 * Shape::TILE);    // [3]: of the tile that is read, the next one and the one after
 
     const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
     const int tile = a.row_tiles - 1 - blockIdx.x / bh_all;      // the rows that see most first
     const int split = blockIdx.y, dv0 = blockIdx.z * DVT, dvn = min(DVT, a.Dv - dv0);
     const int w = threadIdx.x >> 6, l = threadIdx.x & 63, h = l >> 5;
-    const int first = tile * ROWS + (FEW ? 0 : 32 * w);
-    const int mine = first + (l & 31), r = min(mine, a.rows - 1), i = r / a.G, g = r - i * a.G;
+    const int mine = tile * ROWS + 32 * w + (l & 31), r = min(mine, a.rows - 1), i = r / a.G, g = r - i * a.G;
     const int n = keys_of(a, b);
     const int lim = limit_of(a, i, n);
     // limits rise with the rows: of this wavefront's first and last one, and of the workgroup's last one
@@ -116,14 +169,12 @@ __global__ __launch_bounds__(64 * NW, (FwdShape<T, DT, DVT, NW, FEW>::WAVES)) vo
     const auto mark = [&](int j0, int slot) {
         if ((mask || j0 + BN > n) && threadIdx.x < BN) {
             const uint64_t there = __ballot(j0 + (int)threadIdx.x < n && seen);
-            uint32_t* wd = words + slot * (BN / 32);
-            if (l == 0) wd[2 * w] = (uint32_t)there;
-            if (l == 32) wd[2 * w + 1] = (uint32_t)(there >> 32);
+            if (threadIdx.x == 0) words[slot] = (uint32_t)there;
         }
     };
     const auto put = [&](int j0, int turn, int slot) {
-        T* kt = tiles + (Shape::BUFS > 1 ? turn : 0) * Shape::TILE;
-        const uint32_t* wd = mask || j0 + BN > n ? words + slot * (BN / 32) : nullptr;
+        T* kt = tiles + turn * Shape::TILE;
+        const uint32_t* wd = mask || j0 + BN > n ? words + slot : nullptr;
         ks.store(kt, wd, a.D);
         vs.store(kt + BN * KLD, wd, dvn);
     };
@@ -133,48 +184,35 @@ __global__ __launch_bounds__(64 * NW, (FwdShape<T, DT, DVT, NW, FEW>::WAVES)) vo
     if (k0 < k1) {
         fetch(k0);
         mark(k0, 0);
-        if (Shape::BUFS > 1) {
-            if (mask || k0 + BN > n) __syncthreads();
-            put(k0, 0, 0);
-            if (k0 + BN < k1) { fetch(k0 + BN); mark(k0 + BN, 1); }
-        }
+        if (mask || k0 + BN > n) __syncthreads();
+        put(k0, 0, 0);
+        if (k0 + BN < k1) { fetch(k0 + BN); mark(k0 + BN, 1); }
     }
     for (int j0 = k0; j0 < k1; j0 += BN, turn ^= 1, slot = after(slot)) {
-        const bool whole = !mask && j0 + BN <= n;
-        const uint32_t* wd = words + slot * (BN / 32);
         __syncthreads();
-        if (Shape::BUFS > 1) {
-            // (this tile is there; the next one's keys were marked before the barrier)
-            if (j0 + BN < k1) {
-                put(j0 + BN, turn ^ 1, after(slot));
-                if (j0 + 2 * BN < k1) fetch(j0 + 2 * BN);
-            }
-        } else {
-            put(j0, 0, slot);
-            __syncthreads();
-            if (j0 + BN < k1) fetch(j0 + BN);
+        // (this tile is there; the next one's keys were marked before the barrier)
+        if (j0 + BN < k1) {
+            put(j0 + BN, turn ^ 1, after(slot));
+            if (j0 + 2 * BN < k1) fetch(j0 + 2 * BN);
         }
-        const T* kt = tiles + (Shape::BUFS > 1 ? turn : 0) * Shape::TILE;
-        const T* vt = kt + BN * KLD;
-#pragma unroll
-        for (int sub = 0; sub < (FEW ? 1 : BN / 32); ++sub) {
-            const int row0 = FEW ? 32 * w : 32 * sub, js = j0 + row0;
-            if (js >= wmax) continue;
+        if (j0 < wmax) {
+            const T* kt = tiles + turn * Shape::TILE;
+            const T* vt = kt + BN * KLD;
+            const T* krow = kt + (l & 31) * KLD + 8 * h;
             f32x16 s[2];
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[m][e] = 0.0f;
 #pragma unroll
-                for (int t = 0; t < KS; ++t)
-                    s[m] = mma(s[m], row_frag(kt + (row0 + (l & 31)) * KLD + m * DT + 16 * t + 8 * h), qf[m][t]);
+                for (int t = 0; t < KS; ++t) s[m] = mma(s[m], row_frag(krow + m * DT + 16 * t), qf[m][t]);
             }
-            const uint32_t word = whole ? ~0u : wd[row0 >> 5];
-            if (js + 32 > wmin || (mask && word != ~0u)) {
+            const uint32_t word = mask || j0 + BN > n ? words[slot] : ~0u;
+            if (j0 + 32 > wmin || (mask && word != ~0u)) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int j = 8 * (e >> 2) + 4 * h + (e & 3);
-                    const bool ok = js + j < lim && (word >> j & 1);
+                    const bool ok = j0 + j < lim && (word >> j & 1);
                     s[0][e] = ok ? s[0][e] : -INFINITY;
                     s[1][e] = ok ? s[1][e] : -INFINITY;
                 }
@@ -188,159 +226,340 @@ __global__ __launch_bounds__(64 * NW, (FwdShape<T, DT, DVT, NW, FEW>::WAVES)) vo
                 to_frag(s[1], st, p1);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const frag vf = col_frag<VLD>(vt + vcol + (row0 + 16 * st) * VLD + 32 * t);
+                    const frag vf = col_frag<VLD>(vt + vcol + 16 * st * VLD + 32 * t);
                     o[0][t] = mma(o[0][t], vf, p0);
                     o[1][t] = mma(o[1][t], vf, p1);
                 }
             }
+            settle();
         }
-        settle();
-        if (Shape::BUFS > 1) { if (j0 + 2 * BN < k1) mark(j0 + 2 * BN, after(after(slot))); }
-        else if (j0 + BN < k1) mark(j0 + BN, after(slot));
+        if (j0 + 2 * BN < k1) mark(j0 + 2 * BN, after(after(slot)));
     }
 #pragma unroll
     for (int m = 0; m < 2; ++m) sum[m] = half_sum(sum[m]);
-
-    if constexpr (FEW) {
-        // the wavefronts' parts meet in LDS, over the tiles: statistics first, then the sums, halving the wavefronts
-        __syncthreads();
-        float* ml = (float*)lds;                       // [NW][2][2][32]
-        float* acc = ml + NW * 128;                    // [NW / 2][2][DVT][32]
+    if (mine >= a.rows) return;
+    if (a.splits > 1) {
+        const RowPart part(a, split, bh, mine);
+        if (blockIdx.z == 0 && h == 0) part.stats(top, sum);
 #pragma unroll
         for (int m = 0; m < 2; ++m)
-            if (h == 0) { ml[(w * 4 + 2 * m) * 32 + l] = top[m]; ml[(w * 4 + 2 * m + 1) * 32 + l] = sum[m]; }
-        __syncthreads();
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            float most = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < NW; ++k) most = fmaxf(most, ml[(k * 4 + 2 * m) * 32 + (l & 31)]);
-            const float base = most == -INFINITY ? 0.0f : most;
-            float all = 0.0f;
-#pragma unroll
-            for (int k = 0; k < NW; ++k)
-                all += ml[(k * 4 + 2 * m + 1) * 32 + (l & 31)] * __builtin_amdgcn_exp2f(ml[(k * 4 + 2 * m) * 32 + (l & 31)] - base);
-            const float f = __builtin_amdgcn_exp2f(top[m] - base);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[m][t][e] *= f;
-            top[m] = most;
-            sum[m] = all;
-        }
-#pragma unroll
-        for (int half = NW / 2; half > 0; half /= 2) {
-            if (w >= half && w < 2 * half) {
-                float* to = acc + (w - half) * 2 * DVT * 32;
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) to[((m * NT + t) * 16 + e) * 64 + l] = o[m][t][e];
-            }
-            __syncthreads();
-            if (w < half) {
-                const float* from = acc + w * 2 * DVT * 32;
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[m][t][e] += from[((m * NT + t) * 16 + e) * 64 + l];
-            }
-            __syncthreads();
-        }
-        if (w != 0) return;
-    }
-    if (mine >= a.rows) return;
-
-    if (a.splits > 1) {
-        const int64_t at = ((int64_t)split * bh_all + bh) * a.rows + mine;
-        if (blockIdx.z == 0 && h == 0) *(f32x4*)(a.part_ml + 4 * at) = f32x4{top[0], sum[0], top[1], sum[1]};
-        const int wide = (a.Dv + 3) / 4 * 4;
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            if (sum[m] == 0.0f) continue;              // the joining kernel does not read it either
-            float* to = a.part + (at * 2 + m) * wide + dv0;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                    const int d = 32 * t + 8 * (e >> 2) + 4 * h;
-                    if (dv0 + d < wide && d < DVT)
-                        *(f32x4*)(to + d) = f32x4{o[m][t][e], o[m][t][e + 1], o[m][t][e + 2], o[m][t][e + 3]};
-                }
-        }
+                for (int e = 0; e < 16; e += 4)
+                    part.store(m, sum[m], dv0, 32 * t + 8 * (e >> 2) + 4 * h, DVT, o[m][t][e], o[m][t][e + 1], o[m][t][e + 2], o[m][t][e + 3]);
         return;
     }
-    const int head = hk * a.G + g;
-    const float inv0 = sum[0] == 0.0f ? 0.0f : 1.0f / sum[0], inv1 = sum[1] == 0.0f ? 0.0f : 1.0f / sum[1];
-    const float lam = a.lam[head];
-    const int64_t at = (((int64_t)b * a.Sq + i) * a.H + head) * a.Dv + dv0;
-    T* out = (T*)a.out + at;
-    T* second = a.second ? (T*)a.second + at : nullptr;
-    const bool v4 = a.ovec && a.Dv % 4 == 0;
+    const RowOut<T> row(a, b, i, hk * a.G + g, dv0, dvn, sum);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
-            float x[4], y[4];
-#pragma unroll
-            for (int z = 0; z < 4; ++z) {
-                y[z] = o[1][t][e + z] * inv1;
-                // (a query that sees nothing answers 0, whatever lam is)
-                x[z] = sum[1] == 0.0f ? 0.0f : fmaf(-lam, y[z], o[0][t][e + z] * inv0);
-            }
-            const int d = 32 * t + 8 * (e >> 2) + 4 * h;
-            store4(out, d, dvn, v4, x);
-            if (second) store4(second, d, dvn, v4, y);
+            const float x[4] = {o[0][t][e], o[0][t][e + 1], o[0][t][e + 2], o[0][t][e + 3]};
+            const float y[4] = {o[1][t][e], o[1][t][e + 1], o[1][t][e + 2], o[1][t][e + 3]};
+            row.store(32 * t + 8 * (e >> 2) + 4 * h, x, y);
         }
-    if (a.lse && blockIdx.z == 0 && h == 0) {
+    if (blockIdx.z == 0 && h == 0) row.stats(a, top, sum);
+}
+
+// Few rows: RT tiles of 16 to a wavefront, in products of 16 x 16.  A wavefront walks 32 keys at a time of its own, alone: its keys
+// go from memory to registers as the product reads them, its values through LDS of its own (to be read down the keys), and no
+// barrier stands between its loads.  The wavefronts join at the end.
+template <typename T, int DVT>
+struct FewShape {
+    static constexpr int NW = 4, BN = 32, VLD = Tile<T, DVT>::LD;
+    static constexpr int TILE = BN * VLD;              // elements of LDS a wavefront
+};
+
+template <typename T, bool VEC, int DT, int DVT, int RT>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)) void attn_few(AttnArgs a)
+{
+    typedef FewShape<T, DVT> Shape;
+    constexpr int NW = Shape::NW, BN = Shape::BN, VLD = Shape::VLD, KS = DT / 32, NT = DVT / 16, E = 16 / sizeof(T);
+    constexpr int NV = BN * DVT / E / 64, VPER = DVT / E;   // 16-byte vectors of a lane's and a row's share of the values
+    typedef typename Frag<T>::type frag;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+
+    const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
+    const int split = blockIdx.y, dv0 = blockIdx.z * DVT, dvn = min(DVT, a.Dv - dv0);
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, h = l >> 4;
+    T* vt = (T*)lds + w * Shape::TILE;
+    const int n = keys_of(a, b);
+    int lim[RT], wmin = n;
+    frag qf[RT][2][KS];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        const int r = min(16 * x + c, a.rows - 1), i = r / a.G, g = r - i * a.G;
+        lim[x] = limit_of(a, i, n);
+        const T* q = (const T*)a.q + b * a.q_b + i * a.q_s + (int64_t)(hk * a.G + g) * 2 * a.q_h;
 #pragma unroll
         for (int m = 0; m < 2; ++m)
-            a.lse[(((int64_t)m * a.B + b) * a.H + head) * a.Sq + i] =
-                sum[m] == 0.0f ? -INFINITY : (top[m] + log2f(sum[m])) * 0.69314718055994530942f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) qf[x][m][s] = global_frag<VEC>(q + m * a.q_h, 32 * s + 8 * h, a.D);
+    }
+    wmin = __builtin_amdgcn_readfirstlane(lim[0]);          // of the first row: limits rise
+    const int last = limit_of(a, (a.rows - 1) / a.G, n);
+    const int k0 = split * a.split_keys, k1 = (int)min((int64_t)last, (int64_t)k0 + a.split_keys);
+    const uint8_t* mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+
+    f32x4 o[RT][2][NT];
+    float top[RT][2], safe[RT][2], sum[RT][2];
+#pragma unroll
+    for (int x = 0; x < RT; ++x)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            top[x][m] = -INFINITY; safe[x][m] = 0.0f; sum[x][m] = 0.0f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) o[x][m][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+
+    const T* kb = (const T*)a.k + b * a.k_b + (int64_t)hk * 2 * a.k_h;
+    const T* vb = (const T*)a.v + b * a.v_b + (int64_t)hk * a.v_h + dv0;
+    frag kf[2][2][KS];                                 // [16 keys][map][depth]
+    u32x4 vr[NV];
+    uint8_t seen = 1;
+    const auto fetch_keys = [&](int j0) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const T* row = kb + (int64_t)min(j0 + 16 * y + c, n - 1) * a.k_s;
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kf[y][m][s] = global_frag<VEC>(row + m * a.k_h, 32 * s + 8 * h, a.D);
+        }
+    };
+    const auto fetch_values = [&](int j0) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int e = v * 64 + l;
+            vr[v] = load16<VEC>(vb + (int64_t)min(j0 + e / VPER, n - 1) * a.v_s, e % VPER * E, dvn);
+        }
+        if (mask) seen = mask[min(j0 + (l & 31), n - 1)];
+    };
+    int j0 = k0 + BN * w;
+    if (j0 < k1) { fetch_keys(j0); fetch_values(j0); }
+    for (; j0 < k1; j0 += BN * NW) {
+        const int next = j0 + BN * NW;
+        f32x4 s[RT][2][2];                             // [rows][map][16 keys]
+#pragma unroll
+        for (int x = 0; x < RT; ++x)
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    s[x][m][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int t = 0; t < KS; ++t) s[x][m][y] = mma(s[x][m][y], kf[y][m][t], qf[x][m][t]);
+                }
+        if (next < k1) fetch_keys(next);
+        const uint32_t word = mask || j0 + BN > n ? (uint32_t)__ballot(j0 + (l & 31) < n && seen) : ~0u;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int e = v * 64 + l, row = e / VPER;
+            const bool there = e % VPER * E < dvn && (word >> row & 1);
+            *(u32x4*)(vt + row * VLD + e % VPER * E) = there ? vr[v] : u32x4{0, 0, 0, 0};
+        }
+        if (next < k1) fetch_values(next);
+        if (j0 + 32 > wmin || word != ~0u) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = 16 * y + 4 * h + e;
+#pragma unroll
+                    for (int x = 0; x < RT; ++x) {
+                        const bool ok = j0 + j < lim[x] && (word >> j & 1);
+                        s[x][0][y][e] = ok ? s[x][0][y][e] : -INFINITY;
+                        s[x][1][y][e] = ok ? s[x][1][y][e] : -INFINITY;
+                    }
+                }
+        }
+        frag p[RT][2];
+#pragma unroll
+        for (int x = 0; x < RT; ++x)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                f32x4 (&z)[2] = s[x][m];
+                float mx = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
+                mx = half_max(quarter_max(mx)) * a.scale2;
+                if (__any(mx > top[x][m] + 8.0f)) {
+                    const float grown = fmaxf(top[x][m], mx);
+                    safe[x][m] = grown == -INFINITY ? 0.0f : grown;
+                    const float f = __builtin_amdgcn_exp2f(top[x][m] - safe[x][m]);
+                    top[x][m] = grown;
+                    sum[x][m] *= f;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) o[x][m][t] *= f;
+                }
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float v = __builtin_amdgcn_exp2f(fmaf(z[y][e], a.scale2, -safe[x][m]));
+                        sum[x][m] += v;
+                        p[x][m][4 * y + e] = (T)v;
+                    }
+            }
+        const int vcol = few_col_lane<T, VLD>();
+        wave_lds_fence();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const frag vf = few_col_frag<VLD>(vt + vcol + 16 * t);
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                o[x][0][t] = mma(o[x][0][t], vf, p[x][0]);
+                o[x][1][t] = mma(o[x][1][t], vf, p[x][1]);
+            }
+        }
+        wave_lds_fence();
+        settle();
+    }
+    // the wavefronts' parts meet in LDS, over the tiles: statistics first, then the sums, halving the wavefronts
+    __syncthreads();
+    float* ml = (float*)lds;                           // [NW][RT][2][2][16]
+    float* acc = ml + NW * RT * 64;                    // [NW / 2][RT * 2 * NT * 4][64]
+#pragma unroll
+    for (int x = 0; x < RT; ++x)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            sum[x][m] = half_sum(quarter_sum(sum[x][m]));
+            if (h == 0) {
+                float* at = ml + ((w * RT + x) * 2 + m) * 32 + c;
+                at[0] = top[x][m];
+                at[16] = sum[x][m];
+            }
+        }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < RT; ++x)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            float most = -INFINITY, all = 0.0f;
+#pragma unroll
+            for (int k = 0; k < NW; ++k) most = fmaxf(most, ml[((k * RT + x) * 2 + m) * 32 + c]);
+            const float base = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+            for (int k = 0; k < NW; ++k) {
+                const float* at = ml + ((k * RT + x) * 2 + m) * 32 + c;
+                all = fmaf(at[16], __builtin_amdgcn_exp2f(at[0] - base), all);
+            }
+            const float f = __builtin_amdgcn_exp2f(top[x][m] - base);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) o[x][m][t] *= f;
+            top[x][m] = most;
+            sum[x][m] = all;
+        }
+#pragma unroll
+    for (int half = NW / 2; half > 0; half /= 2) {
+        if (w >= half && w < 2 * half) {
+            f32x4* to = (f32x4*)acc + (w - half) * RT * 2 * NT * 64 + l;
+#pragma unroll
+            for (int x = 0; x < RT; ++x)
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) to[((x * 2 + m) * NT + t) * 64] = o[x][m][t];
+        }
+        __syncthreads();
+        if (w < half) {
+            const f32x4* from = (const f32x4*)acc + w * RT * 2 * NT * 64 + l;
+#pragma unroll
+            for (int x = 0; x < RT; ++x)
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) o[x][m][t] += from[((x * 2 + m) * NT + t) * 64];
+        }
+        __syncthreads();
+    }
+    if (w != 0) return;
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        const int mine = 16 * x + c, i = mine / a.G;
+        if (mine >= a.rows) continue;
+        if (a.splits > 1) {
+            const RowPart part(a, split, bh, mine);
+            if (blockIdx.z == 0 && h == 0) part.stats(top[x], sum[x]);
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    part.store(m, sum[x][m], dv0, 16 * t + 4 * h, DVT, o[x][m][t][0], o[x][m][t][1], o[x][m][t][2], o[x][m][t][3]);
+            continue;
+        }
+        const RowOut<T> row(a, b, i, hk * a.G + mine - i * a.G, dv0, dvn, sum[x]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const float u[4] = {o[x][0][t][0], o[x][0][t][1], o[x][0][t][2], o[x][0][t][3]};
+            const float v[4] = {o[x][1][t][0], o[x][1][t][1], o[x][1][t][2], o[x][1][t][3]};
+            row.store(16 * t + 4 * h, u, v);
+        }
+        if (blockIdx.z == 0 && h == 0) row.stats(a, top[x], sum[x]);
     }
 }
 
-// Joins the splits' parts: a workgroup a row, lanes along the values.
+// Joins the splits' parts: a workgroup a row, lanes along the two maps' values.
+constexpr int MAX_SPLITS = 128;
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join(AttnArgs a)
 {
+    __shared__ float f[2][MAX_SPLITS], val[2][256];
     const int bh_all = a.B * a.Hkv;
-    const int64_t row = blockIdx.x;                    // bh * rows + r
+    const int64_t row = blockIdx.x, all_rows = (int64_t)bh_all * a.rows;   // row: bh * rows + r
     const int bh = (int)(row / a.rows), r = (int)(row - (int64_t)bh * a.rows), b = bh / a.Hkv, hk = bh % a.Hkv;
-    const int i = r / a.G, head = hk * a.G + r % a.G, wide = (a.Dv + 3) / 4 * 4, d = threadIdx.x;
-    float val[2], lse[2];
-    bool none = true;
+    const int i = r / a.G, head = hk * a.G + r % a.G, wide = (a.Dv + 3) / 4 * 4;
+    // a wavefront a map: the parts' weights against the largest maximum, over the joined sum
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+    if (w < 2) {
+        float t[2], s[2], most = -INFINITY;
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-        float most = -INFINITY;
-        for (int s = 0; s < a.splits; ++s) most = fmaxf(most, a.part_ml[4 * ((int64_t)s * bh_all * a.rows + row) + 2 * m]);
-        const float base = most == -INFINITY ? 0.0f : most;
-        float all = 0.0f, sum = 0.0f;
-        for (int s = 0; s < a.splits; ++s) {
-            const int64_t at = (int64_t)s * bh_all * a.rows + row;
-            const float l = a.part_ml[4 * at + 2 * m + 1];
-            if (l == 0.0f) continue;
-            const float f = __builtin_amdgcn_exp2f(a.part_ml[4 * at + 2 * m] - base);
-            all += l * f;
-            if (d < a.Dv) sum = fmaf(a.part[(at * 2 + m) * wide + d], f, sum);
+        for (int k = 0; k < 2; ++k) {
+            const int split = l + 64 * k;
+            t[k] = -INFINITY; s[k] = 0.0f;
+            if (split < a.splits) {
+                const float* ml = a.part_ml + 4 * (split * all_rows + row) + 2 * w;
+                t[k] = ml[0]; s[k] = ml[1];
+            }
+            most = fmaxf(most, t[k]);
         }
-        val[m] = all == 0.0f ? 0.0f : sum / all;
-        lse[m] = all == 0.0f ? -INFINITY : (most + log2f(all)) * 0.69314718055994530942f;
-        none = all == 0.0f;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+        const float base = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) t[k] = s[k] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(t[k] - base);
+        const float sum = lanes_sum<64>(fmaf(s[0], t[0], s[1] * t[1])), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        f[w][l] = t[0] * inv;
+        f[w][l + 64] = t[1] * inv;
+        if (l == 0) {
+            val[w][0] = sum;
+            if (a.lse) a.lse[(((int64_t)w * a.B + b) * a.H + head) * a.Sq + i] = sum == 0.0f ? -INFINITY : (most + log2f(sum)) * 0.69314718055994530942f;
+        }
     }
+    __syncthreads();
+    const bool none = val[1][0] == 0.0f;
+    __syncthreads();
+    for (int e = threadIdx.x; e < 2 * a.Dv; e += 256) {
+        const int m = e >= a.Dv, d = e - m * a.Dv;
+        const float* from = a.part + (row * 2 + m) * wide + d;
+        float v = 0.0f;
+#pragma unroll 8
+        for (int s = 0; s < a.splits; ++s) {
+            // (parts of nothing were not written)
+            const float x = from[s * all_rows * 2 * wide];
+            v += f[m][s] == 0.0f ? 0.0f : f[m][s] * x;
+        }
+        val[m][d] = v;
+    }
+    __syncthreads();
+    const int d = threadIdx.x;
     if (d < a.Dv) {
         const int64_t at = (((int64_t)b * a.Sq + i) * a.H + head) * a.Dv + d;
-        ((T*)a.out)[at] = (T)(none ? 0.0f : fmaf(-a.lam[head], val[1], val[0]));
-        if (a.second) ((T*)a.second)[at] = (T)val[1];
+        ((T*)a.out)[at] = (T)(none ? 0.0f : fmaf(-a.lam[head], val[1][d], val[0][d]));
+        if (a.second) ((T*)a.second)[at] = (T)val[1][d];
     }
-    if (a.lse && d < 2) a.lse[(((int64_t)d * a.B + b) * a.H + head) * a.Sq + i] = d ? lse[1] : lse[0];
 }
 
-struct FwdPlan { bool few; int rows_tile, row_tiles, chunks, splits, split_keys; size_t part, ml; };
+struct FwdPlan { bool few; int row_tiles, chunks, splits, split_keys; size_t part, ml; };
 
 int dim_tile(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
 
@@ -348,20 +567,19 @@ FwdPlan fwd_plan(const sconv_diffattn_desc_t& d, size_t ws_bytes)
 {
     FwdPlan p = {};
     const int64_t G = d.H / d.Hkv, rows = d.Sq * G, bh = (int64_t)d.B * d.Hkv;
-    const int DT = dim_tile(d.D), DVT = DT == 32 ? 64 : 128;
+    const int DVT = dim_tile(d.D) == 32 ? 64 : 128;
     p.few = rows <= 32;
-    p.rows_tile = p.few ? 32 : 128;
-    p.row_tiles = (int)((rows + p.rows_tile - 1) / p.rows_tile);
+    p.row_tiles = p.few ? 1 : (int)((rows + 127) / 128);
     p.chunks = (d.Dv + DVT - 1) / DVT;
     p.splits = 1;
     p.split_keys = d.Sk > 0 ? d.Sk : 1;
-    // keys are split, at 512 a part or more, where wide workgroups fill half of the chip at most, and until few ones fill it four
+    // keys are split, at 512 a part or more, where wide workgroups fill half of the chip at most, and until few ones fill it eight
     // times over (requests' lengths differ, and a workgroup without keys ends at once)
     const int64_t base = p.row_tiles * bh * p.chunks;
-    if (base == 0) return p;
-    int64_t splits = std::min<int64_t>(p.few ? (1024 + base - 1) / base : 512 / base, (d.Sk + 511) / 512);
+    if (base == 0 || rows == 0) return p;
+    int64_t splits = std::min<int64_t>(p.few ? (2048 + base - 1) / base : 512 / base, (d.Sk + 511) / 512);
     const int64_t wide = (d.Dv + 3) / 4 * 4, each = bh * rows * (2 * wide + 4) * (int64_t)sizeof(float);
-    splits = std::min<int64_t>(splits, (int64_t)(ws_bytes / (size_t)each));
+    splits = std::min<int64_t>(std::min<int64_t>(splits, MAX_SPLITS), (int64_t)(ws_bytes / (size_t)each));
     if (splits > 1) {
         const int64_t keys = ((d.Sk + splits - 1) / splits + 127) / 128 * 128;
         p.split_keys = (int)keys;
@@ -372,34 +590,43 @@ FwdPlan fwd_plan(const sconv_diffattn_desc_t& d, size_t ws_bytes)
     return p;
 }
 
-template <typename T, bool VEC, int DT, int DVT, int NW, bool FEW>
-int fwd_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
+template <typename T, bool VEC, int DT, int DVT>
+int wide_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
 {
-    constexpr size_t tiles = FwdShape<T, DT, DVT, NW, FEW>::LDS, join = (size_t)(NW * 128 + NW / 2 * 2 * DVT * 32) * 4;
-    constexpr size_t lds = FEW && join > tiles ? join : tiles;
-    const auto kern = attn_fwd<T, VEC, DT, DVT, NW, FEW>;
+    constexpr size_t lds = WideShape<T, DT, DVT>::LDS;
+    const auto kern = attn_wide<T, VEC, DT, DVT>;
     const int rc = allow_lds(kern, lds);
     if (rc) return rc;
     hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv), (unsigned)p.splits, (unsigned)p.chunks),
-                       dim3(64 * NW), lds, stream, a);
+                       dim3(256), lds, stream, a);
     return launch_status();
+}
+
+template <typename T, bool VEC, int DT, int DVT, int RT>
+int few_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
+{
+    constexpr size_t tiles = (size_t)4 * FewShape<T, DVT>::TILE * sizeof(T), join = (size_t)(4 * RT * 64 + 2 * RT * 2 * DVT * 16) * 4;
+    constexpr size_t lds = join > tiles ? join : tiles;
+    const auto kern = attn_few<T, VEC, DT, DVT, RT>;
+    const int rc = allow_lds(kern, lds);
+    if (rc) return rc;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.B * a.Hkv), (unsigned)p.splits, (unsigned)p.chunks), dim3(256), lds, stream, a);
+    return launch_status();
+}
+
+template <typename T, bool VEC, int DT, int DVT>
+int fwd_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
+{
+    if (!p.few) return wide_launch<T, VEC, DT, DVT>(a, p, stream);
+    return a.rows <= 16 ? few_launch<T, VEC, DT, DVT, 1>(a, p, stream) : few_launch<T, VEC, DT, DVT, 2>(a, p, stream);
 }
 
 template <typename T, bool VEC>
 int fwd_run(AttnArgs& a, const FwdPlan& p, hipStream_t stream)
 {
     const int DT = dim_tile(a.D);
-    int rc;
-    if (p.few) {
-        // (tiles of 128 wide rows in 32 bits do not fit a workgroup's LDS: two wavefronts of 32 keys)
-        if (DT == 32) rc = fwd_launch<T, VEC, 32, 64, 4, true>(a, p, stream);
-        else if (DT == 64) rc = fwd_launch<T, VEC, 64, 128, sizeof(T) == 2 ? 4 : 2, true>(a, p, stream);
-        else rc = fwd_launch<T, VEC, 128, 128, sizeof(T) == 2 ? 4 : 2, true>(a, p, stream);
-    } else {
-        if (DT == 32) rc = fwd_launch<T, VEC, 32, 64, 4, false>(a, p, stream);
-        else if (DT == 64) rc = fwd_launch<T, VEC, 64, 128, 4, false>(a, p, stream);
-        else rc = fwd_launch<T, VEC, 128, 128, 4, false>(a, p, stream);
-    }
+    const int rc = DT == 32 ? fwd_launch<T, VEC, 32, 64>(a, p, stream)
+                 : DT == 64 ? fwd_launch<T, VEC, 64, 128>(a, p, stream) : fwd_launch<T, VEC, 128, 128>(a, p, stream);
     if (rc || p.splits == 1) return rc;
     hipLaunchKernelGGL((attn_join<T>), dim3((unsigned)((int64_t)a.B * a.Hkv * a.rows)), dim3(256), 0, stream, a);
     return launch_status();

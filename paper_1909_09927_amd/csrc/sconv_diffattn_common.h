@@ -43,6 +43,17 @@ __device__ __forceinline__ f32x16 mma(f32x16 c, f32x8 a, f32x8 b)
     return c;
 }
 
+// The same in tiles of 16 x 16 (32 deep): a lane has 8 elements at depths 8 (l / 16) .. + 7 of row or column l % 16, and of the result
+// column l % 16, rows 4 (l / 16) + 0..3.  Two results of 16 keys are the next product's B at depths
+//   4 (l / 16) + {0, 1, 2, 3, 16, 17, 18, 19}.
+__device__ __forceinline__ f32x4 mma(f32x4 c, bf16x8 a, bf16x8 b) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(f32x4 c, f32x8 a, f32x8 b)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+
 // Ends a loop's round of products.  The compiler keeps its distance between a product and whoever reads its result, except, seen in
 // 32-bit code, where the first copy of a result stands behind the loop's exit branch: it then read registers a few
 // cycles early.  18 wait states are what the longest product needs.
@@ -93,6 +104,35 @@ __device__ __forceinline__ int col_lane()
     if constexpr (sizeof(T) == 2) return (4 * h + ((l & 15) >> 2)) * LD + ((l >> 4) & 1) * 16 + (l & 3) * 4;
     else return 4 * h * LD + (l & 31);
 }
+
+// For tiles of 16 x 16: column l % 16 of 16, depths 4 (l / 16) + {0..3, 16..19}.
+template <int LD>
+__device__ __forceinline__ bf16x8 few_col_frag(const bf16* p)
+{
+    typedef __attribute__((address_space(3))) s16x4 lds4;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 16 * LD));
+    union { s16x4 s[2]; bf16x8 v; } u;
+    u.s[0] = a; u.s[1] = b;
+    return u.v;
+}
+template <int LD>
+__device__ __forceinline__ f32x8 few_col_frag(const float* p)
+{
+    f32x8 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[i] = p[i * LD]; v[4 + i] = p[(16 + i) * LD]; }
+    return v;
+}
+template <typename T, int LD>
+__device__ __forceinline__ int few_col_lane()
+{
+    const int l = threadIdx.x & 63, h = l >> 4;
+    if constexpr (sizeof(T) == 2) return (4 * h + ((l & 15) >> 2)) * LD + (l & 3) * 4;
+    else return 4 * h * LD + (l & 15);
+}
+// Between a wavefront's own writes and reads of LDS: they are carried out in order; the compiler is told to leave them so.
+__device__ __forceinline__ void wave_lds_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
 
 // Registers 8s..8s+7 of a result as the next product's B.
 __device__ __forceinline__ void to_frag(const f32x16& p, int s, bf16x8& f)
@@ -162,6 +202,18 @@ __device__ __forceinline__ float half_max(float v)
 __device__ __forceinline__ float half_sum(float v)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// The neighbouring 16 lanes' value (lane l ^ 16).
+__device__ __forceinline__ float quarter_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float quarter_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 

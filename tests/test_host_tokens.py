@@ -96,7 +96,8 @@ def test_attention_refusals():
     assert size(ctypes.byref(_attn()), 1, ctypes.byref(n)) == 0 and n.value == 2 * 3 * 4 * 3 * 4
     need = n.value
     assert size(ctypes.byref(_attn()), 0, None) == EINVAL
-    assert size(ctypes.byref(_attn(B=0)), 0, ctypes.byref(n)) == 0 and n.value == 0
+    for empty in (dict(B=0), dict(Sq=0), dict(Sk=0), dict(B=0, Sq=0, Sk=0)):
+        assert size(ctypes.byref(_attn(**empty)), 0, ctypes.byref(n)) == 0 and n.value == 0, empty
     assert size(ctypes.byref(_attn(Sq=1, Sk=4096)), 0, ctypes.byref(n)) == 0 and n.value > 0
     for missing in (dict(dout=None), dict(k=None), dict(dv=None), dict(dlam=None), dict(ws=None), dict(nbytes=need - 4), dict(ws=ODD)):
         assert _attn_backward(_attn(), **missing) == EINVAL, missing
