@@ -113,6 +113,38 @@ struct RowOut {
     }
 };
 
+// The end of a wide kernel: a lane's row, to the results or to its part of them.
+template <typename T, int NT, int DVT>
+__device__ __forceinline__ void wide_end(const AttnArgs& a, int b, int bh, int split, int dv0, int mine, int i, int head, int h,
+                                         const f32x16 (&o)[2][NT], const float (&top)[2], float (&sum)[2])
+{
+#pragma unroll
+    for (int m = 0; m < 2; ++m) sum[m] = half_sum(sum[m]);
+    if (mine >= a.rows) return;
+    if (a.splits > 1) {
+        const RowPart part(a, split, bh, mine);
+        if (dv0 == 0 && h == 0) part.stats(top, sum);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4)
+                    part.store(m, sum[m], dv0, 32 * t + 8 * (e >> 2) + 4 * h, DVT, o[m][t][e], o[m][t][e + 1], o[m][t][e + 2], o[m][t][e + 3]);
+        return;
+    }
+    const RowOut<T> row(a, b, i, head, dv0, min(DVT, a.Dv - dv0), sum);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const float x[4] = {o[0][t][e], o[0][t][e + 1], o[0][t][e + 2], o[0][t][e + 3]};
+            const float y[4] = {o[1][t][e], o[1][t][e + 1], o[1][t][e + 2], o[1][t][e + 3]};
+            row.store(32 * t + 8 * (e >> 2) + 4 * h, x, y);
+        }
+    if (dv0 == 0 && h == 0) row.stats(a, top, sum);
+}
+
 template <typename T, bool VEC, int DT, int DVT>
 __global__ __launch_bounds__(256, (WideShape<T, DT, DVT>::WAVES)) void attn_wide(AttnArgs a)
 {
@@ -235,31 +267,148 @@ __global__ __launch_bounds__(256, (WideShape<T, DT, DVT>::WAVES)) void attn_wide
         }
         if (j0 + 2 * BN < k1) mark(j0 + 2 * BN, after(after(slot)));
     }
+    wide_end<T, NT, DVT>(a, b, bh, split, dv0, mine, i, hk * a.G + g, h, o, top, sum);
+}
+
+// Wide rows in 16 bits, whole vectors everywhere: as attn_wide, with tiles of BN keys that go to LDS directly.
+template <int DT, int DVT>
+struct DirectShape {
+    static constexpr int NW = 4, BN = 64, ROWS = 32 * NW;
+    static constexpr int TILE = BN * (2 * DT + DVT);
+    static constexpr size_t LDS = (size_t)2 * TILE * 2 + 3 * (BN / 32) * 4;
+};
+
+template <int DT, int DVT>
+__global__ __launch_bounds__(256, (DT <= 64 ? 2 : 1)) void attn_direct(AttnArgs a)
+{
+    typedef DirectShape<DT, DVT> Shape;
+    constexpr int NW = Shape::NW, BN = Shape::BN, ROWS = Shape::ROWS, KS = DT / 16, NT = DVT / 32, NB = BN / 32;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    bf16* tiles = (bf16*)lds;
+    uint32_t* words = (uint32_t*)(tiles + 2 * Shape::TILE);    // [3][NB]
+
+    const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
+    const int tile = a.row_tiles - 1 - blockIdx.x / bh_all;      // the rows that see most first
+    const int split = blockIdx.y, dv0 = blockIdx.z * DVT;
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, h = l >> 5;
+    const int mine = tile * ROWS + 32 * w + (l & 31), r = min(mine, a.rows - 1), i = r / a.G, g = r - i * a.G;
+    const int n = keys_of(a, b);
+    const int lim = limit_of(a, i, n);
+    const int wmin = __builtin_amdgcn_readfirstlane(lim), wmax = __builtin_amdgcn_readlane(lim, 31);
+    const int last = limit_of(a, min(tile * ROWS + ROWS - 1, a.rows - 1) / a.G, n);
+    const int k0 = split * a.split_keys, k1 = (int)min((int64_t)last, (int64_t)k0 + a.split_keys);
+    const uint8_t* mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+
+    bf16x8 qf[2][KS];
+    const bf16* q = (const bf16*)a.q + b * a.q_b + i * a.q_s + (int64_t)(hk * a.G + g) * 2 * a.q_h;
 #pragma unroll
-    for (int m = 0; m < 2; ++m) sum[m] = half_sum(sum[m]);
-    if (mine >= a.rows) return;
-    if (a.splits > 1) {
-        const RowPart part(a, split, bh, mine);
-        if (blockIdx.z == 0 && h == 0) part.stats(top, sum);
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+        for (int s = 0; s < KS; ++s) qf[m][s] = row_frag(q + m * a.q_h + 16 * s + 8 * h);
+
+    f32x16 o[2][NT];
+    float top[2], safe[2], sum[2];
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+    for (int m = 0; m < 2; ++m) {
+        top[m] = -INFINITY; safe[m] = 0.0f; sum[m] = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 16; e += 4)
-                    part.store(m, sum[m], dv0, 32 * t + 8 * (e >> 2) + 4 * h, DVT, o[m][t][e], o[m][t][e + 1], o[m][t][e + 2], o[m][t][e + 3]);
-        return;
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[m][t][e] = 0.0f;
     }
-    const RowOut<T> row(a, b, i, hk * a.G + g, dv0, dvn, sum);
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-            const float x[4] = {o[0][t][e], o[0][t][e + 1], o[0][t][e + 2], o[0][t][e + 3]};
-            const float y[4] = {o[1][t][e], o[1][t][e + 1], o[1][t][e + 2], o[1][t][e + 3]};
-            row.store(32 * t + 8 * (e >> 2) + 4 * h, x, y);
+
+    const bf16* kb = (const bf16*)a.k + b * a.k_b + (int64_t)hk * 2 * a.k_h;
+    const bf16* vb = (const bf16*)a.v + b * a.v_b + (int64_t)hk * a.v_h + dv0;
+    typedef Direct<BN, 2, DT, NW> Keys;
+    typedef Direct<BN, 1, DVT, NW> Values;
+    Keys kd;
+    Values vd;
+    kd.init(a.k_s, a.k_h);
+    vd.init(a.v_s, 0);
+    int krow[4], vcol[2];
+    Keys::row_lane(krow);
+    Values::col_lane(vcol);
+    uint8_t seen = 1;
+    const auto fetch = [&](int j0, int turn) {
+        bf16* kt = tiles + turn * Shape::TILE;
+        kd.load(kb, a.k_s, a.k_h, j0, n, kt);
+        vd.load(vb, a.v_s, 0, j0, n, kt + BN * 2 * DT);
+    };
+    const auto fetch_mask = [&](int j0) { if (mask && threadIdx.x < BN) seen = mask[min(j0 + (int)threadIdx.x, n - 1)]; };
+    const auto mark = [&](int j0, int slot) {
+        if (mask && threadIdx.x < BN) {
+            const uint64_t there = __ballot(j0 + (int)threadIdx.x < n && seen);
+            if (threadIdx.x < NB) words[slot * NB + threadIdx.x] = (uint32_t)(threadIdx.x ? there >> 32 : there);
         }
-    if (blockIdx.z == 0 && h == 0) row.stats(a, top, sum);
+    };
+    const auto after = [](int slot) { return slot == 2 ? 0 : slot + 1; };
+    int turn = 0, slot = 0;
+    if (k0 < k1) {
+        fetch(k0, 0);
+        fetch_mask(k0);
+        mark(k0, 0);
+        if (k0 + BN < k1) { fetch_mask(k0 + BN); mark(k0 + BN, 1); }
+    }
+    for (int j0 = k0; j0 < k1; j0 += BN, turn ^= 1, slot = after(slot)) {
+        __syncthreads();                               // this tile is there, the other one has been read
+        if (j0 + BN < k1) fetch(j0 + BN, turn ^ 1);
+        if (j0 + 2 * BN < k1) fetch_mask(j0 + 2 * BN);
+        bf16* kt = tiles + turn * Shape::TILE;
+        bf16* vt = kt + BN * 2 * DT;
+        if (mask) {
+            const uint32_t* wd = words + slot * NB;
+            bool all = true;
+#pragma unroll
+            for (int x = 0; x < NB; ++x) all = all && wd[x] == ~0u;
+            if (!all) {                                // values that the mask leaves out may be anything
+                Values::clear(vt, wd);
+                __syncthreads();
+            }
+        }
+#pragma unroll
+        for (int sub = 0; sub < NB; ++sub) {
+            const int js = j0 + 32 * sub;
+            if (js >= wmax) continue;
+            f32x16 s[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[m][e] = 0.0f;
+#pragma unroll
+                for (int t = 0; t < KS; ++t) {
+                    const int c = m * DT + 16 * t;
+                    s[m] = mma(s[m], row_frag(kt + krow[c / 16 % 4] + 32 * sub * 2 * DT + c / 64 * 64), qf[m][t]);
+                }
+            }
+            const uint32_t word = mask ? words[slot * NB + sub] : ~0u;
+            if (js + 32 > wmin || word != ~0u) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int j = 8 * (e >> 2) + 4 * h + (e & 3);
+                    const bool ok = js + j < lim && (word >> j & 1);
+                    s[0][e] = ok ? s[0][e] : -INFINITY;
+                    s[1][e] = ok ? s[1][e] : -INFINITY;
+                }
+            }
+            soften(s[0], a.scale2, top[0], safe[0], sum[0], o[0]);
+            soften(s[1], a.scale2, top[1], safe[1], sum[1], o[1]);
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                bf16x8 p0, p1;
+                to_frag(s[0], st, p0);
+                to_frag(s[1], st, p1);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const bf16x8 vf = col_frag<DVT>(vt + vcol[t % 2] + t / 2 * 64 + (32 * sub + 16 * st) * DVT);
+                    o[0][t] = mma(o[0][t], vf, p0);
+                    o[1][t] = mma(o[1][t], vf, p1);
+                }
+            }
+            settle();
+        }
+        if (j0 + 2 * BN < k1) mark(j0 + 2 * BN, after(after(slot)));
+    }
+    wide_end<bf16, NT, DVT>(a, b, bh, split, dv0, mine, i, hk * a.G + g, h, o, top, sum);
 }
 
 // Few rows: RT tiles of 16 to a wavefront, in products of 16 x 16.  A wavefront walks 32 keys at a time of its own, alone: its keys
@@ -602,6 +751,18 @@ int wide_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
     return launch_status();
 }
 
+template <int DT, int DVT>
+int direct_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
+{
+    constexpr size_t lds = DirectShape<DT, DVT>::LDS;
+    const auto kern = attn_direct<DT, DVT>;
+    const int rc = allow_lds(kern, lds);
+    if (rc) return rc;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv), (unsigned)p.splits, (unsigned)p.chunks),
+                       dim3(256), lds, stream, a);
+    return launch_status();
+}
+
 template <typename T, bool VEC, int DT, int DVT, int RT>
 int few_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
 {
@@ -617,6 +778,12 @@ int few_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
 template <typename T, bool VEC, int DT, int DVT>
 int fwd_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
 {
+    if constexpr (VEC && sizeof(T) == 2) {
+        // (a tile has to lie within what a buffer's offsets reach; values' rows beside each other)
+        const int64_t far = int64_t(1) << 22;
+        if (!p.few && a.D == DT && a.Dv % DVT == 0 && a.k_s < far && a.k_h < far * 128 && a.v_s >= DVT && a.v_s < far)
+            return direct_launch<DT, DVT>(a, p, stream);
+    }
     if (!p.few) return wide_launch<T, VEC, DT, DVT>(a, p, stream);
     return a.rows <= 16 ? few_launch<T, VEC, DT, DVT, 1>(a, p, stream) : few_launch<T, VEC, DT, DVT, 2>(a, p, stream);
 }

@@ -264,6 +264,66 @@ AttnArgs attn_args(const sconv_diffattn_desc_t& d, const void* q, const void* k,
 // Whether q, k and v can be read 16 bytes at a time.
 bool attn_vector(const AttnArgs& a, int type);
 
+// 16-bit tiles that go from memory to LDS directly: rows of W elements without padding, whose 16-byte chunks stand at chunk ^ (row & 7)
+// of every eight, so that lanes reading one column chunk of consecutive rows meet different banks.  A wavefront's load fills 1024
+// bytes in a row; each lane chooses the chunk of memory that belongs where its 16 bytes come to lie.  The buffer ends with the last
+// row's last part: with one part, and rows that do not overlap, rows that are not there come as zeros; with two parts they may come
+// as what lies between the parts.
+template <int ROWS, int PARTS, int W, int NW>
+struct Direct {
+    static constexpr int RW = PARTS * W, N = ROWS * RW * 2 / 1024 / NW;     // loads of a wavefront
+    static_assert(N * NW * 1024 == ROWS * RW * 2, "whole loads for every wavefront");
+    uint32_t off[N];
+    __device__ __forceinline__ void init(int64_t stride, int64_t part)
+    {
+        const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = ((i * NW + w) * 64 + l) * 8, row = at / RW, chunk = at % RW / 8;
+            const int from = (chunk & ~7) | ((chunk ^ row) & 7), m = from / (W / 8), d = from % (W / 8) * 8;
+            off[i] = (uint32_t)(row * stride + m * part + d) * 2;
+        }
+    }
+    // rows j0 .. j0 + ROWS of base (uniform), of which `rows` exist
+    __device__ __forceinline__ void load(const bf16* base, int64_t stride, int64_t part, int j0, int rows, bf16* tile) const
+    {
+#if defined(__HIP_DEVICE_COMPILE__)                    // (the host's compiler does not know buffer resources)
+        typedef __attribute__((address_space(3))) void lds_t;
+        const int64_t left = ((int64_t)(rows - j0 - 1) * stride + (PARTS - 1) * part + W) * 2, most = (int64_t)1 << 31;
+        const uint64_t at = (uint64_t)(base + (int64_t)j0 * stride);
+        const uint64_t p = ((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, __builtin_amdgcn_readfirstlane((uint32_t)(left < most ? left : most)), 0x00027000);
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_t*)(tile + (i * NW + w) * 512), 16, off[i], 0, 0, 0);
+#endif
+    }
+    // a row's fragment: row l % 32 of the tile, columns c .. c + 7 + 8 (l / 32): tile + at[c / 16 % 4] + c / 64 * 64
+    __device__ __forceinline__ static void row_lane(int (&at)[4])
+    {
+        const int l = threadIdx.x & 63, row = l & 31, h = l >> 5;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at[i] = row * RW + ((2 * i + h) ^ (row & 7)) * 8;
+    }
+    // a column fragment (col_frag): columns 32 t.., rows from 16 s: tile + at[t % 2] + t / 2 * 64 + 16 s * RW
+    __device__ __forceinline__ static void col_lane(int (&at)[2])
+    {
+        const int l = threadIdx.x & 63, row = 4 * (l >> 5) + ((l & 15) >> 2);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) at[i] = row * RW + (((4 * i + 2 * ((l >> 4) & 1) + ((l & 3) >> 1)) ^ (row & 7)) * 8) + (l & 1) * 4;
+    }
+    // clears the rows whose bit is 0
+    __device__ __forceinline__ static void clear(bf16* tile, const uint32_t* words)
+    {
+#pragma unroll
+        for (int e = threadIdx.x; e < ROWS * RW / 8; e += 64 * NW) {
+            const int row = e / (RW / 8);
+            if (!(words[row >> 5] >> (row & 31) & 1)) *(u32x4*)(tile + e * 8) = u32x4{0, 0, 0, 0};
+        }
+    }
+};
+
 // Sets the dynamic LDS size a kernel may ask for, where it is above the default.
 template <typename K>
 inline int allow_lds(K kern, size_t bytes)
