@@ -366,8 +366,8 @@ __global__ __launch_bounds__(256, (DT <= 64 ? 2 : 1)) void attn_direct(AttnArgs 
             }
         }
 #pragma unroll
-        for (int sub = 0; sub < NB; ++sub) {
-            const int js = j0 + 32 * sub;
+        for (int x = 0; x < NB; ++x) {
+            const int js = j0 + 32 * x;
             if (js >= wmax) continue;
             f32x16 s[2];
 #pragma unroll
@@ -377,31 +377,55 @@ __global__ __launch_bounds__(256, (DT <= 64 ? 2 : 1)) void attn_direct(AttnArgs 
 #pragma unroll
                 for (int t = 0; t < KS; ++t) {
                     const int c = m * DT + 16 * t;
-                    s[m] = mma(s[m], row_frag(kt + krow[c / 16 % 4] + 32 * sub * 2 * DT + c / 64 * 64), qf[m][t]);
+                    s[m] = mma(s[m], row_frag(kt + krow[c / 16 % 4] + 32 * x * 2 * DT + c / 64 * 64), qf[m][t]);
                 }
             }
-            const uint32_t word = mask ? words[slot * NB + sub] : ~0u;
-            if (js + 32 > wmin || word != ~0u) {
+            if (js + 32 > wmin || mask) {
+                const uint32_t bits = seen_bits(js, lim, mask ? words[slot * NB + x] : ~0u) >> (4 * h);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int j = 8 * (e >> 2) + 4 * h + (e & 3);
-                    const bool ok = js + j < lim && (word >> j & 1);
-                    s[0][e] = ok ? s[0][e] : -INFINITY;
-                    s[1][e] = ok ? s[1][e] : -INFINITY;
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[m][e] = masked(s[m][e], bits, 8 * (e >> 2) + (e & 3), 0xff800000u);
+            }
+            float mx[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                mx[m] = s[m][0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) mx[m] = fmaxf(mx[m], s[m][e]);
+                mx[m] = half_max(mx[m]) * a.scale2;
+            }
+            if (__any(mx[0] > top[0] + 8.0f || mx[1] > top[1] + 8.0f)) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const float grown = fmaxf(top[m], mx[m]);
+                    safe[m] = grown == -INFINITY ? 0.0f : grown;
+                    const float f = __builtin_amdgcn_exp2f(top[m] - safe[m]);
+                    top[m] = grown;
+                    sum[m] *= f;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[m][t][e] *= f;
                 }
             }
-            soften(s[0], a.scale2, top[0], safe[0], sum[0], o[0]);
-            soften(s[1], a.scale2, top[1], safe[1], sum[1], o[1]);
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                bf16x8 p0, p1;
-                to_frag(s[0], st, p0);
-                to_frag(s[1], st, p1);
+                bf16x8 p[2];
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float v = __builtin_amdgcn_exp2f(fmaf(s[m][8 * st + e], a.scale2, -safe[m]));
+                        sum[m] += v;
+                        p[m][e] = (bf16)v;
+                    }
+                }
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const bf16x8 vf = col_frag<DVT>(vt + vcol[t % 2] + t / 2 * 64 + (32 * sub + 16 * st) * DVT);
-                    o[0][t] = mma(o[0][t], vf, p0);
-                    o[1][t] = mma(o[1][t], vf, p1);
+                    const bf16x8 vf = col_frag<DVT>(vt + vcol[t % 2] + t / 2 * 64 + (32 * x + 16 * st) * DVT);
+                    o[0][t] = mma(o[0][t], vf, p[0]);
+                    o[1][t] = mma(o[1][t], vf, p[1]);
                 }
             }
             settle();

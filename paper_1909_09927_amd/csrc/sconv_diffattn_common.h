@@ -217,6 +217,18 @@ __device__ __forceinline__ float quarter_sum(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Which of 32 keys from js on a query sees that sees `lim` of them, as bits; and what the others' scores become.
+__device__ __forceinline__ uint32_t seen_bits(int js, int lim, uint32_t word)
+{
+    const int left = lim - js;
+    return left >= 32 ? word : left <= 0 ? 0u : word & ((1u << left) - 1u);
+}
+__device__ __forceinline__ float masked(float v, uint32_t bits, int pos, uint32_t other)
+{
+    const uint32_t m = (uint32_t)((int32_t)(bits << (31 - pos)) >> 31);      // all ones where bit pos is set
+    return __uint_as_float((__float_as_uint(v) & m) | (other & ~m));
+}
+
 // Keys of request b that exist.
 __device__ __forceinline__ int keys_of(const AttnArgs& a, int b) { return a.len ? min(max(a.len[b], 0), a.Sk) : a.Sk; }
 // How many of its n keys query i sees, the mask aside.
@@ -264,8 +276,9 @@ AttnArgs attn_args(const sconv_diffattn_desc_t& d, const void* q, const void* k,
 // Whether q, k and v can be read 16 bytes at a time.
 bool attn_vector(const AttnArgs& a, int type);
 
-// 16-bit tiles that go from memory to LDS directly: rows of W elements without padding, whose 16-byte chunks stand at chunk ^ (row & 7)
-// of every eight, so that lanes reading one column chunk of consecutive rows meet different banks.  A wavefront's load fills 1024
+// 16-bit tiles that go from memory to LDS directly: rows of W elements without padding, whose 16-byte chunks stand at chunk ^ turn(row)
+// of every eight.  turn() differs over eight rows, for lanes that read one chunk of each, and by whole 32 bytes over four, for
+// the transposing read of four rows: neither meets a bank twice.  A wavefront's load fills 1024
 // bytes in a row; each lane chooses the chunk of memory that belongs where its 16 bytes come to lie.  The buffer ends with the last
 // row's last part: with one part, and rows that do not overlap, rows that are not there come as zeros; with two parts they may come
 // as what lies between the parts.
@@ -274,13 +287,14 @@ struct Direct {
     static constexpr int RW = PARTS * W, N = ROWS * RW * 2 / 1024 / NW;     // loads of a wavefront
     static_assert(N * NW * 1024 == ROWS * RW * 2, "whole loads for every wavefront");
     uint32_t off[N];
+    __device__ __forceinline__ static int turn(int row) { return (row & 3) << 1 | (row >> 2 & 1); }
     __device__ __forceinline__ void init(int64_t stride, int64_t part)
     {
         const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int at = ((i * NW + w) * 64 + l) * 8, row = at / RW, chunk = at % RW / 8;
-            const int from = (chunk & ~7) | ((chunk ^ row) & 7), m = from / (W / 8), d = from % (W / 8) * 8;
+            const int from = chunk ^ turn(row), m = from / (W / 8), d = from % (W / 8) * 8;
             off[i] = (uint32_t)(row * stride + m * part + d) * 2;
         }
     }
@@ -304,14 +318,14 @@ struct Direct {
     {
         const int l = threadIdx.x & 63, row = l & 31, h = l >> 5;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) at[i] = row * RW + ((2 * i + h) ^ (row & 7)) * 8;
+        for (int i = 0; i < 4; ++i) at[i] = row * RW + ((2 * i + h) ^ turn(row)) * 8;
     }
     // a column fragment (col_frag): columns 32 t.., rows from 16 s: tile + at[t % 2] + t / 2 * 64 + 16 s * RW
     __device__ __forceinline__ static void col_lane(int (&at)[2])
     {
         const int l = threadIdx.x & 63, row = 4 * (l >> 5) + ((l & 15) >> 2);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) at[i] = row * RW + (((4 * i + 2 * ((l >> 4) & 1) + ((l & 3) >> 1)) ^ (row & 7)) * 8) + (l & 1) * 4;
+        for (int i = 0; i < 2; ++i) at[i] = row * RW + (((4 * i + 2 * ((l >> 4) & 1) + ((l & 3) >> 1)) ^ turn(row)) * 8) + (l & 1) * 4;
     }
     // clears the rows whose bit is 0
     __device__ __forceinline__ static void clear(bf16* tile, const uint32_t* words)
