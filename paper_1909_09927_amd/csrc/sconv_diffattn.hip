@@ -355,12 +355,14 @@ __global__ __launch_bounds__(256, (DT <= 64 ? 2 : 1)) void attn_direct(AttnArgs 
         if (j0 + 2 * BN < k1) fetch_mask(j0 + 2 * BN);
         bf16* kt = tiles + turn * Shape::TILE;
         bf16* vt = kt + BN * 2 * DT;
+        int stop = wmax;
         if (mask) {
             const uint32_t* wd = words + slot * NB;
-            bool all = true;
+            bool all = true, none = true;
 #pragma unroll
-            for (int x = 0; x < NB; ++x) all = all && wd[x] == ~0u;
-            if (!all) {                                // values that the mask leaves out may be anything
+            for (int x = 0; x < NB; ++x) { all = all && wd[x] == ~0u; none = none && wd[x] == 0; }
+            if (none) stop = 0;                        // nothing to do here
+            else if (!all) {                           // values that the mask leaves out may be anything
                 Values::clear(vt, wd);
                 __syncthreads();
             }
@@ -368,7 +370,7 @@ __global__ __launch_bounds__(256, (DT <= 64 ? 2 : 1)) void attn_direct(AttnArgs 
 #pragma unroll
         for (int x = 0; x < NB; ++x) {
             const int js = j0 + 32 * x;
-            if (js >= wmax) continue;
+            if (js >= stop) continue;
             f32x16 s[2];
 #pragma unroll
             for (int m = 0; m < 2; ++m) {

@@ -65,6 +65,58 @@ __global__ __launch_bounds__(256) void attn_dlam(const float* part, int B, int H
     if (threadIdx.x == 0) dlam[h] = 0.0f - ((t[0] + t[1]) + (t[2] + t[3]));
 }
 
+// The ends of the two kernels below: a lane's query or key.
+template <typename T, int NT>
+__device__ __forceinline__ void rows_end(const AttnArgs& a, int b, int i, int head, int mine, int h, int64_t stat, float spread,
+                                         const f32x16 (&acc)[2][NT])
+{
+    spread = half_sum(spread);
+    if (mine >= a.rows) return;
+    if (h == 0) a.dlam_part[stat] = spread;
+    T* dq = (T*)a.dq + (((int64_t)b * a.Sq + i) * a.H + head) * 2 * a.D;
+    const bool v4 = a.ovec && a.D % 4 == 0;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                float x[4];
+#pragma unroll
+                for (int z = 0; z < 4; ++z) x[z] = acc[m][t][e + z] * a.scale;
+                store4(dq + m * a.D, 32 * t + 8 * (e >> 2) + 4 * h, a.D, v4, x);
+            }
+}
+
+template <typename T, int NT, int VT, int WHAT>
+__device__ __forceinline__ void keys_end(const AttnArgs& a, int b, int hk, int j, int h, const f32x16 (&dk)[2][NT], const f32x16 (&dv)[VT])
+{
+    if (j >= a.Sk) return;
+    T* kout = (T*)a.dk + (((int64_t)b * a.Sk + j) * a.Hkv + hk) * 2 * a.D;
+    T* vout = (T*)a.dv + (((int64_t)b * a.Sk + j) * a.Hkv + hk) * a.Dv;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        if (!(WHAT >> (m + 1) & 1)) continue;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                float x[4];
+#pragma unroll
+                for (int z = 0; z < 4; ++z) x[z] = dk[m][t][e + z] * a.scale;
+                store4(kout + m * a.D, 32 * t + 8 * (e >> 2) + 4 * h, a.D, a.ovec && a.D % 4 == 0, x);
+            }
+    }
+    if (WHAT & 1)
+#pragma unroll
+        for (int t = 0; t < VT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const float x[4] = {dv[t][e], dv[t][e + 1], dv[t][e + 2], dv[t][e + 3]};
+                store4(vout, 32 * t + 8 * (e >> 2) + 4 * h, a.Dv, a.ovec && a.Dv % 4 == 0, x);
+            }
+}
+
 template <typename T, bool VEC, int DT>
 __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
 {
@@ -182,22 +234,7 @@ __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
         }
         settle();
     }
-    spread = half_sum(spread);
-    if (mine >= a.rows) return;
-    if (h == 0) a.dlam_part[stat] = spread;
-    T* dq = (T*)a.dq + (((int64_t)b * a.Sq + i) * a.H + head) * 2 * a.D;
-    const bool v4 = a.ovec && a.D % 4 == 0;
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                float x[4];
-#pragma unroll
-                for (int z = 0; z < 4; ++z) x[z] = acc[m][t][e + z] * a.scale;
-                store4(dq + m * a.D, 32 * t + 8 * (e >> 2) + 4 * h, a.D, v4, x);
-            }
+    rows_end<T, NT>(a, b, i, head, mine, h, stat, spread, acc);
 }
 
 // WHAT: 1: dv, 2: dk of the first map, 4: of the second (all three where their sums fit the registers).
@@ -354,30 +391,315 @@ __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
         }
         settle();
     }
-    if (j >= a.Sk) return;
-    T* kout = (T*)a.dk + (((int64_t)b * a.Sk + j) * a.Hkv + hk) * 2 * a.D;
-    T* vout = (T*)a.dv + (((int64_t)b * a.Sk + j) * a.Hkv + hk) * a.Dv;
+    keys_end<T, NT, VT, WHAT>(a, b, hk, j, h, dk, dv);
+}
+
+// The same two in 16 bits, whole vectors everywhere, whose tiles go to LDS directly.
+template <int DT>
+__global__ __launch_bounds__(256, 2) void attn_rows_direct(AttnArgs a)
+{
+    constexpr int NW = 4, BN = 64, NB = BN / 32, DVT = 2 * DT, KS = DT / 16, VS = DVT / 16, NT = DT / 32, TILE = BN * 2 * DVT;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    bf16* tiles = (bf16*)lds;
+    uint32_t* words = (uint32_t*)(tiles + 2 * TILE);   // [3][NB]
+
+    const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
+    const int tile = a.row_tiles - 1 - blockIdx.x / bh_all;
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, h = l >> 5;
+    const int mine = tile * 32 * NW + 32 * w + (l & 31), r = min(mine, a.rows - 1), i = r / a.G, g = r - i * a.G;
+    const int head = hk * a.G + g, n = keys_of(a, b);
+    const int64_t stat = ((int64_t)b * a.H + head) * a.Sq + i, half = (int64_t)a.B * a.H * a.Sq;
+    const float lse0 = a.lse_in[stat] * LOG2E, lse1 = a.lse_in[half + stat] * LOG2E;
+    const float d0 = a.delta[stat], d1 = a.delta[half + stat], lam = a.lam[head];
+    const bool none = lse0 == -INFINITY;
+    const int see = limit_of(a, i, n), lim = none ? 0 : see;
+    const int wmin = __any(none) ? 0 : __builtin_amdgcn_readfirstlane(see), wmax = __builtin_amdgcn_readlane(see, 31);
+    const int k1 = limit_of(a, min(tile * 32 * NW + 32 * NW - 1, a.rows - 1) / a.G, n);
+    const uint8_t* mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+
+    bf16x8 qf[2][KS], gf[VS];
+    const bf16* q = (const bf16*)a.q + b * a.q_b + i * a.q_s + (int64_t)head * 2 * a.q_h;
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-        if (!(m ? DK1 : DK0)) continue;
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[m][s] = row_frag(q + m * a.q_h + 16 * s + 8 * h);
+    const bf16* go = (const bf16*)a.dout + (((int64_t)b * a.Sq + i) * a.H + head) * a.Dv;
+#pragma unroll
+    for (int s = 0; s < VS; ++s) gf[s] = row_frag(go + 16 * s + 8 * h);
+
+    f32x16 acc[2][NT];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                float x[4];
-#pragma unroll
-                for (int z = 0; z < 4; ++z) x[z] = dk[m][t][e + z] * a.scale;
-                store4(kout + m * a.D, 32 * t + 8 * (e >> 2) + 4 * h, a.D, a.ovec && a.D % 4 == 0, x);
-            }
+            for (int e = 0; e < 16; ++e) acc[m][t][e] = 0.0f;
+    float spread = 0.0f;
+
+    const bf16* kb = (const bf16*)a.k + b * a.k_b + (int64_t)hk * 2 * a.k_h;
+    const bf16* vb = (const bf16*)a.v + b * a.v_b + (int64_t)hk * a.v_h;
+    typedef Direct<BN, 2, DT, NW> Keys;
+    typedef Direct<BN, 1, DVT, NW> Values;
+    Keys kd;
+    Values vd;
+    kd.init(a.k_s, a.k_h);
+    vd.init(a.v_s, 0);
+    int row4[4], col2[2];                              // (both tiles' rows have 2 DT elements)
+    Keys::row_lane(row4);
+    Keys::col_lane(col2);
+    uint8_t seen = 1;
+    const auto fetch = [&](int j0, int turn) {
+        bf16* kt = tiles + turn * TILE;
+        kd.load(kb, a.k_s, a.k_h, j0, n, kt);
+        vd.load(vb, a.v_s, 0, j0, n, kt + BN * DVT);
+    };
+    const auto fetch_mask = [&](int j0) { if (mask && threadIdx.x < BN) seen = mask[min(j0 + (int)threadIdx.x, n - 1)]; };
+    const auto mark = [&](int j0, int slot) {
+        if (mask && threadIdx.x < BN) {
+            const uint64_t there = __ballot(j0 + (int)threadIdx.x < n && seen);
+            if (threadIdx.x < NB) words[slot * NB + threadIdx.x] = (uint32_t)(threadIdx.x ? there >> 32 : there);
+        }
+    };
+    const auto after = [](int slot) { return slot == 2 ? 0 : slot + 1; };
+    int turn = 0, slot = 0;
+    if (k1 > 0) {
+        fetch(0, 0);
+        fetch_mask(0);
+        mark(0, 0);
+        if (BN < k1) { fetch_mask(BN); mark(BN, 1); }
     }
-    if (DV)
+    for (int j0 = 0; j0 < k1; j0 += BN, turn ^= 1, slot = after(slot)) {
+        __syncthreads();
+        if (j0 + BN < k1) fetch(j0 + BN, turn ^ 1);
+        if (j0 + 2 * BN < k1) fetch_mask(j0 + 2 * BN);
+        bf16* kt = tiles + turn * TILE;
+        bf16* vt = kt + BN * DVT;
+        const uint32_t* wd = words + slot * NB;
+        if (mask) {
+            bool all = true;
 #pragma unroll
-        for (int t = 0; t < VT; ++t)
+            for (int x = 0; x < NB; ++x) all = all && wd[x] == ~0u;
+            if (!all) {
+                Keys::clear(kt, wd);
+                Values::clear(vt, wd);
+                __syncthreads();
+            }
+        }
+#pragma unroll 1
+        for (int x = 0; x < NB; ++x) {
+            const int js = j0 + 32 * x;
+            const uint32_t word = mask ? __builtin_amdgcn_readfirstlane(wd[x]) : ~0u;
+            if (js >= wmax || word == 0) continue;
+            const bf16* ks = kt + 32 * x * DVT;
+            const bf16* vs = vt + 32 * x * DVT;
+            f32x16 s0, s1, gt;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s0[e] = s1[e] = gt[e] = 0.0f;
+#pragma unroll
+            for (int t = 0; t < KS; ++t) {
+                const int c0 = 16 * t, c1 = DT + 16 * t;
+                s0 = mma(s0, row_frag(ks + row4[c0 / 16 % 4] + c0 / 64 * 64), qf[0][t]);
+                s1 = mma(s1, row_frag(ks + row4[c1 / 16 % 4] + c1 / 64 * 64), qf[1][t]);
+            }
+#pragma unroll
+            for (int t = 0; t < VS; ++t) gt = mma(gt, row_frag(vs + row4[t % 4] + t / 4 * 64), gf[t]);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s0[e] = __builtin_amdgcn_exp2f(fmaf(s0[e], a.scale2, -lse0));
+                s1[e] = __builtin_amdgcn_exp2f(fmaf(s1[e], a.scale2, -lse1));
+            }
+            if (js + 32 > wmin || word != ~0u) {
+                const uint32_t bits = seen_bits(js, lim, word) >> (4 * h);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int pos = 8 * (e >> 2) + (e & 3);
+                    s0[e] = masked(s0[e], bits, pos, 0);
+                    s1[e] = masked(s1[e], bits, pos, 0);
+                    gt[e] = masked(gt[e], bits, pos, 0);
+                }
+            }
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                bf16x8 f0, f1;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float gv = gt[8 * st + e], p1 = s1[8 * st + e];
+                    spread = fmaf(p1, gv, spread);
+                    f0[e] = (bf16)(s0[8 * st + e] * (gv - d0));
+                    f1[e] = (bf16)(p1 * (-lam * (gv - d1)));
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const int c0 = 32 * t, c1 = DT + 32 * t;
+                    acc[0][t] = mma(acc[0][t], col_frag<DVT>(ks + col2[c0 / 32 % 2] + c0 / 64 * 64 + 16 * st * DVT), f0);
+                    acc[1][t] = mma(acc[1][t], col_frag<DVT>(ks + col2[c1 / 32 % 2] + c1 / 64 * 64 + 16 * st * DVT), f1);
+                }
+            }
+            settle();
+        }
+        if (j0 + 2 * BN < k1) mark(j0 + 2 * BN, after(after(slot)));
+    }
+    rows_end<bf16, NT>(a, b, i, head, mine, h, stat, spread, acc);
+}
+
+template <int DT>
+__global__ __launch_bounds__(256, (DT == 32 ? 2 : 1)) void attn_keys_direct(AttnArgs a)
+{
+    constexpr int NW = 4, BM = 64, MB = BM / 32, DVT = 2 * DT, KS = DT / 16, VS = DVT / 16, NT = DT / 32, VT = DVT / 32;
+    constexpr int TILE = BM * 2 * DVT;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    bf16* tiles = (bf16*)lds;
+    float* stats = (float*)(tiles + 2 * TILE);         // [2][4][BM]: lse of both maps (log2), d of both
+    uint32_t* words = (uint32_t*)(stats + 8 * BM);     // [2][MB]
+
+    const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
+    const int j0 = (int)(blockIdx.x / bh_all) * 32 * NW;
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, h = l >> 5;
+    const int n = keys_of(a, b), j = j0 + 32 * w + (l & 31), in = min(j, a.Sk - 1);
+    const bool ok = j < n && (!a.mask || a.mask[b * a.mask_b + in]);
+    const bool all_ok = __all(ok), any_ok = __any(ok);
+    const int64_t off = (int64_t)a.Sq - n;
+    const int seen_by = a.causal ? (int)std::max<int64_t>(0, j + off) : 0;
+    const int wfirst = __builtin_amdgcn_readfirstlane(seen_by), wlast = __builtin_amdgcn_readlane(seen_by, 31);
+    const int start = a.causal ? (int)std::max<int64_t>(0, j0 + off) / BM * BM : 0;
+
+    bf16x8 kf[2][KS], vf[VS];
+    const bf16* k = (const bf16*)a.k + b * a.k_b + in * a.k_s + (int64_t)hk * 2 * a.k_h;
+    const bf16* v = (const bf16*)a.v + b * a.v_b + in * a.v_s + (int64_t)hk * a.v_h;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        kf[0][s] = row_frag(k + 16 * s + 8 * h);
+        kf[1][s] = row_frag(k + a.k_h + 16 * s + 8 * h);
+    }
+#pragma unroll
+    for (int s = 0; s < VS; ++s) vf[s] = row_frag(v + 16 * s + 8 * h);
+
+    f32x16 dk[2][NT], dv[VT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dk[0][t][e] = dk[1][t][e] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dv[t][e] = 0.0f;
+
+    typedef Direct<BM, 2, DT, NW> Queries;
+    typedef Direct<BM, 1, DVT, NW> Grads;
+    Queries qd;
+    Grads gd;
+    const int64_t g_s = (int64_t)a.H * a.Dv;
+    qd.init(a.q_s, a.q_h);
+    gd.init(g_s, 0);
+    int row4[4], col2[2];
+    Queries::row_lane(row4);
+    Queries::col_lane(col2);
+    float stat = 0.0f, sum = 0.0f;
+    const int64_t half = (int64_t)a.B * a.H * a.Sq;
+    const auto fetch = [&](int g, int i0, int turn) {
+        const int head = hk * a.G + g;
+        bf16* qt = tiles + turn * TILE;
+        qd.load((const bf16*)a.q + b * a.q_b + (int64_t)head * 2 * a.q_h, a.q_s, a.q_h, i0, a.Sq, qt);
+        gd.load((const bf16*)a.dout + ((int64_t)b * a.Sq * a.H + head) * a.Dv, g_s, 0, i0, a.Sq, qt + BM * DVT);
+        // thread: statistic x row
+        const int i = min(i0 + (int)(threadIdx.x % BM), a.Sq - 1), what = threadIdx.x / BM;
+        const int64_t at = ((int64_t)b * a.H + head) * a.Sq + i;
+        sum = a.lse_in[at];
+        stat = what == 0 ? sum * LOG2E : what == 1 ? a.lse_in[half + at] * LOG2E : a.delta[at + (what == 3 ? half : 0)];
+    };
+    const auto mark = [&](int i0, int turn) {
+        const bool there = i0 + (int)(threadIdx.x % BM) < a.Sq && sum != -INFINITY;
+        stats[turn * 4 * BM + threadIdx.x] = there ? stat : 0.0f;
+        const uint64_t bits = __ballot(there);
+        if (threadIdx.x < MB) words[turn * MB + threadIdx.x] = (uint32_t)(threadIdx.x ? bits >> 32 : bits);
+    };
+    const bool any = j0 < n && start < a.Sq;
+    int turn = 0, g = 0, i0 = start;
+    if (any) { fetch(0, start, 0); mark(start, 0); }
+    while (any && g < a.G) {
+        __syncthreads();
+        const int at = i0, was = g;
+        i0 += BM;
+        if (i0 >= a.Sq) { i0 = start; ++g; }
+        if (g < a.G) fetch(g, i0, turn ^ 1);
+        bf16* qt = tiles + turn * TILE;
+        bf16* gt = qt + BM * DVT;
+        bool whole = true;
+#pragma unroll
+        for (int x = 0; x < MB; ++x) whole = whole && words[turn * MB + x] == ~0u;
+        if (!whole) {                                  // rows that see nothing may hold anything
+            Queries::clear(qt, words + turn * MB);
+            Grads::clear(gt, words + turn * MB);
+            __syncthreads();
+        }
+        const float lam = a.lam[hk * a.G + was];
+#pragma unroll 1
+        for (int x = 0; x < MB; ++x) {
+            const int is = at + 32 * x;
+            if (is + 32 <= wfirst || is >= a.Sq || !any_ok) continue;
+            const bf16* qs = qt + 32 * x * DVT;
+            const bf16* gs = gt + 32 * x * DVT;
+            const float* st = stats + turn * 4 * BM + 32 * x + 4 * h;
+            f32x16 s0, s1, gg;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s0[e] = s1[e] = gg[e] = 0.0f;
+#pragma unroll
+            for (int t = 0; t < KS; ++t) {
+                const int c0 = 16 * t, c1 = DT + 16 * t;
+                s0 = mma(s0, row_frag(qs + row4[c0 / 16 % 4] + c0 / 64 * 64), kf[0][t]);
+                s1 = mma(s1, row_frag(qs + row4[c1 / 16 % 4] + c1 / 64 * 64), kf[1][t]);
+            }
+#pragma unroll
+            for (int t = 0; t < VS; ++t) gg = mma(gg, row_frag(gs + row4[t % 4] + t / 4 * 64), vf[t]);
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
-                const float x[4] = {dv[t][e], dv[t][e + 1], dv[t][e + 2], dv[t][e + 3]};
-                store4(vout, 32 * t + 8 * (e >> 2) + 4 * h, a.Dv, a.ovec && a.Dv % 4 == 0, x);
+                const f32x4 l0 = *(const f32x4*)(st + 2 * e), l1 = *(const f32x4*)(st + BM + 2 * e);
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    s0[e + z] = __builtin_amdgcn_exp2f(fmaf(s0[e + z], a.scale2, -l0[z]));
+                    s1[e + z] = __builtin_amdgcn_exp2f(fmaf(s1[e + z], a.scale2, -l1[z]));
+                }
             }
+            if (!all_ok || is < wlast) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const bool in_sum = ok && is + 8 * (e >> 2) + 4 * h + (e & 3) >= seen_by;
+                    s0[e] = in_sum ? s0[e] : 0.0f;
+                    s1[e] = in_sum ? s1[e] : 0.0f;
+                    gg[e] = in_sum ? gg[e] : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                bf16x8 f, f0, f1;
+#pragma unroll
+                for (int e = 0; e < 8; e += 4) {
+                    const f32x4 d0 = *(const f32x4*)(st + 2 * BM + 2 * (8 * y + e)), d1 = *(const f32x4*)(st + 3 * BM + 2 * (8 * y + e));
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        const int u = 8 * y + e + z;
+                        const float p1 = -lam * s1[u];
+                        f[e + z] = (bf16)(s0[u] + p1);
+                        f0[e + z] = (bf16)(s0[u] * (gg[u] - d0[z]));
+                        f1[e + z] = (bf16)(p1 * (gg[u] - d1[z]));
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < VT; ++t)
+                    dv[t] = mma(dv[t], col_frag<DVT>(gs + col2[t % 2] + t / 2 * 64 + 16 * y * DVT), f);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const int c0 = 32 * t, c1 = DT + 32 * t;
+                    dk[0][t] = mma(dk[0][t], col_frag<DVT>(qs + col2[c0 / 32 % 2] + c0 / 64 * 64 + 16 * y * DVT), f0);
+                    dk[1][t] = mma(dk[1][t], col_frag<DVT>(qs + col2[c1 / 32 % 2] + c1 / 64 * 64 + 16 * y * DVT), f1);
+                }
+            }
+            settle();
+        }
+        if (g < a.G) mark(i0, turn ^ 1);
+        turn ^= 1;
+    }
+    keys_end<bf16, NT, VT, 7>(a, b, hk, j, h, dk, dv);
 }
 
 template <typename T, bool VEC, int DT, int WHAT>
@@ -391,10 +713,31 @@ int keys_launch(const AttnArgs& a, hipStream_t stream)
     return launch_status();
 }
 
+template <int DT>
+int direct_main(const AttnArgs& a, hipStream_t stream)
+{
+    constexpr size_t tiles = (size_t)2 * 64 * 4 * DT * sizeof(bf16), keys = tiles + 8 * 64 * 4 + 4 * 4, rows = tiles + 3 * 2 * 4;
+    int rc = allow_lds(attn_keys_direct<DT>, keys);
+    if (rc) return rc;
+    hipLaunchKernelGGL((attn_keys_direct<DT>), dim3((unsigned)((int64_t)((a.Sk + 127) / 128) * a.B * a.Hkv)), dim3(256), keys, stream, a);
+    rc = launch_status();
+    if (!rc) rc = allow_lds(attn_rows_direct<DT>, rows);
+    if (rc) return rc;
+    hipLaunchKernelGGL((attn_rows_direct<DT>), dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv)), dim3(256), rows, stream, a);
+    return launch_status();
+}
+
 template <typename T, bool VEC, int DT>
 int bwd_main(const AttnArgs& a, hipStream_t stream)
 {
     int rc = SCONV_OK;
+    if constexpr (VEC && sizeof(T) == 2 && DT <= 64) {
+        // (tiles' rows beside each other, and within what a buffer's offsets reach)
+        const int64_t far = int64_t(1) << 22;
+        if (a.Sq > 0 && a.Sk > 0 && a.D == DT && a.Dv == 2 * DT && a.k_h + DT <= a.k_s && a.q_h + DT <= a.q_s && a.v_s >= a.Dv &&
+            a.k_s < far && a.q_s < far && a.v_s < far && (int64_t)a.H * a.Dv < far)
+            return direct_main<DT>(a, stream);
+    }
     if (a.Sk > 0) {
         if constexpr (DT <= 64) rc = keys_launch<T, VEC, DT, 7>(a, stream);
         else {
