@@ -542,9 +542,13 @@ __global__ __launch_bounds__(256, 2) void attn_rows_direct(AttnArgs a)
     rows_end<bf16, NT>(a, b, i, head, mine, h, stat, spread, acc);
 }
 
-template <int DT>
-__global__ __launch_bounds__(256, (DT == 32 ? 2 : 1)) void attn_keys_direct(AttnArgs a)
+// (keys: WHAT as above.  At DT = 64 the sums and operands of all three leave room for one wavefront a SIMD only, which waits for
+// each of its own products; dv and dk apart form the weights twice, and are done sooner with two: 345 against 404 us.)  SUB:
+// tiles of 32 queries whose products stand in one straight line.
+template <int DT, int WHAT, int SUB>
+__global__ __launch_bounds__(256, 2) void attn_keys_direct(AttnArgs a)
 {
+    constexpr bool DV = WHAT & 1, DK = WHAT & 6;
     constexpr int NW = 4, BM = 64, MB = BM / 32, DVT = 2 * DT, KS = DT / 16, VS = DVT / 16, NT = DT / 32, VT = DVT / 32;
     constexpr int TILE = BM * 2 * DVT;
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -571,6 +575,7 @@ __global__ __launch_bounds__(256, (DT == 32 ? 2 : 1)) void attn_keys_direct(Attn
         kf[0][s] = row_frag(k + 16 * s + 8 * h);
         kf[1][s] = row_frag(k + a.k_h + 16 * s + 8 * h);
     }
+    if (DK)
 #pragma unroll
     for (int s = 0; s < VS; ++s) vf[s] = row_frag(v + 16 * s + 8 * h);
 
@@ -634,64 +639,88 @@ __global__ __launch_bounds__(256, (DT == 32 ? 2 : 1)) void attn_keys_direct(Attn
         }
         const float lam = a.lam[hk * a.G + was];
 #pragma unroll 1
-        for (int x = 0; x < MB; ++x) {
-            const int is = at + 32 * x;
-            if (is + 32 <= wfirst || is >= a.Sq || !any_ok) continue;
-            const bf16* qs = qt + 32 * x * DVT;
-            const bf16* gs = gt + 32 * x * DVT;
-            const float* st = stats + turn * 4 * BM + 32 * x + 4 * h;
-            f32x16 s0, s1, gg;
+        for (int x0 = 0; x0 < MB; x0 += SUB) {
+            const int is = at + 32 * x0;
+            if (is + 32 * SUB <= wfirst || is >= a.Sq || !any_ok) continue;
+            const float* st = stats + turn * 4 * BM + 32 * x0 + 4 * h;
+            const bf16* qx = qt + 32 * x0 * DVT;
+            const bf16* gx = gt + 32 * x0 * DVT;
+            f32x16 s0[SUB], s1[SUB], gg[SUB];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s0[e] = s1[e] = gg[e] = 0.0f;
+            for (int x = 0; x < SUB; ++x) {
+                const bf16* qs = qx + 32 * x * DVT;
+                const bf16* gs = gx + 32 * x * DVT;
 #pragma unroll
-            for (int t = 0; t < KS; ++t) {
-                const int c0 = 16 * t, c1 = DT + 16 * t;
-                s0 = mma(s0, row_frag(qs + row4[c0 / 16 % 4] + c0 / 64 * 64), kf[0][t]);
-                s1 = mma(s1, row_frag(qs + row4[c1 / 16 % 4] + c1 / 64 * 64), kf[1][t]);
-            }
+                for (int e = 0; e < 16; ++e) s0[x][e] = s1[x][e] = gg[x][e] = 0.0f;
 #pragma unroll
-            for (int t = 0; t < VS; ++t) gg = mma(gg, row_frag(gs + row4[t % 4] + t / 4 * 64), vf[t]);
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const f32x4 l0 = *(const f32x4*)(st + 2 * e), l1 = *(const f32x4*)(st + BM + 2 * e);
-#pragma unroll
-                for (int z = 0; z < 4; ++z) {
-                    s0[e + z] = __builtin_amdgcn_exp2f(fmaf(s0[e + z], a.scale2, -l0[z]));
-                    s1[e + z] = __builtin_amdgcn_exp2f(fmaf(s1[e + z], a.scale2, -l1[z]));
+                for (int t = 0; t < KS; ++t) {
+                    const int c0 = 16 * t, c1 = DT + 16 * t;
+                    s0[x] = mma(s0[x], row_frag(qs + row4[c0 / 16 % 4] + c0 / 64 * 64), kf[0][t]);
+                    s1[x] = mma(s1[x], row_frag(qs + row4[c1 / 16 % 4] + c1 / 64 * 64), kf[1][t]);
                 }
-            }
-            if (!all_ok || is < wlast) {
+                if (DK)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const bool in_sum = ok && is + 8 * (e >> 2) + 4 * h + (e & 3) >= seen_by;
-                    s0[e] = in_sum ? s0[e] : 0.0f;
-                    s1[e] = in_sum ? s1[e] : 0.0f;
-                    gg[e] = in_sum ? gg[e] : 0.0f;
-                }
+                    for (int t = 0; t < VS; ++t) gg[x] = mma(gg[x], row_frag(gs + row4[t % 4] + t / 4 * 64), vf[t]);
             }
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                bf16x8 f, f0, f1;
+            for (int x = 0; x < SUB; ++x)
 #pragma unroll
-                for (int e = 0; e < 8; e += 4) {
-                    const f32x4 d0 = *(const f32x4*)(st + 2 * BM + 2 * (8 * y + e)), d1 = *(const f32x4*)(st + 3 * BM + 2 * (8 * y + e));
+                for (int e = 0; e < 16; e += 4) {
+                    const f32x4 l0 = *(const f32x4*)(st + 32 * x + 2 * e), l1 = *(const f32x4*)(st + 32 * x + BM + 2 * e);
 #pragma unroll
                     for (int z = 0; z < 4; ++z) {
-                        const int u = 8 * y + e + z;
-                        const float p1 = -lam * s1[u];
-                        f[e + z] = (bf16)(s0[u] + p1);
-                        f0[e + z] = (bf16)(s0[u] * (gg[u] - d0[z]));
-                        f1[e + z] = (bf16)(p1 * (gg[u] - d1[z]));
+                        s0[x][e + z] = __builtin_amdgcn_exp2f(fmaf(s0[x][e + z], a.scale2, -l0[z]));
+                        s1[x][e + z] = __builtin_amdgcn_exp2f(fmaf(s1[x][e + z], a.scale2, -l1[z]));
                     }
                 }
+            if (!all_ok || is < wlast) {
 #pragma unroll
-                for (int t = 0; t < VT; ++t)
-                    dv[t] = mma(dv[t], col_frag<DVT>(gs + col2[t % 2] + t / 2 * 64 + 16 * y * DVT), f);
+                for (int x = 0; x < SUB; ++x) {
+                    // rows from `from` on of this 32 see the lane's key
+                    const int from = seen_by - is - 32 * x;
+                    const uint32_t bits = (!ok || from >= 32 ? 0u : from <= 0 ? ~0u : ~0u << from) >> (4 * h);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const int c0 = 32 * t, c1 = DT + 32 * t;
-                    dk[0][t] = mma(dk[0][t], col_frag<DVT>(qs + col2[c0 / 32 % 2] + c0 / 64 * 64 + 16 * y * DVT), f0);
-                    dk[1][t] = mma(dk[1][t], col_frag<DVT>(qs + col2[c1 / 32 % 2] + c1 / 64 * 64 + 16 * y * DVT), f1);
+                    for (int e = 0; e < 16; ++e) {
+                        const int pos = 8 * (e >> 2) + (e & 3);
+                        s0[x][e] = masked(s0[x][e], bits, pos, 0);
+                        s1[x][e] = masked(s1[x][e], bits, pos, 0);
+                        gg[x][e] = masked(gg[x][e], bits, pos, 0);
+                    }
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < SUB; ++x) {
+                const bf16* qs = qx + 32 * x * DVT;
+                const bf16* gs = gx + 32 * x * DVT;
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    if (DV) {
+                        bf16x8 f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[e] = (bf16)fmaf(-lam, s1[x][8 * y + e], s0[x][8 * y + e]);
+#pragma unroll
+                        for (int t = 0; t < VT; ++t)
+                            dv[t] = mma(dv[t], col_frag<DVT>(gs + col2[t % 2] + t / 2 * 64 + 16 * y * DVT), f);
+                    }
+                    if (DK) {
+                        bf16x8 f0, f1;
+#pragma unroll
+                        for (int e = 0; e < 8; e += 4) {
+                            const f32x4 d0 = *(const f32x4*)(st + 32 * x + 2 * BM + 2 * (8 * y + e)), d1 = *(const f32x4*)(st + 32 * x + 3 * BM + 2 * (8 * y + e));
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) {
+                                const int u = 8 * y + e + z;
+                                f0[e + z] = (bf16)(s0[x][u] * (gg[x][u] - d0[z]));
+                                f1[e + z] = (bf16)(s1[x][u] * (-lam * (gg[x][u] - d1[z])));
+                            }
+                        }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            const int c0 = 32 * t, c1 = DT + 32 * t;
+                            dk[0][t] = mma(dk[0][t], col_frag<DVT>(qs + col2[c0 / 32 % 2] + c0 / 64 * 64 + 16 * y * DVT), f0);
+                            dk[1][t] = mma(dk[1][t], col_frag<DVT>(qs + col2[c1 / 32 % 2] + c1 / 64 * 64 + 16 * y * DVT), f1);
+                        }
+                    }
                 }
             }
             settle();
@@ -699,7 +728,7 @@ __global__ __launch_bounds__(256, (DT == 32 ? 2 : 1)) void attn_keys_direct(Attn
         if (g < a.G) mark(i0, turn ^ 1);
         turn ^= 1;
     }
-    keys_end<bf16, NT, VT, 7>(a, b, hk, j, h, dk, dv);
+    keys_end<bf16, NT, VT, WHAT>(a, b, hk, j, h, dk, dv);
 }
 
 template <typename T, bool VEC, int DT, int WHAT>
@@ -713,17 +742,31 @@ int keys_launch(const AttnArgs& a, hipStream_t stream)
     return launch_status();
 }
 
+template <int DT, int WHAT, int SUB>
+int keys_direct_launch(const AttnArgs& a, hipStream_t stream)
+{
+    constexpr size_t lds = (size_t)2 * 64 * 4 * DT * sizeof(bf16) + 8 * 64 * 4 + 4 * 4;
+    const int rc = allow_lds(attn_keys_direct<DT, WHAT, SUB>, lds);
+    if (rc) return rc;
+    hipLaunchKernelGGL((attn_keys_direct<DT, WHAT, SUB>), dim3((unsigned)((int64_t)((a.Sk + 127) / 128) * a.B * a.Hkv)), dim3(256), lds,
+                       stream, a);
+    return launch_status();
+}
+
 template <int DT>
 int direct_main(const AttnArgs& a, hipStream_t stream)
 {
-    constexpr size_t tiles = (size_t)2 * 64 * 4 * DT * sizeof(bf16), keys = tiles + 8 * 64 * 4 + 4 * 4, rows = tiles + 3 * 2 * 4;
-    int rc = allow_lds(attn_keys_direct<DT>, keys);
+    int rc;
+    if constexpr (DT == 32) rc = keys_direct_launch<DT, 7, 1>(a, stream);
+    else {
+        rc = keys_direct_launch<DT, 1, 2>(a, stream);
+        if (!rc) rc = keys_direct_launch<DT, 6, 1>(a, stream);
+    }
     if (rc) return rc;
-    hipLaunchKernelGGL((attn_keys_direct<DT>), dim3((unsigned)((int64_t)((a.Sk + 127) / 128) * a.B * a.Hkv)), dim3(256), keys, stream, a);
-    rc = launch_status();
-    if (!rc) rc = allow_lds(attn_rows_direct<DT>, rows);
+    constexpr size_t lds = (size_t)2 * 64 * 4 * DT * sizeof(bf16) + 3 * 2 * 4;
+    rc = allow_lds(attn_rows_direct<DT>, lds);
     if (rc) return rc;
-    hipLaunchKernelGGL((attn_rows_direct<DT>), dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv)), dim3(256), rows, stream, a);
+    hipLaunchKernelGGL((attn_rows_direct<DT>), dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv)), dim3(256), lds, stream, a);
     return launch_status();
 }
 
