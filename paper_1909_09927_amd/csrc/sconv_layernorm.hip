@@ -26,6 +26,7 @@ struct LnArgs {
     float* part;                         // backward: [blocks][2][C], or null
     int64_t rows;                        // N * S
     int S, C, N, w_type;
+    int v4;                              // map: four channels of a token, and of the weights, lie aligned
     int64_t x_n, x_s, y_n, y_s;
     float eps, inv_c;
 };
@@ -133,25 +134,27 @@ __global__ __launch_bounds__(256) void ln_fwd_long(LnArgs a, int64_t xs_s, int64
     }
 }
 
-// Map in, tokens out.  P places (lanes), CG = threads / P groups of channels; a thread holds channels cg + CG * j.
+// Map in, tokens out.  P places (lanes), CG = threads / P groups of channels; a thread holds channels cg + CG * j.  Tiles of 8 CG
+// channels are turned in LDS, four channels of a place a thread.
 template <typename TX, typename TY, int P, int THREADS, int NJ>
 __global__ __launch_bounds__(THREADS) void ln_map_fwd(LnArgs a, int tiles)
 {
-    constexpr int CG = THREADS / P, CH = CG * 4;   // channels turned at a time
-    __shared__ float tile[2][P][CH + 1];
+    constexpr int CG = THREADS / P, CH = CG * 8;
+    __shared__ __attribute__((aligned(16))) float tile[P][CH + 4];
     __shared__ float part[2][CG][P];
     const int p = threadIdx.x % P, cg = threadIdx.x / P;
     const int n = blockIdx.x / tiles, s0 = (blockIdx.x % tiles) * P;
     const int places = min(P, a.S - s0);
-    const TX* x = (const TX*)a.x + n * a.x_n + s0 + p;
+    const TX* x = (const TX*)a.x + n * a.x_n + s0 + min(p, places - 1);
     float v[NJ];
     float sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
         const int c = cg + CG * j;
-        v[j] = (c < a.C && p < places) ? (float)x[c * a.x_s] : 0.0f;
-        sum += v[j];
+        v[j] = c < a.C ? (float)x[c * a.x_s] : 0.0f;
     }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) sum += v[j];
     part[0][cg][p] = sum;
     __syncthreads();
     float mean = 0.0f;
@@ -174,19 +177,33 @@ __global__ __launch_bounds__(THREADS) void ln_map_fwd(LnArgs a, int tiles)
     }
     TY* y = (TY*)a.y + n * a.y_n + (int64_t)s0 * a.y_s;
 #pragma unroll
-    for (int jb = 0; jb < NJ / 4; ++jb) {
+    for (int jb = 0; jb < NJ / 8; ++jb) {
         if (jb * CH >= a.C) break;
-        float (*t)[CH + 1] = tile[jb & 1];
+        if (jb) __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t[p][cg + CG * i] = (v[jb * 4 + i] - mean) * rstd;
+        for (int i = 0; i < 8; ++i) tile[p][cg + CG * i] = (v[jb * 8 + i] - mean) * rstd;
         __syncthreads();
-        for (int e = threadIdx.x; e < P * CH; e += THREADS) {
-            const int q = e / CH, c = jb * CH + e % CH;
-            if (q < places && c < a.C) {
-                float o = t[q][e % CH];
-                if (a.w) o *= load_typed(a.w, a.w_type, c);
-                if (a.b) o += load_typed(a.b, a.w_type, c);
-                y[q * a.y_s + c] = (TY)o;
+#pragma unroll
+        for (int e0 = 0; e0 < P * CH / 4; e0 += THREADS) {
+            const int e = e0 + threadIdx.x, q = e / (CH / 4), k = e % (CH / 4) * 4, c = jb * CH + k;
+            if (q >= places || c >= a.C) continue;
+            const f32x4 o = *(const f32x4*)&tile[q][k];
+            float r[4] = {o[0], o[1], o[2], o[3]};
+            if (a.v4) {
+                float w[4], b[4];
+                if (a.w) load_w<4>(a.w, a.w_type, c, w);
+                if (a.b) load_w<4>(a.b, a.w_type, c, b);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { if (a.w) r[i] *= w[i]; if (a.b) r[i] += b[i]; }
+                store_vec<4>(y + q * a.y_s + c, r);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (c + i >= a.C) break;
+                    if (a.w) r[i] *= load_typed(a.w, a.w_type, c + i);
+                    if (a.b) r[i] += load_typed(a.b, a.w_type, c + i);
+                    y[q * a.y_s + c + i] = (TY)r[i];
+                }
             }
         }
     }
@@ -208,23 +225,40 @@ __global__ __launch_bounds__(256) void ln_bwd(LnArgs a)
         for (int i = 0; i < V; ++i) { w[j][i] = 1.0f; aw[j][i] = ab[j][i] = 0.0f; }
         if (a.w && c < a.C) load_w<V>(a.w, a.w_type, c, w[j]);
     }
-    int turn = 0;
-    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB, turn ^= 2) {
-        const int64_t row = r0 + group;
-        const bool live = row < a.rows;
-        int n = 0, s = 0;
-        float mean = 0.0f, rstd = 0.0f;
-        if (live) { place_of(a, row, n, s); mean = a.mean_in[row]; rstd = a.rstd_in[row]; }
+    // the next row is on its way while this one is summed
+    Pack<TX, V> xp[NV];
+    Pack<TY, V> gp[NV];
+    float mean_next = 0.0f, rstd_next = 0.0f;
+    const auto fetch = [&](int64_t row) {
+        if (row >= a.rows) return;
+        int n, s;
+        place_of(a, row, n, s);
         const TX* x = (const TX*)a.x + n * a.x_n + s * a.x_s;
         const TY* dy = (const TY*)a.dy + n * a.y_n + s * a.y_s;
-        float u[NV][V], g[NV][V];
-        float s1 = 0.0f, s2 = 0.0f;
+        mean_next = a.mean_in[row];
+        rstd_next = a.rstd_in[row];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * LPR + lane) * V;
-            if (live && c < a.C) {
-                load_vec<V>(x + c, u[j]);
-                load_vec<V>(dy + c, g[j]);
+            if (c < a.C) { xp[j] = *(const Pack<TX, V>*)(x + c); gp[j] = *(const Pack<TY, V>*)(dy + c); }
+        }
+    };
+    int turn = 0;
+    fetch((int64_t)blockIdx.x * RPB + group);
+    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB, turn ^= 2) {
+        const int64_t row = r0 + group;
+        const bool live = row < a.rows;
+        const float mean = mean_next, rstd = rstd_next;
+        float u[NV][V], g[NV][V];
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) { u[j][i] = (float)xp[j].e[i]; g[j][i] = (float)gp[j].e[i]; }
+        fetch(row + (int64_t)gridDim.x * RPB);
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (live && (j * LPR + lane) * V < a.C) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     u[j][i] = (u[j][i] - mean) * rstd;
@@ -341,8 +375,8 @@ __global__ __launch_bounds__(256) void ln_dw_long(LnArgs a, int64_t xs_s, int64_
 template <typename TX, typename TY, int P, int THREADS, int NJ>
 __global__ __launch_bounds__(THREADS) void ln_map_bwd(LnArgs a, int tiles, int64_t total)
 {
-    constexpr int CG = THREADS / P, CH = CG * 4, KEEP = (NJ + P - 1) / P;
-    __shared__ float tile[2][P][CH + 1];
+    constexpr int CG = THREADS / P, CH = CG * 8, KEEP = (NJ + P - 1) / P;
+    __shared__ __attribute__((aligned(16))) float tile[P][CH + 4];
     __shared__ float part[2][CG][P];
     const int p = threadIdx.x % P, cg = threadIdx.x / P;
     float aw[KEEP], ab[KEEP];
@@ -350,33 +384,43 @@ __global__ __launch_bounds__(THREADS) void ln_map_bwd(LnArgs a, int tiles, int64
     for (int k = 0; k < KEEP; ++k) aw[k] = ab[k] = 0.0f;
     for (int64_t t = blockIdx.x; t < total; t += gridDim.x) {
         const int n = (int)(t / tiles), s0 = (int)(t % tiles) * P;
-        const int places = min(P, a.S - s0);
+        const int places = min(P, a.S - s0), at = min(p, places - 1);
         const bool live = p < places;
-        const TX* x = (const TX*)a.x + n * a.x_n + s0 + p;
+        const TX* x = (const TX*)a.x + n * a.x_n + s0 + at;
         const TY* dy = (const TY*)a.dy + n * a.y_n + (int64_t)s0 * a.y_s;
-        const float mean = live ? a.mean_in[(int64_t)n * a.S + s0 + p] : 0.0f;
-        const float rstd = live ? a.rstd_in[(int64_t)n * a.S + s0 + p] : 0.0f;
+        const float mean = a.mean_in[(int64_t)n * a.S + s0 + at], rstd = a.rstd_in[(int64_t)n * a.S + s0 + at];
         float u[NJ], g[NJ];
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
             const int c = cg + CG * j;
-            u[j] = (live && c < a.C) ? ((float)x[c * a.x_s] - mean) * rstd : 0.0f;
+            u[j] = c < a.C ? (float)x[c * a.x_s] : 0.0f;
         }
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
-        for (int jb = 0; jb < NJ / 4; ++jb) {
+        for (int jb = 0; jb < NJ / 8; ++jb) {
             if (jb * CH < a.C) {
-                float (*m)[CH + 1] = tile[jb & 1];
-                for (int e = threadIdx.x; e < P * CH; e += THREADS) {
-                    const int q = e / CH, c = jb * CH + e % CH;
-                    m[q][e % CH] = (q < places && c < a.C) ? (float)dy[q * a.y_s + c] : 0.0f;
+                __syncthreads();
+#pragma unroll
+                for (int e0 = 0; e0 < P * CH / 4; e0 += THREADS) {
+                    const int e = e0 + threadIdx.x, q = e / (CH / 4), k = e % (CH / 4) * 4, c = jb * CH + k;
+                    float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    if (q < places && c < a.C) {
+                        if (a.v4) load_vec<4>(dy + q * a.y_s + c, d);
+                        else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (c + i < a.C) d[i] = (float)dy[q * a.y_s + c + i];
+                        }
+                    }
+                    *(f32x4*)&tile[q][k] = f32x4{d[0], d[1], d[2], d[3]};
                 }
                 __syncthreads();
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int j = jb * 4 + i, c = cg + CG * j;
-                    const float d = m[p][cg + CG * i];
+                for (int i = 0; i < 8; ++i) {
+                    const int j = jb * 8 + i, c = cg + CG * j;
+                    const float d = tile[p][cg + CG * i];
                     const float w = (a.w && c < a.C) ? load_typed(a.w, a.w_type, c) : 1.0f;
+                    u[j] = (live && c < a.C) ? (u[j] - mean) * rstd : 0.0f;
                     if (a.part) {
                         const float sw = lanes_sum<P>(d * u[j]), sb = lanes_sum<P>(d);
                         if (p == j % P) { aw[j / P] += sw; ab[j / P] += sb; }
@@ -387,7 +431,7 @@ __global__ __launch_bounds__(THREADS) void ln_map_bwd(LnArgs a, int tiles, int64
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) g[jb * 4 + i] = 0.0f;
+                for (int i = 0; i < 8; ++i) u[jb * 8 + i] = g[jb * 8 + i] = 0.0f;
             }
         }
         if (a.dx) {
@@ -406,7 +450,6 @@ __global__ __launch_bounds__(THREADS) void ln_map_bwd(LnArgs a, int tiles, int64
                 if (live && c < a.C) dx[(int64_t)c * a.S] = (TX)(rstd * (g[j] - s1 - u[j] * s2));
             }
         }
-        __syncthreads();    // part and tile are written again
     }
     if (!a.part) return;
     float* out = a.part + (int64_t)blockIdx.x * 2 * a.C;
@@ -417,20 +460,24 @@ __global__ __launch_bounds__(THREADS) void ln_map_bwd(LnArgs a, int tiles, int64
     }
 }
 
-// Partial sums [blocks][2][C] -> dw, db.  64 channels a workgroup, four wavefronts along the blocks.
-__global__ __launch_bounds__(256) void ln_dw_sum(const float* part, int blocks, int C, void* dw, void* db, int type)
+// Partial sums [blocks][2][C] -> dw, db.  32 columns a workgroup, 32 groups of rows, whose loads do not wait for each other.
+__global__ __launch_bounds__(1024) void ln_dw_sum(const float* part, int blocks, int C, void* dw, void* db, int type)
 {
-    __shared__ float t[4][64];
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, e = blockIdx.x * 64 + lane;
+    __shared__ float t[32][33];
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
     float v = 0.0f;
-    if (e < 2 * C)
-        for (int k = wv; k < blocks; k += 4) v += part[(int64_t)k * 2 * C + e];
-    t[wv][lane] = v;
+    if (e < 2 * C) {
+#pragma unroll 16
+        for (int k = group; k < blocks; k += 32) v += part[(int64_t)k * 2 * C + e];
+    }
+    t[group][lane] = v;
     __syncthreads();
-    if (wv == 0 && e < 2 * C) {
-        v = (t[0][lane] + t[1][lane]) + (t[2][lane] + t[3][lane]);
-        if (e < C) store_typed(dw, type, e, v);
-        else store_typed(db, type, e - C, v);
+    // (a wavefront half a column: the groups as lanes)
+    v = lanes_sum<32>(t[lane][group]);
+    const int column = blockIdx.x * 32 + group;
+    if (lane == 0 && column < 2 * C) {
+        if (column < C) store_typed(dw, type, column, v);
+        else store_typed(db, type, column - C, v);
     }
 }
 
@@ -506,6 +553,7 @@ int ln_run(const sconv_layernorm_desc_t& d, LnArgs a, bool backward, hipStream_t
         const int tiles = (d.S + P - 1) / P;
         const int64_t total = (int64_t)tiles * d.N;
         const unsigned bgrid = (unsigned)std::min<int64_t>(blocks, total);
+        a.v4 = (a.y_s | a.y_n | d.C) % 4 == 0 && aligned_to(a.y, 16) && aligned_to(a.dy, 16) && aligned_to(a.w, 16) && aligned_to(a.b, 16);
 #define SCONV_LN_MAP(PP, TH, J)                                                                                                \
     {                                                                                                                          \
         if (backward) hipLaunchKernelGGL((ln_map_bwd<TX, TY, PP, TH, J>), dim3(bgrid), dim3(TH), 0, stream, a, tiles, total);  \
@@ -596,7 +644,7 @@ int launch_layernorm_backward(const sconv_layernorm_desc_t& d, const void* dy, c
         blocks = ln_part_blocks(d, a);
     }
     if (!dw) return SCONV_OK;
-    hipLaunchKernelGGL(ln_dw_sum, dim3((unsigned)((2 * d.C + 63) / 64)), dim3(256), 0, stream, (const float*)ws, blocks, d.C, dw, db, d.w_type);
+    hipLaunchKernelGGL(ln_dw_sum, dim3((unsigned)((2 * d.C + 31) / 32)), dim3(1024), 0, stream, (const float*)ws, blocks, d.C, dw, db, d.w_type);
     return launch_status();
 }
 

@@ -92,14 +92,32 @@ __device__ __forceinline__ void store_typed(void* p, int type, int64_t i, float 
     else ((float*)p)[i] = v;
 }
 
-// Sum over aligned groups of L lanes (L a power of two up to 64); every lane has it.  The order is fixed.
+// Sum over aligned groups of L lanes (16, 32 or 64); every lane has it, and the order is fixed.  Within 16 lanes the neighbours come by
+// rotation as operands of the sums themselves, beyond by swaps of halves: no trip through LDS.
 template <int L>
 __device__ __forceinline__ float lanes_sum(float v)
 {
-#pragma unroll
-    for (int d = 1; d < L; d *= 2) v += __shfl_xor(v, d);
+    static_assert(L == 16 || L == 32 || L == 64, "whole rows of lanes");
+#define SCONV_ROTATED(n) __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + n, 0xf, 0xf, false))
+    v += SCONV_ROTATED(8);
+    v += SCONV_ROTATED(4);
+    v += SCONV_ROTATED(2);
+    v += SCONV_ROTATED(1);
+#undef SCONV_ROTATED
+    if constexpr (L >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if constexpr (L == 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
     return v;
 }
+
+// V elements as they lie in memory, to be loaded ahead of their use.
+template <typename T, int V>
+struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Pack { T e[V]; };
 
 inline bool aligned_to(const void* p, int bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
