@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void ln_fwd(LnArgs a)
     }
 }
 
-// Rows too long for registers (C over 8192) and maps of more than 2048 channels: one workgroup a place, x read three times (from
+// Rows too long for registers (C over 8192) and maps that are not held (ln_map_held): one workgroup a place, x read three times (from
 // the caches after the first).  xs_c: stride between channels.
 template <typename TX, typename TY>
 __global__ __launch_bounds__(256) void ln_fwd_long(LnArgs a, int64_t xs_s, int64_t xs_c)
@@ -145,14 +145,12 @@ __global__ __launch_bounds__(THREADS) void ln_map_fwd(LnArgs a, int tiles)
     const int p = threadIdx.x % P, cg = threadIdx.x / P;
     const int n = blockIdx.x / tiles, s0 = (blockIdx.x % tiles) * P;
     const int places = min(P, a.S - s0);
-    const TX* x = (const TX*)a.x + n * a.x_n + s0 + min(p, places - 1);
+    const TX* x = (const TX*)a.x + n * a.x_n;          // (offsets within an image: 32 bits)
+    const uint32_t xs = (uint32_t)a.x_s, at = cg * xs + s0 + min(p, places - 1);
     float v[NJ];
     float sum = 0.0f;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-        const int c = cg + CG * j;
-        v[j] = c < a.C ? (float)x[c * a.x_s] : 0.0f;
-    }
+    for (int j = 0; j < NJ; ++j) v[j] = cg + CG * j < a.C ? (float)x[at + CG * j * xs] : 0.0f;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) sum += v[j];
     part[0][cg][p] = sum;
@@ -318,7 +316,7 @@ __global__ __launch_bounds__(256) void ln_bwd(LnArgs a)
     }
 }
 
-// dx of rows too long for registers, and of maps of more than 2048 channels.
+// dx of rows too long for registers, and of maps that are not held.
 template <typename TX, typename TY>
 __global__ __launch_bounds__(256) void ln_bwd_long(LnArgs a, int64_t xs_s, int64_t xs_c, int64_t ds_n, int64_t ds_s, int64_t ds_c)
 {
@@ -370,15 +368,20 @@ __global__ __launch_bounds__(256) void ln_dw_long(LnArgs a, int64_t xs_s, int64_
     }
 }
 
-// Backward, map: dx (map) and the sums over the places of a workgroup's tiles.  Lane p keeps the sums of the channels j with
-// j % P == p of its channel group.
+// Backward, map: dx (map) and the sums over the places of a workgroup's tiles.  x stays in registers (channels cg + CG * j of a
+// place), dy of the whole tile in LDS, turned on the way in and read twice.  Lane p keeps the sums of the channels j with j % P == p of
+// its channel group.
+inline int map_row(int C) { const int quads = (C + 3) / 4; return 4 * (quads + (quads & 1 ? 2 : 1)); }   // 4 times an odd number
+
 template <typename TX, typename TY, int P, int THREADS, int NJ>
-__global__ __launch_bounds__(THREADS) void ln_map_bwd(LnArgs a, int tiles, int64_t total)
+__global__ __launch_bounds__(THREADS, 4) void ln_map_bwd(LnArgs a, int tiles, int64_t total, int row)
 {
-    constexpr int CG = THREADS / P, CH = CG * 8, KEEP = (NJ + P - 1) / P;
-    __shared__ __attribute__((aligned(16))) float tile[P][CH + 4];
+    constexpr int CG = THREADS / P, KEEP = (NJ + P - 1) / P;
+    extern __shared__ __attribute__((aligned(16))) float tile[];   // [P][row], then the weights [CG * NJ]
     __shared__ float part[2][CG][P];
-    const int p = threadIdx.x % P, cg = threadIdx.x / P;
+    float* ws = tile + P * row;
+    const int p = threadIdx.x % P, cg = threadIdx.x / P, quads = (a.C + 3) / 4;
+    for (int c = threadIdx.x; c < CG * NJ; c += THREADS) ws[c] = c >= a.C ? 0.0f : a.w ? load_typed(a.w, a.w_type, c) : 1.0f;
     float aw[KEEP], ab[KEEP];
 #pragma unroll
     for (int k = 0; k < KEEP; ++k) aw[k] = ab[k] = 0.0f;
@@ -386,70 +389,59 @@ __global__ __launch_bounds__(THREADS) void ln_map_bwd(LnArgs a, int tiles, int64
         const int n = (int)(t / tiles), s0 = (int)(t % tiles) * P;
         const int places = min(P, a.S - s0), at = min(p, places - 1);
         const bool live = p < places;
-        const TX* x = (const TX*)a.x + n * a.x_n + s0 + at;
+        const TX* x = (const TX*)a.x + n * a.x_n;      // (offsets within an image: 32 bits)
+        const uint32_t xs = (uint32_t)a.x_s, first = cg * xs + s0 + at;
         const TY* dy = (const TY*)a.dy + n * a.y_n + (int64_t)s0 * a.y_s;
         const float mean = a.mean_in[(int64_t)n * a.S + s0 + at], rstd = a.rstd_in[(int64_t)n * a.S + s0 + at];
-        float u[NJ], g[NJ];
+        float u[NJ];
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int c = cg + CG * j;
-            u[j] = c < a.C ? (float)x[c * a.x_s] : 0.0f;
+        for (int j = 0; j < NJ; ++j) u[j] = cg + CG * j < a.C ? (float)x[first + CG * j * xs] : 0.0f;
+        for (int e = threadIdx.x; e < P * quads; e += THREADS) {
+            const int q = e / quads, c = (e - q * quads) * 4;
+            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (q < places) {
+                if (a.v4) load_vec<4>(dy + q * a.y_s + c, d);
+                else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (c + i < a.C) d[i] = (float)dy[q * a.y_s + c + i];
+                }
+            }
+            *(f32x4*)(tile + q * row + c) = f32x4{d[0], d[1], d[2], d[3]};
         }
+        __syncthreads();
+        const float* mine = tile + p * row + cg;
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
-        for (int jb = 0; jb < NJ / 8; ++jb) {
-            if (jb * CH < a.C) {
-                __syncthreads();
-#pragma unroll
-                for (int e0 = 0; e0 < P * CH / 4; e0 += THREADS) {
-                    const int e = e0 + threadIdx.x, q = e / (CH / 4), k = e % (CH / 4) * 4, c = jb * CH + k;
-                    float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    if (q < places && c < a.C) {
-                        if (a.v4) load_vec<4>(dy + q * a.y_s + c, d);
-                        else {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (c + i < a.C) d[i] = (float)dy[q * a.y_s + c + i];
-                        }
-                    }
-                    *(f32x4*)&tile[q][k] = f32x4{d[0], d[1], d[2], d[3]};
-                }
-                __syncthreads();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int j = jb * 8 + i, c = cg + CG * j;
-                    const float d = tile[p][cg + CG * i];
-                    const float w = (a.w && c < a.C) ? load_typed(a.w, a.w_type, c) : 1.0f;
-                    u[j] = (live && c < a.C) ? (u[j] - mean) * rstd : 0.0f;
-                    if (a.part) {
-                        const float sw = lanes_sum<P>(d * u[j]), sb = lanes_sum<P>(d);
-                        if (p == j % P) { aw[j / P] += sw; ab[j / P] += sb; }
-                    }
-                    g[j] = d * w;
-                    s1 += g[j];
-                    s2 = fmaf(g[j], u[j], s2);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) u[jb * 8 + i] = g[jb * 8 + i] = 0.0f;
+        for (int j = 0; j < NJ; ++j) {
+            if (CG * j >= a.C) { u[j] = 0.0f; continue; }
+            const bool there = live && cg + CG * j < a.C;
+            const float d = there ? mine[CG * j] : 0.0f, w = ws[cg + CG * j];
+            u[j] = there ? (u[j] - mean) * rstd : 0.0f;
+            if (a.part) {
+                const float sw = lanes_sum<P>(d * u[j]), sb = lanes_sum<P>(d);
+                if (p == j % P) { aw[j / P] += sw; ab[j / P] += sb; }
             }
+            s1 = fmaf(d, w, s1);
+            s2 = fmaf(d * w, u[j], s2);
         }
+        part[0][cg][p] = s1;
+        part[1][cg][p] = s2;
+        __syncthreads();
         if (a.dx) {
-            part[0][cg][p] = s1;
-            part[1][cg][p] = s2;
-            __syncthreads();
             s1 = s2 = 0.0f;
 #pragma unroll
             for (int k = 0; k < CG; ++k) { s1 += part[0][k][p]; s2 += part[1][k][p]; }
             s1 *= a.inv_c;
             s2 *= a.inv_c;
-            TX* dx = (TX*)a.dx + (int64_t)n * a.C * a.S + s0 + p;
+            TX* dx = (TX*)a.dx + (int64_t)n * a.C * a.S;
+            const uint32_t to = cg * a.S + s0 + p;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const int c = cg + CG * j;
-                if (live && c < a.C) dx[(int64_t)c * a.S] = (TX)(rstd * (g[j] - s1 - u[j] * s2));
-            }
+            for (int j = 0; j < NJ; ++j)
+                if (live && cg + CG * j < a.C)
+                    dx[to + (uint32_t)(CG * j) * a.S] = (TX)(rstd * (mine[CG * j] * ws[cg + CG * j] - s1 - u[j] * s2));
         }
+        __syncthreads();                               // tile and part are written again
     }
     if (!a.part) return;
     float* out = a.part + (int64_t)blockIdx.x * 2 * a.C;
@@ -507,6 +499,25 @@ void ln_shape(int C, int V, int64_t rows, int* lpr, int* nv)
     *nv = n;
 }
 
+// Maps whose places stay in registers: 2048 channels at most, an image within 32 bits of bytes.
+bool ln_map_held(const sconv_layernorm_desc_t& d)
+{
+    const int64_t most = int64_t(1) << 30;
+    return d.layout == SCONV_LAYOUT_MAP && d.C <= 2048 && d.x_s * d.C < most - d.S && (int64_t)d.S * d.C < most;
+}
+
+// Places of a tile: whole 128-byte lines of a map in 32 bits, fewer where the channels would not fit the registers, or two
+// workgroups' tiles of dy the LDS.
+int ln_map_places(const sconv_layernorm_desc_t& d, bool backward) { return d.C <= (backward ? 512 : 1024) ? 32 : 16; }
+
+template <typename K>
+int ln_allow_lds(K kern, size_t bytes)
+{
+    // (beside the kernel's own arrays)
+    return bytes <= 48 * 1024 || hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess
+               ? SCONV_OK : SCONV_ELAUNCH;
+}
+
 // Most workgroups of a backward call, each with a row of partial sums: 512 fill the chip twice over; more would only
 // add to the second kernel's work.
 constexpr int LN_BLOCKS = 512;
@@ -548,17 +559,32 @@ template <typename TX, typename TY>
 int ln_run(const sconv_layernorm_desc_t& d, LnArgs a, bool backward, hipStream_t stream)
 {
     const int blocks = LN_BLOCKS;
-    if (d.layout == SCONV_LAYOUT_MAP && d.C <= 2048) {
-        const int P = d.C <= 1024 ? 32 : 16;
-        const int tiles = (d.S + P - 1) / P;
-        const int64_t total = (int64_t)tiles * d.N;
-        const unsigned bgrid = (unsigned)std::min<int64_t>(blocks, total);
+    if (ln_map_held(d)) {
         a.v4 = (a.y_s | a.y_n | d.C) % 4 == 0 && aligned_to(a.y, 16) && aligned_to(a.dy, 16) && aligned_to(a.w, 16) && aligned_to(a.b, 16);
-#define SCONV_LN_MAP(PP, TH, J)                                                                                                \
-    {                                                                                                                          \
-        if (backward) hipLaunchKernelGGL((ln_map_bwd<TX, TY, PP, TH, J>), dim3(bgrid), dim3(TH), 0, stream, a, tiles, total);  \
-        else hipLaunchKernelGGL((ln_map_fwd<TX, TY, PP, TH, J>), dim3((unsigned)total), dim3(TH), 0, stream, a, tiles);        \
-        return launch_status();                                                                                                \
+        const int P = ln_map_places(d, backward), tiles = (d.S + P - 1) / P;
+        const int64_t total = (int64_t)tiles * d.N;
+        if (backward) {
+            const unsigned grid = (unsigned)std::min<int64_t>(blocks, total);
+            const int row = map_row(d.C);
+#define SCONV_LN_MAP(PP, TH, J)                                                                                     \
+    {                                                                                                               \
+        const size_t lds = ((size_t)PP * row + TH / PP * J) * sizeof(float);                                        \
+        const int rc = ln_allow_lds(ln_map_bwd<TX, TY, PP, TH, J>, lds);                                            \
+        if (rc) return rc;                                                                                          \
+        hipLaunchKernelGGL((ln_map_bwd<TX, TY, PP, TH, J>), dim3(grid), dim3(TH), lds, stream, a, tiles, total, row); \
+        return launch_status();                                                                                     \
+    }
+            if (d.C <= 128) SCONV_LN_MAP(32, 512, 8)
+            if (d.C <= 256) SCONV_LN_MAP(32, 512, 16)
+            if (d.C <= 512) SCONV_LN_MAP(32, 512, 32)
+            if (d.C <= 1024) SCONV_LN_MAP(16, 512, 32)
+            SCONV_LN_MAP(16, 1024, 32)
+#undef SCONV_LN_MAP
+        }
+#define SCONV_LN_MAP(PP, TH, J)                                                                                              \
+    {                                                                                                                        \
+        hipLaunchKernelGGL((ln_map_fwd<TX, TY, PP, TH, J>), dim3((unsigned)total), dim3(TH), 0, stream, a, tiles);           \
+        return launch_status();                                                                                              \
     }
         if (d.C <= 128) SCONV_LN_MAP(32, 512, 8)
         if (d.C <= 256) SCONV_LN_MAP(32, 512, 16)
@@ -597,8 +623,8 @@ int ln_run(const sconv_layernorm_desc_t& d, LnArgs a, bool backward, hipStream_t
 int ln_part_blocks(const sconv_layernorm_desc_t& d, const LnArgs& a)
 {
     const int blocks = LN_BLOCKS;
-    if (d.layout == SCONV_LAYOUT_MAP && d.C <= 2048) {
-        const int P = d.C <= 1024 ? 32 : 16;
+    if (ln_map_held(d)) {
+        const int P = ln_map_places(d, true);
         return (int)std::min<int64_t>(blocks, (int64_t)((d.S + P - 1) / P) * d.N);
     }
     if (d.layout == SCONV_LAYOUT_TOKENS && d.C <= 8192) {
