@@ -673,12 +673,12 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
     }
 }
 
-// Joins the splits' parts: a workgroup a row, lanes along the two maps' values.
+// Joins the splits' parts: a workgroup a row, lanes along the two maps' values, four groups of them along the splits.
 constexpr int MAX_SPLITS = 128;
 template <typename T>
-__global__ __launch_bounds__(256) void attn_join(AttnArgs a)
+__global__ __launch_bounds__(1024) void attn_join(AttnArgs a)
 {
-    __shared__ float f[2][MAX_SPLITS], val[2][256];
+    __shared__ float f[2][MAX_SPLITS], val[4][512], total[2];
     const int bh_all = a.B * a.Hkv;
     const int64_t row = blockIdx.x, all_rows = (int64_t)bh_all * a.rows;   // row: bh * rows + r
     const int bh = (int)(row / a.rows), r = (int)(row - (int64_t)bh * a.rows), b = bh / a.Hkv, hk = bh % a.Hkv;
@@ -706,31 +706,33 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a)
         f[w][l] = t[0] * inv;
         f[w][l + 64] = t[1] * inv;
         if (l == 0) {
-            val[w][0] = sum;
+            total[w] = sum;
             if (a.lse) a.lse[(((int64_t)w * a.B + b) * a.H + head) * a.Sq + i] = sum == 0.0f ? -INFINITY : (most + log2f(sum)) * 0.69314718055994530942f;
         }
     }
     __syncthreads();
-    const bool none = val[1][0] == 0.0f;
-    __syncthreads();
-    for (int e = threadIdx.x; e < 2 * a.Dv; e += 256) {
+    const bool none = total[1] == 0.0f;
+    const int group = threadIdx.x >> 8, lane = threadIdx.x & 255;
+    for (int e = lane; e < 2 * a.Dv; e += 256) {
         const int m = e >= a.Dv, d = e - m * a.Dv;
         const float* from = a.part + (row * 2 + m) * wide + d;
         float v = 0.0f;
 #pragma unroll 8
-        for (int s = 0; s < a.splits; ++s) {
+        for (int s = group; s < a.splits; s += 4) {
             // (parts of nothing were not written)
-            const float x = from[s * all_rows * 2 * wide];
-            v += f[m][s] == 0.0f ? 0.0f : f[m][s] * x;
+            const float x = from[s * all_rows * 2 * wide], g = f[m][s];
+            v += g == 0.0f ? 0.0f : g * x;
         }
-        val[m][d] = v;
+        val[group][e] = v;
     }
     __syncthreads();
     const int d = threadIdx.x;
     if (d < a.Dv) {
+        const int e = d + a.Dv;
+        const float x = (val[0][d] + val[1][d]) + (val[2][d] + val[3][d]), y = (val[0][e] + val[1][e]) + (val[2][e] + val[3][e]);
         const int64_t at = (((int64_t)b * a.Sq + i) * a.H + head) * a.Dv + d;
-        ((T*)a.out)[at] = (T)(none ? 0.0f : fmaf(-a.lam[head], val[1][d], val[0][d]));
-        if (a.second) ((T*)a.second)[at] = (T)val[1][d];
+        ((T*)a.out)[at] = (T)(none ? 0.0f : fmaf(-a.lam[head], y, x));
+        if (a.second) ((T*)a.second)[at] = (T)y;
     }
 }
 
@@ -821,7 +823,7 @@ int fwd_run(AttnArgs& a, const FwdPlan& p, hipStream_t stream)
     const int rc = DT == 32 ? fwd_launch<T, VEC, 32, 64>(a, p, stream)
                  : DT == 64 ? fwd_launch<T, VEC, 64, 128>(a, p, stream) : fwd_launch<T, VEC, 128, 128>(a, p, stream);
     if (rc || p.splits == 1) return rc;
-    hipLaunchKernelGGL((attn_join<T>), dim3((unsigned)((int64_t)a.B * a.Hkv * a.rows)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((attn_join<T>), dim3((unsigned)((int64_t)a.B * a.Hkv * a.rows)), dim3(1024), 0, stream, a);
     return launch_status();
 }
 

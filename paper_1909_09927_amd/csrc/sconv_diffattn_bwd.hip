@@ -52,17 +52,24 @@ __global__ __launch_bounds__(256) void attn_delta(AttnArgs a)
 }
 
 // dlam[h] = -sum over requests and queries, in one order.
-__global__ __launch_bounds__(256) void attn_dlam(const float* part, int B, int H, int Sq, float* dlam)
+__global__ __launch_bounds__(1024) void attn_dlam(const float* part, int B, int H, int Sq, float* dlam)
 {
-    __shared__ float t[4];
+    __shared__ float t[16];
     const int h = blockIdx.x;
+    const int64_t all = (int64_t)B * Sq;
     float v = 0.0f;
-    for (int b = 0; b < B; ++b)
-        for (int i = threadIdx.x; i < Sq; i += 256) v += part[((int64_t)b * H + h) * Sq + i];
+#pragma unroll 8
+    for (int64_t k = threadIdx.x; k < all; k += 1024) {
+        const int b = (int)((uint32_t)k / (uint32_t)Sq), i = (int)((uint32_t)k - (uint32_t)b * (uint32_t)Sq);   // (B H Sq < 2^31)
+        v += part[((int64_t)b * H + h) * Sq + i];
+    }
     v = lanes_sum<64>(v);
     if ((threadIdx.x & 63) == 0) t[threadIdx.x >> 6] = v;
     __syncthreads();
-    if (threadIdx.x == 0) dlam[h] = 0.0f - ((t[0] + t[1]) + (t[2] + t[3]));
+    if (threadIdx.x < 64) {
+        v = lanes_sum<16>(t[threadIdx.x & 15]);
+        if (threadIdx.x == 0) dlam[h] = 0.0f - v;
+    }
 }
 
 // The ends of the two kernels below: a lane's query or key.
@@ -815,7 +822,7 @@ int bwd_run(const AttnArgs& a, float* dlam, hipStream_t stream)
     else if (most <= 64) rc = bwd_main<T, VEC, 64>(a, stream);
     else rc = bwd_main<T, VEC, 128>(a, stream);
     if (rc) return rc;
-    hipLaunchKernelGGL(attn_dlam, dim3((unsigned)a.H), dim3(256), 0, stream, a.dlam_part, a.B, a.H, a.Sq, dlam);
+    hipLaunchKernelGGL(attn_dlam, dim3((unsigned)a.H), dim3(1024), 0, stream, a.dlam_part, a.B, a.H, a.Sq, dlam);
     return launch_status();
 }
 

@@ -43,6 +43,29 @@ class DiffAttnDesc(ctypes.Structure):
                 [(n, _i64) for n in ("q_b", "q_s", "q_h", "k_b", "k_s", "k_h", "v_b", "v_s", "v_h", "mask_b")])
 
 
+# Descriptors of calls seen before, by the shapes, strides and types that they describe (nothing of the tensors themselves): filling
+# one in takes longer than a small call's kernel.
+_plans = {}
+_PLANS_KEPT = 4096
+
+
+def _sig(t):
+    """What a descriptor says of a tensor."""
+    if t is None:
+        return None
+    try:
+        return t.shape, t.stride(), t.dtype, t.is_cuda
+    except (AttributeError, TypeError):
+        raise TypeError("tensors in device memory are wanted") from None
+
+
+def _keep(key, plan):
+    if len(_plans) >= _PLANS_KEPT:
+        _plans.clear()
+    _plans[key] = plan
+    return plan
+
+
 _lib = None
 
 
@@ -151,6 +174,27 @@ def sconv_layernorm_forward(x, weight=None, bias=None, eps: float = 1e-5, layout
     layout "tokens": x is [..., C] and y has its shape; "map": x is a feature map [N, C, H, W] (or [N, C, S]) as
     sconv_forward leaves it and y is tokens [N, H*W, C].  out_dtype: x's type (default), or bf16 under an fp32 x.
     stats: returns (y, mean, rstd), the fp32 statistics of every place that sconv_layernorm_backward reads."""
+    key = (0, _sig(x), _sig(weight), _sig(bias), eps, layout, out_dtype)
+    plan = _plans.get(key)
+    if plan is None:
+        plan = _keep(key, _layernorm_plan(x, weight, bias, eps, layout, out_dtype))
+    _, ref, shape, lead, dtype = plan
+    y = _out(out, shape, dtype, x.device, "out")
+    mean = rstd = mp = rp = None
+    if stats:
+        mean = torch.empty(lead, dtype=torch.float32, device=x.device)
+        rstd = torch.empty(lead, dtype=torch.float32, device=x.device)
+        mp, rp = mean.data_ptr(), rstd.data_ptr()
+    rc = _tokens_lib().sconv_layernorm_forward(ref, x.data_ptr(), None if weight is None else weight.data_ptr(),
+                                               None if bias is None else bias.data_ptr(), y.data_ptr(), mp, rp,
+                                               _raw_stream(torch))
+    if rc:
+        raise SconvError(rc, "sconv_layernorm_forward")
+    return (y, mean, rstd) if stats else y
+
+
+def _layernorm_plan(x, weight, bias, eps, layout, out_dtype):
+    """(descriptor, reference to it, y's shape, the statistics', y's type)"""
     xt = _check(x, "x")
     if layout not in _LAYOUTS:
         raise ValueError('layout must be "tokens" or "map"')
@@ -160,23 +204,39 @@ def sconv_layernorm_forward(x, weight=None, bias=None, eps: float = 1e-5, layout
         shape, lead = (N, S, C), (N, S)
     else:
         N, S, xn, xs = _rows(x, "x")
-        C, shape, lead = x.shape[-1], x.shape, x.shape[:-1]
+        C, shape, lead = x.shape[-1], tuple(x.shape), tuple(x.shape[:-1])
     wt = _weight_type(C, weight, bias)
-    y = _out(out, shape, x.dtype if out_dtype is None else out_dtype, x.device, "out") if yt >= 0 else None
+    if yt < 0:
+        raise SconvError(-1, "sconv_layernorm_forward")
     desc = LayerNormDesc(N, S, C, _LAYOUTS[layout], xt, yt, wt, eps, xn, xs, S * C, C)
-    mean = rstd = None
-    if stats:
-        mean, rstd = torch.empty((2,) + tuple(lead), dtype=torch.float32, device=x.device)
-    rc = _tokens_lib().sconv_layernorm_forward(ctypes.byref(desc), x.data_ptr(), _opt(weight), _opt(bias), _opt(y),
-                                               _opt(mean), _opt(rstd), _raw_stream(torch))
-    if rc:
-        raise SconvError(rc, "sconv_layernorm_forward")
-    return (y, mean, rstd) if stats else y
+    return desc, ctypes.byref(desc), shape, lead, x.dtype if out_dtype is None else out_dtype
 
 
 def sconv_layernorm_backward(dy, x, mean, rstd, weight=None, layout: str = "tokens", param_grads: bool = True, ws=None):
     """Gradient of sconv_layernorm_forward: (dx, dweight, dbias); dx has x's shape, layout and type, dweight and dbias
     weight's type (fp32 without one; None with param_grads False).  ws: a device tensor as scratch (optional)."""
+    key = (1, _sig(dy), _sig(x), _sig(mean), _sig(rstd), _sig(weight), layout)
+    plan = _plans.get(key)
+    if plan is None:
+        plan = _keep(key, _layernorm_grad_plan(dy, x, mean, rstd, weight, layout))
+    _, ref, C, wdtype, need = plan
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dw = db = ptr = None
+    nbytes = 0
+    if param_grads:
+        dw = torch.empty(C, dtype=wdtype, device=x.device)
+        db = torch.empty(C, dtype=wdtype, device=x.device)
+        ws, ptr, nbytes = _ws(ws, need, x.device)
+    rc = _tokens_lib().sconv_layernorm_backward(ref, dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                                None if weight is None else weight.data_ptr(), dx.data_ptr(), _opt(dw),
+                                                _opt(db), ptr, nbytes, _raw_stream(torch))
+    if rc:
+        raise SconvError(rc, "sconv_layernorm_backward")
+    return dx, dw, db
+
+
+def _layernorm_grad_plan(dy, x, mean, rstd, weight, layout):
+    """(descriptor, reference to it, channels, type of the weight's gradient, bytes of scratch)"""
     xt, yt = _check(x, "x"), _check(dy, "dy")
     if layout not in _LAYOUTS:
         raise ValueError('layout must be "tokens" or "map"')
@@ -195,24 +255,12 @@ def sconv_layernorm_backward(dy, x, mean, rstd, weight=None, layout: str = "toke
         _check_dev(t, torch.float32, what)
         if t.numel() != N * S:
             raise ValueError(f"{what} must have one value a place")
-    wt = _weight_type(C, weight, None)
-    desc = LayerNormDesc(N, S, C, _LAYOUTS[layout], xt, yt, wt, 0.0, xn, xs, yn, ys)
-    L = _tokens_lib()
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dw = db = ptr = None
-    nbytes = 0
-    if param_grads:
-        need = _sz()
-        rc = L.sconv_layernorm_workspace_size(ctypes.byref(desc), ctypes.byref(need))
-        if rc:
-            raise SconvError(rc, "sconv_layernorm_backward")
-        dw, db = torch.empty((2, C), dtype=torch.float32 if weight is None else weight.dtype, device=x.device)
-        ws, ptr, nbytes = _ws(ws, need.value, x.device)
-    rc = L.sconv_layernorm_backward(ctypes.byref(desc), dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-                                    _opt(weight), dx.data_ptr(), _opt(dw), _opt(db), ptr, nbytes, _raw_stream(torch))
+    desc = LayerNormDesc(N, S, C, _LAYOUTS[layout], xt, yt, _weight_type(C, weight, None), 0.0, xn, xs, yn, ys)
+    need = _sz()
+    rc = _tokens_lib().sconv_layernorm_workspace_size(ctypes.byref(desc), ctypes.byref(need))
     if rc:
         raise SconvError(rc, "sconv_layernorm_backward")
-    return dx, dw, db
+    return desc, ctypes.byref(desc), C, torch.float32 if weight is None else weight.dtype, need.value
 
 
 # ---- rotary positions
@@ -226,6 +274,33 @@ def sconv_rotary_axes(sections: Sequence[int]) -> bytes:
 
 
 def _rotary(q, k, positions, freq, axes, interleaved, inverse, out, what):
+    key = (2 + inverse, _sig(q), _sig(k), _sig(positions), _sig(freq), axes, interleaved)
+    try:
+        plan = _plans.get(key)
+    except TypeError:      # (axes as a list)
+        axes = bytes(axes)
+        key = key[:5] + (axes, interleaved)
+        plan = _plans.get(key)
+    if plan is None:
+        plan = _keep(key, _rotary_plan(q, k, positions, freq, axes, interleaved, inverse, what))
+    _, ref = plan
+    qo, ko = (None, None) if out is None else out
+    qo = _out(qo, q.shape, q.dtype, q.device, "out[0]")
+    kp = kop = None
+    if k is None:
+        ko = None
+    else:
+        ko = _out(ko, k.shape, k.dtype, k.device, "out[1]")
+        kp, kop = k.data_ptr(), ko.data_ptr()
+    rc = _tokens_lib().sconv_rotary(ref, q.data_ptr(), kp, positions.data_ptr(), freq.data_ptr(), qo.data_ptr(), kop,
+                                    _raw_stream(torch))
+    if rc:
+        raise SconvError(rc, what)
+    return qo, ko
+
+
+def _rotary_plan(q, k, positions, freq, axes, interleaved, inverse, what):
+    """(descriptor, reference to it)"""
     qt = _check(q, "q", 4)
     B, S, Hq, D = q.shape
     Hk = 0
@@ -238,29 +313,20 @@ def _rotary(q, k, positions, freq, axes, interleaved, inverse, out, what):
     _check_dev(freq, torch.float32, "inv_freq")
     _check_dev(positions, torch.int32, "positions")
     pairs = len(axes)
-    if positions.dim() == 2:
-        positions = positions.unsqueeze(0)
-    if positions.dim() != 3 or positions.shape[0] not in (1, B) or positions.shape[1] != S:
+    batch = positions.shape[0] if positions.dim() == 3 else 1
+    if positions.dim() not in (2, 3) or batch not in (1, B) or positions.shape[-2] != S:
         raise ValueError("positions must be [B or 1, S, axes] or [S, axes]")
-    n_axes = positions.shape[2]
+    n_axes = positions.shape[-1]
     if freq.dim() != 1 or freq.shape[0] != pairs:
         raise ValueError("inv_freq must have one value a pair, as axes has")
     if pairs > SCONV_ROTARY_MAX_PAIRS:
         raise SconvError(-2, what)
-    qo, ko = (None, None) if out is None else out
-    qo = _out(qo, q.shape, q.dtype, q.device, "out[0]")
-    ko = None if k is None else _out(ko, k.shape, k.dtype, k.device, "out[1]")
     desc = RotaryDesc(B, S, Hq, Hk, D, qt, pairs, n_axes, 1 if interleaved else 0, inverse, q.stride(0), q.stride(1),
-                      q.stride(2), 0, 0, 0, S * Hq * D, Hq * D, D, S * Hk * D, Hk * D, D,
-                      S * n_axes if positions.shape[0] > 1 else 0)
+                      q.stride(2), 0, 0, 0, S * Hq * D, Hq * D, D, S * Hk * D, Hk * D, D, S * n_axes if batch > 1 else 0)
     if Hk:
         desc.k_b, desc.k_s, desc.k_h = k.stride(0), k.stride(1), k.stride(2)
     ctypes.memmove(ctypes.addressof(desc) + RotaryDesc.axis.offset, bytes(axes), pairs)
-    rc = _tokens_lib().sconv_rotary(ctypes.byref(desc), q.data_ptr(), _opt(k), positions.data_ptr(), freq.data_ptr(),
-                                    qo.data_ptr(), _opt(ko), _raw_stream(torch))
-    if rc:
-        raise SconvError(rc, what)
-    return qo, ko
+    return desc, ctypes.byref(desc)
 
 
 def sconv_rotary_forward(q, k, positions, inv_freq, axes: bytes, interleaved: bool = False, out=None):
@@ -279,6 +345,22 @@ def sconv_rotary_backward(dq, dk, positions, inv_freq, axes: bytes, interleaved:
 
 
 # ---- differential attention
+
+def _attn_plan(q, k, v, lam, scale, causal, k_lengths, k_mask):
+    """(descriptor, reference to it, out's shape, lse's, bytes of scratch forward and backward)"""
+    key = (4, _sig(q), _sig(k), _sig(v), _sig(lam), scale, causal, _sig(k_lengths), _sig(k_mask))
+    plan = _plans.get(key)
+    if plan is None:
+        desc = _attn_desc(q, k, v, lam, scale, causal, k_lengths, k_mask)
+        need = [_sz(), _sz()]
+        for backward in (0, 1):
+            rc = _tokens_lib().sconv_diffattn_workspace_size(ctypes.byref(desc), backward, ctypes.byref(need[backward]))
+            if rc:
+                raise SconvError(rc, "sconv_diffattn")
+        plan = _keep(key, (desc, ctypes.byref(desc), (desc.B, desc.Sq, desc.H, desc.Dv), (2, desc.B, desc.H, desc.Sq),
+                           need[0].value, need[1].value))
+    return plan
+
 
 def _attn_desc(q, k, v, lam, scale, causal, k_lengths, k_mask):
     qt = _check(q, "q", 4)
@@ -313,11 +395,7 @@ def _attn_desc(q, k, v, lam, scale, causal, k_lengths, k_mask):
 
 def sconv_diffattn_workspace_size(q, k, v, lam, backward: bool = False) -> int:
     """Bytes of scratch that a call on these tensors can use (forward) or needs (backward)."""
-    desc, n = _attn_desc(q, k, v, lam, None, False, None, None), _sz()
-    rc = _tokens_lib().sconv_diffattn_workspace_size(ctypes.byref(desc), 1 if backward else 0, ctypes.byref(n))
-    if rc:
-        raise SconvError(rc, "sconv_diffattn_workspace_size")
-    return n.value
+    return _attn_plan(q, k, v, lam, None, False, None, None)[5 if backward else 4]
 
 
 def sconv_diffattn_forward(q, k, v, lam, scale: Optional[float] = None, causal: bool = False, k_lengths=None, k_mask=None,
@@ -330,22 +408,16 @@ def sconv_diffattn_forward(q, k, v, lam, scale: Optional[float] = None, causal: 
     that sees nothing gives zeros.  One token over a cache is the same call with Sq = 1 and k, v the cache.  Returns out
     [B, Sq, H, Dv]; save: (out, second, lse), the last two for sconv_diffattn_backward.  ws: a device tensor as
     scratch for calls of few queries (by default torch's allocator is asked)."""
-    desc = _attn_desc(q, k, v, lam, scale, causal, k_lengths, k_mask)
-    shape = (desc.B, desc.Sq, desc.H, desc.Dv)
-    L = _tokens_lib()
+    _, ref, shape, lse_shape, need, _ = _attn_plan(q, k, v, lam, scale, causal, k_lengths, k_mask)
     out = _out(out, shape, q.dtype, q.device, "out")
-    second = lse = None
+    second = lse = sp = lp = None
     if save:
         second = torch.empty(shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty((2, desc.B, desc.H, desc.Sq), dtype=torch.float32, device=q.device)
-    need = _sz()
-    rc = L.sconv_diffattn_workspace_size(ctypes.byref(desc), 0, ctypes.byref(need))
-    if rc:
-        raise SconvError(rc, "sconv_diffattn_forward")
-    ws, ptr, nbytes = _ws(ws, need.value, q.device)
-    rc = L.sconv_diffattn_forward(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), lam.data_ptr(),
-                                  _opt(k_lengths), _opt(k_mask), out.data_ptr(), _opt(second), _opt(lse), ptr, nbytes,
-                                  _raw_stream(torch))
+        lse = torch.empty(lse_shape, dtype=torch.float32, device=q.device)
+        sp, lp = second.data_ptr(), lse.data_ptr()
+    ws, ptr, nbytes = _ws(ws, need, q.device)
+    rc = _tokens_lib().sconv_diffattn_forward(ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), lam.data_ptr(), _opt(k_lengths),
+                                              _opt(k_mask), out.data_ptr(), sp, lp, ptr, nbytes, _raw_stream(torch))
     if rc:
         raise SconvError(rc, "sconv_diffattn_forward")
     return (out, second, lse) if save else out
@@ -355,29 +427,23 @@ def sconv_diffattn_backward(dout, q, k, v, lam, out, second, lse, scale: Optiona
                             k_lengths=None, k_mask=None, ws=None):
     """Gradient of sconv_diffattn_forward: (dq, dk, dv, dlam), contiguous, in the shapes and types of q, k, v, lam.
     out, second, lse: what the forward call returned with save; the other arguments as they were given to it."""
-    desc = _attn_desc(q, k, v, lam, scale, causal, k_lengths, k_mask)
-    shape = (desc.B, desc.Sq, desc.H, desc.Dv)
+    _, ref, shape, lse_shape, _, need = _attn_plan(q, k, v, lam, scale, causal, k_lengths, k_mask)
     for t, what in ((dout, "dout"), (out, "out"), (second, "second")):
         _check_dev(t, q.dtype, what)
-        if tuple(t.shape) != shape:
+        if t.shape != shape:
             raise ValueError(f"{what} must be [B, Sq, H, Dv]")
     _check_dev(lse, torch.float32, "lse")
-    if tuple(lse.shape) != (2, desc.B, desc.H, desc.Sq):
+    if lse.shape != lse_shape:
         raise ValueError("lse must be [2, B, H, Sq]")
-    L = _tokens_lib()
-    need = _sz()
-    rc = L.sconv_diffattn_workspace_size(ctypes.byref(desc), 1, ctypes.byref(need))
-    if rc:
-        raise SconvError(rc, "sconv_diffattn_backward")
     dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
     dv = torch.empty(v.shape, dtype=v.dtype, device=v.device)
     dlam = torch.empty(lam.shape, dtype=torch.float32, device=lam.device)
-    ws, ptr, nbytes = _ws(ws, need.value, q.device)
-    rc = L.sconv_diffattn_backward(ctypes.byref(desc), dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                   lam.data_ptr(), _opt(k_lengths), _opt(k_mask), out.data_ptr(), second.data_ptr(),
-                                   lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dlam.data_ptr(), ptr, nbytes,
-                                   _raw_stream(torch))
+    ws, ptr, nbytes = _ws(ws, need, q.device)
+    rc = _tokens_lib().sconv_diffattn_backward(ref, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), lam.data_ptr(),
+                                               _opt(k_lengths), _opt(k_mask), out.data_ptr(), second.data_ptr(),
+                                               lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dlam.data_ptr(),
+                                               ptr, nbytes, _raw_stream(torch))
     if rc:
         raise SconvError(rc, "sconv_diffattn_backward")
     return dq, dk, dv, dlam
