@@ -53,8 +53,10 @@ template <typename T, int DT, int DVT>
 struct WideShape {
     static constexpr int NW = 4, BN = 32, ROWS = 32 * NW;
     static constexpr int WAVES = sizeof(T) == 2 && DT <= 64 ? 2 : 1;
-    static constexpr int TILE = BN * (Tile<T, 2 * DT>::LD + Tile<T, DVT>::LD);
-    static constexpr size_t LDS = (size_t)2 * TILE * sizeof(T) + 3 * 4;    // (one tile is written while the other is read)
+    typedef Tile<T, BN, 2 * DT> Keys;
+    typedef Tile<T, BN, DVT> Values;
+    static constexpr int TILE = Keys::SIZE + Values::SIZE;
+    static constexpr size_t LDS = (size_t)2 * TILE * 2 + 3 * 4;    // (one tile is written while the other is read)
 };
 
 // A row's part of a call whose keys are split: unweighted sums and statistics, for the joining kernel.
@@ -150,10 +152,12 @@ __global__ __launch_bounds__(256, (WideShape<T, DT, DVT>::WAVES)) void attn_wide
 {
     typedef WideShape<T, DT, DVT> Shape;
     constexpr int NW = Shape::NW, BN = Shape::BN, ROWS = Shape::ROWS;
-    constexpr int KLD = Tile<T, 2 * DT>::LD, VLD = Tile<T, DVT>::LD, KS = DT / 16, NT = DVT / 32, TH = 64 * NW;
+    typedef typename Shape::Keys Keys;
+    typedef typename Shape::Values Values;
+    constexpr int KS = DT / 16, NT = DVT / 32, TH = 64 * NW;
     typedef typename Frag<T>::type frag;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    T* tiles = (T*)lds;
+    bf16* tiles = (bf16*)lds;
     uint32_t* words = (uint32_t*)(tiles + 2 * Shape::TILE);    // [3]: of the tile that is read, the next one and the one after
 
     const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
@@ -205,12 +209,12 @@ __global__ __launch_bounds__(256, (WideShape<T, DT, DVT>::WAVES)) void attn_wide
         }
     };
     const auto put = [&](int j0, int turn, int slot) {
-        T* kt = tiles + turn * Shape::TILE;
+        bf16* kt = tiles + turn * Shape::TILE;
         const uint32_t* wd = mask || j0 + BN > n ? words + slot : nullptr;
         ks.store(kt, wd, a.D);
-        vs.store(kt + BN * KLD, wd, dvn);
+        vs.store(kt + Keys::SIZE, wd, dvn);
     };
-    const int vcol = col_lane<T, VLD>();
+    const int vcol = col_lane<Values::LD>();
     const auto after = [](int slot) { return slot == 2 ? 0 : slot + 1; };
     int turn = 0, slot = 0;
     if (k0 < k1) {
@@ -228,16 +232,16 @@ __global__ __launch_bounds__(256, (WideShape<T, DT, DVT>::WAVES)) void attn_wide
             if (j0 + 2 * BN < k1) fetch(j0 + 2 * BN);
         }
         if (j0 < wmax) {
-            const T* kt = tiles + turn * Shape::TILE;
-            const T* vt = kt + BN * KLD;
-            const T* krow = kt + (l & 31) * KLD + 8 * h;
+            const bf16* kt = tiles + turn * Shape::TILE;
+            const bf16* vt = kt + Keys::SIZE;
+            const bf16* krow = kt + (l & 31) * Keys::LD + 8 * h;
             f32x16 s[2];
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[m][e] = 0.0f;
 #pragma unroll
-                for (int t = 0; t < KS; ++t) s[m] = mma(s[m], row_frag(krow + m * DT + 16 * t), qf[m][t]);
+                for (int t = 0; t < KS; ++t) s[m] = mma(s[m], tile_row<T, Keys::PLANE>(krow + m * DT + 16 * t), qf[m][t]);
             }
             const uint32_t word = mask || j0 + BN > n ? words[slot] : ~0u;
             if (j0 + 32 > wmin || (mask && word != ~0u)) {
@@ -258,7 +262,7 @@ __global__ __launch_bounds__(256, (WideShape<T, DT, DVT>::WAVES)) void attn_wide
                 to_frag(s[1], st, p1);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const frag vf = col_frag<VLD>(vt + vcol + 16 * st * VLD + 32 * t);
+                    const frag vf = tile_col<T, Values::LD, Values::PLANE>(vt + vcol + 16 * st * Values::LD + 32 * t);
                     o[0][t] = mma(o[0][t], vf, p0);
                     o[1][t] = mma(o[1][t], vf, p1);
                 }
@@ -442,29 +446,31 @@ __global__ __launch_bounds__(256, (DT <= 64 ? 2 : 1)) void attn_direct(AttnArgs 
 // barrier stands between its loads.  The wavefronts join at the end.
 template <typename T, int DVT>
 struct FewShape {
-    static constexpr int NW = 4, BN = 32, VLD = Tile<T, DVT>::LD;
-    static constexpr int TILE = BN * VLD;              // elements of LDS a wavefront
+    static constexpr int NW = 4, BN = 32;
+    typedef Tile<T, BN, DVT> Values;                   // of a wavefront
 };
 
 template <typename T, bool VEC, int DT, int DVT, int RT>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)) void attn_few(AttnArgs a)
 {
     typedef FewShape<T, DVT> Shape;
-    constexpr int NW = Shape::NW, BN = Shape::BN, VLD = Shape::VLD, KS = DT / 32, NT = DVT / 16, E = 16 / sizeof(T);
+    typedef typename Shape::Values Values;
+    constexpr int NW = Shape::NW, BN = Shape::BN, KS = DT / 32, NT = DVT / 16, E = 16 / sizeof(T);
     constexpr int NV = BN * DVT / E / 64, VPER = DVT / E;   // 16-byte vectors of a lane's and a row's share of the values
     typedef typename Frag<T>::type frag;
     extern __shared__ __attribute__((aligned(16))) char lds[];
 
     const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
+    const int first = (int)(blockIdx.x / bh_all) * 16 * RT;
     const int split = blockIdx.y, dv0 = blockIdx.z * DVT, dvn = min(DVT, a.Dv - dv0);
     const int w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, h = l >> 4;
-    T* vt = (T*)lds + w * Shape::TILE;
+    bf16* vt = (bf16*)lds + w * Values::SIZE;
     const int n = keys_of(a, b);
     int lim[RT], wmin = n;
     frag qf[RT][2][KS];
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
-        const int r = min(16 * x + c, a.rows - 1), i = r / a.G, g = r - i * a.G;
+        const int r = min(first + 16 * x + c, a.rows - 1), i = r / a.G, g = r - i * a.G;
         lim[x] = limit_of(a, i, n);
         const T* q = (const T*)a.q + b * a.q_b + i * a.q_s + (int64_t)(hk * a.G + g) * 2 * a.q_h;
 #pragma unroll
@@ -473,7 +479,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
             for (int s = 0; s < KS; ++s) qf[x][m][s] = global_frag<VEC>(q + m * a.q_h, 32 * s + 8 * h, a.D);
     }
     wmin = __builtin_amdgcn_readfirstlane(lim[0]);          // of the first row: limits rise
-    const int last = limit_of(a, (a.rows - 1) / a.G, n);
+    const int last = limit_of(a, min(first + 16 * RT - 1, a.rows - 1) / a.G, n);
     const int k0 = split * a.split_keys, k1 = (int)min((int64_t)last, (int64_t)k0 + a.split_keys);
     const uint8_t* mask = a.mask ? a.mask + b * a.mask_b : nullptr;
 
@@ -532,7 +538,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
         for (int v = 0; v < NV; ++v) {
             const int e = v * 64 + l, row = e / VPER;
             const bool there = e % VPER * E < dvn && (word >> row & 1);
-            *(u32x4*)(vt + row * VLD + e % VPER * E) = there ? vr[v] : u32x4{0, 0, 0, 0};
+            put16<Values::PLANE>(vt + row * Values::LD + e % VPER * E, vr[v], there, T());
         }
         if (next < k1) fetch_values(next);
         if (j0 + 32 > wmin || word != ~0u) {
@@ -549,7 +555,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
                     }
                 }
         }
-        frag p[RT][2];
+        float p[RT][2][8];
 #pragma unroll
         for (int x = 0; x < RT; ++x)
 #pragma unroll
@@ -572,18 +578,21 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
                     for (int e = 0; e < 4; ++e) {
                         const float v = __builtin_amdgcn_exp2f(fmaf(z[y][e], a.scale2, -safe[x][m]));
                         sum[x][m] += v;
-                        p[x][m][4 * y + e] = (T)v;
+                        p[x][m][4 * y + e] = v;
                     }
             }
-        const int vcol = few_col_lane<T, VLD>();
+        const int vcol = few_col_lane<Values::LD>();
+        frag pf[RT][2];
+#pragma unroll
+        for (int x = 0; x < RT; ++x) { to_frag(p[x][0], pf[x][0]); to_frag(p[x][1], pf[x][1]); }
         wave_lds_fence();
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const frag vf = few_col_frag<VLD>(vt + vcol + 16 * t);
+            const frag vf = tile_col<T, Values::LD, Values::PLANE, 16>(vt + vcol + 16 * t);
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
-                o[x][0][t] = mma(o[x][0][t], vf, p[x][0]);
-                o[x][1][t] = mma(o[x][1][t], vf, p[x][1]);
+                o[x][0][t] = mma(o[x][0][t], vf, pf[x][0]);
+                o[x][1][t] = mma(o[x][1][t], vf, pf[x][1]);
             }
         }
         wave_lds_fence();
@@ -650,7 +659,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
     if (w != 0) return;
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
-        const int mine = 16 * x + c, i = mine / a.G;
+        const int mine = first + 16 * x + c, i = mine / a.G;
         if (mine >= a.rows) continue;
         if (a.splits > 1) {
             const RowPart part(a, split, bh, mine);
@@ -736,7 +745,44 @@ __global__ __launch_bounds__(1024) void attn_join(AttnArgs a)
     }
 }
 
-struct FwdPlan { bool few; int row_tiles, chunks, splits, split_keys; size_t part, ml; };
+// The same for many rows in few parts (16 at most): a thread takes four values of a row, and each part's weight with them.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_join_wide(AttnArgs a)
+{
+    const int quads = (a.Dv + 3) / 4, wide = 4 * quads;
+    const int64_t all_rows = (int64_t)a.B * a.Hkv * a.rows, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= all_rows * quads) return;
+    const int64_t row = at / quads;
+    const int d = (int)(at - row * quads) * 4;
+    const int bh = (int)(row / a.rows), r = (int)(row - (int64_t)bh * a.rows), b = bh / a.Hkv, hk = bh % a.Hkv;
+    const int i = r / a.G, head = hk * a.G + r % a.G;
+    float most[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f}, o[2][4] = {};
+    for (int s = 0; s < a.splits; ++s) {
+        const f32x4 ml = *(const f32x4*)(a.part_ml + 4 * (s * all_rows + row));
+        most[0] = fmaxf(most[0], ml[0]);
+        most[1] = fmaxf(most[1], ml[2]);
+    }
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+        const f32x4 ml = *(const f32x4*)(a.part_ml + 4 * (s * all_rows + row));
+        const float* from = a.part + (s * all_rows + row) * 2 * wide + d;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const f32x4 x = *(const f32x4*)(from + m * wide);
+            // (parts of nothing were not written)
+            const bool some = ml[2 * m + 1] != 0.0f;
+            const float f = some ? __builtin_amdgcn_exp2f(ml[2 * m] - most[m]) : 0.0f;
+            sum[m] = fmaf(some ? ml[2 * m + 1] : 0.0f, f, sum[m]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[m][e] = fmaf(some ? x[e] : 0.0f, f, o[m][e]);
+        }
+    }
+    const RowOut<T> out(a, b, i, head, 0, a.Dv, sum);
+    out.store(d, o[0], o[1]);
+    if (d == 0) out.stats(a, most, sum);
+}
+
+struct FwdPlan { bool few; int rt, row_tiles, chunks, splits, split_keys; size_t part, ml; };
 
 int dim_tile(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
 
@@ -745,16 +791,22 @@ FwdPlan fwd_plan(const sconv_diffattn_desc_t& d, size_t ws_bytes)
     FwdPlan p = {};
     const int64_t G = d.H / d.Hkv, rows = d.Sq * G, bh = (int64_t)d.B * d.Hkv;
     const int DVT = dim_tile(d.D) == 32 ? 64 : 128;
+    // (32 rows at once: in 32 bits their pieces would not fit the registers)
     p.few = rows <= 32;
-    p.row_tiles = p.few ? 1 : (int)((rows + 127) / 128);
+    p.rt = rows > 16 && d.type == SCONV_BF16 ? 2 : 1;
+    const int tile = p.few ? 16 * p.rt : 128;
+    p.row_tiles = (int)((rows + tile - 1) / tile);
     p.chunks = (d.Dv + DVT - 1) / DVT;
     p.splits = 1;
     p.split_keys = d.Sk > 0 ? d.Sk : 1;
-    // keys are split, at 512 a part or more, where wide workgroups fill half of the chip at most, and until few ones fill it eight
-    // times over (requests' lengths differ, and a workgroup without keys ends at once)
+    // Keys are split until few rows' workgroups fill the chip eight times over (requests' lengths differ, and a workgroup without
+    // keys ends at once), at 512 a part or more; wide ones' where they fill half of the chip at most, at so many a part that the
+    // join, which reads 8 Dv bytes of every row and part, stays behind what it saves: 1024 in 16 bits (50 workgroups over 3136 keys: 48 us,
+    // unsplit 103; 112 over 784: 31 us unsplit, 38 in two), 256 in 32 (28 over 784: 90 us, unsplit 210).
     const int64_t base = p.row_tiles * bh * p.chunks;
     if (base == 0 || rows == 0) return p;
-    int64_t splits = std::min<int64_t>(p.few ? (2048 + base - 1) / base : 512 / base, (d.Sk + 511) / 512);
+    const int64_t least = p.few ? 512 : d.type == SCONV_BF16 ? 1024 : 256;
+    int64_t splits = std::min<int64_t>(p.few ? (2048 + base - 1) / base : 512 / base, (d.Sk + least - 1) / least);
     const int64_t wide = (d.Dv + 3) / 4 * 4, each = bh * rows * (2 * wide + 4) * (int64_t)sizeof(float);
     splits = std::min<int64_t>(std::min<int64_t>(splits, MAX_SPLITS), (int64_t)(ws_bytes / (size_t)each));
     if (splits > 1) {
@@ -794,12 +846,13 @@ int direct_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
 template <typename T, bool VEC, int DT, int DVT, int RT>
 int few_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
 {
-    constexpr size_t tiles = (size_t)4 * FewShape<T, DVT>::TILE * sizeof(T), join = (size_t)(4 * RT * 64 + 2 * RT * 2 * DVT * 16) * 4;
+    constexpr size_t tiles = (size_t)4 * FewShape<T, DVT>::Values::SIZE * 2, join = (size_t)(4 * RT * 64 + 2 * RT * 2 * DVT * 16) * 4;
     constexpr size_t lds = join > tiles ? join : tiles;
     const auto kern = attn_few<T, VEC, DT, DVT, RT>;
     const int rc = allow_lds(kern, lds);
     if (rc) return rc;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(a.B * a.Hkv), (unsigned)p.splits, (unsigned)p.chunks), dim3(256), lds, stream, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv), (unsigned)p.splits, (unsigned)p.chunks),
+                       dim3(256), lds, stream, a);
     return launch_status();
 }
 
@@ -813,7 +866,9 @@ int fwd_launch(const AttnArgs& a, const FwdPlan& p, hipStream_t stream)
             return direct_launch<DT, DVT>(a, p, stream);
     }
     if (!p.few) return wide_launch<T, VEC, DT, DVT>(a, p, stream);
-    return a.rows <= 16 ? few_launch<T, VEC, DT, DVT, 1>(a, p, stream) : few_launch<T, VEC, DT, DVT, 2>(a, p, stream);
+    if constexpr (sizeof(T) == 2)
+        if (p.rt == 2) return few_launch<T, VEC, DT, DVT, 2>(a, p, stream);
+    return few_launch<T, VEC, DT, DVT, 1>(a, p, stream);
 }
 
 template <typename T, bool VEC>
@@ -823,6 +878,11 @@ int fwd_run(AttnArgs& a, const FwdPlan& p, hipStream_t stream)
     const int rc = DT == 32 ? fwd_launch<T, VEC, 32, 64>(a, p, stream)
                  : DT == 64 ? fwd_launch<T, VEC, 64, 128>(a, p, stream) : fwd_launch<T, VEC, 128, 128>(a, p, stream);
     if (rc || p.splits == 1) return rc;
+    if (!p.few) {
+        const int64_t threads = (int64_t)a.B * a.Hkv * a.rows * ((a.Dv + 3) / 4);
+        hipLaunchKernelGGL((attn_join_wide<T>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, a);
+        return launch_status();
+    }
     hipLaunchKernelGGL((attn_join<T>), dim3((unsigned)((int64_t)a.B * a.Hkv * a.rows)), dim3(1024), 0, stream, a);
     return launch_status();
 }

@@ -128,12 +128,13 @@ template <typename T, bool VEC, int DT>
 __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
 {
     constexpr int NW = 4, TH = 256, BN = 32, DVT = 2 * DT;
-    constexpr int KLD = Tile<T, 2 * DT>::LD, VLD = Tile<T, DVT>::LD, KS = DT / 16, VS = DVT / 16, NT = DT / 32;
+    typedef Tile<T, BN, DVT> In;                       // (keys and values alike)
+    constexpr int KS = DT / 16, VS = DVT / 16, NT = DT / 32;
     typedef typename Frag<T>::type frag;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    T* kt = (T*)lds;
-    T* vt = kt + BN * KLD;
-    uint32_t* words = (uint32_t*)(vt + BN * VLD);      // [2]
+    bf16* kt = (bf16*)lds;
+    bf16* vt = kt + In::SIZE;
+    uint32_t* words = (uint32_t*)(vt + In::SIZE);      // [2]
 
     const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
     const int tile = a.row_tiles - 1 - blockIdx.x / bh_all;
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
         if (mask && threadIdx.x < BN) seen = mask[min(j0 + (int)threadIdx.x, n - 1)];
     };
     if (k1 > 0) fetch(0);
-    const int kcol = col_lane<T, KLD>();
+    const int kcol = col_lane<In::LD>();
     int turn = 0;
     for (int j0 = 0; j0 < k1; j0 += BN, turn ^= 1) {
         const bool whole = !mask && j0 + BN <= n;
@@ -198,14 +199,14 @@ __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
         f32x16 s0, s1, gt;
 #pragma unroll
         for (int e = 0; e < 16; ++e) s0[e] = s1[e] = gt[e] = 0.0f;
-        const T* krow = kt + (l & 31) * KLD + 8 * h;
-        const T* vrow = vt + (l & 31) * VLD + 8 * h;
+        const bf16* krow = kt + (l & 31) * In::LD + 8 * h;
+        const bf16* vrow = vt + (l & 31) * In::LD + 8 * h;
 #pragma unroll
-        for (int t = 0; t < KS; ++t) s0 = mma(s0, row_frag(krow + 16 * t), qf[0][t]);
+        for (int t = 0; t < KS; ++t) s0 = mma(s0, tile_row<T, In::PLANE>(krow + 16 * t), qf[0][t]);
 #pragma unroll
-        for (int t = 0; t < KS; ++t) s1 = mma(s1, row_frag(krow + DT + 16 * t), qf[1][t]);
+        for (int t = 0; t < KS; ++t) s1 = mma(s1, tile_row<T, In::PLANE>(krow + DT + 16 * t), qf[1][t]);
 #pragma unroll
-        for (int t = 0; t < VS; ++t) gt = mma(gt, row_frag(vrow + 16 * t), gf[t]);
+        for (int t = 0; t < VS; ++t) gt = mma(gt, tile_row<T, In::PLANE>(vrow + 16 * t), gf[t]);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             s0[e] = __builtin_amdgcn_exp2f(fmaf(s0[e], a.scale2, -lse0));
@@ -235,8 +236,8 @@ __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
             to_frag(s1, st, f1);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                acc[0][t] = mma(acc[0][t], col_frag<KLD>(kt + kcol + 16 * st * KLD + 32 * t), f0);
-                acc[1][t] = mma(acc[1][t], col_frag<KLD>(kt + kcol + 16 * st * KLD + DT + 32 * t), f1);
+                acc[0][t] = mma(acc[0][t], tile_col<T, In::LD, In::PLANE>(kt + kcol + 16 * st * In::LD + 32 * t), f0);
+                acc[1][t] = mma(acc[1][t], tile_col<T, In::LD, In::PLANE>(kt + kcol + 16 * st * In::LD + DT + 32 * t), f1);
             }
         }
         settle();
@@ -249,13 +250,14 @@ template <typename T, bool VEC, int DT, int WHAT>
 __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
 {
     constexpr int NW = 4, TH = 256, BM = 32, DVT = 2 * DT;
-    constexpr int QLD = Tile<T, 2 * DT>::LD, GLD = Tile<T, DVT>::LD, KS = DT / 16, VS = DVT / 16, NT = DT / 32, VT = DVT / 32;
+    typedef Tile<T, BM, DVT> In;                       // (queries and dout alike)
+    constexpr int KS = DT / 16, VS = DVT / 16, NT = DT / 32, VT = DVT / 32;
     constexpr bool DV = WHAT & 1, DK0 = WHAT & 2, DK1 = WHAT & 4, MAP0 = DV || DK0, MAP1 = DV || DK1, NEED_G = DK0 || DK1;
     typedef typename Frag<T>::type frag;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    T* qt = (T*)lds;
-    T* gt = qt + BM * QLD;
-    float* stats = (float*)(gt + BM * GLD);            // [2][4][32]: lse of both maps (log2), d of both
+    bf16* qt = (bf16*)lds;
+    bf16* gt = qt + In::SIZE;
+    float* stats = (float*)(gt + In::SIZE);            // [2][4][32]: lse of both maps (log2), d of both
     uint32_t* words = (uint32_t*)(stats + 256);        // [2]
 
     const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
@@ -309,7 +311,7 @@ __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
     };
     const bool any = j0 < n && start < a.Sq;
     if (any) fetch(0, start);
-    const int qcol = col_lane<T, QLD>(), gcol = col_lane<T, GLD>();
+    const int col = col_lane<In::LD>();
     int turn = 0;
     for (int g = 0, i0 = start; any && g < a.G; turn ^= 1) {
         float* st = stats + 128 * turn;
@@ -333,17 +335,17 @@ __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
         f32x16 s0, s1, gg;
 #pragma unroll
         for (int e = 0; e < 16; ++e) s0[e] = s1[e] = gg[e] = 0.0f;
-        const T* qrow = qt + (l & 31) * QLD + 8 * h;
-        const T* grow = gt + (l & 31) * GLD + 8 * h;
+        const bf16* qrow = qt + (l & 31) * In::LD + 8 * h;
+        const bf16* grow = gt + (l & 31) * In::LD + 8 * h;
         if (MAP0)
 #pragma unroll
-            for (int t = 0; t < KS; ++t) s0 = mma(s0, row_frag(qrow + 16 * t), kf[0][t]);
+            for (int t = 0; t < KS; ++t) s0 = mma(s0, tile_row<T, In::PLANE>(qrow + 16 * t), kf[0][t]);
         if (MAP1)
 #pragma unroll
-            for (int t = 0; t < KS; ++t) s1 = mma(s1, row_frag(qrow + DT + 16 * t), kf[1][t]);
+            for (int t = 0; t < KS; ++t) s1 = mma(s1, tile_row<T, In::PLANE>(qrow + DT + 16 * t), kf[1][t]);
         if (NEED_G)
 #pragma unroll
-            for (int t = 0; t < VS; ++t) gg = mma(gg, row_frag(grow + 16 * t), vf[t]);
+            for (int t = 0; t < VS; ++t) gg = mma(gg, tile_row<T, In::PLANE>(grow + 16 * t), vf[t]);
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
             const f32x4 l0 = *(const f32x4*)(st + 2 * e + 4 * h), l1 = *(const f32x4*)(st + 32 + 2 * e + 4 * h);
@@ -371,7 +373,7 @@ __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
                 frag f;
                 to_frag(p, x, f);
 #pragma unroll
-                for (int t = 0; t < VT; ++t) dv[t] = mma(dv[t], col_frag<GLD>(gt + gcol + 16 * x * GLD + 32 * t), f);
+                for (int t = 0; t < VT; ++t) dv[t] = mma(dv[t], tile_col<T, In::LD, In::PLANE>(gt + col + 16 * x * In::LD + 32 * t), f);
             }
         }
         if (NEED_G) {
@@ -391,8 +393,8 @@ __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
                 to_frag(s1, x, f1);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    if (DK0) dk[0][t] = mma(dk[0][t], col_frag<QLD>(qt + qcol + 16 * x * QLD + 32 * t), f0);
-                    if (DK1) dk[1][t] = mma(dk[1][t], col_frag<QLD>(qt + qcol + 16 * x * QLD + DT + 32 * t), f1);
+                    if (DK0) dk[0][t] = mma(dk[0][t], tile_col<T, In::LD, In::PLANE>(qt + col + 16 * x * In::LD + 32 * t), f0);
+                    if (DK1) dk[1][t] = mma(dk[1][t], tile_col<T, In::LD, In::PLANE>(qt + col + 16 * x * In::LD + DT + 32 * t), f1);
                 }
             }
         }
@@ -741,7 +743,7 @@ __global__ __launch_bounds__(256, 2) void attn_keys_direct(AttnArgs a)
 template <typename T, bool VEC, int DT, int WHAT>
 int keys_launch(const AttnArgs& a, hipStream_t stream)
 {
-    constexpr size_t lds = 32 * (Tile<T, 2 * DT>::LD + Tile<T, 2 * DT>::LD) * sizeof(T) + 256 * 4 + 8;
+    constexpr size_t lds = (size_t)2 * Tile<T, 32, 2 * DT>::SIZE * 2 + 256 * 4 + 8;
     const int rc = allow_lds(attn_bwd_keys<T, VEC, DT, WHAT>, lds);
     if (rc) return rc;
     const int64_t grid = (int64_t)((a.Sk + 127) / 128) * a.B * a.Hkv;
@@ -799,7 +801,7 @@ int bwd_main(const AttnArgs& a, hipStream_t stream)
         if (rc) return rc;
     }
     if (a.Sq == 0) return rc;
-    constexpr size_t lds = 32 * (Tile<T, 2 * DT>::LD + Tile<T, 2 * DT>::LD) * sizeof(T) + 8;
+    constexpr size_t lds = (size_t)2 * Tile<T, 32, 2 * DT>::SIZE * 2 + 8;
     rc = allow_lds(attn_bwd_rows<T, VEC, DT>, lds);
     if (rc) return rc;
     hipLaunchKernelGGL((attn_bwd_rows<T, VEC, DT>), dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv)), dim3(256), lds, stream, a);

@@ -1,9 +1,11 @@
 // Differential attention: what its kernels share.
 //
 // Layout of the matrix products.  A 32 x 32 product tile takes from each lane 8 elements of a row of A (row l % 32) and 8 of a
-// column of B (column l % 32), both at depths 8 (l / 32) .. + 7 of a 16-deep step (16-bit: one instruction; 32-bit: eight
-// of depth 2, element by element - the depths they pair differ, the sum of products is the same).  Of the result each lane
-// holds column l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4 in registers r = 0..15.
+// column of B (column l % 32), both at depths 8 (l / 32) .. + 7 of a 16-deep step.  Of the result each lane holds column
+// l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4 in registers r = 0..15.
+// 32-bit operands go through the 16-bit matrix pipe as well, as three pieces that hold 8 bits of the value each (their sum is the
+// value) and six of the nine products of pieces; the three left out are below 2^-24 of the product.  That is 192 cycles for what the
+// 32-bit pipe does in 512.
 // So a result can be the next product's B as it stands in its lane: registers 8s..8s+7 are the depths
 //   16 s + 4 (l / 32) + {0, 1, 2, 3, 8, 9, 10, 11}
 // of step s, provided that A's elements come in that order (col_frag below).  Scores are therefore formed transposed - keys down,
@@ -31,28 +33,50 @@ struct AttnArgs {
     int64_t q_b, q_s, q_h, k_b, k_s, k_h, v_b, v_s, v_h, mask_b;
 };
 
+struct bf16x8x3 { bf16x8 p[3]; };
 template <typename T> struct Frag;
-template <> struct Frag<bf16> { typedef bf16x8 type; };
-template <> struct Frag<float> { typedef f32x8 type; };
+template <> struct Frag<bf16> { typedef bf16x8 type; static constexpr int PLANES = 1; };
+template <> struct Frag<float> { typedef bf16x8x3 type; static constexpr int PLANES = 3; };
 
 __device__ __forceinline__ f32x16 mma(f32x16 c, bf16x8 a, bf16x8 b) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x16 mma(f32x16 c, f32x8 a, f32x8 b)
+__device__ __forceinline__ f32x4 mma(f32x4 c, bf16x8 a, bf16x8 b) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+template <typename C>
+__device__ __forceinline__ C mma(C c, const bf16x8x3& a, const bf16x8x3& b)
 {
+    c = mma(c, a.p[2], b.p[0]);
+    c = mma(c, a.p[0], b.p[2]);
+    c = mma(c, a.p[1], b.p[1]);
+    c = mma(c, a.p[1], b.p[0]);
+    c = mma(c, a.p[0], b.p[1]);
+    return mma(c, a.p[0], b.p[0]);
+}
+
+// Two values as pieces: the upper 16 bits of the value, of what is left, and of what is left then.  FINITE: neither Inf nor NaN comes
+// (Inf would leave Inf - Inf behind).
+template <bool FINITE>
+__device__ __forceinline__ void pieces(float x, float y, uint32_t& hi, uint32_t& mid, uint32_t& lo)
+{
+    const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
+    float xr = x - __uint_as_float(xb & 0xffff0000u), yr = y - __uint_as_float(yb & 0xffff0000u);
+    if constexpr (!FINITE) { xr = xr == xr ? xr : 0.0f; yr = yr == yr ? yr : 0.0f; }
+    const uint32_t xm = __float_as_uint(xr), ym = __float_as_uint(yr);
+    const float xl = xr - __uint_as_float(xm & 0xffff0000u), yl = yr - __uint_as_float(ym & 0xffff0000u);
+    hi = __builtin_amdgcn_perm(yb, xb, 0x07060302u);
+    mid = __builtin_amdgcn_perm(ym, xm, 0x07060302u);
+    lo = __builtin_amdgcn_perm(__float_as_uint(yl), __float_as_uint(xl), 0x07060302u);
+}
+template <bool FINITE>
+__device__ __forceinline__ bf16x8x3 in_pieces(const float (&v)[8])
+{
+    union { uint32_t u[4]; bf16x8 f; } p[3];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
-    return c;
+    for (int i = 0; i < 4; ++i) pieces<FINITE>(v[2 * i], v[2 * i + 1], p[0].u[i], p[1].u[i], p[2].u[i]);
+    return bf16x8x3{{p[0].f, p[1].f, p[2].f}};
 }
 
 // The same in tiles of 16 x 16 (32 deep): a lane has 8 elements at depths 8 (l / 16) .. + 7 of row or column l % 16, and of the result
 // column l % 16, rows 4 (l / 16) + 0..3.  Two results of 16 keys are the next product's B at depths
 //   4 (l / 16) + {0, 1, 2, 3, 16, 17, 18, 19}.
-__device__ __forceinline__ f32x4 mma(f32x4 c, bf16x8 a, bf16x8 b) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x4 mma(f32x4 c, f32x8 a, f32x8 b)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
-    return c;
-}
 
 // Ends a loop's round of products.  The compiler keeps its distance between a product and whoever reads its result, except, seen in
 // 32-bit code, where the first copy of a result stands behind the loop's exit branch: it then read registers a few
@@ -64,86 +88,91 @@ __device__ __forceinline__ void settle()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// A tile in LDS: rows of W elements and 16 bytes of padding, so that lanes reading one column chunk of consecutive
-// rows meet different banks.
-template <typename T, int W> struct Tile { static constexpr int E = 16 / sizeof(T), LD = W + E; };
+// A tile in LDS: rows of W 16-bit elements and 16 bytes of padding, so that lanes reading one column chunk of consecutive rows meet
+// different banks; 32-bit values in three such planes.
+template <typename T, int ROWS, int W>
+struct Tile { static constexpr int LD = W + 8, PLANE = ROWS * LD, SIZE = Frag<T>::PLANES * PLANE; };
 
 // 8 consecutive elements from an address aligned to 16 bytes.
 __device__ __forceinline__ bf16x8 row_frag(const bf16* p) { return *(const bf16x8*)p; }
-__device__ __forceinline__ f32x8 row_frag(const float* p)
+template <typename T, int PLANE>
+__device__ __forceinline__ typename Frag<T>::type tile_row(const bf16* p)
 {
-    const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
-    return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    if constexpr (sizeof(T) == 2) return row_frag(p);
+    else return bf16x8x3{{row_frag(p), row_frag(p + PLANE), row_frag(p + 2 * PLANE)}};
 }
 
-// The transposed tile's row fragment: column l % 32 of 32, depths (rows) 4 (l / 32) + {0..3, 8..11}.  p: the tile at its first row
+// The transposed tile's row fragment: column l % 32 of 32, depths (rows) 4 (l / 32) + {0..3} and SKIP more.  p: the tile at its first row
 // and column, plus col_lane().
-template <int LD>
+template <int LD, int SKIP = 8>
 __device__ __forceinline__ bf16x8 col_frag(const bf16* p)
 {
     typedef __attribute__((address_space(3))) s16x4 lds4;
     const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 8 * LD));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + SKIP * LD));
     union { s16x4 s[2]; bf16x8 v; } u;
     u.s[0] = a; u.s[1] = b;
     return u.v;
 }
-template <int LD>
-__device__ __forceinline__ f32x8 col_frag(const float* p)
+template <typename T, int LD, int PLANE, int SKIP = 8>
+__device__ __forceinline__ typename Frag<T>::type tile_col(const bf16* p)
 {
-    f32x8 v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[i] = p[i * LD]; v[4 + i] = p[(8 + i) * LD]; }
-    return v;
+    if constexpr (sizeof(T) == 2) return col_frag<LD, SKIP>(p);
+    else return bf16x8x3{{col_frag<LD, SKIP>(p), col_frag<LD, SKIP>(p + PLANE), col_frag<LD, SKIP>(p + 2 * PLANE)}};
 }
 // Where a lane reads (16 lanes of the transposing read take four rows of 16 columns; lane i has row i / 4, four columns).
-template <typename T, int LD>
+template <int LD>
 __device__ __forceinline__ int col_lane()
 {
-    const int l = threadIdx.x & 63, h = l >> 5;
-    if constexpr (sizeof(T) == 2) return (4 * h + ((l & 15) >> 2)) * LD + ((l >> 4) & 1) * 16 + (l & 3) * 4;
-    else return 4 * h * LD + (l & 31);
+    const int l = threadIdx.x & 63;
+    return (4 * (l >> 5) + ((l & 15) >> 2)) * LD + ((l >> 4) & 1) * 16 + (l & 3) * 4;
 }
-
 // For tiles of 16 x 16: column l % 16 of 16, depths 4 (l / 16) + {0..3, 16..19}.
 template <int LD>
-__device__ __forceinline__ bf16x8 few_col_frag(const bf16* p)
-{
-    typedef __attribute__((address_space(3))) s16x4 lds4;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 16 * LD));
-    union { s16x4 s[2]; bf16x8 v; } u;
-    u.s[0] = a; u.s[1] = b;
-    return u.v;
-}
-template <int LD>
-__device__ __forceinline__ f32x8 few_col_frag(const float* p)
-{
-    f32x8 v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[i] = p[i * LD]; v[4 + i] = p[(16 + i) * LD]; }
-    return v;
-}
-template <typename T, int LD>
 __device__ __forceinline__ int few_col_lane()
 {
-    const int l = threadIdx.x & 63, h = l >> 4;
-    if constexpr (sizeof(T) == 2) return (4 * h + ((l & 15) >> 2)) * LD + (l & 3) * 4;
-    else return 4 * h * LD + (l & 15);
+    const int l = threadIdx.x & 63;
+    return (4 * (l >> 4) + ((l & 15) >> 2)) * LD + (l & 3) * 4;
 }
 // Between a wavefront's own writes and reads of LDS: they are carried out in order; the compiler is told to leave them so.
 __device__ __forceinline__ void wave_lds_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
 
 // Registers 8s..8s+7 of a result as the next product's B.
-__device__ __forceinline__ void to_frag(const f32x16& p, int s, bf16x8& f)
+__device__ __forceinline__ void to_frag(const float (&v)[8], bf16x8& f)
 {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (bf16)p[8 * s + i];
+    for (int i = 0; i < 8; ++i) f[i] = (bf16)v[i];
 }
-__device__ __forceinline__ void to_frag(const f32x16& p, int s, f32x8& f)
+__device__ __forceinline__ void to_frag(const float (&v)[8], bf16x8x3& f) { f = in_pieces<true>(v); }
+template <typename F>
+__device__ __forceinline__ void to_frag(const f32x16& p, int s, F& f)
 {
+    float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = p[8 * s + i];
+    for (int i = 0; i < 8; ++i) v[i] = p[8 * s + i];
+    to_frag(v, f);
+}
+
+// 16 bytes of a row in memory into a tile (rows that are not there: zeros).
+template <int PLANE>
+__device__ __forceinline__ void put16(bf16* to, u32x4 r, bool there, bf16)
+{
+    *(u32x4*)to = there ? r : u32x4{0, 0, 0, 0};
+}
+template <int PLANE>
+__device__ __forceinline__ void put16(bf16* to, u32x4 r, bool there, float)
+{
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    if (!there) r = u32x4{0, 0, 0, 0};
+    u32x2 p[3];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t hi, mid, lo;
+        pieces<false>(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]), hi, mid, lo);
+        p[0][i] = hi; p[1][i] = mid; p[2][i] = lo;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *(u32x2*)(to + k * PLANE) = p[k];
 }
 
 // 16 bytes of elements d.. of a row that has `have` of them.  VEC: d and the row are aligned and `have` is whole 16 bytes;
@@ -170,14 +199,14 @@ __device__ __forceinline__ bf16x8 global_frag(const bf16* row, int d, int have)
     return r.v;
 }
 template <bool VEC>
-__device__ __forceinline__ f32x8 global_frag(const float* row, int d, int have)
+__device__ __forceinline__ bf16x8x3 global_frag(const float* row, int d, int have)
 {
-    union { u32x4 u[2]; f32x8 v; } r;
+    union { u32x4 u[2]; float v[8]; } r;
     r.u[0] = load16<VEC>(row, d, have);
     r.u[1] = load16<VEC>(row, d + 4, have);
     if (d >= have) r.u[0] = u32x4{0, 0, 0, 0};
     if (d + 4 >= have) r.u[1] = u32x4{0, 0, 0, 0};
-    return r.v;
+    return in_pieces<false>(r.v);
 }
 
 // Four neighbouring results of a row (columns d..d+3 of `have`).
@@ -243,7 +272,8 @@ __device__ __forceinline__ int limit_of(const AttnArgs& a, int i, int n)
 // the one before.  A row has PARTS rows of W elements of memory beside each other (the two keys of a head).
 template <typename T, bool VEC, int ROWS, int PARTS, int W, int THREADS>
 struct Stage {
-    static constexpr int E = 16 / sizeof(T), PER = PARTS * W / E, N = ROWS * PER / THREADS, LD = Tile<T, PARTS * W>::LD;
+    typedef Tile<T, ROWS, PARTS * W> To;
+    static constexpr int E = 16 / sizeof(T), PER = PARTS * W / E, N = ROWS * PER / THREADS;
     static_assert(N * THREADS == ROWS * PER, "whole vectors for every thread");
     u32x4 r[N];
 
@@ -258,13 +288,13 @@ struct Stage {
         }
     }
     // words: a bit for every row that is there (LDS), null: all are
-    __device__ __forceinline__ void store(T* tile, const uint32_t* words, int have) const
+    __device__ __forceinline__ void store(bf16* tile, const uint32_t* words, int have) const
     {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int e = n * THREADS + threadIdx.x, row = e / PER, c = e % PER, d = (c % (W / E)) * E;
             const bool there = d < have && (!words || (words[row >> 5] >> (row & 31) & 1));
-            *(u32x4*)(tile + row * LD + c * E) = there ? r[n] : u32x4{0, 0, 0, 0};
+            put16<To::PLANE>(tile + row * To::LD + c * E, r[n], there, T());
         }
     }
 };
