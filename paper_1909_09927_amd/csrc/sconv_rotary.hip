@@ -39,14 +39,21 @@ __device__ __forceinline__ void turn_of(int pos, float freq, float* c, float* s)
 template <typename T, int V, bool INTER>
 __global__ __launch_bounds__(256) void rotary_kernel(RotArgs a, int TT)
 {
-    extern __shared__ float cs[];        // [TT][pairs] cosines, then sines
-    const int64_t t0 = (int64_t)blockIdx.x * TT;
-    const int here = (int)min((int64_t)TT, a.tokens - t0);
+    extern __shared__ __attribute__((aligned(16))) float cs[];   // [TT][pairs] cosines, then sines; then where the tokens' heads begin
+    const uint32_t t0 = blockIdx.x * (uint32_t)TT;               // (tokens fit 31 bits)
+    const int here = (int)min((uint32_t)TT, (uint32_t)a.tokens - t0);
     float* sn = cs + TT * a.pairs;
+    int64_t* begin = (int64_t*)(sn + TT * a.pairs);              // [TT][4]: q, k, and the results
+    if ((int)threadIdx.x < here) {
+        const uint32_t tok = t0 + threadIdx.x, b = tok / (uint32_t)a.S, s = tok - b * (uint32_t)a.S;
+        begin[4 * threadIdx.x] = b * a.q_b + s * a.q_s;
+        begin[4 * threadIdx.x + 1] = b * a.k_b + s * a.k_s;
+        begin[4 * threadIdx.x + 2] = b * a.qo_b + s * a.qo_s;
+        begin[4 * threadIdx.x + 3] = b * a.ko_b + s * a.ko_s;
+    }
     for (int e = threadIdx.x; e < here * a.pairs; e += 256) {
         const int t = e / a.pairs, p = e - t * a.pairs;
-        const int64_t tok = t0 + t;
-        const int b = (int)(tok / a.S), s = (int)(tok - (int64_t)b * a.S);
+        const uint32_t tok = t0 + t, b = tok / (uint32_t)a.S, s = tok - b * (uint32_t)a.S;
         float c, v;
         turn_of(a.pos[b * a.pos_b + (int64_t)s * a.axes + a.axis[p]], a.freq[p], &c, &v);
         cs[e] = c;
@@ -57,13 +64,10 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotArgs a, int TT)
     const int turning = a.pairs / V, rest = (a.D - 2 * a.pairs) / V, units = turning + rest;
     const int heads = a.Hq + a.Hk, per = heads * units, all = here * per;
     for (int e = threadIdx.x; e < all; e += 256) {
-        const int t = e / per, r = e - t * per, hh = r / units, u = r - hh * units;
-        const int64_t tok = t0 + t;
-        const int64_t b = tok / a.S, s = tok - b * a.S;
+        const int t = (int)((uint32_t)e / (uint32_t)per), r = e - t * per, hh = (int)((uint32_t)r / (uint32_t)units), u = r - hh * units;
         const bool key = hh >= a.Hq;
-        const int h = key ? hh - a.Hq : hh;
-        const T* x = key ? (const T*)a.k + b * a.k_b + s * a.k_s + h * a.k_h : (const T*)a.q + b * a.q_b + s * a.q_s + h * a.q_h;
-        T* y = key ? (T*)a.ko + b * a.ko_b + s * a.ko_s + h * a.ko_h : (T*)a.qo + b * a.qo_b + s * a.qo_s + h * a.qo_h;
+        const T* x = key ? (const T*)a.k + begin[4 * t + 1] + (hh - a.Hq) * a.k_h : (const T*)a.q + begin[4 * t] + hh * a.q_h;
+        T* y = key ? (T*)a.ko + begin[4 * t + 3] + (hh - a.Hq) * a.ko_h : (T*)a.qo + begin[4 * t + 2] + hh * a.qo_h;
         float v0[V], v1[V], o0[V], o1[V];
         if (u >= turning) {
             const int i = 2 * a.pairs + (u - turning) * V;
@@ -108,9 +112,9 @@ int rotary_run(const RotArgs& a, bool inter, bool vec, hipStream_t stream)
     // about 2048 vectors a workgroup, and at least two workgroups a compute unit where there are so many tokens
     const int64_t per = std::max<int64_t>(1, (int64_t)(a.Hq + a.Hk) * a.D / (2 * (vec ? V : 1)));
     int64_t TT = std::max<int64_t>(1, std::min<int64_t>(2048 / per, a.tokens / 512));
-    TT = std::min<int64_t>(TT, 4096 / a.pairs);
+    TT = std::min<int64_t>(std::min<int64_t>(TT, 4096 / a.pairs), 256);
     const unsigned grid = (unsigned)((a.tokens + TT - 1) / TT);
-    const size_t lds = (size_t)TT * a.pairs * 2 * sizeof(float);
+    const size_t lds = (size_t)TT * (a.pairs * 2 * sizeof(float) + 4 * sizeof(int64_t));
     if (vec && inter) hipLaunchKernelGGL((rotary_kernel<T, V, true>), dim3(grid), dim3(256), lds, stream, a, (int)TT);
     else if (vec) hipLaunchKernelGGL((rotary_kernel<T, V, false>), dim3(grid), dim3(256), lds, stream, a, (int)TT);
     else if (inter) hipLaunchKernelGGL((rotary_kernel<T, 1, true>), dim3(grid), dim3(256), lds, stream, a, (int)TT);

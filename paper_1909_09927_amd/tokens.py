@@ -18,6 +18,7 @@ SCONV_F32, SCONV_BF16 = 0, 1
 SCONV_LAYOUT_TOKENS, SCONV_LAYOUT_MAP = 0, 1
 SCONV_ROTARY_MAX_AXES, SCONV_ROTARY_MAX_PAIRS = 8, 256
 
+_CONTIGUOUS = torch.contiguous_format
 _TYPES = {torch.float32: SCONV_F32, torch.bfloat16: SCONV_BF16}
 _LAYOUTS = {"tokens": SCONV_LAYOUT_TOKENS, "map": SCONV_LAYOUT_MAP}
 _i32, _i64, _vp, _sz, _f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
@@ -179,7 +180,10 @@ def sconv_layernorm_forward(x, weight=None, bias=None, eps: float = 1e-5, layout
     if plan is None:
         plan = _keep(key, _layernorm_plan(x, weight, bias, eps, layout, out_dtype))
     _, ref, shape, lead, dtype = plan
-    y = _out(out, shape, dtype, x.device, "out")
+    if out is None and dtype is x.dtype and layout == "tokens":
+        y = torch.empty_like(x, memory_format=_CONTIGUOUS)
+    else:
+        y = _out(out, shape, dtype, x.device, "out")
     mean = rstd = mp = rp = None
     if stats:
         mean = torch.empty(lead, dtype=torch.float32, device=x.device)
@@ -220,7 +224,7 @@ def sconv_layernorm_backward(dy, x, mean, rstd, weight=None, layout: str = "toke
     if plan is None:
         plan = _keep(key, _layernorm_grad_plan(dy, x, mean, rstd, weight, layout))
     _, ref, C, wdtype, need = plan
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dx = torch.empty_like(x, memory_format=_CONTIGUOUS)
     dw = db = ptr = None
     nbytes = 0
     if param_grads:
@@ -284,13 +288,16 @@ def _rotary(q, k, positions, freq, axes, interleaved, inverse, out, what):
     if plan is None:
         plan = _keep(key, _rotary_plan(q, k, positions, freq, axes, interleaved, inverse, what))
     _, ref = plan
-    qo, ko = (None, None) if out is None else out
-    qo = _out(qo, q.shape, q.dtype, q.device, "out[0]")
-    kp = kop = None
-    if k is None:
-        ko = None
+    ko = kp = kop = None
+    if out is None:
+        qo = torch.empty_like(q, memory_format=_CONTIGUOUS)
+        if k is not None:
+            ko = torch.empty_like(k, memory_format=_CONTIGUOUS)
     else:
-        ko = _out(ko, k.shape, k.dtype, k.device, "out[1]")
+        qo = _out(out[0], q.shape, q.dtype, q.device, "out[0]")
+        if k is not None:
+            ko = _out(out[1], k.shape, k.dtype, k.device, "out[1]")
+    if k is not None:
         kp, kop = k.data_ptr(), ko.data_ptr()
     rc = _tokens_lib().sconv_rotary(ref, q.data_ptr(), kp, positions.data_ptr(), freq.data_ptr(), qo.data_ptr(), kop,
                                     _raw_stream(torch))
@@ -435,10 +442,7 @@ def sconv_diffattn_backward(dout, q, k, v, lam, out, second, lse, scale: Optiona
     _check_dev(lse, torch.float32, "lse")
     if lse.shape != lse_shape:
         raise ValueError("lse must be [2, B, H, Sq]")
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device)
-    dlam = torch.empty(lam.shape, dtype=torch.float32, device=lam.device)
+    dq, dk, dv, dlam = (torch.empty_like(t, memory_format=_CONTIGUOUS) for t in (q, k, v, lam))
     ws, ptr, nbytes = _ws(ws, need, q.device)
     rc = _tokens_lib().sconv_diffattn_backward(ref, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), lam.data_ptr(),
                                                _opt(k_lengths), _opt(k_mask), out.data_ptr(), second.data_ptr(),
