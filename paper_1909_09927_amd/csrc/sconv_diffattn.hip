@@ -460,7 +460,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
     typedef typename Frag<T>::type frag;
     extern __shared__ __attribute__((aligned(16))) char lds[];
 
-    const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
+    // (a request's splits on different chiplets, whose blocks go round: requests' lengths differ)
+    const int bh_all = a.B * a.Hkv, bh = (int)((blockIdx.x + blockIdx.y) % (uint32_t)bh_all), b = bh / a.Hkv, hk = bh % a.Hkv;
     const int first = (int)(blockIdx.x / bh_all) * 16 * RT;
     const int split = blockIdx.y, dv0 = blockIdx.z * DVT, dvn = min(DVT, a.Dv - dv0);
     const int w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, h = l >> 4;
@@ -496,7 +497,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
 
     const T* kb = (const T*)a.k + b * a.k_b + (int64_t)hk * 2 * a.k_h;
     const T* vb = (const T*)a.v + b * a.v_b + (int64_t)hk * a.v_h + dv0;
-    frag kf[2][2][KS];                                 // [16 keys][map][depth]
+    Raw<T> kr[2][2][KS];                               // [16 keys][map][depth]
     u32x4 vr[NV];
     uint8_t seen = 1;
     const auto fetch_keys = [&](int j0) {
@@ -506,7 +507,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int s = 0; s < KS; ++s) kf[y][m][s] = global_frag<VEC>(row + m * a.k_h, 32 * s + 8 * h, a.D);
+                for (int s = 0; s < KS; ++s) load_raw<VEC>(kr[y][m][s], row + m * a.k_h, 32 * s + 8 * h, a.D);
         }
     };
     const auto fetch_values = [&](int j0) {
@@ -522,16 +523,20 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
     for (; j0 < k1; j0 += BN * NW) {
         const int next = j0 + BN * NW;
         f32x4 s[RT][2][2];                             // [rows][map][16 keys]
+        const bool ragged = a.D < DT;
 #pragma unroll
-        for (int x = 0; x < RT; ++x)
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+            for (int y = 0; y < 2; ++y) {
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    s[x][m][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                for (int x = 0; x < RT; ++x) s[x][m][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int t = 0; t < KS; ++t) s[x][m][y] = mma(s[x][m][y], kf[y][m][t], qf[x][m][t]);
+                for (int t = 0; t < KS; ++t) {
+                    const frag kf = raw_frag(kr[y][m][t], 32 * t + 8 * h, a.D, ragged);
+#pragma unroll
+                    for (int x = 0; x < RT; ++x) s[x][m][y] = mma(s[x][m][y], kf, qf[x][m][t]);
                 }
+            }
         if (next < k1) fetch_keys(next);
         const uint32_t word = mask || j0 + BN > n ? (uint32_t)__ballot(j0 + (l & 31) < n && seen) : ~0u;
 #pragma unroll
@@ -786,7 +791,7 @@ struct FwdPlan { bool few; int rt, row_tiles, chunks, splits, split_keys; size_t
 
 int dim_tile(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
 
-FwdPlan fwd_plan(const sconv_diffattn_desc_t& d, size_t ws_bytes)
+FwdPlan fwd_plan(const sconv_diffattn_desc_t& d, bool lengths, size_t ws_bytes)
 {
     FwdPlan p = {};
     const int64_t G = d.H / d.Hkv, rows = d.Sq * G, bh = (int64_t)d.B * d.Hkv;
@@ -799,14 +804,15 @@ FwdPlan fwd_plan(const sconv_diffattn_desc_t& d, size_t ws_bytes)
     p.chunks = (d.Dv + DVT - 1) / DVT;
     p.splits = 1;
     p.split_keys = d.Sk > 0 ? d.Sk : 1;
-    // Keys are split until few rows' workgroups fill the chip eight times over (requests' lengths differ, and a workgroup without
-    // keys ends at once), at 512 a part or more; wide ones' where they fill half of the chip at most, at so many a part that the
-    // join, which reads 8 Dv bytes of every row and part, stays behind what it saves: 1024 in 16 bits (50 workgroups over 3136 keys: 48 us,
-    // unsplit 103; 112 over 784: 31 us unsplit, 38 in two), 256 in 32 (28 over 784: 90 us, unsplit 210).
+    // Keys are split.  Few rows': until their workgroups fill the chip twice over at two a compute unit, at 512 keys a part or more;
+    // four times over and 1024 where requests' lengths differ (16 requests of up to 32768 keys: 16 parts).  Wide ones':
+    // where they fill half of the chip at most, at so many a part that the join, which reads 8 Dv bytes of every row and part,
+    // stays behind what it saves: 1024 in 16 bits (50 workgroups over 3136 keys: 48 us, unsplit 103; 112 over 784: 31 us
+    // unsplit, 38 in two), 256 in 32 (28 over 784: 90 us, unsplit 210).
     const int64_t base = p.row_tiles * bh * p.chunks;
     if (base == 0 || rows == 0) return p;
-    const int64_t least = p.few ? 512 : d.type == SCONV_BF16 ? 1024 : 256;
-    int64_t splits = std::min<int64_t>(p.few ? (2048 + base - 1) / base : 512 / base, (d.Sk + least - 1) / least);
+    const int64_t least = p.few ? (lengths ? 1024 : 512) : d.type == SCONV_BF16 ? 1024 : 256, most = lengths ? 1024 : 512;
+    int64_t splits = std::min<int64_t>(p.few ? (most + base - 1) / base : 512 / base, (d.Sk + least - 1) / least);
     const int64_t wide = (d.Dv + 3) / 4 * 4, each = bh * rows * (2 * wide + 4) * (int64_t)sizeof(float);
     splits = std::min<int64_t>(std::min<int64_t>(splits, MAX_SPLITS), (int64_t)(ws_bytes / (size_t)each));
     if (splits > 1) {
@@ -911,8 +917,12 @@ bool attn_vector(const AttnArgs& a, int type)
 
 size_t diffattn_forward_workspace(const sconv_diffattn_desc_t& d)
 {
-    const FwdPlan p = fwd_plan(d, ~(size_t)0 >> 1);
-    return p.part + p.ml;
+    size_t most = 0;
+    for (const bool lengths : {false, true}) {
+        const FwdPlan p = fwd_plan(d, lengths, ~(size_t)0 >> 1);
+        most = std::max(most, p.part + p.ml);
+    }
+    return most;
 }
 
 int launch_diffattn_forward(const sconv_diffattn_desc_t& d, const void* q, const void* k, const void* v, const float* lam,
@@ -921,7 +931,7 @@ int launch_diffattn_forward(const sconv_diffattn_desc_t& d, const void* q, const
 {
     AttnArgs a = attn_args(d, q, k, v, lam, lengths, mask);
     if (d.B == 0 || d.Sq == 0) return SCONV_OK;
-    const FwdPlan p = fwd_plan(d, ws_bytes);
+    const FwdPlan p = fwd_plan(d, lengths != nullptr, ws_bytes);
     a.out = out; a.second = second; a.lse = lse;
     a.ovec = aligned_to(out, 16) && aligned_to(second, 16);
     a.splits = p.splits; a.split_keys = p.split_keys; a.row_tiles = p.row_tiles;

@@ -189,24 +189,37 @@ __device__ __forceinline__ u32x4 load16(const T* row, int d, int have)
     for (int i = 0; i < E; ++i) if (d + i >= have) r.e[i] = (T)0.0f;
     return r.u;
 }
-// (the fragment of a row that is read from memory, cleared beyond `have`)
-template <bool VEC>
-__device__ __forceinline__ bf16x8 global_frag(const bf16* row, int d, int have)
+// A fragment of a row in memory as it is loaded, and as it is used (cleared beyond `have`): apart, so that nothing waits for the load
+// before its use.
+template <typename T> struct Raw { u32x4 u[sizeof(T) / 2]; };
+template <bool VEC, typename T>
+__device__ __forceinline__ void load_raw(Raw<T>& r, const T* row, int d, int have)
 {
-    union { u32x4 u; bf16x8 v; } r;
-    r.u = load16<VEC>(row, d, have);
-    if (d >= have) r.u = u32x4{0, 0, 0, 0};
-    return r.v;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.u[i] = load16<VEC>(row, d + 4 * i, have);
 }
-template <bool VEC>
-__device__ __forceinline__ bf16x8x3 global_frag(const float* row, int d, int have)
+__device__ __forceinline__ bf16x8 raw_frag(const Raw<bf16>& r, int d, int have, bool ragged)
 {
-    union { u32x4 u[2]; float v[8]; } r;
-    r.u[0] = load16<VEC>(row, d, have);
-    r.u[1] = load16<VEC>(row, d + 4, have);
-    if (d >= have) r.u[0] = u32x4{0, 0, 0, 0};
-    if (d + 4 >= have) r.u[1] = u32x4{0, 0, 0, 0};
-    return in_pieces<false>(r.v);
+    union { u32x4 u; bf16x8 v; } x;
+    x.u = r.u[0];
+    if (ragged && d >= have) x.u = u32x4{0, 0, 0, 0};
+    return x.v;
+}
+__device__ __forceinline__ bf16x8x3 raw_frag(const Raw<float>& r, int d, int have, bool ragged)
+{
+    union { u32x4 u[2]; float v[8]; } x;
+    x.u[0] = r.u[0];
+    x.u[1] = r.u[1];
+    if (ragged && d >= have) x.u[0] = u32x4{0, 0, 0, 0};
+    if (ragged && d + 4 >= have) x.u[1] = u32x4{0, 0, 0, 0};
+    return in_pieces<false>(x.v);
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ typename Frag<T>::type global_frag(const T* row, int d, int have)
+{
+    Raw<T> r;
+    load_raw<VEC>(r, row, d, have);
+    return raw_frag(r, d, have, true);
 }
 
 // Four neighbouring results of a row (columns d..d+3 of `have`).
