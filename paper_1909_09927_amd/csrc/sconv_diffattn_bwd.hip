@@ -562,7 +562,9 @@ __global__ __launch_bounds__(256, 2) void attn_keys_direct(AttnArgs a)
     constexpr int TILE = BM * 2 * DVT;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     bf16* tiles = (bf16*)lds;
-    float* stats = (float*)(tiles + 2 * TILE);         // [2][4][BM]: lse of both maps (log2), d of both
+    // [2][4][BM]: lse of both maps (log2) and d of both; lam's size is taken into the second lse - |lam| A_2 = exp2(S_2 - it) - and
+    // its sign into the second d
+    float* stats = (float*)(tiles + 2 * TILE);
     uint32_t* words = (uint32_t*)(stats + 8 * BM);     // [2][MB]
 
     const int bh_all = a.B * a.Hkv, bh = blockIdx.x % bh_all, b = bh / a.Hkv, hk = bh % a.Hkv;
@@ -618,8 +620,10 @@ __global__ __launch_bounds__(256, 2) void attn_keys_direct(AttnArgs a)
         // thread: statistic x row
         const int i = min(i0 + (int)(threadIdx.x % BM), a.Sq - 1), what = threadIdx.x / BM;
         const int64_t at = ((int64_t)b * a.H + head) * a.Sq + i;
+        const float lam = a.lam[head];
         sum = a.lse_in[at];
-        stat = what == 0 ? sum * LOG2E : what == 1 ? a.lse_in[half + at] * LOG2E : a.delta[at + (what == 3 ? half : 0)];
+        stat = what == 0 ? sum * LOG2E : what == 1 ? a.lse_in[half + at] * LOG2E - log2f(fabsf(lam)) : a.delta[at + (what == 3 ? half : 0)];
+        if (what == 3) stat = copysignf(1.0f, lam) * stat;
     };
     const auto mark = [&](int i0, int turn) {
         const bool there = i0 + (int)(threadIdx.x % BM) < a.Sq && sum != -INFINITY;
@@ -646,7 +650,7 @@ __global__ __launch_bounds__(256, 2) void attn_keys_direct(AttnArgs a)
             Grads::clear(gt, words + turn * MB);
             __syncthreads();
         }
-        const float lam = a.lam[hk * a.G + was];
+        const float sign = -copysignf(1.0f, a.lam[hk * a.G + was]);   // of the second map
 #pragma unroll 1
         for (int x0 = 0; x0 < MB; x0 += SUB) {
             const int is = at + 32 * x0;
@@ -706,7 +710,7 @@ __global__ __launch_bounds__(256, 2) void attn_keys_direct(AttnArgs a)
                     if (DV) {
                         bf16x8 f;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) f[e] = (bf16)fmaf(-lam, s1[x][8 * y + e], s0[x][8 * y + e]);
+                        for (int e = 0; e < 8; ++e) f[e] = (bf16)fmaf(sign, s1[x][8 * y + e], s0[x][8 * y + e]);
 #pragma unroll
                         for (int t = 0; t < VT; ++t)
                             dv[t] = mma(dv[t], col_frag<DVT>(gs + col2[t % 2] + t / 2 * 64 + 16 * y * DVT), f);
@@ -720,7 +724,7 @@ __global__ __launch_bounds__(256, 2) void attn_keys_direct(AttnArgs a)
                             for (int z = 0; z < 4; ++z) {
                                 const int u = 8 * y + e + z;
                                 f0[e + z] = (bf16)(s0[x][u] * (gg[x][u] - d0[z]));
-                                f1[e + z] = (bf16)(s1[x][u] * (-lam * (gg[x][u] - d1[z])));
+                                f1[e + z] = (bf16)(s1[x][u] * fmaf(sign, gg[x][u], d1[z]));
                             }
                         }
 #pragma unroll
