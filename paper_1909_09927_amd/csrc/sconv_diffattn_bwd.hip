@@ -79,8 +79,24 @@ __device__ __forceinline__ void rows_end(const AttnArgs& a, int b, int i, int he
 {
     spread = half_sum(spread);
     if (mine >= a.rows) return;
+    const int64_t at = (((int64_t)b * a.Sq + i) * a.H + head) * 2 * a.D;
+    if (a.row_splits > 1) {
+        const int64_t split = blockIdx.y, all = (int64_t)a.B * a.Sq * a.H;
+        if (h == 0) a.part_s[split * all + stat] = spread;
+        float* to = a.part_q + split * all * 2 * a.D + at;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const float x[4] = {acc[m][t][e], acc[m][t][e + 1], acc[m][t][e + 2], acc[m][t][e + 3]};
+                    store4(to + m * a.D, 32 * t + 8 * (e >> 2) + 4 * h, a.D, a.D % 4 == 0, x);
+                }
+        return;
+    }
     if (h == 0) a.dlam_part[stat] = spread;
-    T* dq = (T*)a.dq + (((int64_t)b * a.Sq + i) * a.H + head) * 2 * a.D;
+    T* dq = (T*)a.dq + at;
     const bool v4 = a.ovec && a.D % 4 == 0;
 #pragma unroll
     for (int m = 0; m < 2; ++m)
@@ -99,8 +115,8 @@ template <typename T, int NT, int VT, int WHAT>
 __device__ __forceinline__ void keys_end(const AttnArgs& a, int b, int hk, int j, int h, const f32x16 (&dk)[2][NT], const f32x16 (&dv)[VT])
 {
     if (j >= a.Sk) return;
-    T* kout = (T*)a.dk + (((int64_t)b * a.Sk + j) * a.Hkv + hk) * 2 * a.D;
-    T* vout = (T*)a.dv + (((int64_t)b * a.Sk + j) * a.Hkv + hk) * a.Dv;
+    const int64_t row = ((int64_t)b * a.Sk + j) * a.Hkv + hk, all = (int64_t)a.B * a.Sk * a.Hkv, split = blockIdx.y;
+    const bool parts = a.key_splits > 1;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
         if (!(WHAT >> (m + 1) & 1)) continue;
@@ -108,10 +124,11 @@ __device__ __forceinline__ void keys_end(const AttnArgs& a, int b, int hk, int j
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
-                float x[4];
-#pragma unroll
-                for (int z = 0; z < 4; ++z) x[z] = dk[m][t][e + z] * a.scale;
-                store4(kout + m * a.D, 32 * t + 8 * (e >> 2) + 4 * h, a.D, a.ovec && a.D % 4 == 0, x);
+                const int d = 32 * t + 8 * (e >> 2) + 4 * h;
+                const float f = parts ? 1.0f : a.scale;
+                const float x[4] = {dk[m][t][e] * f, dk[m][t][e + 1] * f, dk[m][t][e + 2] * f, dk[m][t][e + 3] * f};
+                if (parts) store4(a.part_k + (split * all + row) * 2 * a.D + m * a.D, d, a.D, a.D % 4 == 0, x);
+                else store4((T*)a.dk + row * 2 * a.D + m * a.D, d, a.D, a.ovec && a.D % 4 == 0, x);
             }
     }
     if (WHAT & 1)
@@ -119,9 +136,29 @@ __device__ __forceinline__ void keys_end(const AttnArgs& a, int b, int hk, int j
         for (int t = 0; t < VT; ++t)
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
+                const int d = 32 * t + 8 * (e >> 2) + 4 * h;
                 const float x[4] = {dv[t][e], dv[t][e + 1], dv[t][e + 2], dv[t][e + 3]};
-                store4(vout, 32 * t + 8 * (e >> 2) + 4 * h, a.Dv, a.ovec && a.Dv % 4 == 0, x);
+                if (parts) store4(a.part_v + (split * all + row) * a.Dv, d, a.Dv, a.Dv % 4 == 0, x);
+                else store4((T*)a.dv + row * a.Dv, d, a.Dv, a.ovec && a.Dv % 4 == 0, x);
             }
+}
+
+// Parts of dq, dk, dv and of dlam's rows, added in one order: one launch for up to four arrays.
+struct PartSums { const float* from[4]; void* to[4]; int64_t n[4]; int splits[4], wide[4]; float scale[4]; };   // wide: 32-bit results
+template <typename T>
+__global__ __launch_bounds__(256) void attn_add_parts(PartSums p, int64_t all)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        int64_t k = i;
+        int w = 0;
+        while (w < 3 && k >= p.n[w]) k -= p.n[w++];
+        float v = 0.0f;
+#pragma unroll 4
+        for (int s = 0; s < p.splits[w]; ++s) v += p.from[w][s * p.n[w] + k];
+        v *= p.scale[w];
+        if (p.wide[w]) ((float*)p.to[w])[k] = v;
+        else ((T*)p.to[w])[k] = (T)v;
+    }
 }
 
 template <typename T, bool VEC, int DT>
@@ -148,7 +185,7 @@ __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
     const int see = limit_of(a, i, n), lim = none ? 0 : see;
     // (limits of the rows rise; a row that the mask leaves empty only makes its wavefront test every key)
     const int wmin = __any(none) ? 0 : __builtin_amdgcn_readfirstlane(see), wmax = __builtin_amdgcn_readlane(see, 31);
-    const int k1 = limit_of(a, min(tile * 32 * NW + 32 * NW - 1, a.rows - 1) / a.G, n);
+    const int k0 = blockIdx.y * a.row_keys, k1 = min(limit_of(a, min(tile * 32 * NW + 32 * NW - 1, a.rows - 1) / a.G, n), k0 + a.row_keys);
     const uint8_t* mask = a.mask ? a.mask + b * a.mask_b : nullptr;
 
     frag qf[2][KS], gf[VS];
@@ -180,10 +217,10 @@ __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
         vs.load(vb, a.v_s, 0, j0, n, a.Dv);
         if (mask && threadIdx.x < BN) seen = mask[min(j0 + (int)threadIdx.x, n - 1)];
     };
-    if (k1 > 0) fetch(0);
+    if (k0 < k1) fetch(k0);
     const int kcol = col_lane<In::LD>();
     int turn = 0;
-    for (int j0 = 0; j0 < k1; j0 += BN, turn ^= 1) {
+    for (int j0 = k0; j0 < k1; j0 += BN, turn ^= 1) {
         const bool whole = !mask && j0 + BN <= n;
         uint32_t* wd = words + turn;
         if (!whole && threadIdx.x < BN) {
@@ -309,11 +346,17 @@ __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
             stat = what == 0 ? sum * LOG2E : what == 1 ? a.lse_in[half + at] * LOG2E : a.delta[at + (what == 3 ? half : 0)];
         }
     };
-    const bool any = j0 < n && start < a.Sq;
-    if (any) fetch(0, start);
+    // this part of the (head, tile of queries) pairs
+    const int per = start < a.Sq && j0 < n ? (a.Sq - start + BM - 1) / BM : 0;
+    const int64_t pairs = (int64_t)per * a.G;
+    int64_t left = pairs * (blockIdx.y + 1) / a.key_splits;
+    const int64_t from = pairs * blockIdx.y / a.key_splits;
+    left -= from;
+    int g = per ? (int)(from / per) : 0, i0 = per ? start + (int)(from % per) * BM : 0;
+    if (left > 0) fetch(g, i0);
     const int col = col_lane<In::LD>();
     int turn = 0;
-    for (int g = 0, i0 = start; any && g < a.G; turn ^= 1) {
+    for (; left > 0; turn ^= 1) {
         float* st = stats + 128 * turn;
         if (threadIdx.x < 128) {
             // a row that is not there, or sees nothing, is cleared: its weights, all 1 then, meet zeros
@@ -330,7 +373,7 @@ __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
         const float lam = a.lam[hk * a.G + g];
         i0 += BM;
         if (i0 >= a.Sq) { i0 = start; ++g; }
-        if (g < a.G) fetch(g, i0);
+        if (--left > 0) fetch(g, i0);
         if (at + BM <= wfirst || j0 + 32 * w >= n) continue;
         f32x16 s0, s1, gg;
 #pragma unroll
@@ -423,7 +466,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_direct(AttnArgs a)
     const bool none = lse0 == -INFINITY;
     const int see = limit_of(a, i, n), lim = none ? 0 : see;
     const int wmin = __any(none) ? 0 : __builtin_amdgcn_readfirstlane(see), wmax = __builtin_amdgcn_readlane(see, 31);
-    const int k1 = limit_of(a, min(tile * 32 * NW + 32 * NW - 1, a.rows - 1) / a.G, n);
+    const int k0 = blockIdx.y * a.row_keys, k1 = min(limit_of(a, min(tile * 32 * NW + 32 * NW - 1, a.rows - 1) / a.G, n), k0 + a.row_keys);
     const uint8_t* mask = a.mask ? a.mask + b * a.mask_b : nullptr;
 
     bf16x8 qf[2][KS], gf[VS];
@@ -471,13 +514,13 @@ __global__ __launch_bounds__(256, 2) void attn_rows_direct(AttnArgs a)
     };
     const auto after = [](int slot) { return slot == 2 ? 0 : slot + 1; };
     int turn = 0, slot = 0;
-    if (k1 > 0) {
-        fetch(0, 0);
-        fetch_mask(0);
-        mark(0, 0);
-        if (BN < k1) { fetch_mask(BN); mark(BN, 1); }
+    if (k0 < k1) {
+        fetch(k0, 0);
+        fetch_mask(k0);
+        mark(k0, 0);
+        if (k0 + BN < k1) { fetch_mask(k0 + BN); mark(k0 + BN, 1); }
     }
-    for (int j0 = 0; j0 < k1; j0 += BN, turn ^= 1, slot = after(slot)) {
+    for (int j0 = k0; j0 < k1; j0 += BN, turn ^= 1, slot = after(slot)) {
         __syncthreads();
         if (j0 + BN < k1) fetch(j0 + BN, turn ^ 1);
         if (j0 + 2 * BN < k1) fetch_mask(j0 + 2 * BN);
@@ -631,15 +674,20 @@ __global__ __launch_bounds__(256, 2) void attn_keys_direct(AttnArgs a)
         const uint64_t bits = __ballot(there);
         if (threadIdx.x < MB) words[turn * MB + threadIdx.x] = (uint32_t)(threadIdx.x ? bits >> 32 : bits);
     };
-    const bool any = j0 < n && start < a.Sq;
-    int turn = 0, g = 0, i0 = start;
-    if (any) { fetch(0, start, 0); mark(start, 0); }
-    while (any && g < a.G) {
+    // this part of the (head, tile of queries) pairs
+    const int per = start < a.Sq && j0 < n ? (a.Sq - start + BM - 1) / BM : 0;
+    const int64_t pairs = (int64_t)per * a.G;
+    int64_t left = pairs * (blockIdx.y + 1) / a.key_splits;
+    const int64_t from = pairs * blockIdx.y / a.key_splits;
+    left -= from;
+    int turn = 0, g = per ? (int)(from / per) : 0, i0 = per ? start + (int)(from % per) * BM : 0;
+    if (left > 0) { fetch(g, i0, 0); mark(i0, 0); }
+    while (left > 0) {
         __syncthreads();
         const int at = i0, was = g;
         i0 += BM;
         if (i0 >= a.Sq) { i0 = start; ++g; }
-        if (g < a.G) fetch(g, i0, turn ^ 1);
+        if (--left > 0) fetch(g, i0, turn ^ 1);
         bf16* qt = tiles + turn * TILE;
         bf16* gt = qt + BM * DVT;
         bool whole = true;
@@ -738,7 +786,7 @@ __global__ __launch_bounds__(256, 2) void attn_keys_direct(AttnArgs a)
             }
             settle();
         }
-        if (g < a.G) mark(i0, turn ^ 1);
+        if (left > 0) mark(i0, turn ^ 1);
         turn ^= 1;
     }
     keys_end<bf16, NT, VT, WHAT>(a, b, hk, j, h, dk, dv);
@@ -751,7 +799,7 @@ int keys_launch(const AttnArgs& a, hipStream_t stream)
     const int rc = allow_lds(attn_bwd_keys<T, VEC, DT, WHAT>, lds);
     if (rc) return rc;
     const int64_t grid = (int64_t)((a.Sk + 127) / 128) * a.B * a.Hkv;
-    hipLaunchKernelGGL((attn_bwd_keys<T, VEC, DT, WHAT>), dim3((unsigned)grid), dim3(256), lds, stream, a);
+    hipLaunchKernelGGL((attn_bwd_keys<T, VEC, DT, WHAT>), dim3((unsigned)grid, (unsigned)a.key_splits), dim3(256), lds, stream, a);
     return launch_status();
 }
 
@@ -761,8 +809,8 @@ int keys_direct_launch(const AttnArgs& a, hipStream_t stream)
     constexpr size_t lds = (size_t)2 * 64 * 4 * DT * sizeof(bf16) + 8 * 64 * 4 + 4 * 4;
     const int rc = allow_lds(attn_keys_direct<DT, WHAT, SUB>, lds);
     if (rc) return rc;
-    hipLaunchKernelGGL((attn_keys_direct<DT, WHAT, SUB>), dim3((unsigned)((int64_t)((a.Sk + 127) / 128) * a.B * a.Hkv)), dim3(256), lds,
-                       stream, a);
+    hipLaunchKernelGGL((attn_keys_direct<DT, WHAT, SUB>), dim3((unsigned)((int64_t)((a.Sk + 127) / 128) * a.B * a.Hkv), (unsigned)a.key_splits),
+                       dim3(256), lds, stream, a);
     return launch_status();
 }
 
@@ -779,7 +827,7 @@ int direct_main(const AttnArgs& a, hipStream_t stream)
     constexpr size_t lds = (size_t)2 * 64 * 4 * DT * sizeof(bf16) + 3 * 2 * 4;
     rc = allow_lds(attn_rows_direct<DT>, lds);
     if (rc) return rc;
-    hipLaunchKernelGGL((attn_rows_direct<DT>), dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv)), dim3(256), lds, stream, a);
+    hipLaunchKernelGGL((attn_rows_direct<DT>), dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv), (unsigned)a.row_splits), dim3(256), lds, stream, a);
     return launch_status();
 }
 
@@ -808,7 +856,7 @@ int bwd_main(const AttnArgs& a, hipStream_t stream)
     constexpr size_t lds = (size_t)2 * Tile<T, 32, 2 * DT>::SIZE * 2 + 8;
     rc = allow_lds(attn_bwd_rows<T, VEC, DT>, lds);
     if (rc) return rc;
-    hipLaunchKernelGGL((attn_bwd_rows<T, VEC, DT>), dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv)), dim3(256), lds, stream, a);
+    hipLaunchKernelGGL((attn_bwd_rows<T, VEC, DT>), dim3((unsigned)((int64_t)a.row_tiles * a.B * a.Hkv), (unsigned)a.row_splits), dim3(256), lds, stream, a);
     return launch_status();
 }
 
@@ -828,13 +876,62 @@ int bwd_run(const AttnArgs& a, float* dlam, hipStream_t stream)
     else if (most <= 64) rc = bwd_main<T, VEC, 64>(a, stream);
     else rc = bwd_main<T, VEC, 128>(a, stream);
     if (rc) return rc;
+    PartSums p = {};
+    int64_t all = 0;
+    const auto add = [&](int w, const float* from, void* to, int64_t n, int splits, float scale, bool wide) {
+        if (splits < 2) return;
+        p.from[w] = from; p.to[w] = to; p.n[w] = n; p.splits[w] = splits; p.scale[w] = scale; p.wide[w] = wide;
+        all += n;
+    };
+    const int64_t queries = (int64_t)a.B * a.Sq * a.H, keys = (int64_t)a.B * a.Sk * a.Hkv;
+    add(0, a.part_q, a.dq, queries * 2 * a.D, a.row_splits, a.scale, false);
+    add(1, a.part_k, a.dk, keys * 2 * a.D, a.key_splits, a.scale, false);
+    add(2, a.part_v, a.dv, keys * a.Dv, a.key_splits, 1.0f, false);
+    add(3, a.part_s, a.dlam_part, queries, a.row_splits, 1.0f, true);
+    if (all > 0) {
+        hipLaunchKernelGGL((attn_add_parts<T>), dim3((unsigned)std::min<int64_t>((all + 255) / 256, 1 << 20)), dim3(256), 0, stream, p, all);
+        rc = launch_status();
+        if (rc) return rc;
+    }
     hipLaunchKernelGGL(attn_dlam, dim3((unsigned)a.H), dim3(1024), 0, stream, a.dlam_part, a.B, a.H, a.Sq, dlam);
     return launch_status();
 }
 
 }  // namespace
 
-size_t diffattn_backward_workspace(const sconv_diffattn_desc_t& d) { return (size_t)d.B * d.H * d.Sq * 3 * sizeof(float); }
+namespace {
+
+// Parts where the workgroups of a kernel do not fill the chip: of the keys for dq, of the (head, tile of queries) pairs for dk and dv; up to
+// a workgroup a compute unit, two tiles a part at least.
+struct BwdPlan { int row_splits, row_keys, key_splits; size_t rows, q, s, k, v; };
+
+BwdPlan bwd_plan(const sconv_diffattn_desc_t& d)
+{
+    BwdPlan p = {1, d.Sk > 0 ? d.Sk : 1, 1, 0, 0, 0, 0, 0};
+    const int64_t G = d.H / d.Hkv, bh = (int64_t)d.B * d.Hkv, queries = (int64_t)d.B * d.Sq * d.H, keys = bh * d.Sk;
+    p.rows = (size_t)(3 * queries) * sizeof(float);
+    if (queries == 0 || keys == 0) return p;
+    const int64_t row_blocks = (d.Sq * G + 127) / 128 * bh, key_blocks = ((int64_t)d.Sk + 127) / 128 * bh;
+    const int64_t row = std::min<int64_t>(256 / row_blocks, d.Sk / 128), key = std::min<int64_t>(256 / key_blocks, G * ((d.Sq + 63) / 64) / 2);
+    if (row > 1) {
+        p.row_keys = (int)((d.Sk + row - 1) / row + 63) / 64 * 64;
+        p.row_splits = (d.Sk + p.row_keys - 1) / p.row_keys;
+    }
+    if (key > 1) p.key_splits = (int)key;
+    const auto whole = [](int64_t floats) { return (size_t)((floats + 3) / 4 * 4) * sizeof(float); };    // (16-byte steps)
+    p.rows = whole(3 * queries);
+    if (p.row_splits > 1) { p.q = whole(p.row_splits * queries * 2 * d.D); p.s = whole(p.row_splits * queries); }
+    if (p.key_splits > 1) { p.k = whole(p.key_splits * keys * 2 * d.D); p.v = whole(p.key_splits * keys * d.Dv); }
+    return p;
+}
+
+}  // namespace
+
+size_t diffattn_backward_workspace(const sconv_diffattn_desc_t& d)
+{
+    const BwdPlan p = bwd_plan(d);
+    return p.rows + p.q + p.s + p.k + p.v;
+}
 
 int launch_diffattn_backward(const sconv_diffattn_desc_t& d, const void* dout, const void* q, const void* k, const void* v,
                              const float* lam, const int32_t* lengths, const uint8_t* mask, const void* out,
@@ -849,6 +946,13 @@ int launch_diffattn_backward(const sconv_diffattn_desc_t& d, const void* dout, c
     a.delta = (float*)ws;
     a.dlam_part = a.delta + 2 * (int64_t)d.B * d.H * d.Sq;
     a.row_tiles = (a.rows + 127) / 128;
+    const BwdPlan p = bwd_plan(d);
+    a.row_splits = p.row_splits; a.row_keys = p.row_keys; a.key_splits = p.key_splits;
+    char* at = (char*)ws + p.rows;
+    a.part_q = (float*)at;
+    a.part_s = (float*)(at += p.q);
+    a.part_k = (float*)(at += p.s);
+    a.part_v = (float*)(at += p.k);
     if (d.B == 0) a.Sq = a.Sk = 0;                     // nothing but lam's gradient to clear
     if (d.type == SCONV_BF16) return vec ? bwd_run<bf16, true>(a, dlam, stream) : bwd_run<bf16, false>(a, dlam, stream);
     return vec ? bwd_run<float, true>(a, dlam, stream) : bwd_run<float, false>(a, dlam, stream);

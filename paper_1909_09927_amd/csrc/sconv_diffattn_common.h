@@ -26,6 +26,8 @@ struct AttnArgs {
     void* dq; void* dk; void* dv;
     float* part; float* part_ml;                             // forward over several splits: [split][B Hkv][rows]..
     float* delta; float* dlam_part;                          // backward: [2][B][H][Sq], [B][H][Sq]
+    float* part_q; float* part_s; float* part_k; float* part_v;   // parts of dq, dlam_part, dk, dv, in their layouts
+    int row_splits, row_keys, key_splits;                    // keys a part of dq; parts of dk and dv
     int B, Sq, Sk, H, Hkv, G, D, Dv, causal, rows;           // rows = Sq * G: of one request and key head, r = i * G + g
     int splits, split_keys, row_tiles;
     int ovec;                                                // outputs can be written 16 bytes at a time
@@ -176,12 +178,25 @@ __device__ __forceinline__ void put16(bf16* to, u32x4 r, bool there, float)
 }
 
 // 16 bytes of elements d.. of a row that has `have` of them.  VEC: d and the row are aligned and `have` is whole 16 bytes;
-// where d lies beyond, an address inside is read and the result is to be cleared.
+// where d lies beyond, an address inside is read and the result is to be cleared.  Otherwise 16 bytes at any address, the last ones of
+// the row where d + 16 bytes would pass its end, shifted down; rows shorter than that element by element.
 template <bool VEC, typename T>
 __device__ __forceinline__ u32x4 load16(const T* row, int d, int have)
 {
     constexpr int E = 16 / sizeof(T);
     if constexpr (VEC) return *(const u32x4*)(row + (d < have ? d : 0));
+    if (have >= E) {
+        typedef u32x4 u32x4_any __attribute__((aligned(2)));
+        const int at = min(d, have - E), drop = min(d - at, E);      // elements before d
+        const u32x4 v = *(const u32x4_any*)(row + at);
+        uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+        if (drop >= E / 2) { lo = hi; hi = 0; }
+        const int bits = drop % (E / 2) * (int)sizeof(T) * 8;
+        lo = bits ? lo >> bits | hi << (64 - bits) : lo;
+        hi >>= bits;
+        if (drop >= E) lo = 0;
+        return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+    }
     union { u32x4 u; T e[E]; } r;
 #pragma unroll
     for (int i = 0; i < E; ++i) r.e[i] = row[d + i < have ? d + i : 0];
