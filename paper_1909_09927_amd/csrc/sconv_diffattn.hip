@@ -532,7 +532,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
                 for (int x = 0; x < RT; ++x) s[x][m][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int t = 0; t < KS; ++t) {
-                    const frag kf = raw_frag(kr[y][m][t], 32 * t + 8 * h, a.D, ragged);
+                    const frag kf = raw_frag<VEC>(kr[y][m][t], 32 * t + 8 * h, a.D, ragged);
 #pragma unroll
                     for (int x = 0; x < RT; ++x) s[x][m][y] = mma(s[x][m][y], kf, qf[x][m][t]);
                 }
@@ -543,7 +543,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
         for (int v = 0; v < NV; ++v) {
             const int e = v * 64 + l, row = e / VPER;
             const bool there = e % VPER * E < dvn && (word >> row & 1);
-            put16<Values::PLANE>(vt + row * Values::LD + e % VPER * E, vr[v], there, T());
+            put16<Values::PLANE>(vt + row * Values::LD + e % VPER * E, shift16<VEC, T>(vr[v], e % VPER * E, dvn), there, T());
         }
         if (next < k1) fetch_values(next);
         if (j0 + 32 > wmin || word != ~0u) {

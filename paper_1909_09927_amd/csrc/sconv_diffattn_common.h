@@ -177,9 +177,10 @@ __device__ __forceinline__ void put16(bf16* to, u32x4 r, bool there, float)
     for (int k = 0; k < 3; ++k) *(u32x2*)(to + k * PLANE) = p[k];
 }
 
-// 16 bytes of elements d.. of a row that has `have` of them.  VEC: d and the row are aligned and `have` is whole 16 bytes;
-// where d lies beyond, an address inside is read and the result is to be cleared.  Otherwise 16 bytes at any address, the last ones of
-// the row where d + 16 bytes would pass its end, shifted down; rows shorter than that element by element.
+// 16 bytes of elements d.. of a row that has `have` of them, in two steps, so that nothing waits for the load before its use.  VEC: d
+// and the row are aligned and `have` is whole 16 bytes; where d lies beyond, an address inside is read and the result is to be cleared.
+// Otherwise 16 bytes at any address, the last ones of the row where 16 bytes from d would pass its end, which shift16 then moves down
+// (clearing what lies beyond); rows shorter than 16 bytes come element by element.
 template <bool VEC, typename T>
 __device__ __forceinline__ u32x4 load16(const T* row, int d, int have)
 {
@@ -187,15 +188,7 @@ __device__ __forceinline__ u32x4 load16(const T* row, int d, int have)
     if constexpr (VEC) return *(const u32x4*)(row + (d < have ? d : 0));
     if (have >= E) {
         typedef u32x4 u32x4_any __attribute__((aligned(2)));
-        const int at = min(d, have - E), drop = min(d - at, E);      // elements before d
-        const u32x4 v = *(const u32x4_any*)(row + at);
-        uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
-        if (drop >= E / 2) { lo = hi; hi = 0; }
-        const int bits = drop % (E / 2) * (int)sizeof(T) * 8;
-        lo = bits ? lo >> bits | hi << (64 - bits) : lo;
-        hi >>= bits;
-        if (drop >= E) lo = 0;
-        return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+        return *(const u32x4_any*)(row + min(d, have - E));
     }
     union { u32x4 u; T e[E]; } r;
 #pragma unroll
@@ -203,6 +196,20 @@ __device__ __forceinline__ u32x4 load16(const T* row, int d, int have)
 #pragma unroll
     for (int i = 0; i < E; ++i) if (d + i >= have) r.e[i] = (T)0.0f;
     return r.u;
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ u32x4 shift16(u32x4 v, int d, int have)
+{
+    constexpr int E = 16 / sizeof(T);
+    if (VEC || have < E) return v;
+    const int drop = min(max(d - (have - E), 0), E);   // elements before d
+    uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+    if (drop >= E / 2) { lo = hi; hi = 0; }
+    const int bits = drop % (E / 2) * (int)sizeof(T) * 8;
+    lo = bits ? lo >> bits | hi << (64 - bits) : lo;
+    hi >>= bits;
+    if (drop >= E) lo = 0;
+    return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 // A fragment of a row in memory as it is loaded, and as it is used (cleared beyond `have`): apart, so that nothing waits for the load
 // before its use.
@@ -213,18 +220,20 @@ __device__ __forceinline__ void load_raw(Raw<T>& r, const T* row, int d, int hav
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.u[i] = load16<VEC>(row, d + 4 * i, have);
 }
+template <bool VEC>
 __device__ __forceinline__ bf16x8 raw_frag(const Raw<bf16>& r, int d, int have, bool ragged)
 {
     union { u32x4 u; bf16x8 v; } x;
-    x.u = r.u[0];
+    x.u = shift16<VEC, bf16>(r.u[0], d, have);
     if (ragged && d >= have) x.u = u32x4{0, 0, 0, 0};
     return x.v;
 }
+template <bool VEC>
 __device__ __forceinline__ bf16x8x3 raw_frag(const Raw<float>& r, int d, int have, bool ragged)
 {
     union { u32x4 u[2]; float v[8]; } x;
-    x.u[0] = r.u[0];
-    x.u[1] = r.u[1];
+    x.u[0] = shift16<VEC, float>(r.u[0], d, have);
+    x.u[1] = shift16<VEC, float>(r.u[1], d + 4, have);
     if (ragged && d >= have) x.u[0] = u32x4{0, 0, 0, 0};
     if (ragged && d + 4 >= have) x.u[1] = u32x4{0, 0, 0, 0};
     return in_pieces<false>(x.v);
@@ -234,7 +243,7 @@ __device__ __forceinline__ typename Frag<T>::type global_frag(const T* row, int 
 {
     Raw<T> r;
     load_raw<VEC>(r, row, d, have);
-    return raw_frag(r, d, have, true);
+    return raw_frag<VEC>(r, d, have, true);
 }
 
 // Four neighbouring results of a row (columns d..d+3 of `have`).
@@ -322,7 +331,7 @@ struct Stage {
         for (int n = 0; n < N; ++n) {
             const int e = n * THREADS + threadIdx.x, row = e / PER, c = e % PER, d = (c % (W / E)) * E;
             const bool there = d < have && (!words || (words[row >> 5] >> (row & 31) & 1));
-            put16<To::PLANE>(tile + row * To::LD + c * E, r[n], there, T());
+            put16<To::PLANE>(tile + row * To::LD + c * E, shift16<VEC, T>(r[n], d, have), there, T());
         }
     }
 };
