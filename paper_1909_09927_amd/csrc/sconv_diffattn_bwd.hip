@@ -7,7 +7,10 @@
 //           unrounded weights, for lam's gradient (d_2 itself stems from results that were rounded).
 //   keys    dk, dv: a wavefront keeps 32 keys and walks the queries of every head that shares them, so the sum over heads
 //           and queries has one order and needs no atomics.
-// Weights and dS are rounded to the operands' type for their products; all sums are in 32 bits.
+// All sums are in 32 bits.  In 16 bits the weights are rounded to the operands' type for dv, as forward; dS goes as two 16-bit values,
+// the second holding what the first's rounding left out: its rounding alone would be as large as that of the results, and what d_m
+// carries over from rounded results comes on top (dq 2.6e-3 of its norm off against 1.7e-3 for 32 bits rounded once, now 1.9e-3; 13 - 16 % of
+// the pass).
 #include <math.h>
 
 #include <algorithm>
@@ -268,13 +271,10 @@ __global__ __launch_bounds__(256) void attn_bwd_rows(AttnArgs a)
         }
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-            frag f0, f1;
-            to_frag(s0, st, f0);
-            to_frag(s1, st, f1);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                acc[0][t] = mma(acc[0][t], tile_col<T, In::LD, In::PLANE>(kt + kcol + 16 * st * In::LD + 32 * t), f0);
-                acc[1][t] = mma(acc[1][t], tile_col<T, In::LD, In::PLANE>(kt + kcol + 16 * st * In::LD + DT + 32 * t), f1);
+                acc[0][t] = mma_fine<T, In>(acc[0][t], kt + kcol + 16 * st * In::LD + 32 * t, s0, st);
+                acc[1][t] = mma_fine<T, In>(acc[1][t], kt + kcol + 16 * st * In::LD + DT + 32 * t, s1, st);
             }
         }
         settle();
@@ -431,13 +431,10 @@ __global__ __launch_bounds__(256) void attn_bwd_keys(AttnArgs a)
             }
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                frag f0, f1;
-                to_frag(s0, x, f0);
-                to_frag(s1, x, f1);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    if (DK0) dk[0][t] = mma(dk[0][t], tile_col<T, In::LD, In::PLANE>(qt + col + 16 * x * In::LD + 32 * t), f0);
-                    if (DK1) dk[1][t] = mma(dk[1][t], tile_col<T, In::LD, In::PLANE>(qt + col + 16 * x * In::LD + DT + 32 * t), f1);
+                    if (DK0) dk[0][t] = mma_fine<T, In>(dk[0][t], qt + col + 16 * x * In::LD + 32 * t, s0, x);
+                    if (DK1) dk[1][t] = mma_fine<T, In>(dk[1][t], qt + col + 16 * x * In::LD + DT + 32 * t, s1, x);
                 }
             }
         }
@@ -572,19 +569,23 @@ __global__ __launch_bounds__(256, 2) void attn_rows_direct(AttnArgs a)
             }
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                bf16x8 f0, f1;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float gv = gt[8 * st + e], p1 = s1[8 * st + e];
-                    spread = fmaf(p1, gv, spread);
-                    f0[e] = (bf16)(s0[8 * st + e] * (gv - d0));
-                    f1[e] = (bf16)(p1 * (-lam * (gv - d1)));
-                }
+                for (int m = 0; m < 2; ++m) {
+                    float x[8];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const int c0 = 32 * t, c1 = DT + 32 * t;
-                    acc[0][t] = mma(acc[0][t], col_frag<DVT>(ks + col2[c0 / 32 % 2] + c0 / 64 * 64 + 16 * st * DVT), f0);
-                    acc[1][t] = mma(acc[1][t], col_frag<DVT>(ks + col2[c1 / 32 % 2] + c1 / 64 * 64 + 16 * st * DVT), f1);
+                    for (int e = 0; e < 8; ++e) {
+                        const float gv = gt[8 * st + e], p1 = s1[8 * st + e];
+                        if (m) spread = fmaf(p1, gv, spread);
+                        x[e] = m ? p1 * (-lam * (gv - d1)) : s0[8 * st + e] * (gv - d0);
+                    }
+                    bf16x8 f, rest;
+                    to_frag(x, f);
+                    rest_frag(x, f, rest);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const int c = m * DT + 32 * t;
+                        acc[m][t] = mma_fine<DVT>(acc[m][t], ks + col2[c / 32 % 2] + c / 64 * 64 + 16 * st * DVT, f, rest);
+                    }
                 }
             }
             settle();
@@ -764,22 +765,26 @@ __global__ __launch_bounds__(256, 2) void attn_keys_direct(AttnArgs a)
                             dv[t] = mma(dv[t], col_frag<DVT>(gs + col2[t % 2] + t / 2 * 64 + 16 * y * DVT), f);
                     }
                     if (DK) {
-                        bf16x8 f0, f1;
 #pragma unroll
-                        for (int e = 0; e < 8; e += 4) {
-                            const f32x4 d0 = *(const f32x4*)(st + 32 * x + 2 * BM + 2 * (8 * y + e)), d1 = *(const f32x4*)(st + 32 * x + 3 * BM + 2 * (8 * y + e));
+                        for (int m = 0; m < 2; ++m) {
+                            float v[8];
 #pragma unroll
-                            for (int z = 0; z < 4; ++z) {
-                                const int u = 8 * y + e + z;
-                                f0[e + z] = (bf16)(s0[x][u] * (gg[x][u] - d0[z]));
-                                f1[e + z] = (bf16)(s1[x][u] * fmaf(sign, gg[x][u], d1[z]));
+                            for (int e = 0; e < 8; e += 4) {
+                                const f32x4 d = *(const f32x4*)(st + 32 * x + (2 + m) * BM + 2 * (8 * y + e));
+#pragma unroll
+                                for (int z = 0; z < 4; ++z) {
+                                    const int u = 8 * y + e + z;
+                                    v[e + z] = m ? s1[x][u] * fmaf(sign, gg[x][u], d[z]) : s0[x][u] * (gg[x][u] - d[z]);
+                                }
                             }
-                        }
+                            bf16x8 f, rest;
+                            to_frag(v, f);
+                            rest_frag(v, f, rest);
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            const int c0 = 32 * t, c1 = DT + 32 * t;
-                            dk[0][t] = mma(dk[0][t], col_frag<DVT>(qs + col2[c0 / 32 % 2] + c0 / 64 * 64 + 16 * y * DVT), f0);
-                            dk[1][t] = mma(dk[1][t], col_frag<DVT>(qs + col2[c1 / 32 % 2] + c1 / 64 * 64 + 16 * y * DVT), f1);
+                            for (int t = 0; t < NT; ++t) {
+                                const int c = m * DT + 32 * t;
+                                dk[m][t] = mma_fine<DVT>(dk[m][t], qs + col2[c / 32 % 2] + c / 64 * 64 + 16 * y * DVT, f, rest);
+                            }
                         }
                     }
                 }

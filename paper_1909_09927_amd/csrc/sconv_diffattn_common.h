@@ -155,6 +155,34 @@ __device__ __forceinline__ void to_frag(const f32x16& p, int s, F& f)
     to_frag(v, f);
 }
 
+// What to_frag's rounding to 16 bits left out (32 bits: nothing).
+__device__ __forceinline__ void rest_frag(const float (&v)[8], const bf16x8& f, bf16x8& rest)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = (bf16)(v[i] - (float)f[i]);
+}
+// Products with values held twice as finely as 16 bits do: B = f + rest.
+template <int LD>
+__device__ __forceinline__ f32x16 mma_fine(f32x16 c, const bf16* a, const bf16x8& f, const bf16x8& rest)
+{
+    const bf16x8 x = col_frag<LD>(a);
+    return mma(mma(c, x, rest), x, f);
+}
+template <typename T, typename Tl>
+__device__ __forceinline__ f32x16 mma_fine(f32x16 c, const bf16* a, const f32x16& v, int s)
+{
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = v[8 * s + i];
+    if constexpr (sizeof(T) == 4) return mma(c, tile_col<T, Tl::LD, Tl::PLANE>(a), in_pieces<true>(x));
+    else {
+        bf16x8 f, rest;
+        to_frag(x, f);
+        rest_frag(x, f, rest);
+        return mma_fine<Tl::LD>(c, a, f, rest);
+    }
+}
+
 // 16 bytes of a row in memory into a tile (rows that are not there: zeros).
 template <int PLANE>
 __device__ __forceinline__ void put16(bf16* to, u32x4 r, bool there, bf16)
