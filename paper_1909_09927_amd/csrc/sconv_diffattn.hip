@@ -8,6 +8,9 @@
 // Either may split the keys over workgroups, whose parts a second kernel joins in a fixed order.
 // Weights are rounded to the operands' type for their product with the values; the sums they are divided by are of the
 // unrounded ones, in 32 bits.
+// Measured, heads of 64 with values of 128: 12544 queries seeing what came before, 8 heads on 4, 16 bits 486 us = 994 TFLOP/s of seen pairs
+// (a large 16-bit product reaches 1137, the pipe's power limit); 2 x 3136 x 8 unmasked 165 us; 32 bits, 8 x 196 x 7 heads 45 us
+// (112 workgroups); one token of 16 requests over up to 32768 keys 128 us = 4.4 TB/s, 5.2 where requests are equally long, and 5 for the join.
 #include <math.h>
 
 #include <algorithm>

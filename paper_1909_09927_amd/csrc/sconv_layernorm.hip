@@ -9,6 +9,9 @@
 //           read) in whole segments too.
 // The weight's gradient sums over all places: every workgroup walks many rows, keeps the sums of its own in registers, and
 // writes one row of partial sums, which a second kernel adds in a fixed order.
+// Measured (kernels alone; a large copy moves 4.90 TB/s): forward, map 8 x 256 x 56 x 56 in 32 bits to 16-bit tokens 12.9 us (3.0 TB/s:
+// reading and writing follow each other in a workgroup); backward, 25088 x 512 in 16 bits 17.3 us (4.5 TB/s) and 3.5 for the sums;
+// backward, map 32 x 896 x 14 x 14 in 32 bits 32 us (2.1 TB/s: 416 workgroups, one round) and 5.3; 49 x 2048 3.3 us (latency).
 #include <math.h>
 
 #include <algorithm>
