@@ -352,6 +352,66 @@ def test_attention_extreme_scores(device):
     _attention_check(device, q.abs(), -k.abs() * 3, v, lam, dout, causal=True)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", [(1, 300, 520, 4, 1, 64, 128), (2, 150, 300, 6, 2, 32, 64), (1, 200, 300, 4, 2, 128, 256), (1, 260, 260, 8, 1, 74, 148),
+                                   (3, 257, 259, 2, 2, 32, 64), (1, 500, 64, 3, 3, 64, 128)], ids=str)
+def test_attention_in_parts(device, shape, causal, dtype):
+    """Gradients whose keys, or heads and queries, are split over workgroups; tiles that end inside, with lengths, masks and lam of any sign."""
+    g = _gen(sum(shape) + 1)
+    B, Sq, Sk, H = shape[:4]
+    q, k, v, lam, dout = _attention_inputs(g, *shape, dtype)
+    lam[0] = -0.7
+    lam[-1] = 0.0
+    lengths = torch.tensor([Sk - 3, 65, Sk][:B], dtype=torch.int32)
+    mask = torch.rand(B, Sk, generator=g) < 0.8
+    mask[:, 32:128] = False
+    mask[:, 40] = True
+    _attention_check(device, q, k, v, lam, dout, causal=causal, lengths=lengths)
+    _attention_check(device, q, k, v, lam, dout, causal=causal, lengths=lengths, mask=mask)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("D", [64, 72])
+def test_attention_junk_in_whole_tiles(device, D, dtype):
+    """Keys that are left out over whole tiles and at a cache's end, holding NaN and Inf, under heads whose tiles go to LDS directly
+    (64) and through registers (72)."""
+    g = _gen(41 + D)
+    B, Sq, Sk = 2, 70, 200
+    q, k, v, lam, dout = _attention_inputs(g, B, Sq, Sk, 2, 2, D, 2 * D, dtype)
+    lengths = torch.tensor([193, 130], dtype=torch.int32)
+    mask = torch.rand(B, Sk, generator=g) < 0.9
+    mask[0, 64:128] = False
+    for m in (None, mask):
+        gone = ~ref.visible(B, Sq, Sk, False, lengths, m)[:, 0]
+        clean = _attention_check(device, q, k, v, lam, dout, lengths=lengths, mask=m)
+        for junk in (float("nan"), float("inf")):
+            kj, vj = k.clone(), v.clone()
+            kj[gone], vj[gone] = junk, junk
+            assert torch.equal(clean, _attention_check(device, q, kj, vj, lam, dout, lengths=lengths, mask=m))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+def test_attention_keys_head_by_head(device, dtype):
+    """Keys and values laid out [B, heads, capacity, D], as a cache of heads is, with NaN in the places beyond the last key: forward,
+    backward and single tokens."""
+    g = _gen(51)
+    B, Sk, H, D = 2, 100, 2, 64
+    q, kk, vv, lam, dout = _attention_inputs(g, B, 80, Sk, H, H, D, 2 * D, dtype)
+    k = torch.full((B, 2 * H, 130, D), float("nan"), dtype=dtype, device=device).transpose(1, 2)[:, :Sk]
+    v = torch.full((B, H, 130, 2 * D), float("nan"), dtype=dtype, device=device).transpose(1, 2)[:, :Sk]
+    k.copy_(kk.to(device))
+    v.copy_(vv.to(device))
+    r, e = ref.attention(q, kk, vv, lam, None, True, None, None, dout)
+    dev = q.to(device), k, v, lam.to(device)
+    out, second, lse = sconv.sconv_diffattn_forward(*dev, causal=True, save=True)
+    ref.within(out, r["out"], e["out"], "out")
+    for name, t in zip(("dq", "dk", "dv", "dlam"), sconv.sconv_diffattn_backward(dout.to(device), *dev, out, second, lse, causal=True)):
+        ref.within(t, r[name], e[name], name)
+    r, e = ref.attention(q[:, -1:], kk, vv, lam, None, True, None, None)
+    ref.within(sconv.sconv_diffattn_forward(q[:, -1:].contiguous().to(device), *dev[1:], causal=True), r["out"], e["out"], "one token")
+
+
 def test_attention_empty_axes(device):
     for B, Sq, Sk in ((0, 3, 4), (2, 0, 4), (2, 3, 0)):
         q, k = torch.randn(B, Sq, 4, 32, device=device), torch.randn(B, Sk, 4, 32, device=device)
