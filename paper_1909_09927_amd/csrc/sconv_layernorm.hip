@@ -515,9 +515,10 @@ bool ln_map_held(const sconv_layernorm_desc_t& d)
     return d.layout == SCONV_LAYOUT_MAP && d.C <= 2048 && d.x_s * d.C < most - d.S && (int64_t)d.S * d.C < most;
 }
 
-// Places of a tile: whole 128-byte lines of a map in 32 bits, fewer where the channels would not fit the registers, or two
-// workgroups' tiles of dy the LDS.
-int ln_map_places(const sconv_layernorm_desc_t& d, bool backward) { return d.C <= (backward ? 512 : 1024) ? 32 : 16; }
+// Places of a tile: whole 128-byte lines of a map in 32 bits, fewer where the channels would not fit the registers.  Backward over 128
+// channels: half lines, whose smaller tiles of dy let more workgroups share a compute unit while neighbours share a cache (16 against 32
+// places: 32 x 512 x 28 x 28 46.6 and 57.6 us, 8 x 256 x 56 x 56 25.3 and 28.1; 16 x 128 x 56 x 56 28.5 and 25.3, 16 x 64 x 112 x 112 78 and 53).
+int ln_map_places(const sconv_layernorm_desc_t& d, bool backward) { return d.C <= (backward ? 128 : 1024) ? 32 : 16; }
 
 template <typename K>
 int ln_allow_lds(K kern, size_t bytes)
@@ -584,8 +585,14 @@ int ln_run(const sconv_layernorm_desc_t& d, LnArgs a, bool backward, hipStream_t
         return launch_status();                                                                                     \
     }
             if (d.C <= 128) SCONV_LN_MAP(32, 512, 8)
-            if (d.C <= 256) SCONV_LN_MAP(32, 512, 16)
-            if (d.C <= 512) SCONV_LN_MAP(32, 512, 32)
+            // (a workgroup a compute unit at most: twice the threads on a tile, 64 x 1024 x 7 x 7 24.8 -> 22.0 us, 32 x 896 x 7 x 7
+            // 19.3 -> 17.4; with more tiles they push out the second workgroup, 32 x 896 x 14 x 14 33.7 -> 37.4)
+            if (total <= 256 && d.C > 256) {
+                if (d.C <= 512) SCONV_LN_MAP(16, 1024, 8)
+                if (d.C <= 1024) SCONV_LN_MAP(16, 1024, 16)
+            }
+            if (d.C <= 256) SCONV_LN_MAP(16, 512, 8)
+            if (d.C <= 512) SCONV_LN_MAP(16, 512, 16)
             if (d.C <= 1024) SCONV_LN_MAP(16, 512, 32)
             SCONV_LN_MAP(16, 1024, 32)
 #undef SCONV_LN_MAP

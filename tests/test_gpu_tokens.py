@@ -76,6 +76,13 @@ def test_norm_map(device, shape, types):
     ref.within(db, rb, bb + 2 * ref.E * rb.abs(), "dbias")
 
 
+@pytest.mark.parametrize("types", TYPES, ids=["fp32", "bf16", "fp32-bf16"])
+@pytest.mark.parametrize("shape", [(300, 70, 1, 5), (48, 200, 14, 14), (20, 300, 14, 15), (64, 520, 5, 13)], ids=str)
+def test_norm_map_of_many_tiles(device, shape, types):
+    """More tiles than compute units, and than rows of partial sums."""
+    test_norm_map(device, shape, types)
+
+
 @pytest.mark.parametrize("layout", ["tokens", "map"])
 def test_norm_plain_and_weight_types(device, layout):
     g = _gen(5)
