@@ -44,10 +44,16 @@ class DiffAttnDesc(ctypes.Structure):
                 [(n, _i64) for n in ("q_b", "q_s", "q_h", "k_b", "k_s", "k_h", "v_b", "v_s", "v_h", "mask_b")])
 
 
-# Descriptors of calls seen before, by the shapes, strides and types that they describe (nothing of the tensors themselves): filling
-# one in takes longer than a small call's kernel.
+# Descriptors of calls seen before, by what they are made of: the tensors' shapes, strides and types and the call's numbers and switches,
+# by value (nothing of the tensors themselves).  Filling one in takes longer than a small call's kernel.
 _plans = {}
 _PLANS_KEPT = 4096
+
+
+def _number(x):
+    """A number as the C call takes it.  A tensor of one element is read here, at every call: as part of a key it would stand for itself,
+    whatever it came to hold."""
+    return x if type(x) is float else _f32(x).value
 
 
 def _sig(t):
@@ -175,6 +181,7 @@ def sconv_layernorm_forward(x, weight=None, bias=None, eps: float = 1e-5, layout
     layout "tokens": x is [..., C] and y has its shape; "map": x is a feature map [N, C, H, W] (or [N, C, S]) as
     sconv_forward leaves it and y is tokens [N, H*W, C].  out_dtype: x's type (default), or bf16 under an fp32 x.
     stats: returns (y, mean, rstd), the fp32 statistics of every place that sconv_layernorm_backward reads."""
+    eps = _number(eps)
     key = (0, _sig(x), _sig(weight), _sig(bias), eps, layout, out_dtype)
     plan = _plans.get(key)
     if plan is None:
@@ -278,13 +285,11 @@ def sconv_rotary_axes(sections: Sequence[int]) -> bytes:
 
 
 def _rotary(q, k, positions, freq, axes, interleaved, inverse, out, what):
+    if type(axes) is not bytes:
+        axes = bytes(list(axes))
+    interleaved = bool(interleaved)
     key = (2 + inverse, _sig(q), _sig(k), _sig(positions), _sig(freq), axes, interleaved)
-    try:
-        plan = _plans.get(key)
-    except TypeError:      # (axes as a list)
-        axes = bytes(axes)
-        key = key[:5] + (axes, interleaved)
-        plan = _plans.get(key)
+    plan = _plans.get(key)
     if plan is None:
         plan = _keep(key, _rotary_plan(q, k, positions, freq, axes, interleaved, inverse, what))
     _, ref = plan
@@ -332,7 +337,7 @@ def _rotary_plan(q, k, positions, freq, axes, interleaved, inverse, what):
                       q.stride(2), 0, 0, 0, S * Hq * D, Hq * D, D, S * Hk * D, Hk * D, D, S * n_axes if batch > 1 else 0)
     if Hk:
         desc.k_b, desc.k_s, desc.k_h = k.stride(0), k.stride(1), k.stride(2)
-    ctypes.memmove(ctypes.addressof(desc) + RotaryDesc.axis.offset, bytes(axes), pairs)
+    ctypes.memmove(ctypes.addressof(desc) + RotaryDesc.axis.offset, axes, pairs)
     return desc, ctypes.byref(desc)
 
 
@@ -355,6 +360,9 @@ def sconv_rotary_backward(dq, dk, positions, inv_freq, axes: bytes, interleaved:
 
 def _attn_plan(q, k, v, lam, scale, causal, k_lengths, k_mask):
     """(descriptor, reference to it, out's shape, lse's, bytes of scratch forward and backward)"""
+    if scale is not None:
+        scale = _number(scale)
+    causal = bool(causal)
     key = (4, _sig(q), _sig(k), _sig(v), _sig(lam), scale, causal, _sig(k_lengths), _sig(k_mask))
     plan = _plans.get(key)
     if plan is None:
@@ -396,7 +404,7 @@ def _attn_desc(q, k, v, lam, scale, causal, k_lengths, k_mask):
         mask_b = k_mask.stride(0)
     qs, ks, vs = q.stride(), k.stride(), v.stride()
     return DiffAttnDesc(B, Sq, Sk, H, Hkv, D, v.shape[3], qt, 1 if causal else 0,
-                        1.0 / math.sqrt(D) if scale is None and D else scale or 0.0, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2],
+                        (1.0 / math.sqrt(D) if D else 0.0) if scale is None else scale, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2],
                         vs[0], vs[1], vs[2], mask_b)
 
 
@@ -410,7 +418,7 @@ def sconv_diffattn_forward(q, k, v, lam, scale: Optional[float] = None, causal: 
     """Differential attention: out = (softmax(scale Q1 K1^T) - lam softmax(scale Q2 K2^T)) V for every head.
 
     q [B, Sq, 2H, D] (queries of the two maps at heads 2h, 2h + 1), k [B, Sk, 2Hkv, D], v [B, Sk, Hkv, Dv], H a multiple
-    of Hkv; lam: fp32 [H]; scale: 1/sqrt(D) by default.  k_lengths: int32 [B], keys of every request; k_mask: bool or
+    of Hkv; lam: fp32 [H]; scale: a number, 1/sqrt(D) by default (a tensor of one element is read by the host).  k_lengths: int32 [B], keys of every request; k_mask: bool or
     uint8 [B, Sk], false where a key is not to be seen; causal: the last query stands at the request's last key.  A query
     that sees nothing gives zeros.  One token over a cache is the same call with Sq = 1 and k, v the cache.  Returns out
     [B, Sq, H, Dv]; save: (out, second, lse), the last two for sconv_diffattn_backward.  ws: a device tensor as
