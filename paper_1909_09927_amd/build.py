@@ -16,6 +16,9 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          # packed fp32 instructions stay off: the compiler must not form them on its own
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+         # spilled registers go to memory whole: where part of one went to an accumulation register and all of it came back into
+         # such registers, the compiler left that part's copy out (seen in a 32-bit attention kernel: one of a fragment's four was stale)
+         "-mllvm", "-amdgpu-spill-vgpr-to-agpr=0",
          "-I", INCLUDE, "-I", CSRC]
 
 
