@@ -94,6 +94,8 @@ int sconv_rotary(const sconv_rotary_desc_t* desc, const void* q_dev, const void*
  * last query stands at the request's last key.  A query that sees nothing gives zeros and takes no gradient.  Keys and values
  * that k_lengths or k_mask leave out are never part of a sum, whatever they hold (Inf, NaN); one that causal alone hides from a
  * query has to be finite, as 0 * NaN may stand in the query's sum.
+ * Inf in what a query sees goes through the formulas: a score of -Inf has no weight (a query with no other sees nothing), +Inf or NaN
+ * makes the query's results NaN, an Inf in V is Inf or NaN in its column.  Gradients through such places are not finite.
  * One token of every request over a long cache (Sq = 1) is the same call: its keys are split over workgroups, whose parts a
  * second kernel joins.
  */

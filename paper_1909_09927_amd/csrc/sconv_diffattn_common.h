@@ -53,26 +53,32 @@ __device__ __forceinline__ C mma(C c, const bf16x8x3& a, const bf16x8x3& b)
     return mma(c, a.p[0], b.p[0]);
 }
 
-// Two values as pieces: the upper 16 bits of the value, of what is left, and of what is left then.  FINITE: neither Inf nor NaN comes
-// (Inf would leave Inf - Inf behind).
-template <bool FINITE>
+// Two values as pieces: the upper 16 bits of the value, of what is left, and of what is left then.  An Inf stands in the third piece alone,
+// behind two of the type's largest value: the third meets the other operand's first only, which is 0 under a value of 0 alone, while the other
+// operand's lower pieces are 0 wherever its bits are few, and Inf * 0 would be NaN for a product that is Inf.  NaN ends there too.  WEIGHT: a
+// softmax weight, never Inf.
+template <bool WEIGHT>
+__device__ __forceinline__ float upper(float x)
+{
+    const float most = __uint_as_float(0x7f7f0000u);
+    if constexpr (!WEIGHT) x = __builtin_amdgcn_fmed3f(x, -most, most);
+    return __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+}
+template <bool WEIGHT>
 __device__ __forceinline__ void pieces(float x, float y, uint32_t& hi, uint32_t& mid, uint32_t& lo)
 {
-    const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
-    float xr = x - __uint_as_float(xb & 0xffff0000u), yr = y - __uint_as_float(yb & 0xffff0000u);
-    if constexpr (!FINITE) { xr = xr == xr ? xr : 0.0f; yr = yr == yr ? yr : 0.0f; }
-    const uint32_t xm = __float_as_uint(xr), ym = __float_as_uint(yr);
-    const float xl = xr - __uint_as_float(xm & 0xffff0000u), yl = yr - __uint_as_float(ym & 0xffff0000u);
-    hi = __builtin_amdgcn_perm(yb, xb, 0x07060302u);
-    mid = __builtin_amdgcn_perm(ym, xm, 0x07060302u);
+    const float xh = upper<WEIGHT>(x), yh = upper<WEIGHT>(y), xr = x - xh, yr = y - yh;
+    const float xm = upper<WEIGHT>(xr), ym = upper<WEIGHT>(yr), xl = xr - xm, yl = yr - ym;
+    hi = __builtin_amdgcn_perm(__float_as_uint(yh), __float_as_uint(xh), 0x07060302u);
+    mid = __builtin_amdgcn_perm(__float_as_uint(ym), __float_as_uint(xm), 0x07060302u);
     lo = __builtin_amdgcn_perm(__float_as_uint(yl), __float_as_uint(xl), 0x07060302u);
 }
-template <bool FINITE>
+template <bool WEIGHT>
 __device__ __forceinline__ bf16x8x3 in_pieces(const float (&v)[8])
 {
     union { uint32_t u[4]; bf16x8 f; } p[3];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) pieces<FINITE>(v[2 * i], v[2 * i + 1], p[0].u[i], p[1].u[i], p[2].u[i]);
+    for (int i = 0; i < 4; ++i) pieces<WEIGHT>(v[2 * i], v[2 * i + 1], p[0].u[i], p[1].u[i], p[2].u[i]);
     return bf16x8x3{{p[0].f, p[1].f, p[2].f}};
 }
 
@@ -174,7 +180,7 @@ __device__ __forceinline__ f32x16 mma_fine(f32x16 c, const bf16* a, const f32x16
     float x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = v[8 * s + i];
-    if constexpr (sizeof(T) == 4) return mma(c, tile_col<T, Tl::LD, Tl::PLANE>(a), in_pieces<true>(x));
+    if constexpr (sizeof(T) == 4) return mma(c, tile_col<T, Tl::LD, Tl::PLANE>(a), in_pieces<false>(x));
     else {
         bf16x8 f, rest;
         to_frag(x, f);

@@ -54,3 +54,71 @@ def test_rotary_axes_and_order_are_read_at_every_call(device):
             assert torch.equal(got, want), (type(axes), p)
     with pytest.raises(TypeError):
         sconv.sconv_diffattn_forward(q, q, q[:, :, :1], torch.ones(1, device=device), scale="0.5")
+
+
+# ---- infinities that a query sees: what the formulas make of them
+
+SHAPES = [(1, 40, 50, 2, 1, 64, 128), (1, 1, 300, 4, 2, 64, 128), (2, 150, 97, 2, 2, 72, 144), (1, 33, 70, 1, 1, 128, 256), (1, 1, 1, 1, 1, 32, 64),
+          (1, 130, 200, 1, 1, 32, 64)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_attention_visible_minus_infinity_key_has_no_weight(device, shape, dtype):
+    """Scores of -Inf: the key counts for nothing, as if it were not there.  Queries of few bits (1, 1.5), whose lower parts are zero, and
+    of many."""
+    B, Sq, Sk, H, Hkv, D, Dv = shape
+    q, k, v = _randn(11, B, Sq, 2 * H, D, dtype=dtype), _randn(12, B, Sk, 2 * Hkv, D, dtype=dtype), _randn(13, B, Sk, Hkv, Dv, dtype=dtype)
+    lam = 0.5 + 0.1 * _randn(14, H)
+    q[..., 3] = torch.tensor([1.0, 1.5, 0.1, 2.0 ** -20]).to(dtype)[torch.arange(q[..., 3].numel()) % 4].view(q.shape[:-1])
+    gone = torch.zeros(B, Sk, dtype=torch.bool)
+    gone[:, Sk // 2] = gone[:, Sk - 1] = True
+    clean = k.clone()
+    k[gone] = k[gone].index_fill(2, torch.tensor([3]), -math.inf)
+    r, e = ref.attention(q, clean, v, lam, None, False, None, ~gone)
+    out, second, lse = sconv.sconv_diffattn_forward(q.to(device), k.to(device), v.to(device), lam.to(device), save=True)
+    for name, got in (("out", out), ("second", second), ("lse", lse)):
+        ref.within(got, r[name], e[name], name)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_attention_visible_infinite_value(device, shape, dtype):
+    """A column of V with an Inf: Inf in that column of every result (lam below 0, so that the maps' parts have one sign), the other columns
+    as they are."""
+    B, Sq, Sk, H, Hkv, D, Dv = shape
+    q, k, v = _randn(15, B, Sq, 2 * H, D, dtype=dtype), _randn(16, B, Sk, 2 * Hkv, D, dtype=dtype), _randn(17, B, Sk, Hkv, Dv, dtype=dtype)
+    lam = -0.5 - 0.1 * _randn(18, H).abs()
+    r, e = ref.attention(q, k, v, lam, None, False, None, None)
+    v[:, Sk // 2, :, 5], v[:, Sk // 2, :, 9] = math.inf, -math.inf
+    out, second, _ = sconv.sconv_diffattn_forward(q.to(device), k.to(device), v.to(device), lam.to(device), save=True)
+    for name, got in (("out", out), ("second", second)):
+        for c, s in ((5, math.inf), (9, -math.inf)):
+            r[name][..., c] = s
+        ref.within(got, r[name], e[name], name)
+
+
+def test_attention_infinite_scores_and_their_rows(device):
+    """+Inf among a row's scores, and 0 * Inf in one: that row is NaN and no other."""
+    for dtype in (F32, BF16):
+        q, k, v = _randn(21, 1, 64, 2, 64, dtype=dtype), _randn(22, 1, 90, 2, 64, dtype=dtype), _randn(23, 1, 90, 1, 128, dtype=dtype)
+        q[..., 3] = 1.0
+        k[:, 7, :, 3] = -math.inf
+        q[0, 10, :, 3], q[0, 40, :, 3] = -1.0, 0.0
+        out = sconv.sconv_diffattn_forward(q.to(device), k.to(device), v.to(device), torch.full((1,), 0.5, device=device)).cpu()
+        bad = out[0].isnan().flatten(1).all(1)
+        assert bad.nonzero().flatten().tolist() == [10, 40] and out[0, ~bad].isfinite().all()
+
+
+def test_attention_gradient_that_overflows(device):
+    """dout V^T beyond 32 bits under weights of a half: dS is Inf, and dq = Inf times keys of one sign each, not NaN."""
+    D, Dv, H = 16, 32, 1
+    q, k, v = torch.zeros(1, 3, 2, D), torch.ones(1, 2, 2, D), torch.zeros(1, 2, 1, Dv)
+    k[0, 1] = -1.0
+    v[0, 0], v[0, 1] = 3e38, -3e38
+    lam, dout = torch.tensor([-1.0]), torch.full((1, 3, 1, Dv), 2.0)
+    dev = [t.to(device) for t in (q, k, v, lam)]
+    out, second, lse = sconv.sconv_diffattn_forward(*dev, save=True)
+    assert not out.any() and not second.any()
+    dq = sconv.sconv_diffattn_backward(dout.to(device), *dev, out, second, lse)[0]
+    assert (dq == math.inf).all()
