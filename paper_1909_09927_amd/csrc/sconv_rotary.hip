@@ -31,7 +31,7 @@ __device__ __forceinline__ void turn_of(int pos, float freq, float* c, float* s)
     const int k = (int)(whole - 4.0 * floor(whole * 0.25));
     const float z = x * x;
     const float sn = x + x * z * fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880.0f, -1.0f / 5040.0f), 1.0f / 120.0f), -1.0f / 6.0f);
-    const float cs = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 40320.0f, -1.0f / 720.0f), 1.0f / 24.0f), -0.5f), 1.0f);
+    const float cs = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.0f / 3628800.0f, 1.0f / 40320.0f), -1.0f / 720.0f), 1.0f / 24.0f), -0.5f), 1.0f);
     const float a = (k & 1) ? sn : cs, b = (k & 1) ? cs : sn;
     *c = (k == 1 || k == 2) ? -a : a;
     *s = (k >= 2) ? -b : b;

@@ -122,3 +122,19 @@ def test_attention_gradient_that_overflows(device):
     assert not out.any() and not second.any()
     dq = sconv.sconv_diffattn_backward(dout.to(device), *dev, out, second, lse)[0]
     assert (dq == math.inf).all()
+
+
+# ---- the last bits
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotary_cosine_is_centred(device, interleaved):
+    """Cosines short of an eighth of a turn, where a polynomial cut off too early is off to one side.  Each of the 11200 is within about 2^-24, in
+    either direction by its roundings: their mean is within 2^-24 / 100 of 0 then, and 2^-28 is asked for."""
+    pairs, pos = 8, torch.arange(49900, 51300, dtype=torch.int32).view(1, -1, 1)
+    freq = 2.0 ** -16 * (1.0 + torch.arange(pairs) * 2.0 ** -13)
+    x = torch.zeros(1, pos.shape[1], 1, 2 * pairs)
+    first = slice(0, None, 2) if interleaved else slice(0, pairs)
+    x[..., first] = 1.0
+    y, _ = sconv.sconv_rotary_forward(x.to(device), None, pos.to(device), freq.to(device), bytes(pairs), interleaved=interleaved)
+    off = y.cpu().double()[..., first] - (pos.double() * freq.double()).cos().unsqueeze(2)
+    assert off.abs().max() <= 2.0 ** -23 and abs(off.mean()) <= 2.0 ** -28
