@@ -6,8 +6,11 @@
 //   wide   128 rows a workgroup, 32 a wavefront; every wavefront walks all keys of the tile.
 //   few    up to 32 rows a workgroup: its wavefronts walk keys of their own, and join at the end.
 // Either may split the keys over workgroups, whose parts a second kernel joins in a fixed order.
-// Weights are rounded to the operands' type for their product with the values; the sums they are divided by are of the
-// unrounded ones, in 32 bits.
+// In 16 bits wide calls round their weights to the operands' type for the product with the values, which is two thirds of their matrix
+// work: a second product with what the rounding leaves out would bring the result from 2.4e-3 of its norm off to its own rounding's
+// 1.7e-3, and 12544 queries from 502 to 774 us, 2 x 3136 from 148 to 223, a training pass of 784 places from 155 to 177.  Few rows' wait
+// for memory and take that second product (16 requests of up to 32768 keys 132.7 us
+// without, 134.2 with, one of 32 rows 23.7 and 25.8).  The sums that weights are divided by are of the unrounded ones, in 32 bits.
 // Measured, heads of 64 with values of 128: 12544 queries seeing what came before, 8 heads on 4, 16 bits 486 us = 994 TFLOP/s of seen pairs
 // (a large 16-bit product reaches 1137, the pipe's power limit); 2 x 3136 x 8 unmasked 165 us; 32 bits, 8 x 196 x 7 heads 45 us
 // (112 workgroups); one token of 16 requests over up to 32768 keys 128 us = 4.4 TB/s, 5.2 where requests are equally long, and 5 for the join.
@@ -590,15 +593,24 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
                     }
             }
         const int vcol = few_col_lane<Values::LD>();
-        frag pf[RT][2];
+        frag pf[RT][2], rest[RT][2];                   // (rest: 16 bits)
 #pragma unroll
-        for (int x = 0; x < RT; ++x) { to_frag(p[x][0], pf[x][0]); to_frag(p[x][1], pf[x][1]); }
+        for (int x = 0; x < RT; ++x)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                if constexpr (sizeof(T) == 2) weight_frags(p[x][m], pf[x][m], rest[x][m]);
+                else to_frag(p[x][m], pf[x][m]);
+            }
         wave_lds_fence();
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const frag vf = tile_col<T, Values::LD, Values::PLANE, 16>(vt + vcol + 16 * t);
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
+                if constexpr (sizeof(T) == 2) {
+                    o[x][0][t] = mma(o[x][0][t], vf, rest[x][0]);
+                    o[x][1][t] = mma(o[x][1][t], vf, rest[x][1]);
+                }
                 o[x][0][t] = mma(o[x][0][t], vf, pf[x][0]);
                 o[x][1][t] = mma(o[x][1][t], vf, pf[x][1]);
             }

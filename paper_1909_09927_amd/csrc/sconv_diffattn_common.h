@@ -167,6 +167,16 @@ __device__ __forceinline__ void rest_frag(const float (&v)[8], const bf16x8& f, 
 #pragma unroll
     for (int i = 0; i < 8; ++i) rest[i] = (bf16)(v[i] - (float)f[i]);
 }
+// Weights in two values, cut off and not rounded so that both are positive where the weight is: an Inf that meets them stays one.
+__device__ __forceinline__ void weight_frags(const float (&v)[8], bf16x8& f, bf16x8& rest)
+{
+    union { uint32_t u[4]; bf16x8 f; } hi;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) hi.u[i] = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302u);
+    f = hi.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = (bf16)fmaxf(v[i] - upper<true>(v[i]), v[i] * 0x1p-17f);
+}
 // Products with values held twice as finely as 16 bits do: B = f + rest.
 template <int LD>
 __device__ __forceinline__ f32x16 mma_fine(f32x16 c, const bf16* a, const bf16x8& f, const bf16x8& rest)

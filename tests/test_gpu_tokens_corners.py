@@ -138,3 +138,18 @@ def test_rotary_cosine_is_centred(device, interleaved):
     y, _ = sconv.sconv_rotary_forward(x.to(device), None, pos.to(device), freq.to(device), bytes(pairs), interleaved=interleaved)
     off = y.cpu().double()[..., first] - (pos.double() * freq.double()).cos().unsqueeze(2)
     assert off.abs().max() <= 2.0 ** -23 and abs(off.mean()) <= 2.0 ** -28
+
+
+@pytest.mark.parametrize("shape", [(2, 1, 900, 4, 2, 64, 128), (1, 1, 70, 2, 2, 32, 64), (1, 4, 300, 8, 1, 64, 128), (2, 3, 400, 2, 1, 61, 122),
+                                   (1, 5, 500, 10, 2, 128, 256), (1, 8, 300, 4, 1, 100, 37)], ids=str)
+def test_attention_of_few_rows_is_rounded_once(device, shape):
+    """16-bit results of up to 32 rows a key head: as far off as the exact ones rounded to 16 bits are, to a twentieth (weights to 2^-16, 32-bit
+    sums; weights to 2^-8 would add as much again)."""
+    B, Sq, Sk, H, Hkv, D, Dv = shape
+    q, k, v = 1.5 * _randn(41, B, Sq, 2 * H, D), _randn(42, B, Sk, 2 * Hkv, D, dtype=BF16), _randn(43, B, Sk, Hkv, Dv, dtype=BF16)
+    q, lam = q.to(BF16), 0.5 + 0.1 * _randn(44, H)
+    r, _ = ref.attention(q, k, v, lam, None, True, None, None)
+    got = sconv.sconv_diffattn_forward(q.to(device), k.to(device), v.to(device), lam.to(device), causal=True, save=True)
+    for name, t in zip(("out", "second"), got):
+        own = (r[name].to(BF16).double() - r[name]).norm()
+        assert (t.cpu().double() - r[name]).norm() <= 1.05 * own, name
