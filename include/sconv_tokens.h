@@ -13,6 +13,8 @@
  * rounded once.  (16-bit half is left out: a training program's small gradients leave its range without a scale that
  * follows the loss.)  Strides count elements; the last axis of a strided tensor is contiguous.
  * Sizes of zero are allowed where a call says so; such a call does what is left to do (it clears gradients, say).
+ * SCONV_EUNSUPPORTED, before anything is enqueued, where a size passes a limit given below or a kernel's grid would have 2^32 threads:
+ * that takes 2^24 rows of layer norm, tokens of rotary, tiles of 16 (query, head) pairs or of 128 keys at least.
  */
 #ifndef SCONV_TOKENS_H
 #define SCONV_TOKENS_H

@@ -549,6 +549,7 @@ int ln_tokens(const LnArgs& a, bool backward, int blocks, hipStream_t stream)
     ln_shape(a.C, V, a.rows, &lpr, &nv);
     const int rpb = 256 / lpr;
     const unsigned grid = (unsigned)((a.rows + rpb - 1) / rpb);
+    if (!backward && !grid_fits(grid, 256)) return SCONV_EUNSUPPORTED;
     const unsigned bgrid = (unsigned)std::min<int64_t>(blocks, grid);
     const size_t lds = rpb > 1 && a.part ? (size_t)rpb * a.C * 4 : 0;
 #define SCONV_LN(L, M)                                                                                          \
@@ -599,6 +600,7 @@ int ln_run(const sconv_layernorm_desc_t& d, LnArgs a, bool backward, hipStream_t
         }
 #define SCONV_LN_MAP(PP, TH, J)                                                                                              \
     {                                                                                                                        \
+        if (!grid_fits(total, TH)) return SCONV_EUNSUPPORTED;                                                                \
         hipLaunchKernelGGL((ln_map_fwd<TX, TY, PP, TH, J>), dim3((unsigned)total), dim3(TH), 0, stream, a, tiles);           \
         return launch_status();                                                                                              \
     }
@@ -617,6 +619,7 @@ int ln_run(const sconv_layernorm_desc_t& d, LnArgs a, bool backward, hipStream_t
                                         : ln_tokens<TX, TY, 1>(a, backward, blocks, stream);
     }
     const int64_t xs_s = map ? 1 : a.x_s, xs_c = map ? a.x_s : 1;
+    if ((!backward || a.dx) && !grid_fits(a.rows, 256)) return SCONV_EUNSUPPORTED;
     if (!backward) {
         hipLaunchKernelGGL((ln_fwd_long<TX, TY>), dim3((unsigned)a.rows), dim3(256), 0, stream, a, xs_s, xs_c);
         return launch_status();

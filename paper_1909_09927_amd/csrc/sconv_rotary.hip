@@ -116,6 +116,7 @@ int rotary_run(const RotArgs& a, bool inter, bool vec, hipStream_t stream)
     int64_t TT = std::max<int64_t>(1, std::min<int64_t>(2048 / per, a.tokens / 512));
     TT = std::min<int64_t>(std::min<int64_t>(TT, 4096 / a.pairs), 256);
     const unsigned grid = (unsigned)((a.tokens + TT - 1) / TT);
+    if (!grid_fits(grid, 256)) return SCONV_EUNSUPPORTED;
     const size_t lds = (size_t)TT * (a.pairs * 2 * sizeof(float) + 4 * sizeof(int64_t));
     if (vec && inter) hipLaunchKernelGGL((rotary_kernel<T, V, true>), dim3(grid), dim3(256), lds, stream, a, (int)TT);
     else if (vec) hipLaunchKernelGGL((rotary_kernel<T, V, false>), dim3(grid), dim3(256), lds, stream, a, (int)TT);

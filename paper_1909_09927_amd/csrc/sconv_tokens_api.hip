@@ -48,7 +48,19 @@ int check_diffattn(const sconv_diffattn_desc_t* d)
     // (grids: a workgroup a row of the joining kernel, a tile of rows or keys elsewhere)
     if (bh * ((d->Sq * G + 31) / 32) >= (int64_t(1) << 31) || bh * ((d->Sk + 127) / 128) >= (int64_t(1) << 31)) return SCONV_EUNSUPPORTED;
     if ((int64_t)d->B * d->H * (int64_t)d->Sq >= (int64_t(1) << 31)) return SCONV_EUNSUPPORTED;
+    const int64_t rows = d->Sq * G, tile = rows > 32 ? 128 : rows > 16 && d->type == SCONV_BF16 ? 32 : 16;   // rows of a forward workgroup
+    if (!grid_fits(bh * ((rows + tile - 1) / tile), 256)) return SCONV_EUNSUPPORTED;
     return SCONV_OK;
+}
+
+// What the backward kernels' grids take beyond that: 16 rows a workgroup, 128 keys, a head.
+int check_diffattn_backward(const sconv_diffattn_desc_t* d)
+{
+    const int rc = check_diffattn(d);
+    if (rc) return rc;
+    const bool fits = grid_fits(((int64_t)d->B * d->Sq * d->H + 15) / 16, 256) &&
+                      grid_fits((int64_t)d->B * d->Hkv * (((int64_t)d->Sk + 127) / 128), 256) && grid_fits(d->H, 1024);
+    return fits ? SCONV_OK : SCONV_EUNSUPPORTED;
 }
 
 }  // namespace
@@ -130,7 +142,7 @@ int sconv_diffattn_backward(const sconv_diffattn_desc_t* desc, const void* dout_
                             void* dq_dev, void* dk_dev, void* dv_dev, float* dlam_dev, void* ws_dev, size_t ws_bytes,
                             void* hip_stream)
 {
-    const int rc = check_diffattn(desc);
+    const int rc = check_diffattn_backward(desc);
     if (rc) return rc;
     if (!aligned_ws(ws_dev, ws_bytes) || ws_bytes < diffattn_backward_workspace(*desc) || !dlam_dev || !lam_dev) return SCONV_EINVAL;
     const bool queries = desc->B > 0 && desc->Sq > 0, keys = desc->B > 0 && desc->Sk > 0;

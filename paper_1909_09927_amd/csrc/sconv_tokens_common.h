@@ -119,6 +119,9 @@ __device__ __forceinline__ float lanes_sum(float v)
 template <typename T, int V>
 struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Pack { T e[V]; };
 
+// Whether the runtime takes a grid of so many workgroups of so many threads: threads are counted in 32 bits.
+inline bool grid_fits(int64_t blocks, int threads) { return blocks * threads < (int64_t(1) << 32); }
+
 inline bool aligned_to(const void* p, int bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
 int launch_layernorm_forward(const sconv_layernorm_desc_t& d, const void* x, const void* w, const void* b, void* y,

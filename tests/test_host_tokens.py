@@ -112,3 +112,16 @@ def test_device_tensors_are_asked_for():
         sconv.sconv_rotary_forward(torch.zeros(1, 1, 1, 4), None, torch.zeros(1, 1, 1, dtype=torch.int32), torch.ones(2), bytes(2))
     with pytest.raises(AttributeError):
         sconv.sconv_no_such_call
+
+
+def test_grids_of_2_to_32_threads_are_refused_before_a_launch():
+    for big in (dict(N=1, S=1 << 28), dict(N=1, S=1 << 24, C=9000), dict(N=1, S=1 << 24, C=2100, layout=1, x_s=1 << 24),
+                dict(N=1 << 21, S=128, C=8, layout=1, x_s=128)):
+        assert _forward(_ln(**big)) == EUNSUPPORTED, big
+    for big in (dict(N=1, S=1 << 24, C=9000), dict(N=1, S=1 << 24, C=2100, layout=1, x_s=1 << 24)):
+        assert _backward(_ln(**big)) == EUNSUPPORTED, big
+    assert _rotary(B=1 << 12, S=1 << 12, Hq=64, D=1024) == EUNSUPPORTED
+    assert _attn_forward(_attn(B=1 << 24, Sq=1, H=1, Hkv=1)) == EUNSUPPORTED
+    assert _attn_forward(_attn(B=1 << 10, Sq=1 << 21, H=1, Hkv=1)) == EUNSUPPORTED
+    for big in (dict(B=1, Sq=1 << 28, H=1, Hkv=1), dict(B=1 << 14, Sq=1, Sk=1 << 17, H=1, Hkv=1), dict(B=1, Sq=1, H=1 << 22, Hkv=1)):
+        assert _attn_backward(_attn(**big), nbytes=1 << 45) == EUNSUPPORTED, big
