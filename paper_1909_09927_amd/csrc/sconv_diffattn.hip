@@ -360,6 +360,7 @@ __global__ __launch_bounds__(256, (DT <= 64 ? 2 : 1)) void attn_direct(AttnArgs 
         if (k0 + BN < k1) { fetch_mask(k0 + BN); mark(k0 + BN, 1); }
     }
     for (int j0 = k0; j0 < k1; j0 += BN, turn ^= 1, slot = after(slot)) {
+        Keys::arrived();
         __syncthreads();                               // this tile is there, the other one has been read
         if (j0 + BN < k1) fetch(j0 + BN, turn ^ 1);
         if (j0 + 2 * BN < k1) fetch_mask(j0 + 2 * BN);

@@ -521,6 +521,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_direct(AttnArgs a)
         if (k0 + BN < k1) { fetch_mask(k0 + BN); mark(k0 + BN, 1); }
     }
     for (int j0 = k0; j0 < k1; j0 += BN, turn ^= 1, slot = after(slot)) {
+        Keys::arrived();
         __syncthreads();
         if (j0 + BN < k1) fetch(j0 + BN, turn ^ 1);
         if (j0 + 2 * BN < k1) fetch_mask(j0 + 2 * BN);
@@ -687,6 +688,7 @@ __global__ __launch_bounds__(256, 2) void attn_keys_direct(AttnArgs a)
     int turn = 0, g = per ? (int)(from / per) : 0, i0 = per ? start + (int)(from % per) * BM : 0;
     if (left > 0) { fetch(g, i0, 0); mark(i0, 0); }
     while (left > 0) {
+        Queries::arrived();
         __syncthreads();
         const int at = i0, was = g;
         i0 += BM;

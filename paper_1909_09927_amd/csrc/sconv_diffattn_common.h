@@ -424,6 +424,13 @@ struct Direct {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_t*)(tile + (i * NW + w) * 512), 16, off[i], 0, 0, 0);
 #endif
     }
+    // this wavefront's loads have come: before the barrier behind which others read them, as nothing in the language ties loads to LDS to it
+    __device__ __forceinline__ static void arrived()
+    {
+#if defined(__HIP_DEVICE_COMPILE__)
+        __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0)
+#endif
+    }
     // a row's fragment: row l % 32 of the tile, columns c .. c + 7 + 8 (l / 32): tile + at[c / 16 % 4] + c / 64 * 64
     __device__ __forceinline__ static void row_lane(int (&at)[4])
     {
