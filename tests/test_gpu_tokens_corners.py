@@ -153,3 +153,18 @@ def test_attention_of_few_rows_is_rounded_once(device, shape):
     for name, t in zip(("out", "second"), got):
         own = (r[name].to(BF16).double() - r[name]).norm()
         assert (t.cpu().double() - r[name]).norm() <= 1.05 * own, name
+
+
+@pytest.mark.parametrize("D", [32, 64])
+def test_attention_gradients_are_near_their_rounding(device, D):
+    """16-bit dq and dk over 784 places: their own rounding is 1.66e-3 of their norm, d_m from rounded results brings dq to 1.9e-3.  With dS rounded
+    to 16 bits alone, instead of going as two values, dq is 2.5e-3 (64) and 2.6e-3 (32) off."""
+    S, H = 784, 2
+    q, k, v = (1.5 * _randn(31, 2, S, 2 * H, D)).to(BF16), _randn(32, 2, S, 2 * H, D, dtype=BF16), _randn(33, 2, S, H, 2 * D, dtype=BF16)
+    dout, lam = _randn(34, 2, S, H, 2 * D, dtype=BF16), 0.5 + 0.1 * _randn(35, H)
+    r, _ = ref.attention(q, k, v, lam, None, False, None, None, dout)
+    dev = [t.to(device) for t in (q, k, v, lam)]
+    grads = sconv.sconv_diffattn_backward(dout.to(device), *dev, *sconv.sconv_diffattn_forward(*dev, save=True))
+    for name, got in zip(("dq", "dk"), grads):
+        off = (got.cpu().double() - r[name]).norm() / r[name].norm()
+        assert off <= 2.2e-3, (name, float(off))
