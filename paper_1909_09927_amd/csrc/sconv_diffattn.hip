@@ -11,9 +11,10 @@
 // 1.7e-3, and 12544 queries from 502 to 774 us, 2 x 3136 from 148 to 223, a training pass of 784 places from 155 to 177.  Few rows' wait
 // for memory and take that second product (16 requests of up to 32768 keys 132.7 us
 // without, 134.2 with, one of 32 rows 23.7 and 25.8).  The sums that weights are divided by are of the unrounded ones, in 32 bits.
-// Measured, heads of 64 with values of 128: 12544 queries seeing what came before, 8 heads on 4, 16 bits 486 us = 994 TFLOP/s of seen pairs
-// (a large 16-bit product reaches 1137, the pipe's power limit); 2 x 3136 x 8 unmasked 165 us; 32 bits, 8 x 196 x 7 heads 45 us
-// (112 workgroups); one token of 16 requests over up to 32768 keys 128 us = 4.4 TB/s, 5.2 where requests are equally long, and 5 for the join.
+// Measured, heads of 64 with values of 128: 12544 queries seeing what came before, 8 heads on 4, 16 bits 491 us = 984 TFLOP/s of seen pairs
+// (a large 16-bit product reaches 1137, the pipe's power limit); 2 x 3136 x 8 unmasked 158 us; 32 bits, 8 x 196 x 7 heads 44 us
+// (112 workgroups); one token of 16 requests over up to 32768 keys 130 us = 4.4 TB/s, and 5 for the join.
+// Heads of 65 to 128 do not fit the registers everywhere: attn_wide spills 500 bytes a lane in 32 bits, attn_few up to 550.
 #include <math.h>
 
 #include <algorithm>
@@ -766,7 +767,9 @@ __global__ __launch_bounds__(1024) void attn_join(AttnArgs a)
     }
 }
 
-// The same for many rows in few parts (16 at most): a thread takes four values of a row, and each part's weight with them.
+// The same for the wide kernels' rows: a thread takes four values of a row and walks its parts, twice - a few as a rule; few rows over long
+// caches have up to 32 in 16 bits (32768 keys) and 128 in 32 bits, which take the longer for it (40 rows over 32768 keys 52 us, 32 rows, which
+// attn_few takes, 26).
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join_wide(AttnArgs a)
 {

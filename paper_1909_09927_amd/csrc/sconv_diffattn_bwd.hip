@@ -7,9 +7,11 @@
 //           unrounded weights, for lam's gradient (d_2 itself stems from results that were rounded).
 //   keys    dk, dv: a wavefront keeps 32 keys and walks the queries of every head that shares them, so the sum over heads
 //           and queries has one order and needs no atomics.
-// Measured in 16 bits: 8 x 784 x 8 heads of 32 (values of 64): delta 7, keys 60, rows 47 us (bound by exp, a quarter-rate instruction, and
-// by latency: 448 workgroups are 1.75 a compute unit); 2 x 3136 x 8 heads of 64 (128): dv 145, dk 271, rows 243 us (560, 600 and 660
-// TFLOP/s with what is formed again).
+// Measured in 16 bits, each kernel by itself under the profiler: 8 x 784 x 8 heads of 32 (values of 64): delta 6.5, keys 66, rows 51, dlam 4.7 us
+// (bound by exp, a quarter-rate instruction, and by latency: 448 workgroups are 1.75 a compute unit; with the forward's 37 they add up
+// to 166, a pass without the profiler takes 149); 2 x 3136 x 8 heads of 64 (128): dv 145, dk 271, rows 243 us (560, 600 and 660
+// TFLOP/s with what is formed again).  Heads of 65 to 128 go over the keys three times, form the weights each time and spill (dq in 32 bits
+// 1.5 KB a lane): 2 x 784 x 4 heads of 128 (256) 212 us forward and backward in 16 bits, 662 in 32.
 // All sums are in 32 bits.  In 16 bits the weights are rounded to the operands' type for dv, as forward; dS goes as two 16-bit values,
 // the second holding what the first's rounding left out: its rounding alone would be as large as that of the results, and what d_m
 // carries over from rounded results comes on top (dq 2.6e-3 of its norm off against 1.7e-3 for 32 bits rounded once, now 1.9e-3; 13 - 16 % of

@@ -4,8 +4,9 @@
 // column of B (column l % 32), both at depths 8 (l / 32) .. + 7 of a 16-deep step.  Of the result each lane holds column
 // l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4 in registers r = 0..15.
 // 32-bit operands go through the 16-bit matrix pipe as well, as three pieces that hold 8 bits of the value each (their sum is the
-// value) and six of the nine products of pieces; the three left out are below 2^-24 of the product.  That is 192 cycles for what the
-// 32-bit pipe does in 512.
+// value) and six of the nine products of pieces.  The three left out are within 2^-21 of the product and, as pieces are cut off, of its sign:
+// a product comes out 0.63 * 2^-24 short on average, which is what a 32-bit rounding may do.  That is 192 cycles for what the 32-bit
+// pipe does in 512.
 // So a result can be the next product's B as it stands in its lane: registers 8s..8s+7 are the depths
 //   16 s + 4 (l / 32) + {0, 1, 2, 3, 8, 9, 10, 11}
 // of step s, provided that A's elements come in that order (col_frag below).  Scores are therefore formed transposed - keys down,
@@ -389,7 +390,8 @@ bool attn_vector(const AttnArgs& a, int type);
 
 // 16-bit tiles that go from memory to LDS directly: rows of W elements without padding, whose 16-byte chunks stand at chunk ^ turn(row)
 // of every eight.  turn() differs over eight rows, for lanes that read one chunk of each, and by whole 32 bytes over four, for
-// the transposing read of four rows: neither meets a bank twice.  A wavefront's load fills 1024
+// the transposing read of four rows, so that these lie in different banks (2.7 conflict cycles an LDS instruction are counted all the same
+// over 12544 queries; which lanes the hardware takes together was not looked into).  A wavefront's load fills 1024
 // bytes in a row; each lane chooses the chunk of memory that belongs where its 16 bytes come to lie.  The buffer ends with the last
 // row's last part: with one part, and rows that do not overlap, rows that are not there come as zeros; with two parts they may come
 // as what lies between the parts.

@@ -1,15 +1,16 @@
 // Layer norm over the channels of every place, forward and backward (formulas in sconv_tokens.h).
 //
 // Bound by memory: forward reads x and writes y once, backward reads dy and x and writes dx once.  So a row stays in registers
-// between the statistics and the result: its sums are formed in two steps (mean, then squared distances from it), which loses
-// nothing where the mean is large against the spread, and costs no second read.
+// between the statistics and the result: its sums are formed in two steps (mean, then squared distances from it), so that no
+// large squares cancel where the mean is large against the spread, and that costs no second read.
 //   tokens  a row of C contiguous channels belongs to 16, 64 or 256 lanes, which hold NV vectors each.
 //   map     x[c][s] is contiguous along the places: a workgroup takes P places and all channels, lanes along the places read
-//           whole segments of every channel, and tiles of 128 channels are turned in LDS so that tokens are written (dy:
-//           read) in whole segments too.
+//           whole segments of every channel, and tiles of 128 to 512 channels (backward: dy's of all channels) are turned in LDS so
+//           that tokens are written (dy: read) in whole segments too.
 // The weight's gradient sums over all places: every workgroup walks many rows, keeps the sums of its own in registers, and
 // writes one row of partial sums, which a second kernel adds in a fixed order.
-// Measured (kernels alone; a large copy moves 4.90 TB/s): forward, map 8 x 256 x 56 x 56 in 32 bits to 16-bit tokens 12.9 us (3.0 TB/s:
+// Measured (kernels alone; a large copy moves 4.90 TB/s): forward, 25088 x 512 in 16 bits 12.0 us (4.3 TB/s), 6272 x 4096 19.6; rows that do not
+// lie at whole vectors are read an element a lane (6272 x 4100 77 us); map 8 x 256 x 56 x 56 in 32 bits to 16-bit tokens 12.9 us (3.0 TB/s:
 // reading and writing follow each other in a workgroup); backward, 25088 x 512 in 16 bits 17.3 us (4.5 TB/s) and 3.5 for the sums;
 // backward, map 32 x 896 x 14 x 14 in 32 bits 27 us (2.5 TB/s: 416 workgroups, one round) and 5.3; 49 x 2048 3.3 us (latency).
 #include <math.h>

@@ -4,7 +4,7 @@
 // token, so a workgroup takes whole tokens: it forms them once into LDS - the angle in 64 bits, reduced to an eighth of a turn
 // there, then the two Taylor polynomials in 32 bits - and then turns the tokens' heads with them, 16 bytes a lane.
 // Measured: 12544 tokens of 28 heads of 64 in 32 bits 29 us (6.1 TB/s, part of it from the last-level cache), 6272 tokens of 16 heads of 64
-// in 16 bits 7.2 us (3.6 TB/s), 64 single tokens 3.5 us (latency).
+// in 16 bits 6.9 us (3.7 TB/s), 64 single tokens 3.6 us (latency).
 #include <algorithm>
 
 #include "sconv_tokens_common.h"

@@ -2,7 +2,9 @@
 over several axes, differential attention, and their gradients.
 
 Argument marshalling only, as in the package itself: every sum runs in the HIP kernels behind the C ABI.  Calls go to
-torch's current stream; scratch that a call is not given is taken from torch's allocator for the call.
+torch's current stream; scratch that a call is not given is taken from torch's allocator for the call.  Like the package's other
+calls, these are not part of torch's autograd: results do not require a gradient whatever the operands do, and a training program makes
+the backward calls itself (examples/attention_block.py, or inside a torch.autograd.Function).
 """
 from __future__ import annotations
 
