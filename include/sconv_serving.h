@@ -1,0 +1,155 @@
+/*
+ * sconv, serving operators: a step of an attention block in 8 bits, from one token's residual stream to the next, on AMD MI355X
+ * (gfx950) - root-mean-square norm with the residual's addition (and its gradient), 8-bit operands with block scales, their product, a
+ * paged cache of keys and values that is quantised as it is written, and differential attention of new tokens over it.
+ *
+ * The conventions are those of sconv_tokens.h: device memory is the caller's, work goes to the given stream, calls return without
+ * synchronising, int functions return 0 or a negative SCONV_E* code, argument checks are host code and come first, nothing is kept
+ * between calls, no sum's order depends on timing.  Strides count elements; the last axis of every tensor is contiguous.
+ * SCONV_EUNSUPPORTED, before anything is enqueued, where a size passes a limit given below or a kernel's grid would have 2^32 threads.
+ *
+ * Values in 8 bits (SCONV_E4M3): sign, four bits of exponent, three of mantissa, largest 448, no Inf, NaN at 0x7f and 0xff.  A block of
+ * them shares a scale byte s, which stands for 2^(s - 127): the smallest s, at least 1, for which no finite value of the block
+ * passes 448 * 2^(s - 127).  A value x is held as x * 2^(127 - s), rounded to the nearest, half a step to the even one; Inf and NaN
+ * are held as NaN, and their block's scale does not know of them.  Scales are powers of two, so scaling rounds nothing, what is read back is
+ * exact in 16 bits, and the matrix pipe takes the bytes as they are.  Scale bytes are 1 to 247; those that a caller brings are 1 to 254.
+ */
+#ifndef SCONV_SERVING_H
+#define SCONV_SERVING_H
+
+#include "sconv_tokens.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+enum { SCONV_E4M3 = 2, SCONV_SCALE_BLOCK = 128 };
+
+/*
+ * Root-mean-square norm of rows of C channels, a residual stream's addition in front of it:
+ *   t = x + residual (or x);  rstd = 1 / sqrt(sum_c t^2 / C + eps);  y = t * rstd * w[c].
+ * The sum is formed in 32 bits; y comes from it as it is, and it is rounded to the stream's type where it is stored.
+ */
+typedef struct {
+    int32_t rows, C;           /* rows >= 0; 1 <= C <= 16384                                                      */
+    int32_t x_type, t_type;    /* t_type (of residual and sum): x_type, or SCONV_F32 over a 16-bit x              */
+    int32_t y_type;            /* x_type, SCONV_BF16 or SCONV_E4M3                                                */
+    int32_t w_type;            /* of w and its gradient                                                           */
+    float eps;                 /* >= 0, finite                                                                    */
+    int64_t x_r, res_r, t_r, y_r;   /* strides of the rows of x, residual, sum, y (y_r: and dy; res_r: and dt)    */
+} sconv_rmsnorm_desc_t;
+/*
+ *   x_dev    device, in;  residual_dev: device, in, optional;  w_dev: device, in, [C], optional (NULL: 1)
+ *   y_dev    device, out;  y_scale_dev: device, out, bytes [rows][ceil(C / 128)], with SCONV_E4M3 and then only: a scale for 128 channels
+ *   total_dev  device, out, with residual_dev and then only; may be residual_dev (same stride)
+ *   rstd_dev device, out, fp32 [rows], optional: what the backward call reads
+ */
+int sconv_rmsnorm_forward(const sconv_rmsnorm_desc_t* desc, const void* x_dev, const void* residual_dev, const void* w_dev, void* y_dev,
+                          uint8_t* y_scale_dev, void* total_dev, float* rstd_dev, void* hip_stream);
+/*
+ * Its gradient.  With u = t * rstd and g = dy * w:
+ *   d = dt + rstd * (g - u * mean_c(g * u)),  dw[c] = sum over rows of dy * u;
+ * d is the gradient of x and of residual alike, dt (optional) the one that reaches the sum along the stream.
+ *   dy_dev   device, in, of y_type (SCONV_F32 or SCONV_BF16; the rounding to 8 bits has no gradient of its own)
+ *   total_dev, dt_dev  device, in, of t_type: the sum as it was stored (without residual: x)
+ *   dx_dev, dres_dev   device, out, contiguous, optional: d in x_type and in t_type
+ *   dw_dev   device, out, [C] of w_type, optional
+ *   ws_dev   device, scratch, 16-byte aligned, at least sconv_rmsnorm_workspace_size (read with dw_dev only)
+ */
+int sconv_rmsnorm_backward(const sconv_rmsnorm_desc_t* desc, const void* dy_dev, const void* total_dev, const float* rstd_dev,
+                           const void* w_dev, const void* dt_dev, void* dx_dev, void* dres_dev, void* dw_dev, void* ws_dev,
+                           size_t ws_bytes, void* hip_stream);
+int sconv_rmsnorm_workspace_size(const sconv_rmsnorm_desc_t* desc, size_t* bytes);
+
+/*
+ * Rows into 8 bits, with a scale for 128 values of a row (block_rows 1: what a product's tokens are) or for 128 of each of 128 rows
+ * (block_rows 128: its weights).
+ *   x_dev  device, in, [M][K];  q_dev: device, out, [M][K];  scale_dev: device, out, bytes [ceil(M / block_rows)][ceil(K / 128)]
+ */
+typedef struct {
+    int32_t M, K;              /* >= 0                                                                            */
+    int32_t type;              /* of x: SCONV_F32, SCONV_BF16                                                     */
+    int32_t block_rows;        /* 1 or 128                                                                        */
+    int64_t x_m, q_m;          /* strides of the rows                                                             */
+} sconv_quant8_desc_t;
+int sconv_quant8(const sconv_quant8_desc_t* desc, const void* x_dev, void* q_dev, uint8_t* scale_dev, void* hip_stream);
+
+/*
+ * Product of 8-bit operands: y[m][n] = sum_b 2^(xs[m][b] + ws[n / 128][b] - 254) sum_(k in block b) x[m][k] w[n][k], blocks of 128.
+ *   x_dev [M][K], w_dev [N][K] (a filter or projection as stored), x_scale_dev [M][ceil(K / 128)], w_scale_dev [ceil(N / 128)][ceil(K / 128)]
+ *   y_dev  device, out, [M][N], SCONV_F32 or SCONV_BF16
+ * Products are exact and sums held in 32 bits.
+ */
+typedef struct {
+    int32_t M, N, K;           /* >= 0; K 0 gives zeros                                                           */
+    int32_t y_type;
+    int64_t x_m, w_n, y_m;     /* strides of the rows                                                             */
+} sconv_linear8_desc_t;
+int sconv_linear8(const sconv_linear8_desc_t* desc, const void* x_dev, const uint8_t* x_scale_dev, const void* w_dev,
+                  const uint8_t* w_scale_dev, void* y_dev, void* hip_stream);
+
+/*
+ * A paged cache of keys and values: pages of page_size slots; position p of request b stands in slot p % page_size of page
+ * table[b][p / page_size].  Slots hold Hk keys of D and Hv values of Dv elements, in the tokens' type or in 8 bits with a scale
+ * for every key and value.  A table's entry outside 0 .. pages - 1 is a page that is not there: nothing is written to it, it is read as zeros,
+ * and attention does not see its keys.  The same holds for positions below 0 and from table_width * page_size on.
+ */
+typedef struct {
+    int32_t pages, page_size;  /* pages >= 0, page_size >= 1                                                      */
+    int32_t table_width;       /* >= 0; table_width * page_size < 2^31                                            */
+    int32_t type;              /* of the pages: the tokens' type, or SCONV_E4M3                                   */
+    int32_t Hk, D, Hv, Dv;     /* 1 <= D, Dv <= 256                                                               */
+    int64_t k_p, k_s, k_h, v_p, v_s, v_h;             /* strides of the pages: page, slot, head                  */
+    int64_t ks_p, ks_s, ks_h, vs_p, vs_s, vs_h;       /* strides of the scales                                   */
+    int64_t table_b;           /* stride of the table's rows                                                      */
+} sconv_pages_t;
+/* What the calls on a cache take: k_pages, v_pages, their scales (NULL unless SCONV_E4M3), int32 table [B][table_width]; all device. */
+typedef struct { void* k; void* v; uint8_t* ks; uint8_t* vs; const int32_t* table; } sconv_pages_dev_t;
+typedef struct {
+    int32_t B, S;              /* >= 0                                                                            */
+    int32_t type;              /* of the tokens' keys and values                                                  */
+    int64_t k_b, k_s, k_h, v_b, v_s, v_h;             /* their strides                                           */
+    sconv_pages_t pages;
+} sconv_cache_desc_t;
+/*
+ * write: tokens i < counts[b] (or S) of request b go to positions starts[b] + i; other slots stay as they were.  Two tokens of one call
+ * must not have one slot.
+ *   k_dev [B][S][Hk][D], v_dev [B][S][Hv][Dv]  device, in;  starts_dev: int32 [B];  counts_dev: int32 [B], optional
+ * read: the reverse; rows that are not there are written as zeros.
+ */
+int sconv_cache_write(const sconv_cache_desc_t* desc, const void* k_dev, const void* v_dev, const int32_t* starts_dev,
+                      const int32_t* counts_dev, const sconv_pages_dev_t* pages, void* hip_stream);
+int sconv_cache_read(const sconv_cache_desc_t* desc, const sconv_pages_dev_t* pages, const int32_t* starts_dev,
+                     const int32_t* counts_dev, void* k_dev, void* v_dev, void* hip_stream);
+
+/*
+ * Differential attention (sconv_tokens.h has the formulas) of new tokens over a paged cache: Hk = 2 Hkv keys (the two of head g at 2g,
+ * 2g + 1) and Hv = Hkv values a slot.  Request b has lengths[b] positions (taken as 0 below 0, and as table_width * page_size above); causal:
+ * the last query stands at the last of them.  A query that sees nothing gives zeros.  Keys and values behind the length, or on
+ * pages that are not there, are never part of a sum; one that causal alone hides has to be finite.  Inf, and NaN as 8-bit values hold it, go
+ * through the formulas.  The keys of all requests are shared out among workgroups by their number, whose parts a second kernel joins.
+ * For single tokens and a few (a prompt's own attention is sconv_diffattn_forward's: 32 (query, head) rows of a key head are
+ * the most that one read of the cache serves).
+ */
+typedef struct {
+    int32_t B, Sq;             /* >= 0                                                                            */
+    int32_t H, Hkv;            /* H % Hkv == 0                                                                    */
+    int32_t type;              /* of q and out; the pages' type is this or SCONV_E4M3                             */
+    int32_t causal;
+    float scale;               /* > 0, finite                                                                     */
+    int64_t q_b, q_s, q_h;     /* strides of q                                                                    */
+    sconv_pages_t pages;       /* D 1..128, Dv 1..256                                                             */
+} sconv_paged_desc_t;
+/*
+ *   q_dev [B][Sq][2H][D], lam_dev fp32 [H], lengths_dev int32 [B]  device, in;  out_dev [B][Sq][H][Dv]: device, out, contiguous
+ *   ws_dev, ws_bytes  device, scratch, optional (NULL, 0), 16-byte aligned: parts; with less than sconv_diffattn_paged_workspace_size
+ *                     every request is one workgroup's
+ */
+int sconv_diffattn_paged(const sconv_paged_desc_t* desc, const void* q_dev, const sconv_pages_dev_t* pages, const float* lam_dev,
+                         const int32_t* lengths_dev, void* out_dev, void* ws_dev, size_t ws_bytes, void* hip_stream);
+int sconv_diffattn_paged_workspace_size(const sconv_paged_desc_t* desc, size_t* bytes);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* SCONV_SERVING_H */

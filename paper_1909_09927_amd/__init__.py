@@ -544,11 +544,17 @@ def sconv_tune(x, w, stride=1, pad=0, groups=1, pool=None, relu=False, out=None,
 _TOKEN_NAMES = frozenset((
     "sconv_layernorm_forward", "sconv_layernorm_backward", "sconv_rotary_axes", "sconv_rotary_forward",
     "sconv_rotary_backward", "sconv_diffattn_forward", "sconv_diffattn_backward", "sconv_diffattn_workspace_size"))
+_SERVING_NAMES = frozenset((
+    "PagedCache", "sconv_rmsnorm_forward", "sconv_rmsnorm_backward", "sconv_quant8", "sconv_linear8", "sconv_cache_new",
+    "sconv_cache_write", "sconv_cache_read", "sconv_diffattn_paged", "sconv_diffattn_paged_workspace_size"))
 
 
 def __getattr__(name):
-    """The token operators (tokens.py), loaded with torch by the first program that names one."""
+    """The token and serving operators (tokens.py, serving.py), loaded with torch by the first program that names one."""
     if name in _TOKEN_NAMES:
         from . import tokens
         return globals().setdefault(name, getattr(tokens, name))
+    if name in _SERVING_NAMES:
+        from . import serving
+        return globals().setdefault(name, getattr(serving, name))
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

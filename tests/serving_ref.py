@@ -1,0 +1,140 @@
+"""Plain serving operators in 64 bits on the CPU, each with a bound on what a computation in a given type may be off by.
+
+Bounds are built from the inputs alone: U is a type's unit roundoff, sums of n terms in 32 bits are within n * E of their absolute terms.
+"""
+import numpy as np
+import torch
+
+from tokens_ref import E, U, visible, within  # noqa: F401
+
+E4M3 = torch.float8_e4m3fn
+HALF8 = 2.0 ** -4                                      # half a step of e4m3, relative; 2^-10 of the scale where it has no leading one
+
+
+def _values8():
+    """The value of every byte, from the format's definition."""
+    out = []
+    for b in range(256):
+        e, m = b >> 3 & 15, b & 7
+        v = (m / 8.0) * 2.0 ** -6 if e == 0 else (1.0 + m / 8.0) * 2.0 ** (e - 7)
+        if b & 127 == 127:
+            v = float("nan")
+        out.append(-v if b & 128 else v)
+    return np.array(out)
+
+
+VALUES8 = _values8()
+
+
+def scale_byte(top):
+    """The smallest s >= 1 for which top <= 448 * 2^(s - 127); top: array of finite numbers >= 0."""
+    top = np.asarray(top, np.float64)
+    s = np.ones(top.shape, np.int64)
+    for k in range(1, 248):                            # (no finite 32-bit number needs more than 247)
+        s = np.where(top > 448.0 * 2.0 ** (k - 127), k + 1, s)
+    return s
+
+
+def _to8(v):
+    """The byte nearest to each value of at most 448, half a step to the even byte; NaN: 0x7f."""
+    pos = VALUES8[:127]                                # 0 .. 448, rising
+    a = np.abs(v)
+    a = np.where(np.isfinite(a), a, 0.0)
+    hi = np.clip(np.searchsorted(pos, a), 0, 126)
+    lo = np.maximum(hi - 1, 0)
+    dl, dh = a - pos[lo], pos[hi] - a
+    b = np.where(dl < dh, lo, np.where(dl > dh, hi, np.where(lo % 2 == 0, lo, hi)))
+    b = np.where(np.isfinite(v), b, 127)
+    return np.ascontiguousarray(b | np.where(np.signbit(v) & np.isfinite(v), 128, 0), np.uint8)
+
+
+def _block_tops(x, rows):
+    M, K = x.shape
+    RB, KB = -(-M // rows), -(-K // 128)
+    p = np.zeros((RB * rows, KB * 128))
+    p[:M, :K] = np.where(np.isfinite(x), np.abs(x), 0.0)
+    return p.reshape(RB, rows, KB, 128).max((1, 3))
+
+
+def quant8(x, rows=1):
+    """x [M, K] -> (bytes, scale bytes)"""
+    x = x.double().numpy()
+    s = scale_byte(_block_tops(x, rows))
+    M, K = x.shape
+    e = s[np.arange(M) // rows][:, np.arange(K) // 128]
+    return _to8(x * 2.0 ** (127.0 - e)), s.astype(np.uint8)
+
+
+def same_bytes(got, want, what):
+    """8-bit values as bytes; one NaN is as good as the other."""
+    got = got.cpu().contiguous().view(torch.uint8).numpy().reshape(want.shape)
+    nan = (got & 127) == 127
+    assert ((want & 127 == 127) == nan).all(), f"{what}: NaN elsewhere"
+    bad = (got != want) & ~nan
+    assert not bad.any(), f"{what}: {int(bad.sum())} bytes off, first at {np.argwhere(bad)[0]}: {got[bad][0]} for {want[bad][0]}"
+
+
+def held(q, s, rows=1):
+    """What values [M, K] (e4m3) and scales stand for, in 64 bits."""
+    M, K = q.shape
+    v = torch.from_numpy(VALUES8[q.cpu().contiguous().view(torch.uint8).numpy()])
+    f = 2.0 ** (s.cpu().double() - 127.0)
+    return v * f[torch.arange(M) // rows][:, torch.arange(K) // 128]
+
+
+def rmsnorm(x, residual, w, eps, out_dtype):
+    """x [R, C] -> (y, t, rstd) and their bounds; y's bound without the rounding to 8 bits where that is asked."""
+    t = x.double() + (0.0 if residual is None else residual.double())
+    C = t.shape[1]
+    rstd = 1.0 / (t.square().mean(1, keepdim=True) + eps).sqrt()
+    y = t * rstd * (1.0 if w is None else w.double())
+    # squares: at most 32 in a lane's own order, ten steps over lanes and wavefronts; the sum itself is rounded once
+    rel = (min(C, 32) + 18) * E
+    by = y.abs() * (rel + 8 * E + (0.0 if out_dtype == E4M3 else 1.01 * U[out_dtype]))
+    bt = t.abs() * 1.01 * (E + (0.0 if residual is None else U[residual.dtype]))
+    return (y, t, rstd.squeeze(1)), (by + 1e-30, bt + 1e-30, (rel * rstd).squeeze(1) + 1e-30)
+
+
+def rmsnorm_grad(dy, t, rstd, w, dt):
+    """-> (d, dw), their bounds (32-bit sums; the types' own rounding apart)"""
+    dy, t, rstd = dy.double(), t.double(), rstd.double().unsqueeze(1)
+    C = t.shape[1]
+    w = torch.ones(C, dtype=torch.float64) if w is None else w.double()
+    u, g = t * rstd, dy * w
+    mean = (g * u).mean(1, keepdim=True)
+    d = rstd * (g - u * mean)
+    n = min(C, 32) + 20
+    bm = n * E * (g * u).abs().mean(1, keepdim=True)
+    bd = rstd * (4 * E * (g.abs() + (u * mean).abs()) + u.abs() * bm)
+    if dt is not None:
+        d = d + dt.double()
+        bd = bd + 2 * E * (dt.double().abs() + d.abs())
+    rows = min(dy.shape[0], 700) + 40
+    return (d, (dy * u).sum(0)), (bd + 1e-30, rows * E * (dy * u).abs().sum(0) + 1e-30)
+
+
+def linear8(x, w, out_dtype, coarse):
+    """x [M, K], w [N, K] in 64 bits -> y and its bound.  coarse: products as the 8-bit matrix pipe adds them, which leaves out what lies 2^-15
+    or more below the absolute sum (twice what was measured over normal operands)."""
+    y, mag = x @ w.t(), x.abs() @ w.abs().t()
+    K = x.shape[1]
+    return y, ((K + 16) * E + (2.0 ** -15 if coarse else 0.0)) * mag + 1.01 * U[out_dtype] * y.abs() + 1e-30
+
+
+def gathered(cache, lengths, b):
+    """Keys, values [n, heads, width] of request b in 64 bits (positions that are not there: zeros), and which are there."""
+    k, v, table, ks, vs = (None if t is None else t.cpu() for t in cache)
+    pages, size = k.shape[:2]
+    n = min(max(int(lengths[b]), 0), table.shape[1] * size) if pages else 0
+    p = torch.arange(n)
+    page = table[b].long()[p // size] if n else torch.zeros(0, dtype=torch.long)
+    ok = (page >= 0) & (page < pages)
+    page = torch.where(ok, page, 0)
+    out = []
+    for x, s in ((k, ks), (v, vs)):
+        if s is None:
+            got = x[page, p % size].double() if n else torch.zeros(0, *x.shape[2:], dtype=torch.float64)
+        else:
+            got = torch.from_numpy(VALUES8[x.view(torch.uint8)[page, p % size].numpy()]) * (2.0 ** (s[page, p % size].double() - 127.0)).unsqueeze(-1)
+        out.append(torch.where(ok[:, None, None], got, 0.0))
+    return out[0], out[1], ok
