@@ -3,7 +3,9 @@
 // Few rows (up to 64, single tokens): bound by the weights' read.  A workgroup takes 16 weight rows, its wavefronts share out the blocks of
 // 128, read weights from memory straight into the product's registers and meet in LDS.  The 8-bit values become 16-bit ones, exactly, a
 // block's product is exact to 32 bits and takes its scale as it joins the sum.
-// Many rows: tiles of 64 x 64, operands from memory in the same way.
+// Many rows: tiles through LDS.  16-bit results take 8-bit products with the scales as operands; the matrix pipe then leaves out what lies some
+// 2^-16 below the largest product of a group (measured 1.4e-5 of a result's norm, at any depth), which rounding to 16
+// bits hides.  32-bit results take 16-bit products of the converted values, as few rows do.
 //
 // Layout of the products: weights are A, tokens are B, so that a lane's results are neighbours of one token's row.  Which depths of a block a
 // lane holds does not matter, as long as both operands have the same.
@@ -38,10 +40,10 @@ __device__ __forceinline__ i32x4 bytes16(const uint8_t* p, int have)
 }
 
 // Eight bytes as 16-bit values.
-__device__ __forceinline__ bf16x8 widened(int lo, int hi)
+__device__ __forceinline__ bf16x8 widened(int lo, int hi, float scale = 1.0f)
 {
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
@@ -120,41 +122,195 @@ __global__ __launch_bounds__(64 * NW) void linear_few(LinArgs a)
     }
 }
 
-// Many rows, simple form: 64 x 64 results a workgroup, a wavefront 16 weight rows by 64 tokens, operands from memory.
-template <typename T>
-__global__ __launch_bounds__(256) void linear_tile(LinArgs a, int row_tiles)
+// Many rows.  WM x WN wavefronts, each 32 TM tokens by 32 TN weight rows; blocks of 128 of both operands pass through two buffers in LDS,
+// the next one's loads under this one's products.  A row of a block is eight chunks of 16 bytes, which stand at chunk ^ turn(row), so that lanes
+// that read one chunk of consecutive rows meet different banks.  DIRECT: chunks go from memory to LDS without registers (rows at whole
+// chunks); a chunk behind a row's end is asked for behind the buffer's and comes as zeros.
+template <int WM, int WN, int TM, int TN>
+struct TileShape {
+    static constexpr int BM = WM * TM * 32, BN = WN * TN * 32, WAVES = WM * WN, THREADS = 64 * WAVES;
+    static constexpr int ROWS = BN + BM, N = ROWS / 8 / WAVES;           // rows of a buffer (weights, then tokens), its loads by one wavefront
+    static_assert(N * WAVES * 8 == ROWS && BN % (8 * WAVES) == 0, "whole loads of one operand each");
+    static constexpr size_t LDS = (size_t)2 * ROWS * 128;
+};
+
+__device__ __forceinline__ int turn(int row) { return (row >> 1) & 7; }
+
+template <typename T, bool FAST, bool DIRECT, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void linear_tile(LinArgs a, int tiles_m, int tiles_n)
 {
-    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, h = l >> 4;
-    const int nt = blockIdx.x / row_tiles, n0 = nt * 64 + 16 * w, m0 = (blockIdx.x - nt * row_tiles) * 64;
-    const uint8_t* wr = a.w + (int64_t)min(n0 + c, a.N - 1) * a.w_n + 32 * h;
-    const uint8_t* ws = a.ws + (int64_t)(min(n0, a.N - 1) >> 7) * a.KB;
-    f32x4 sum[4] = {};
-    for (int kb = 0; kb < a.KB; ++kb) {
-        const int k = kb * 128, have = a.K - k - 32 * h;
-        const i32x4 w0 = bytes16(wr + k, have), w1 = bytes16(wr + k + 16, have - 16);
-        const int we = ws[kb];
-        bf16x8 wf[4] = {widened(w0[0], w0[1]), widened(w0[2], w0[3]), widened(w1[0], w1[1]), widened(w1[2], w1[3])};
+    typedef TileShape<WM, WN, TM, TN> Shape;
+    constexpr int N = Shape::N, WAVES = Shape::WAVES, NW_LOADS = Shape::BN / 8 / WAVES;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 31, h = l >> 5;
+    // blocks go round the chiplets: each gets a stretch of tiles, in groups of eight tiles of tokens that share their weights
+    const int total = tiles_m * tiles_n, id = blockIdx.x, each = total / 8, more = total % 8, chip = id % 8;
+    const int lin = chip * each + min(chip, more) + id / 8, width = 8 * tiles_n, group = lin / width, in = lin - group * width;
+    const int high = min(8, tiles_m - 8 * group), tn = in / high, tm = 8 * group + in - tn * high;
+    const int n0 = tn * Shape::BN, m0 = tm * Shape::BM;
+
+    // a load is eight rows of eight chunks; lane l writes chunk l % 8 of row l / 8
+    const auto source = [&](int i, bool& weights, int& row, int& chunk) {
+        weights = i < NW_LOADS;
+        row = ((weights ? i : i - NW_LOADS) * WAVES + w) * 8 + (l >> 3);
+        chunk = (l & 7) ^ turn(row);
+    };
+    uint32_t off[DIRECT ? N : 1];
+    if constexpr (DIRECT) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int m = min(m0 + 16 * t + c, a.M - 1);
-            const uint8_t* xr = a.x + m * a.x_m + 32 * h + k;
-            const i32x4 x0 = bytes16(xr, have), x1 = bytes16(xr + 16, have - 16);
-            const int e = we + a.xs[(int64_t)m * a.KB + kb] - 254;
-            f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
-            p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[0], widened(x0[0], x0[1]), p, 0, 0, 0);
-            p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[1], widened(x0[2], x0[3]), p, 0, 0, 0);
-            p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[2], widened(x1[0], x1[1]), p, 0, 0, 0);
-            p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[3], widened(x1[2], x1[3]), p, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[t][i] += __builtin_ldexpf(p[i], e);
+        for (int i = 0; i < N; ++i) {
+            bool weights; int row, chunk;
+            source(i, weights, row, chunk);
+            off[i] = (uint32_t)(row * (weights ? a.w_n : a.x_m) + 16 * chunk);
         }
     }
+    i32x4 held[DIRECT ? 1 : N];
+    const auto slot = [&](int i, int buffer) {           // in bytes, of a load's first row
+        return ((buffer * Shape::ROWS) + (i < NW_LOADS ? 0 : Shape::BN) + ((i < NW_LOADS ? i : i - NW_LOADS) * WAVES + w) * 8) * 128;
+    };
+    const auto fetch = [&](int kb, int buffer) {
+        const int k = kb * 128, left = a.K - k;
+        if constexpr (DIRECT) {
+#if defined(__HIP_DEVICE_COMPILE__)
+            typedef __attribute__((address_space(3))) void lds_t;
+            // (buffers end with the operand's last row's last byte: rows behind it come as zeros)
+            const auto buffer_of = [&](const uint8_t* base, int64_t stride, int first, int rows) {
+                const int64_t size = ((int64_t)(rows - first - 1) * stride + left), most = (int64_t)1 << 31;
+                const uint64_t at = (uint64_t)(base + first * stride + k);
+                const uint64_t p = ((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
+                return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, __builtin_amdgcn_readfirstlane((uint32_t)(size < most ? size : most)), 0x00027000);
+            };
+            const auto wb = buffer_of(a.w, a.w_n, n0, a.N), xb = buffer_of(a.x, a.x_m, m0, a.M);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const int m = m0 + 16 * t + c, n = n0 + 4 * h;
-        const float o[4] = {sum[t][0], sum[t][1], sum[t][2], sum[t][3]};
-        if (m < a.M) store_row4((T*)a.y + m * a.y_m + n, a.N - n, a.vec, o);
+            for (int i = 0; i < N; ++i) {
+                uint32_t o = off[i];
+                if (left < 128) {
+                    bool weights; int row, chunk;
+                    source(i, weights, row, chunk);
+                    if (16 * chunk >= left) o = 0x80000000u;
+                }
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(i < NW_LOADS ? wb : xb, (lds_t*)(lds + slot(i, buffer)), 16, o, 0, 0, 0);
+            }
+#endif
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                bool weights; int row, chunk;
+                source(i, weights, row, chunk);
+                const uint8_t* p = weights ? a.w + (int64_t)min(n0 + row, a.N - 1) * a.w_n : a.x + (int64_t)min(m0 + row, a.M - 1) * a.x_m;
+                held[i] = bytes16(p + k + 16 * chunk, left - 16 * chunk);
+            }
+        }
+    };
+    const auto arrive = [&](int buffer) {
+        if constexpr (DIRECT) {
+#if defined(__HIP_DEVICE_COMPILE__)
+            __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0): nothing in the language ties loads to LDS to the barrier behind which others read them
+#endif
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) *(i32x4*)(lds + slot(i, buffer) + 16 * l) = held[i];
+        }
+    };
+
+    const int wm = w / WN, wn = w - wm * WN, mine_n = n0 + wn * TN * 32, mine_m = m0 + wm * TM * 32;
+    const uint8_t* ws = a.ws + (int64_t)(min(mine_n, a.N - 1) >> 7) * a.KB;
+    const uint8_t* xs[TM];
+#pragma unroll
+    for (int t = 0; t < TM; ++t) xs[t] = a.xs + (int64_t)min(mine_m + 32 * t + c, a.M - 1) * a.KB;
+    f32x16 sum[TM][TN];
+#pragma unroll
+    for (int t = 0; t < TM; ++t)
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum[t][n][e] = 0.0f;
+    int we = 0, xe[TM] = {}, we_next = 0, xe_next[TM] = {};
+    const auto scales = [&](int kb) {
+        we_next = ws[kb];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) xe_next[t] = xs[t][kb];
+    };
+    // a lane's 32 bytes of a row at depths 64 s: chunks 4 s + 2 h and the next
+    const auto frag = [&](int first, int s) {
+        const int row = first + c;
+        union { i32x8 v; i32x4 q[2]; } r;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) r.q[i] = *(const i32x4*)(lds + row * 128 + 16 * ((4 * s + 2 * h + i) ^ turn(row)));
+        return r.v;
+    };
+    if (a.KB > 0) { fetch(0, 0); scales(0); arrive(0); }
+    __syncthreads();
+    for (int kb = 0; kb < a.KB; ++kb) {
+        const int buffer = kb & 1, base = buffer * Shape::ROWS;
+        we = we_next;
+#pragma unroll
+        for (int t = 0; t < TM; ++t) xe[t] = xe_next[t];
+        if (kb + 1 < a.KB) { fetch(kb + 1, buffer ^ 1); scales(kb + 1); }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            i32x8 wf[TN];
+#pragma unroll
+            for (int n = 0; n < TN; ++n) wf[n] = frag(base + wn * TN * 32 + 32 * n, s);
+            if constexpr (FAST) {
+#pragma unroll
+                for (int t = 0; t < TM; ++t) {
+                    const i32x8 xf = frag(base + Shape::BN + wm * TM * 32 + 32 * t, s);
+#pragma unroll
+                    for (int n = 0; n < TN; ++n) sum[t][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[n], xf, sum[t][n], 0, 0, 0, we, 0, xe[t]);
+                }
+            } else {
+                // (the tokens take both scales: a product whose scale passes 2^119 is out of their range)
+                bf16x8 wv[TN][4];
+#pragma unroll
+                for (int n = 0; n < TN; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) wv[n][i] = widened(wf[n][2 * i], wf[n][2 * i + 1]);
+#pragma unroll
+                for (int t = 0; t < TM; ++t) {
+                    const i32x8 xf = frag(base + Shape::BN + wm * TM * 32 + 32 * t, s);
+                    const float f = __builtin_ldexpf(1.0f, we + xe[t] - 254);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bf16x8 xv = widened(xf[2 * i], xf[2 * i + 1], f);
+#pragma unroll
+                        for (int n = 0; n < TN; ++n) sum[t][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv[n][i], xv, sum[t][n], 0, 0, 0);
+                    }
+                }
+            }
+        }
+        if constexpr (!DIRECT) __syncthreads();          // (registers go to the buffer that was read a block ago)
+        if (kb + 1 < a.KB) arrive(buffer ^ 1);
+        __syncthreads();
     }
+#pragma unroll
+    for (int t = 0; t < TM; ++t) {
+        const int m = mine_m + 32 * t + c;
+        if (m >= a.M) continue;
+        T* y = (T*)a.y + m * a.y_m;
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int at = mine_n + 32 * n + 8 * q + 4 * h;
+                const float o[4] = {sum[t][n][4 * q], sum[t][n][4 * q + 1], sum[t][n][4 * q + 2], sum[t][n][4 * q + 3]};
+                store_row4(y + at, a.N - at, a.vec, o);
+            }
+    }
+}
+
+template <typename T, bool DIRECT, int WM, int WN, int TM, int TN>
+int tile_launch(const LinArgs& a, hipStream_t stream)
+{
+    typedef TileShape<WM, WN, TM, TN> Shape;
+    const int64_t tiles_m = ((int64_t)a.M + Shape::BM - 1) / Shape::BM, tiles_n = ((int64_t)a.N + Shape::BN - 1) / Shape::BN;
+    if (!grid_fits(tiles_m * tiles_n, Shape::THREADS)) return SCONV_EUNSUPPORTED;
+    const auto kern = linear_tile<T, sizeof(T) == 2, DIRECT, WM, WN, TM, TN>;
+    if (Shape::LDS > 64 * 1024 &&
+        hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::LDS) != hipSuccess)
+        return SCONV_ELAUNCH;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n)), dim3(Shape::THREADS), Shape::LDS, stream, a, (int)tiles_m, (int)tiles_n);
+    return launch_status();
 }
 
 template <typename T>
@@ -169,10 +325,11 @@ int linear_run(const LinArgs& a, hipStream_t stream)
         else hipLaunchKernelGGL((linear_few<T, 4, 8>), blocks, threads, 0, stream, a);
         return launch_status();
     }
-    const int64_t row_tiles = ((int64_t)a.M + 63) / 64, grid = row_tiles * (((int64_t)a.N + 63) / 64);
-    if (!grid_fits(grid, 256)) return SCONV_EUNSUPPORTED;
-    hipLaunchKernelGGL((linear_tile<T>), dim3((unsigned)grid), dim3(256), 0, stream, a, (int)row_tiles);
-    return launch_status();
+    // (a tile has to lie within what a buffer's offsets reach)
+    const bool direct = (a.K | a.x_m | a.w_n) % 16 == 0 && aligned_to(a.x, 16) && aligned_to(a.w, 16) && a.x_m < (int64_t(1) << 22) && a.w_n < (int64_t(1) << 22);
+    const int64_t big = (((int64_t)a.M + 255) / 256) * (((int64_t)a.N + 255) / 256);
+    if (direct && big >= 256) return tile_launch<T, true, 2, 4, 4, 2>(a, stream);
+    return direct ? tile_launch<T, true, 2, 2, 2, 2>(a, stream) : tile_launch<T, false, 2, 2, 2, 2>(a, stream);
 }
 
 }  // namespace
