@@ -131,6 +131,7 @@ struct TileShape {
     static constexpr int BM = WM * TM * 32, BN = WN * TN * 32, WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int ROWS = BN + BM, N = ROWS / 8 / WAVES;           // rows of a buffer (weights, then tokens), its loads by one wavefront
     static_assert(N * WAVES * 8 == ROWS && BN % (8 * WAVES) == 0, "whole loads of one operand each");
+    static_assert(WAVES % 2 == 0, "a lane's chunk is the same in all its loads");
     static constexpr size_t LDS = (size_t)2 * ROWS * 128;
 };
 
@@ -150,19 +151,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void linear_tile(LinArgs a, int ti
     const int n0 = tn * Shape::BN, m0 = tm * Shape::BM;
 
     // a load is eight rows of eight chunks; lane l writes chunk l % 8 of row l / 8
-    const auto source = [&](int i, bool& weights, int& row, int& chunk) {
-        weights = i < NW_LOADS;
-        row = ((weights ? i : i - NW_LOADS) * WAVES + w) * 8 + (l >> 3);
-        chunk = (l & 7) ^ turn(row);
-    };
+    const auto row_of = [&](int i) { return ((i < NW_LOADS ? i : i - NW_LOADS) * WAVES + w) * 8 + (l >> 3); };
+    const int chunk = (l & 7) ^ turn(row_of(0));
     uint32_t off[DIRECT ? N : 1];
     if constexpr (DIRECT) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            bool weights; int row, chunk;
-            source(i, weights, row, chunk);
-            off[i] = (uint32_t)(row * (weights ? a.w_n : a.x_m) + 16 * chunk);
-        }
+        for (int i = 0; i < N; ++i) off[i] = (uint32_t)(row_of(i) * (i < NW_LOADS ? a.w_n : a.x_m) + 16 * chunk);
     }
     i32x4 held[DIRECT ? 1 : N];
     const auto slot = [&](int i, int buffer) {           // in bytes, of a load's first row
@@ -181,23 +175,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void linear_tile(LinArgs a, int ti
                 return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, __builtin_amdgcn_readfirstlane((uint32_t)(size < most ? size : most)), 0x00027000);
             };
             const auto wb = buffer_of(a.w, a.w_n, n0, a.N), xb = buffer_of(a.x, a.x_m, m0, a.M);
+            const bool behind = 16 * chunk >= left;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                uint32_t o = off[i];
-                if (left < 128) {
-                    bool weights; int row, chunk;
-                    source(i, weights, row, chunk);
-                    if (16 * chunk >= left) o = 0x80000000u;
-                }
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(i < NW_LOADS ? wb : xb, (lds_t*)(lds + slot(i, buffer)), 16, o, 0, 0, 0);
-            }
+            for (int i = 0; i < N; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(i < NW_LOADS ? wb : xb, (lds_t*)(lds + slot(i, buffer)), 16, behind ? 0x80000000u : off[i], 0, 0, 0);
 #endif
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                bool weights; int row, chunk;
-                source(i, weights, row, chunk);
-                const uint8_t* p = weights ? a.w + (int64_t)min(n0 + row, a.N - 1) * a.w_n : a.x + (int64_t)min(m0 + row, a.M - 1) * a.x_m;
+                const uint8_t* p = i < NW_LOADS ? a.w + (int64_t)min(n0 + row_of(i), a.N - 1) * a.w_n : a.x + (int64_t)min(m0 + row_of(i), a.M - 1) * a.x_m;
                 held[i] = bytes16(p + k + 16 * chunk, left - 16 * chunk);
             }
         }
@@ -239,14 +225,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void linear_tile(LinArgs a, int ti
         for (int i = 0; i < 2; ++i) r.q[i] = *(const i32x4*)(lds + row * 128 + 16 * ((4 * s + 2 * h + i) ^ turn(row)));
         return r.v;
     };
-    if (a.KB > 0) { fetch(0, 0); scales(0); arrive(0); }
-    __syncthreads();
-    for (int kb = 0; kb < a.KB; ++kb) {
-        const int buffer = kb & 1, base = buffer * Shape::ROWS;
-        we = we_next;
-#pragma unroll
-        for (int t = 0; t < TM; ++t) xe[t] = xe_next[t];
-        if (kb + 1 < a.KB) { fetch(kb + 1, buffer ^ 1); scales(kb + 1); }
+    const auto products = [&](int buffer) {
+        const int base = buffer * Shape::ROWS;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             i32x8 wf[TN];
@@ -279,9 +259,41 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void linear_tile(LinArgs a, int ti
                 }
             }
         }
-        if constexpr (!DIRECT) __syncthreads();          // (registers go to the buffer that was read a block ago)
-        if (kb + 1 < a.KB) arrive(buffer ^ 1);
+        if constexpr (FAST) {
+            // the next fragments are read under this one's products
+            __builtin_amdgcn_sched_group_barrier(0x100, 2 * TN + 2, 0);
+#pragma unroll
+            for (int i = 0; i < 2 * TM; ++i) {
+                if (i % TM < TM - 1) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                else if (i < TM) __builtin_amdgcn_sched_group_barrier(0x100, 2 * TN + 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, TN, 0);
+            }
+        }
+    };
+    const auto take = [&]() {
+        we = we_next;
+#pragma unroll
+        for (int t = 0; t < TM; ++t) xe[t] = xe_next[t];
+    };
+    if (a.KB > 0) {
+        fetch(0, 0);
+        scales(0);
+        arrive(0);
         __syncthreads();
+        // (without a branch in the loop: the compiler moves products over one, behind the wait for the next block)
+        for (int kb = 1; kb < a.KB; ++kb) {
+            const int buffer = kb & 1;
+            take();
+            fetch(kb, buffer);
+            scales(kb);
+            __builtin_amdgcn_sched_barrier(0);           // (the loads stay in front)
+            products(buffer ^ 1);
+            __builtin_amdgcn_sched_barrier(0);
+            arrive(buffer);
+            __syncthreads();
+        }
+        take();
+        products((a.KB & 1) ^ 1);
     }
 #pragma unroll
     for (int t = 0; t < TM; ++t) {
