@@ -3,9 +3,9 @@
 // Few rows (up to 64, single tokens): bound by the weights' read.  A workgroup takes 16 weight rows, its wavefronts share out the blocks of
 // 128, read weights from memory straight into the product's registers and meet in LDS.  The 8-bit values become 16-bit ones, exactly, a
 // block's product is exact to 32 bits and takes its scale as it joins the sum.
-// Many rows: tiles through LDS.  16-bit results take 8-bit products with the scales as operands; the matrix pipe then leaves out what lies some
-// 2^-16 below the largest product of a group (measured 1.4e-5 of a result's norm, at any depth), which rounding to 16
-// bits hides.  32-bit results take 16-bit products of the converted values, as few rows do.
+// Many rows: tiles through LDS.  16-bit results take 8-bit products with the scales as operands; the matrix pipe takes eight products at a
+// time and cuts off what lies 2^-13 or more below the largest of them (measured: 1.4e-5 of a result's norm, at any depth), which rounding to
+// 16 bits hides.  32-bit results take 16-bit products of the converted values, as few rows do.
 //
 // Layout of the products: weights are A, tokens are B, so that a lane's results are neighbours of one token's row.  Which depths of a block a
 // lane holds does not matter, as long as both operands have the same.
@@ -26,6 +26,9 @@ struct LinArgs {
     int M, N, K, KB, vec;
     int64_t x_m, w_n, y_m;
 };
+
+// Between a wavefront's own writes and reads of LDS: they are carried out in order; the compiler is told to leave them so.
+__device__ __forceinline__ void wave_lds_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
 
 // 16 bytes of a row of which `have` are there, from any address.
 __device__ __forceinline__ i32x4 bytes16(const uint8_t* p, int have)
@@ -122,206 +125,281 @@ __global__ __launch_bounds__(64 * NW) void linear_few(LinArgs a)
     }
 }
 
-// Many rows.  WM x WN wavefronts, each 32 TM tokens by 32 TN weight rows; blocks of 128 of both operands pass through two buffers in LDS,
-// the next one's loads under this one's products.  A row of a block is eight chunks of 16 bytes, which stand at chunk ^ turn(row), so that lanes
-// that read one chunk of consecutive rows meet different banks.  DIRECT: chunks go from memory to LDS without registers (rows at whole
-// chunks); a chunk behind a row's end is asked for behind the buffer's and comes as zeros.
+// Many rows.  WM x WN wavefronts, each 32 TM tokens by 32 TN weight rows, walk tiles of their own, and every tile's depth in stages of 64, which
+// pass through a ring of four buffers in LDS: three stages' loads are under way beneath one's products, also across the end of a tile,
+// whose results go out meanwhile.  (Two buffers of 128 wait for the memory's latency at every block: 12544 x 2048 to 8192 317 us.)
+// A row of a stage is four chunks of 16 bytes, which stand at chunk ^ turn(row), so that lanes that read one chunk of 16 consecutive rows meet
+// different banks.  DIRECT: chunks go from memory to LDS without registers (rows at whole chunks); a chunk behind a row's end is asked
+// for behind the buffer's and comes as zeros.  Results are turned in LDS, so that a token's are written in whole lines.
 template <int WM, int WN, int TM, int TN>
-struct TileShape {
-    static constexpr int BM = WM * TM * 32, BN = WN * TN * 32, WAVES = WM * WN, THREADS = 64 * WAVES;
-    static constexpr int ROWS = BN + BM, N = ROWS / 8 / WAVES;           // rows of a buffer (weights, then tokens), its loads by one wavefront
-    static_assert(N * WAVES * 8 == ROWS && BN % (8 * WAVES) == 0, "whole loads of one operand each");
-    static_assert(WAVES % 2 == 0, "a lane's chunk is the same in all its loads");
-    static constexpr size_t LDS = (size_t)2 * ROWS * 128;
+struct RingShape {
+    static constexpr int BM = WM * TM * 32, BN = WN * TN * 32, WAVES = WM * WN, THREADS = 64 * WAVES, STAGES = 4;
+    static constexpr int ROWS = BN + BM, N = ROWS / 16 / WAVES;          // rows of a buffer (weights, then tokens), its loads by one wavefront
+    static_assert(N * WAVES * 16 == ROWS && BN % (16 * WAVES) == 0, "whole loads of one operand each");
+    static constexpr int OUT = 4096;                                     // of a wavefront's results on their way out
+    static constexpr size_t LDS = (size_t)STAGES * ROWS * 64 + WAVES * OUT;
 };
 
-__device__ __forceinline__ int turn(int row) { return (row >> 1) & 7; }
+// vmcnt(n), nothing of the other counters
+template <int n>
+__device__ __forceinline__ void loads_left()
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (n & 15) | (n >> 4) << 14);
+#endif
+}
+// A barrier that waits for none of this wavefront's loads (a fence would, for those to LDS).
+__device__ __forceinline__ void bare_barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
 
 template <typename T, bool FAST, bool DIRECT, int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void linear_tile(LinArgs a, int tiles_m, int tiles_n)
+__global__ __launch_bounds__(64 * WM * WN, 2) void linear_ring(LinArgs a, int tiles_m, int tiles_n)
 {
-    typedef TileShape<WM, WN, TM, TN> Shape;
-    constexpr int N = Shape::N, WAVES = Shape::WAVES, NW_LOADS = Shape::BN / 8 / WAVES;
+    typedef RingShape<WM, WN, TM, TN> Shape;
+    constexpr int N = Shape::N, WAVES = Shape::WAVES, NWL = Shape::BN / 16 / WAVES, STAGES = Shape::STAGES;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 31, h = l >> 5;
+    const int wm = w / WN, wn = w - wm * WN, total = tiles_m * tiles_n;
     // blocks go round the chiplets: each gets a stretch of tiles, in groups of eight tiles of tokens that share their weights
-    const int total = tiles_m * tiles_n, id = blockIdx.x, each = total / 8, more = total % 8, chip = id % 8;
-    const int lin = chip * each + min(chip, more) + id / 8, width = 8 * tiles_n, group = lin / width, in = lin - group * width;
-    const int high = min(8, tiles_m - 8 * group), tn = in / high, tm = 8 * group + in - tn * high;
-    const int n0 = tn * Shape::BN, m0 = tm * Shape::BM;
+    const auto place = [&](int id, int& n0, int& m0) {
+        const int each = total / 8, more = total % 8, chip = id % 8;
+        const int lin = chip * each + min(chip, more) + id / 8, width = 8 * tiles_n, group = lin / width, in = lin - group * width;
+        const int high = min(8, tiles_m - 8 * group), tn = in / high, tm = 8 * group + in - tn * high;
+        n0 = tn * Shape::BN;
+        m0 = tm * Shape::BM;
+    };
 
-    // a load is eight rows of eight chunks; lane l writes chunk l % 8 of row l / 8
-    const auto row_of = [&](int i) { return ((i < NW_LOADS ? i : i - NW_LOADS) * WAVES + w) * 8 + (l >> 3); };
-    const int chunk = (l & 7) ^ turn(row_of(0));
+    // a load is 16 rows of four chunks; lane l writes chunk l % 4 of row l / 4
+    const auto row_of = [&](int i) { return ((i < NWL ? i : i - NWL) * WAVES + w) * 16 + (l >> 2); };
+    const int chunk = (l & 3) ^ (l >> 4);
     uint32_t off[DIRECT ? N : 1];
     if constexpr (DIRECT) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) off[i] = (uint32_t)(row_of(i) * (i < NW_LOADS ? a.w_n : a.x_m) + 16 * chunk);
+        for (int i = 0; i < N; ++i) off[i] = (uint32_t)(row_of(i) * (i < NWL ? a.w_n : a.x_m) + 16 * chunk);
     }
     i32x4 held[DIRECT ? 1 : N];
     const auto slot = [&](int i, int buffer) {           // in bytes, of a load's first row
-        return ((buffer * Shape::ROWS) + (i < NW_LOADS ? 0 : Shape::BN) + ((i < NW_LOADS ? i : i - NW_LOADS) * WAVES + w) * 8) * 128;
+        return (buffer * Shape::ROWS + (i < NWL ? 0 : Shape::BN) + ((i < NWL ? i : i - NWL) * WAVES + w) * 16) * 64;
     };
-    const auto fetch = [&](int kb, int buffer) {
-        const int k = kb * 128, left = a.K - k;
+    // Which stage is loaded next and whose scales: of this tile or already of the next one (a tile has four stages at least, the last
+    // of which may lie behind the depth: zeros).  Without branches: the compiler moves products over one, behind the wait for the next stage.
+    const int blocks = max(a.KB, 2), stages = 2 * blocks;
+    int n0, m0, next_n = 0, next_m = 0;
+    bool next_live;
+    const auto look = [&](int id) {
+        next_live = id < total;
+        if (next_live) place(id, next_n, next_m);
+    };
+    place(blockIdx.x, n0, m0);
+    look(blockIdx.x + gridDim.x);
+    int f_stage = 0, f_buffer = 0, f_n = n0, f_m = m0, s_kb = 0, s_n = n0, s_m = m0;
+    bool f_live = true;
+    const auto fetch = [&]() {
+        const bool over = f_stage == stages;
+        f_stage = over ? 0 : f_stage;
+        f_n = over ? next_n : f_n;
+        f_m = over ? next_m : f_m;
+        f_live = over ? next_live : f_live;
+        const int k = f_stage * 64, left = f_live ? a.K - k : 0;
         if constexpr (DIRECT) {
 #if defined(__HIP_DEVICE_COMPILE__)
             typedef __attribute__((address_space(3))) void lds_t;
             // (buffers end with the operand's last row's last byte: rows behind it come as zeros)
             const auto buffer_of = [&](const uint8_t* base, int64_t stride, int first, int rows) {
-                const int64_t size = ((int64_t)(rows - first - 1) * stride + left), most = (int64_t)1 << 31;
+                const int64_t size = (int64_t)(rows - first - 1) * stride + left, most = (int64_t)1 << 31;
                 const uint64_t at = (uint64_t)(base + first * stride + k);
                 const uint64_t p = ((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
-                return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, __builtin_amdgcn_readfirstlane((uint32_t)(size < most ? size : most)), 0x00027000);
+                return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, __builtin_amdgcn_readfirstlane((uint32_t)(left <= 0 ? 0 : size < most ? size : most)), 0x00027000);
             };
-            const auto wb = buffer_of(a.w, a.w_n, n0, a.N), xb = buffer_of(a.x, a.x_m, m0, a.M);
+            const auto wb = buffer_of(a.w, a.w_n, f_n, a.N), xb = buffer_of(a.x, a.x_m, f_m, a.M);
             const bool behind = 16 * chunk >= left;
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(i < NW_LOADS ? wb : xb, (lds_t*)(lds + slot(i, buffer)), 16, behind ? 0x80000000u : off[i], 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(i < NWL ? wb : xb, (lds_t*)(lds + slot(i, f_buffer)), 16, behind ? 0x80000000u : off[i], 0, 0, 0);
 #endif
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const uint8_t* p = i < NW_LOADS ? a.w + (int64_t)min(n0 + row_of(i), a.N - 1) * a.w_n : a.x + (int64_t)min(m0 + row_of(i), a.M - 1) * a.x_m;
+                const uint8_t* p = i < NWL ? a.w + (int64_t)min(f_n + row_of(i), a.N - 1) * a.w_n : a.x + (int64_t)min(f_m + row_of(i), a.M - 1) * a.x_m;
                 held[i] = bytes16(p + k + 16 * chunk, left - 16 * chunk);
             }
         }
+        f_buffer = (f_buffer + 1) % STAGES;
+        ++f_stage;
     };
-    const auto arrive = [&](int buffer) {
-        if constexpr (DIRECT) {
-#if defined(__HIP_DEVICE_COMPILE__)
-            __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0): nothing in the language ties loads to LDS to the barrier behind which others read them
-#endif
-        } else {
+    const auto put = [&](int buffer) {
+        if constexpr (!DIRECT)
 #pragma unroll
             for (int i = 0; i < N; ++i) *(i32x4*)(lds + slot(i, buffer) + 16 * l) = held[i];
-        }
     };
-
-    const int wm = w / WN, wn = w - wm * WN, mine_n = n0 + wn * TN * 32, mine_m = m0 + wm * TM * 32;
-    const uint8_t* ws = a.ws + (int64_t)(min(mine_n, a.N - 1) >> 7) * a.KB;
-    const uint8_t* xs[TM];
+    int we[3] = {}, xe[3][TM] = {};
+    const auto scales = [&](int to) {
+        const bool over = s_kb == blocks;
+        s_kb = over ? 0 : s_kb;
+        s_n = over ? next_n : s_n;
+        s_m = over ? next_m : s_m;
+        const int kb = min(s_kb, a.KB - 1);
+        we[to] = a.ws[(int64_t)(min(s_n + wn * TN * 32, a.N - 1) >> 7) * a.KB + kb];
 #pragma unroll
-    for (int t = 0; t < TM; ++t) xs[t] = a.xs + (int64_t)min(mine_m + 32 * t + c, a.M - 1) * a.KB;
+        for (int t = 0; t < TM; ++t) xe[to][t] = a.xs[(int64_t)min(s_m + (wm * TM + t) * 32 + c, a.M - 1) * a.KB + kb];
+        ++s_kb;
+    };
     f32x16 sum[TM][TN];
+    // a lane's 32 bytes of a row: chunks 2 h and the next
+    const uint8_t* mine[2];
 #pragma unroll
-    for (int t = 0; t < TM; ++t)
-#pragma unroll
-        for (int n = 0; n < TN; ++n)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) sum[t][n][e] = 0.0f;
-    int we = 0, xe[TM] = {}, we_next = 0, xe_next[TM] = {};
-    const auto scales = [&](int kb) {
-        we_next = ws[kb];
-#pragma unroll
-        for (int t = 0; t < TM; ++t) xe_next[t] = xs[t][kb];
-    };
-    // a lane's 32 bytes of a row at depths 64 s: chunks 4 s + 2 h and the next
-    const auto frag = [&](int first, int s) {
-        const int row = first + c;
+    for (int i = 0; i < 2; ++i) mine[i] = lds + c * 64 + 16 * ((2 * h + i) ^ (c >> 2 & 3));
+    const auto frag = [&](int row) {
         union { i32x8 v; i32x4 q[2]; } r;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) r.q[i] = *(const i32x4*)(lds + row * 128 + 16 * ((4 * s + 2 * h + i) ^ turn(row)));
+        for (int i = 0; i < 2; ++i) r.q[i] = *(const i32x4*)(mine[i] + row * 64);
         return r.v;
     };
     const auto products = [&](int buffer) {
-        const int base = buffer * Shape::ROWS;
+        const int first = buffer * Shape::ROWS;
+        i32x8 wf[TN];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            i32x8 wf[TN];
-#pragma unroll
-            for (int n = 0; n < TN; ++n) wf[n] = frag(base + wn * TN * 32 + 32 * n, s);
-            if constexpr (FAST) {
-#pragma unroll
-                for (int t = 0; t < TM; ++t) {
-                    const i32x8 xf = frag(base + Shape::BN + wm * TM * 32 + 32 * t, s);
-#pragma unroll
-                    for (int n = 0; n < TN; ++n) sum[t][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[n], xf, sum[t][n], 0, 0, 0, we, 0, xe[t]);
-                }
-            } else {
-                // (the tokens take both scales: a product whose scale passes 2^119 is out of their range)
-                bf16x8 wv[TN][4];
-#pragma unroll
-                for (int n = 0; n < TN; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) wv[n][i] = widened(wf[n][2 * i], wf[n][2 * i + 1]);
-#pragma unroll
-                for (int t = 0; t < TM; ++t) {
-                    const i32x8 xf = frag(base + Shape::BN + wm * TM * 32 + 32 * t, s);
-                    const float f = __builtin_ldexpf(1.0f, we + xe[t] - 254);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const bf16x8 xv = widened(xf[2 * i], xf[2 * i + 1], f);
-#pragma unroll
-                        for (int n = 0; n < TN; ++n) sum[t][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv[n][i], xv, sum[t][n], 0, 0, 0);
-                    }
-                }
-            }
-        }
+        for (int n = 0; n < TN; ++n) wf[n] = frag(first + (wn * TN + n) * 32);
         if constexpr (FAST) {
+#pragma unroll
+            for (int t = 0; t < TM; ++t) {
+                const i32x8 xf = frag(first + Shape::BN + (wm * TM + t) * 32);
+#pragma unroll
+                for (int n = 0; n < TN; ++n) sum[t][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[n], xf, sum[t][n], 0, 0, 0, we[0], 0, xe[0][t]);
+            }
             // the next fragments are read under this one's products
             __builtin_amdgcn_sched_group_barrier(0x100, 2 * TN + 2, 0);
 #pragma unroll
-            for (int i = 0; i < 2 * TM; ++i) {
-                if (i % TM < TM - 1) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-                else if (i < TM) __builtin_amdgcn_sched_group_barrier(0x100, 2 * TN + 2, 0);
+            for (int t = 0; t < TM; ++t) {
+                if (t < TM - 1) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
                 __builtin_amdgcn_sched_group_barrier(0x008, TN, 0);
             }
+        } else {
+            // (the tokens take both scales: a product whose scale passes 2^119 is out of their range)
+            bf16x8 wv[TN][4];
+#pragma unroll
+            for (int n = 0; n < TN; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) wv[n][i] = widened(wf[n][2 * i], wf[n][2 * i + 1]);
+#pragma unroll
+            for (int t = 0; t < TM; ++t) {
+                const i32x8 xf = frag(first + Shape::BN + (wm * TM + t) * 32);
+                const float f = __builtin_ldexpf(1.0f, we[0] + xe[0][t] - 254);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bf16x8 xv = widened(xf[2 * i], xf[2 * i + 1], f);
+#pragma unroll
+                    for (int n = 0; n < TN; ++n) sum[t][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv[n][i], xv, sum[t][n], 0, 0, 0);
+                }
+            }
         }
     };
-    const auto take = [&]() {
-        we = we_next;
-#pragma unroll
-        for (int t = 0; t < TM; ++t) xe[t] = xe_next[t];
+    // A stage: its loads have come (others' behind the barrier), then the loads of a later one go out.  At least so many loads of this wavefront
+    // are younger than the stage's: two stages and a block's scales, in whatever order a step between two fences has them.
+    constexpr int YOUNGER = 2 * N + TM;
+    int buffer = 0;
+    const auto arrived = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (DIRECT) {
+            loads_left<YOUNGER>();
+            bare_barrier();
+        } else {
+            __syncthreads();
+            put((buffer + 1) % STAGES);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        fetch();
+    };
+    const auto step = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
     };
     if (a.KB > 0) {
-        fetch(0, 0);
         scales(0);
-        arrive(0);
-        __syncthreads();
-        // (without a branch in the loop: the compiler moves products over one, behind the wait for the next block)
-        for (int kb = 1; kb < a.KB; ++kb) {
-            const int buffer = kb & 1;
-            take();
-            fetch(kb, buffer);
-            scales(kb);
-            __builtin_amdgcn_sched_barrier(0);           // (the loads stay in front)
-            products(buffer ^ 1);
-            __builtin_amdgcn_sched_barrier(0);
-            arrive(buffer);
-            __syncthreads();
-        }
-        take();
-        products((a.KB & 1) ^ 1);
+        step();
+        fetch();
+        step();
+        if constexpr (!DIRECT) put(0);
+        fetch();
+        step();
+        scales(1);
+        step();
+        if constexpr (DIRECT) fetch();
     }
+    for (int id = blockIdx.x; id < total; id += gridDim.x) {
 #pragma unroll
-    for (int t = 0; t < TM; ++t) {
-        const int m = mine_m + 32 * t + c;
-        if (m >= a.M) continue;
-        T* y = (T*)a.y + m * a.y_m;
+        for (int t = 0; t < TM; ++t)
 #pragma unroll
-        for (int n = 0; n < TN; ++n)
+            for (int n = 0; n < TN; ++n)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int at = mine_n + 32 * n + 8 * q + 4 * h;
-                const float o[4] = {sum[t][n][4 * q], sum[t][n][4 * q + 1], sum[t][n][4 * q + 2], sum[t][n][4 * q + 3]};
-                store_row4(y + at, a.N - at, a.vec, o);
+                for (int e = 0; e < 16; ++e) sum[t][n][e] = 0.0f;
+        for (int kb = 0; kb < blocks && a.KB > 0; ++kb) {
+            arrived();
+            scales(2);
+            step();                                      // (the loads stay in front)
+            products(buffer);
+            buffer = (buffer + 1) % STAGES;
+            arrived();
+            step();
+            products(buffer);
+            buffer = (buffer + 1) % STAGES;
+            we[0] = we[1]; we[1] = we[2];
+#pragma unroll
+            for (int t = 0; t < TM; ++t) { xe[0][t] = xe[1][t]; xe[1][t] = xe[2][t]; }
+        }
+        const int out_n = n0 + wn * TN * 32, out_m = m0 + wm * TM * 32;
+        n0 = next_n;
+        m0 = next_m;
+        look(id + 2 * gridDim.x);
+        // 32 tokens by as many results as 4 KB hold, a row of 16-byte chunks turned by the token
+        constexpr int WIDE = Shape::OUT / 32 / (int)sizeof(T) < TN * 32 ? Shape::OUT / 32 / (int)sizeof(T) : TN * 32, E = 16 / (int)sizeof(T), CH = WIDE / E;
+        T* out = (T*)(lds + STAGES * Shape::ROWS * 64 + w * Shape::OUT);
+        const bool whole = a.vec && a.y_m % E == 0;
+#pragma unroll
+        for (int t = 0; t < TM; ++t)
+#pragma unroll
+            for (int n = 0; n < TN * 32; n += WIDE) {
+#pragma unroll
+                for (int q = 0; q < WIDE / 8; ++q) {
+                    const int at = 8 * q + 4 * h, e = 4 * (q & 3);
+                    const f32x16& s = sum[t][n / 32 + q / 4];
+                    const float o[4] = {s[e], s[e + 1], s[e + 2], s[e + 3]};
+                    store_vec<4>(out + c * WIDE + ((at / E) ^ (c & (CH - 1))) * E + at % E, o);
+                }
+                wave_lds_fence();
+#pragma unroll
+                for (int i = 0; i < 32 * CH / 64; ++i) {
+                    const int row = (i * 64 + l) / CH, at = (i * 64 + l) % CH, m = out_m + 32 * t + row, have = a.N - out_n - n - at * E;
+                    const i32x4 v = *(const i32x4*)(out + row * WIDE + (at ^ (row & (CH - 1))) * E);
+                    if (m >= a.M) continue;
+                    T* y = (T*)a.y + m * a.y_m + out_n + n + at * E;
+                    if (whole && have >= E) *(i32x4*)y = v;
+                    else {
+                        union { i32x4 v; T e[E]; } r;
+                        r.v = v;
+#pragma unroll
+                        for (int j = 0; j < E; ++j) if (j < have) y[j] = r.e[j];
+                    }
+                }
+                wave_lds_fence();
             }
     }
+    if constexpr (DIRECT) loads_left<0>();               // (of stages behind the last: none outlives its workgroup's LDS)
 }
 
 template <typename T, bool DIRECT, int WM, int WN, int TM, int TN>
-int tile_launch(const LinArgs& a, hipStream_t stream)
+int ring_launch(const LinArgs& a, int most, hipStream_t stream)
 {
-    typedef TileShape<WM, WN, TM, TN> Shape;
+    typedef RingShape<WM, WN, TM, TN> Shape;
     const int64_t tiles_m = ((int64_t)a.M + Shape::BM - 1) / Shape::BM, tiles_n = ((int64_t)a.N + Shape::BN - 1) / Shape::BN;
     if (!grid_fits(tiles_m * tiles_n, Shape::THREADS)) return SCONV_EUNSUPPORTED;
-    const auto kern = linear_tile<T, sizeof(T) == 2, DIRECT, WM, WN, TM, TN>;
-    if (Shape::LDS > 64 * 1024 &&
-        hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::LDS) != hipSuccess)
-        return SCONV_ELAUNCH;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n)), dim3(Shape::THREADS), Shape::LDS, stream, a, (int)tiles_m, (int)tiles_n);
+    const auto kern = linear_ring<T, sizeof(T) == 2, DIRECT, WM, WN, TM, TN>;
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::LDS) != hipSuccess) return SCONV_ELAUNCH;
+    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>(tiles_m * tiles_n, most)), dim3(Shape::THREADS), Shape::LDS, stream, a, (int)tiles_m, (int)tiles_n);
     return launch_status();
 }
 
@@ -340,8 +418,8 @@ int linear_run(const LinArgs& a, hipStream_t stream)
     // (a tile has to lie within what a buffer's offsets reach)
     const bool direct = (a.K | a.x_m | a.w_n) % 16 == 0 && aligned_to(a.x, 16) && aligned_to(a.w, 16) && a.x_m < (int64_t(1) << 22) && a.w_n < (int64_t(1) << 22);
     const int64_t big = (((int64_t)a.M + 255) / 256) * (((int64_t)a.N + 255) / 256);
-    if (direct && big >= 256) return tile_launch<T, true, 2, 4, 4, 2>(a, stream);
-    return direct ? tile_launch<T, true, 2, 2, 2, 2>(a, stream) : tile_launch<T, false, 2, 2, 2, 2>(a, stream);
+    if (direct && big >= 256) return ring_launch<T, true, 2, 4, 4, 2>(a, 256, stream);
+    return direct ? ring_launch<T, true, 2, 2, 2, 2>(a, 512, stream) : ring_launch<T, false, 2, 2, 2, 2>(a, 512, stream);
 }
 
 }  // namespace

@@ -104,10 +104,10 @@ __device__ __forceinline__ u32x4 load16_any(const uint8_t* row, int d, int have)
     typedef u32x4 any __attribute__((aligned(1)));
     if constexpr (FULL) return *(const any*)(row + d);
     if (have >= 16) return *(const any*)(row + min(d, have - 16));
-    union { u32x4 u; uint8_t e[16]; } r;
+    u32x4 r = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) r.e[i] = d + i < have ? row[d + i] : 0;
-    return r.u;
+    for (int i = 0; i < 16; ++i) if (d + i < have) r[i >> 2] |= (uint32_t)row[d + i] << (8 * (i & 3));
+    return r;
 }
 template <bool FULL, typename T>
 __device__ __forceinline__ u32x4 load16_any(const T* row, int d, int have)

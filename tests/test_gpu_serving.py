@@ -225,18 +225,22 @@ def operands(M, N, K, g):
 
 
 LINEAR = [(1, 1, 1), (1, 16, 128), (2, 17, 129), (16, 1000, 256), (17, 64, 1024), (33, 130, 383), (64, 2048, 2048), (65, 128, 128), (65, 1, 1), (100, 129, 200), (128, 256, 512),
-          (200, 1000, 896), (257, 300, 1040), (300, 136, 4096), (1000, 520, 640), (784, 1024, 384), (4100, 4099, 400), (4096, 4096, 256)]
+          (200, 1000, 896), (257, 300, 1040), (300, 136, 4096), (1000, 520, 640), (784, 1024, 384), (4100, 4099, 400), (4096, 4096, 256),
+          (2304, 9000, 144), (5000, 4300, 64), (9000, 9000, 80)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 @pytest.mark.parametrize("M,N,K", LINEAR)
 def test_linear8(device, M, N, K, dtype):
     (xq, xs), (wq, ws) = operands(M, N, K, gen(M, N, K))
-    want, bound = ref.linear8(ref.held(xq, xs), ref.held(wq, ws, 128), dtype, dtype == BF16 and M > 64)
+    want, bound = ref.linear8(ref.held(xq, xs), ref.held(wq, ws, 128), dtype, (xs, ws) if dtype == BF16 and M > 64 else None)
     x, w = (xq.to(device), xs.to(device)), (wq.to(device), ws.to(device))
     y = sconv.sconv_linear8(x, w, out_dtype=dtype)
     assert y.dtype == dtype
     within(y, want, bound, "y")
+    # what is cut off has the products' random signs: of the whole it is far less than the bound of each (2^-13 of the largest of eight, a product)
+    if M * N > 1000:
+        assert (y.cpu().double() - want).norm() <= (U[dtype] + (2.0 ** -11 if dtype == BF16 else (K + 16) * E)) * want.norm()
     assert torch.equal(y, sconv.sconv_linear8(x, w, out_dtype=dtype))
     # rows at no aligned address; the result is the same but for what another kernel's order of sums does
     odd = [(spread_rows(q.view(torch.uint8), device).view(E4M3), s.to(device)) for q, s in ((xq, xs), (wq, ws))]
@@ -284,7 +288,7 @@ def test_linear8_of_far_scales(device, M):
     """Blocks of the smallest and largest scales that are made, whose product has an ordinary size."""
     (xq, xs), (wq, ws) = operands(M, 20, 256, gen(8, M))
     xs[:, 0], ws[:, 0], xs[:, 1], ws[:, 1] = 1, 247, 240, 10
-    want, bound = ref.linear8(ref.held(xq, xs), ref.held(wq, ws, 128), F32, False)
+    want, bound = ref.linear8(ref.held(xq, xs), ref.held(wq, ws, 128), F32)
     within(sconv.sconv_linear8((xq.to(device), xs.to(device)), (wq.to(device), ws.to(device)), out_dtype=F32), want, bound, "y")
 
 
@@ -578,7 +582,7 @@ def test_a_step_against_its_definition(device):
     within(total, wt, 2 * E * bt.abs(), "total")
     n = sconv.sconv_rmsnorm_forward(o, out_dtype=BF16)[0].view(6, -1).cpu()
     qn, sn = ref.quant8(n)
-    wy, by = ref.linear8(ref.held(torch.from_numpy(qn), torch.from_numpy(sn)), ref.held(*s["w_out"], 128), BF16, False)
+    wy, by = ref.linear8(ref.held(torch.from_numpy(qn), torch.from_numpy(sn)), ref.held(*s["w_out"], 128), BF16)
     within(y, wy, by, "y")
 
 
