@@ -10,6 +10,7 @@
 // Layout of the products: weights are A, tokens are B, so that a lane's results are neighbours of one token's row.  Which depths of a block a
 // lane holds does not matter, as long as both operands have the same.
 #include <algorithm>
+#include <type_traits>
 
 #include "sconv_serving_common.h"
 
@@ -125,9 +126,9 @@ __global__ __launch_bounds__(64 * NW) void linear_few(LinArgs a)
     }
 }
 
-// Many rows.  WM x WN wavefronts, each 32 TM tokens by 32 TN weight rows, walk tiles of their own, and every tile's depth in stages of 64, which
-// pass through a ring of four buffers in LDS: three stages' loads are under way beneath one's products, also across the end of a tile,
-// whose results go out meanwhile.  (Two buffers of 128 wait for the memory's latency at every block: 12544 x 2048 to 8192 317 us.)
+// Many rows.  WM x WN wavefronts, each 32 TM tokens by 32 TN weight rows, walk the depth in stages of 64, which pass through a ring of four
+// buffers in LDS: beneath a stage's products three later ones' loads are under way and the next one's fragments go to registers, so that no
+// product waits for memory.  (Two buffers of 128 wait for it at every block: 12544 x 2048 to 8192 317 us.)
 // A row of a stage is four chunks of 16 bytes, which stand at chunk ^ turn(row), so that lanes that read one chunk of 16 consecutive rows meet
 // different banks.  DIRECT: chunks go from memory to LDS without registers (rows at whole chunks); a chunk behind a row's end is asked
 // for behind the buffer's and comes as zeros.  Results are turned in LDS, so that a token's are written in whole lines.
@@ -140,12 +141,12 @@ struct RingShape {
     static constexpr size_t LDS = (size_t)STAGES * ROWS * 64 + WAVES * OUT;
 };
 
-// vmcnt(n), nothing of the other counters
+// vmcnt(n) lgkmcnt(0): all loads but the n youngest have come, and all reads of LDS
 template <int n>
 __device__ __forceinline__ void loads_left()
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __builtin_amdgcn_s_waitcnt(0x0f70 | (n & 15) | (n >> 4) << 14);
+    __builtin_amdgcn_s_waitcnt(0x0070 | (n & 15) | (n >> 4) << 14);
 #endif
 }
 // A barrier that waits for none of this wavefront's loads (a fence would, for those to LDS).
@@ -157,7 +158,7 @@ __device__ __forceinline__ void bare_barrier()
 }
 
 template <typename T, bool FAST, bool DIRECT, int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void linear_ring(LinArgs a, int tiles_m, int tiles_n)
+__global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring(LinArgs a, int tiles_m, int tiles_n)
 {
     typedef RingShape<WM, WN, TM, TN> Shape;
     constexpr int N = Shape::N, WAVES = Shape::WAVES, NWL = Shape::BN / 16 / WAVES, STAGES = Shape::STAGES;
@@ -185,68 +186,57 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void linear_ring(LinArgs a, int ti
     const auto slot = [&](int i, int buffer) {           // in bytes, of a load's first row
         return (buffer * Shape::ROWS + (i < NWL ? 0 : Shape::BN) + ((i < NWL ? i : i - NWL) * WAVES + w) * 16) * 64;
     };
-    // Which stage is loaded next and whose scales: of this tile or already of the next one (a tile has four stages at least, the last
-    // of which may lie behind the depth: zeros).  Without branches: the compiler moves products over one, behind the wait for the next stage.
-    const int blocks = max(a.KB, 2), stages = 2 * blocks;
-    int n0, m0, next_n = 0, next_m = 0;
-    bool next_live;
-    const auto look = [&](int id) {
-        next_live = id < total;
-        if (next_live) place(id, next_n, next_m);
-    };
+    int n0, m0;
     place(blockIdx.x, n0, m0);
-    look(blockIdx.x + gridDim.x);
-    int f_stage = 0, f_buffer = 0, f_n = n0, f_m = m0, s_kb = 0, s_n = n0, s_m = m0;
-    bool f_live = true;
-    const auto fetch = [&]() {
-        const bool over = f_stage == stages;
-        f_stage = over ? 0 : f_stage;
-        f_n = over ? next_n : f_n;
-        f_m = over ? next_m : f_m;
-        f_live = over ? next_live : f_live;
-        const int k = f_stage * 64, left = f_live ? a.K - k : 0;
+    int f_buffer = 0, left = a.K, s_kb = 0;              // of the stage to be loaded: its buffer, the depth from it on; the block whose scales are
+    [[maybe_unused]] const uint32_t size_w = (uint32_t)((min(a.N - n0, Shape::BN) - 1) * a.w_n), size_x = (uint32_t)((min(a.M - m0, Shape::BM) - 1) * a.x_m);
+    const uint8_t* from_w = a.w + n0 * a.w_n;
+    const uint8_t* from_x = a.x + m0 * a.x_m;
+    // (buffers end with the tile's last row's last byte: rows behind it, and a stage behind the depth, come as zeros)
+    const auto load = [&](int i) __attribute__((always_inline)) {
         if constexpr (DIRECT) {
 #if defined(__HIP_DEVICE_COMPILE__)
             typedef __attribute__((address_space(3))) void lds_t;
-            // (buffers end with the operand's last row's last byte: rows behind it come as zeros)
-            const auto buffer_of = [&](const uint8_t* base, int64_t stride, int first, int rows) {
-                const int64_t size = (int64_t)(rows - first - 1) * stride + left, most = (int64_t)1 << 31;
-                const uint64_t at = (uint64_t)(base + first * stride + k);
-                const uint64_t p = ((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
-                return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, __builtin_amdgcn_readfirstlane((uint32_t)(left <= 0 ? 0 : size < most ? size : most)), 0x00027000);
-            };
-            const auto wb = buffer_of(a.w, a.w_n, f_n, a.N), xb = buffer_of(a.x, a.x_m, f_m, a.M);
-            const bool behind = 16 * chunk >= left;
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(i < NWL ? wb : xb, (lds_t*)(lds + slot(i, f_buffer)), 16, behind ? 0x80000000u : off[i], 0, 0, 0);
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(i < NWL ? from_w : from_x), 0, (i < NWL ? size_w : size_x) + max(left, 0), 0x00027000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_t*)(lds + slot(i, f_buffer)), 16, 16 * chunk >= left ? 0x80000000u : off[i], 0, 0, 0);
 #endif
         } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const uint8_t* p = i < NWL ? a.w + (int64_t)min(f_n + row_of(i), a.N - 1) * a.w_n : a.x + (int64_t)min(f_m + row_of(i), a.M - 1) * a.x_m;
-                held[i] = bytes16(p + k + 16 * chunk, left - 16 * chunk);
-            }
+            const uint8_t* p = i < NWL ? from_w + min(row_of(i), a.N - 1 - n0) * a.w_n : from_x + min(row_of(i), a.M - 1 - m0) * a.x_m;
+            held[i] = bytes16(p + 16 * chunk, left - 16 * chunk);
         }
+    };
+    const auto loaded = [&]() {
         f_buffer = (f_buffer + 1) % STAGES;
-        ++f_stage;
+        left -= 64;
+        from_w += 64;
+        from_x += 64;
+    };
+    const auto fetch = [&]() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) load(i);
+        loaded();
     };
     const auto put = [&](int buffer) {
         if constexpr (!DIRECT)
 #pragma unroll
             for (int i = 0; i < N; ++i) *(i32x4*)(lds + slot(i, buffer) + 16 * l) = held[i];
     };
-    int we[3] = {}, xe[3][TM] = {};
-    const auto scales = [&](int to) {
-        const bool over = s_kb == blocks;
-        s_kb = over ? 0 : s_kb;
-        s_n = over ? next_n : s_n;
-        s_m = over ? next_m : s_m;
-        const int kb = min(s_kb, a.KB - 1);
-        we[to] = a.ws[(int64_t)(min(s_n + wn * TN * 32, a.N - 1) >> 7) * a.KB + kb];
+    int we = 0, xe[TM] = {}, we_next = 0, xe_next[TM] = {};
+    const uint8_t* ws = a.ws + (int64_t)(min(n0 + wn * TN * 32, a.N - 1) >> 7) * a.KB;
+    const uint8_t* xs[TM];
 #pragma unroll
-        for (int t = 0; t < TM; ++t) xe[to][t] = a.xs[(int64_t)min(s_m + (wm * TM + t) * 32 + c, a.M - 1) * a.KB + kb];
+    for (int t = 0; t < TM; ++t) xs[t] = a.xs + (int64_t)min(m0 + (wm * TM + t) * 32 + c, a.M - 1) * a.KB;
+    const auto load_scales = [&]() {
+        const int kb = min(s_kb, a.KB - 1);
+        we_next = ws[kb];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) xe_next[t] = xs[t][kb];
         ++s_kb;
+    };
+    const auto take_scales = [&]() {
+        we = we_next;
+#pragma unroll
+        for (int t = 0; t < TM; ++t) xe[t] = xe_next[t];
     };
     f32x16 sum[TM][TN];
     // a lane's 32 bytes of a row: chunks 2 h and the next
@@ -259,147 +249,153 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void linear_ring(LinArgs a, int ti
         for (int i = 0; i < 2; ++i) r.q[i] = *(const i32x4*)(mine[i] + row * 64);
         return r.v;
     };
-    const auto products = [&](int buffer) {
+    struct Frags { i32x8 w[TN], x[TM]; };
+    static_assert(TM == TN && N % TM == 0, "loads, reads and products in TM equal steps");
+    const auto read = [&](Frags& f, int buffer, int t) __attribute__((always_inline)) {
         const int first = buffer * Shape::ROWS;
-        i32x8 wf[TN];
-#pragma unroll
-        for (int n = 0; n < TN; ++n) wf[n] = frag(first + (wn * TN + n) * 32);
+        f.w[t] = frag(first + (wn * TN + t) * 32);
+        f.x[t] = frag(first + Shape::BN + (wm * TM + t) * 32);
+    };
+    const auto multiply = [&](const Frags& f, int t) {
         if constexpr (FAST) {
 #pragma unroll
-            for (int t = 0; t < TM; ++t) {
-                const i32x8 xf = frag(first + Shape::BN + (wm * TM + t) * 32);
-#pragma unroll
-                for (int n = 0; n < TN; ++n) sum[t][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[n], xf, sum[t][n], 0, 0, 0, we[0], 0, xe[0][t]);
-            }
-            // the next fragments are read under this one's products
-            __builtin_amdgcn_sched_group_barrier(0x100, 2 * TN + 2, 0);
-#pragma unroll
-            for (int t = 0; t < TM; ++t) {
-                if (t < TM - 1) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, TN, 0);
-            }
+            for (int n = 0; n < TN; ++n) sum[t][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.w[n], f.x[t], sum[t][n], 0, 0, 0, we, 0, xe[t]);
         } else {
             // (the tokens take both scales: a product whose scale passes 2^119 is out of their range)
-            bf16x8 wv[TN][4];
+            const float e = __builtin_ldexpf(1.0f, we + xe[t] - 254);
 #pragma unroll
-            for (int n = 0; n < TN; ++n)
+            for (int i = 0; i < 4; ++i) {
+                const bf16x8 xv = widened(f.x[t][2 * i], f.x[t][2 * i + 1], e);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) wv[n][i] = widened(wf[n][2 * i], wf[n][2 * i + 1]);
-#pragma unroll
-            for (int t = 0; t < TM; ++t) {
-                const i32x8 xf = frag(first + Shape::BN + (wm * TM + t) * 32);
-                const float f = __builtin_ldexpf(1.0f, we[0] + xe[0][t] - 254);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bf16x8 xv = widened(xf[2 * i], xf[2 * i + 1], f);
-#pragma unroll
-                    for (int n = 0; n < TN; ++n) sum[t][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv[n][i], xv, sum[t][n], 0, 0, 0);
-                }
+                for (int n = 0; n < TN; ++n)
+                    sum[t][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widened(f.w[n][2 * i], f.w[n][2 * i + 1]), xv, sum[t][n], 0, 0, 0);
             }
         }
     };
-    // A stage: its loads have come (others' behind the barrier), then the loads of a later one go out.  At least so many loads of this wavefront
-    // are younger than the stage's: two stages and a block's scales, in whatever order a step between two fences has them.
-    constexpr int YOUNGER = 2 * N + TM;
-    int buffer = 0;
-    const auto arrived = [&]() {
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (DIRECT) {
-            loads_left<YOUNGER>();
-            bare_barrier();
-        } else {
-            __syncthreads();
-            put((buffer + 1) % STAGES);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        fetch();
-    };
+    // Where stage i is multiplied, stage i + 1 is read into registers and stage i + 4 asked for, into the buffer that stage i has left.  arrived: stage
+    // i + 1's loads have come (others' behind the barrier).  At least so many loads of this wavefront are younger than that stage's: two stages
+    // and a block's scales, in whatever order a step between two fences has them.
+    constexpr std::integral_constant<int, 2 * N + TM> YOUNGER;
+    int buffer = 0;                                      // of stage i
     const auto step = [&]() {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    if (a.KB > 0) {
-        scales(0);
+    const auto arrived = [&](auto younger) {
         step();
-        fetch();
-        step();
-        if constexpr (!DIRECT) put(0);
-        fetch();
-        step();
-        scales(1);
-        step();
-        if constexpr (DIRECT) fetch();
-    }
-    for (int id = blockIdx.x; id < total; id += gridDim.x) {
-#pragma unroll
-        for (int t = 0; t < TM; ++t)
-#pragma unroll
-            for (int n = 0; n < TN; ++n)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) sum[t][n][e] = 0.0f;
-        for (int kb = 0; kb < blocks && a.KB > 0; ++kb) {
-            arrived();
-            scales(2);
-            step();                                      // (the loads stay in front)
-            products(buffer);
-            buffer = (buffer + 1) % STAGES;
-            arrived();
-            step();
-            products(buffer);
-            buffer = (buffer + 1) % STAGES;
-            we[0] = we[1]; we[1] = we[2];
-#pragma unroll
-            for (int t = 0; t < TM; ++t) { xe[0][t] = xe[1][t]; xe[1][t] = xe[2][t]; }
+        if constexpr (DIRECT) {
+            loads_left<decltype(younger)::value>();
+            bare_barrier();
+        } else {
+            __syncthreads();
         }
-        const int out_n = n0 + wn * TN * 32, out_m = m0 + wm * TM * 32;
-        n0 = next_n;
-        m0 = next_m;
-        look(id + 2 * gridDim.x);
-        // 32 tokens by as many results as 4 KB hold, a row of 16-byte chunks turned by the token
-        constexpr int WIDE = Shape::OUT / 32 / (int)sizeof(T) < TN * 32 ? Shape::OUT / 32 / (int)sizeof(T) : TN * 32, E = 16 / (int)sizeof(T), CH = WIDE / E;
-        T* out = (T*)(lds + STAGES * Shape::ROWS * 64 + w * Shape::OUT);
-        const bool whole = a.vec && a.y_m % E == 0;
+        step();
+    };
+    // A stage's products; between them the next one's fragments are read and a later one's loads go out, a few at a time (all at once they hold
+    // up the wavefront that issues them).  FIRST of a block: the next block's scales are asked for in front of the loads, so that taking
+    // them waits for nothing younger than the next stage.
+    const auto multiply_stage = [&](const Frags& now, Frags& next, auto first) {
+        constexpr bool FIRST = decltype(first)::value;
+        if constexpr (!DIRECT) put((buffer + 2) % STAGES);
+        const int following = (buffer + 1) % STAGES;
 #pragma unroll
-        for (int t = 0; t < TM; ++t)
+        for (int t = 0; t < TM; ++t) {
+            if (FIRST && t == 0) load_scales();
 #pragma unroll
-            for (int n = 0; n < TN * 32; n += WIDE) {
+            for (int i = FIRST ? max(t - 1, 0) * N / (TM - 1) : t * N / TM; i < (FIRST ? t * N / (TM - 1) : (t + 1) * N / TM); ++i) load(i);
+            read(next, following, t);
+            multiply(now, t);
+            if constexpr (FAST && DIRECT) {
 #pragma unroll
-                for (int q = 0; q < WIDE / 8; ++q) {
-                    const int at = 8 * q + 4 * h, e = 4 * (q & 3);
-                    const f32x16& s = sum[t][n / 32 + q / 4];
-                    const float o[4] = {s[e], s[e + 1], s[e + 2], s[e + 3]};
-                    store_vec<4>(out + c * WIDE + ((at / E) ^ (c & (CH - 1))) * E + at % E, o);
+                for (int n = 0; n < TN; ++n) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    if (n < TN / 2) __builtin_amdgcn_sched_group_barrier(0x010, FIRST ? 4 : 2 * N / TM / TN + 1, 0);
+                    else __builtin_amdgcn_sched_group_barrier(0x100, 8 / TN, 0);
                 }
-                wave_lds_fence();
-#pragma unroll
-                for (int i = 0; i < 32 * CH / 64; ++i) {
-                    const int row = (i * 64 + l) / CH, at = (i * 64 + l) % CH, m = out_m + 32 * t + row, have = a.N - out_n - n - at * E;
-                    const i32x4 v = *(const i32x4*)(out + row * WIDE + (at ^ (row & (CH - 1))) * E);
-                    if (m >= a.M) continue;
-                    T* y = (T*)a.y + m * a.y_m + out_n + n + at * E;
-                    if (whole && have >= E) *(i32x4*)y = v;
-                    else {
-                        union { i32x4 v; T e[E]; } r;
-                        r.v = v;
-#pragma unroll
-                        for (int j = 0; j < E; ++j) if (j < have) y[j] = r.e[j];
-                    }
-                }
-                wave_lds_fence();
             }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        loaded();
+        buffer = following;
+    };
+    Frags even, odd;
+    if (a.KB > 0) {
+        load_scales();
+        step();
+#pragma unroll
+        for (int i = 0; i < (DIRECT ? 4 : 3); ++i) {
+            fetch();
+            if (!DIRECT && i < 2) put(i);
+            step();
+        }
+        take_scales();
+        arrived(std::integral_constant<int, 2 * N>());   // (of both first stages: behind the second there are no scales yet)
+#pragma unroll
+        for (int t = 0; t < TM; ++t) read(even, 0, t);
     }
+#pragma unroll
+    for (int t = 0; t < TM; ++t)
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum[t][n][e] = 0.0f;
+    for (int kb = 0; kb < a.KB; ++kb) {
+        arrived(YOUNGER);
+        multiply_stage(even, odd, std::true_type());
+        arrived(YOUNGER);
+        multiply_stage(odd, even, std::false_type());
+        take_scales();
+        // (18 wait states are what the longest product needs: seen in another kernel, the compiler counts too few where a result's first
+        // reader stands behind a loop's exit)
+        step();
+        asm volatile("s_nop 15\n\ts_nop 3");
+        step();
+    }
+    const int out_n = n0 + wn * TN * 32, out_m = m0 + wm * TM * 32;
+    // 32 tokens by as many results as 4 KB hold, a row of 16-byte chunks turned by the token
+    constexpr int WIDE = Shape::OUT / 32 / (int)sizeof(T) < TN * 32 ? Shape::OUT / 32 / (int)sizeof(T) : TN * 32, E = 16 / (int)sizeof(T), CH = WIDE / E;
+    T* out = (T*)(lds + STAGES * Shape::ROWS * 64 + w * Shape::OUT);
+    const bool whole = a.vec && a.y_m % E == 0;
+#pragma unroll
+    for (int t = 0; t < TM; ++t)
+#pragma unroll
+        for (int n = 0; n < TN * 32; n += WIDE) {
+#pragma unroll
+            for (int q = 0; q < WIDE / 8; ++q) {
+                const int at = 8 * q + 4 * h, e = 4 * (q & 3);
+                const f32x16& s = sum[t][n / 32 + q / 4];
+                const float o[4] = {s[e], s[e + 1], s[e + 2], s[e + 3]};
+                store_vec<4>(out + c * WIDE + ((at / E) ^ (c & (CH - 1))) * E + at % E, o);
+            }
+            wave_lds_fence();
+#pragma unroll
+            for (int i = 0; i < 32 * CH / 64; ++i) {
+                const int row = (i * 64 + l) / CH, at = (i * 64 + l) % CH, m = out_m + 32 * t + row, have = a.N - out_n - n - at * E;
+                const i32x4 v = *(const i32x4*)(out + row * WIDE + (at ^ (row & (CH - 1))) * E);
+                if (m >= a.M) continue;
+                T* y = (T*)a.y + m * a.y_m + out_n + n + at * E;
+                if (whole && have >= E) *(i32x4*)y = v;
+                else {
+                    union { i32x4 v; T e[E]; } r;
+                    r.v = v;
+#pragma unroll
+                    for (int j = 0; j < E; ++j) if (j < have) y[j] = r.e[j];
+                }
+            }
+            wave_lds_fence();
+        }
     if constexpr (DIRECT) loads_left<0>();               // (of stages behind the last: none outlives its workgroup's LDS)
 }
 
 template <typename T, bool DIRECT, int WM, int WN, int TM, int TN>
-int ring_launch(const LinArgs& a, int most, hipStream_t stream)
+int ring_launch(const LinArgs& a, hipStream_t stream)
 {
     typedef RingShape<WM, WN, TM, TN> Shape;
     const int64_t tiles_m = ((int64_t)a.M + Shape::BM - 1) / Shape::BM, tiles_n = ((int64_t)a.N + Shape::BN - 1) / Shape::BN;
     if (!grid_fits(tiles_m * tiles_n, Shape::THREADS)) return SCONV_EUNSUPPORTED;
     const auto kern = linear_ring<T, sizeof(T) == 2, DIRECT, WM, WN, TM, TN>;
     if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::LDS) != hipSuccess) return SCONV_ELAUNCH;
-    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>(tiles_m * tiles_n, most)), dim3(Shape::THREADS), Shape::LDS, stream, a, (int)tiles_m, (int)tiles_n);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n)), dim3(Shape::THREADS), Shape::LDS, stream, a, (int)tiles_m, (int)tiles_n);
     return launch_status();
 }
 
@@ -418,8 +414,8 @@ int linear_run(const LinArgs& a, hipStream_t stream)
     // (a tile has to lie within what a buffer's offsets reach)
     const bool direct = (a.K | a.x_m | a.w_n) % 16 == 0 && aligned_to(a.x, 16) && aligned_to(a.w, 16) && a.x_m < (int64_t(1) << 22) && a.w_n < (int64_t(1) << 22);
     const int64_t big = (((int64_t)a.M + 255) / 256) * (((int64_t)a.N + 255) / 256);
-    if (direct && big >= 256) return ring_launch<T, true, 2, 4, 4, 2>(a, 256, stream);
-    return direct ? ring_launch<T, true, 2, 2, 2, 2>(a, 512, stream) : ring_launch<T, false, 2, 2, 2, 2>(a, 512, stream);
+    if (direct && big >= 256) return ring_launch<T, true, 2, 2, 4, 4>(a, stream);
+    return direct ? ring_launch<T, true, 2, 2, 2, 2>(a, stream) : ring_launch<T, false, 2, 2, 2, 2>(a, stream);
 }
 
 }  // namespace
