@@ -10,7 +10,6 @@
 // Layout of the products: weights are A, tokens are B, so that a lane's results are neighbours of one token's row.  Which depths of a block a
 // lane holds does not matter, as long as both operands have the same.
 #include <algorithm>
-#include <type_traits>
 
 #include "sconv_serving_common.h"
 
@@ -137,8 +136,10 @@ struct RingShape {
     static constexpr int BM = WM * TM * 32, BN = WN * TN * 32, WAVES = WM * WN, THREADS = 64 * WAVES, STAGES = 4;
     static constexpr int ROWS = BN + BM, N = ROWS / 16 / WAVES;          // rows of a buffer (weights, then tokens), its loads by one wavefront
     static_assert(N * WAVES * 16 == ROWS && BN % (16 * WAVES) == 0, "whole loads of one operand each");
-    static constexpr int OUT = 4096;                                     // of a wavefront's results on their way out
-    static constexpr size_t LDS = (size_t)STAGES * ROWS * 64 + WAVES * OUT;
+    static constexpr int OUT = 4096;                                     // of a wavefront's results on their way out, in the ring
+    static constexpr int RING = STAGES * ROWS * 64, CHUNK = 120;         // blocks whose scales are in LDS: of the tokens, then of the weights
+    static_assert(WAVES * OUT <= RING, "results go out through the ring");
+    static constexpr size_t LDS = (size_t)RING + CHUNK * (BM + BN / 128);
 };
 
 // vmcnt(n) lgkmcnt(0): all loads but the n youngest have come, and all reads of LDS
@@ -188,7 +189,7 @@ __global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring
     };
     int n0, m0;
     place(blockIdx.x, n0, m0);
-    int f_buffer = 0, left = a.K, s_kb = 0;              // of the stage to be loaded: its buffer, the depth from it on; the block whose scales are
+    int f_buffer = 0, left = a.K;                        // of the stage to be loaded: its buffer, the depth from it on
     [[maybe_unused]] const uint32_t size_w = (uint32_t)((min(a.N - n0, Shape::BN) - 1) * a.w_n), size_x = (uint32_t)((min(a.M - m0, Shape::BM) - 1) * a.x_m);
     const uint8_t* from_w = a.w + n0 * a.w_n;
     const uint8_t* from_x = a.x + m0 * a.x_m;
@@ -221,17 +222,31 @@ __global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring
 #pragma unroll
             for (int i = 0; i < N; ++i) *(i32x4*)(lds + slot(i, buffer) + 16 * l) = held[i];
     };
+    // The scales of a stretch of blocks, block after block, the tile's tokens beside each other: read from memory in the loop, a line for every
+    // token and block, they cost more than the operands (4096 x 8192 to 8192 284 us, without them 219).
+    uint8_t* x_scales = lds + Shape::RING;
+    uint8_t* w_scales = x_scales + Shape::CHUNK * Shape::BM;
+    const auto stretch = [&](int kb0) {
+        const int count = min(Shape::CHUNK, a.KB - kb0);
+        for (int r = threadIdx.x; r < Shape::BM; r += Shape::THREADS) {
+            const uint8_t* from = a.xs + (int64_t)min(m0 + r, a.M - 1) * a.KB + kb0;
+            for (int k = 0; k < count; k += 16) {
+                const i32x4 v = bytes16(from + k, count - k);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (k + i < count) x_scales[(k + i) * Shape::BM + r] = (uint8_t)(v[i >> 2] >> (8 * (i & 3)));
+            }
+        }
+        for (int e = threadIdx.x; e < Shape::BN / 128 * count; e += Shape::THREADS) {
+            const int n = e / count, k = e - n * count;
+            w_scales[n * Shape::CHUNK + k] = a.ws[(int64_t)min((n0 >> 7) + n, (a.N - 1) >> 7) * a.KB + kb0 + k];
+        }
+    };
     int we = 0, xe[TM] = {}, we_next = 0, xe_next[TM] = {};
-    const uint8_t* ws = a.ws + (int64_t)(min(n0 + wn * TN * 32, a.N - 1) >> 7) * a.KB;
-    const uint8_t* xs[TM];
+    const auto load_scales = [&](int k) {                // of block k of the stretch
+        we_next = w_scales[wn * TN * 32 / 128 * Shape::CHUNK + k];
 #pragma unroll
-    for (int t = 0; t < TM; ++t) xs[t] = a.xs + (int64_t)min(m0 + (wm * TM + t) * 32 + c, a.M - 1) * a.KB;
-    const auto load_scales = [&]() {
-        const int kb = min(s_kb, a.KB - 1);
-        we_next = ws[kb];
-#pragma unroll
-        for (int t = 0; t < TM; ++t) xe_next[t] = xs[t][kb];
-        ++s_kb;
+        for (int t = 0; t < TM; ++t) xe_next[t] = x_scales[k * Shape::BM + (wm * TM + t) * 32 + c];
     };
     const auto take_scales = [&]() {
         we = we_next;
@@ -273,18 +288,16 @@ __global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring
         }
     };
     // Where stage i is multiplied, stage i + 1 is read into registers and stage i + 4 asked for, into the buffer that stage i has left.  arrived: stage
-    // i + 1's loads have come (others' behind the barrier).  At least so many loads of this wavefront are younger than that stage's: two stages
-    // and a block's scales, in whatever order a step between two fences has them.
-    constexpr std::integral_constant<int, 2 * N + TM> YOUNGER;
+    // i + 1's loads have come (others' behind the barrier); those of two stages are younger.
     int buffer = 0;                                      // of stage i
     const auto step = [&]() {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    const auto arrived = [&](auto younger) {
+    const auto arrived = [&]() {
         step();
         if constexpr (DIRECT) {
-            loads_left<decltype(younger)::value>();
+            loads_left<2 * N>();
             bare_barrier();
         } else {
             __syncthreads();
@@ -292,24 +305,22 @@ __global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring
         step();
     };
     // A stage's products; between them the next one's fragments are read and a later one's loads go out, a few at a time (all at once they hold
-    // up the wavefront that issues them).  FIRST of a block: the next block's scales are asked for in front of the loads, so that taking
-    // them waits for nothing younger than the next stage.
-    const auto multiply_stage = [&](const Frags& now, Frags& next, auto first) {
-        constexpr bool FIRST = decltype(first)::value;
+    // up the wavefront that issues them).  ahead: the block whose scales are read, or -1.
+    const auto multiply_stage = [&](const Frags& now, Frags& next, int ahead) {
         if constexpr (!DIRECT) put((buffer + 2) % STAGES);
         const int following = (buffer + 1) % STAGES;
 #pragma unroll
         for (int t = 0; t < TM; ++t) {
-            if (FIRST && t == 0) load_scales();
 #pragma unroll
-            for (int i = FIRST ? max(t - 1, 0) * N / (TM - 1) : t * N / TM; i < (FIRST ? t * N / (TM - 1) : (t + 1) * N / TM); ++i) load(i);
+            for (int i = 0; i < N / TM; ++i) load(t * (N / TM) + i);
             read(next, following, t);
+            if (t == TM - 1 && ahead >= 0) load_scales(ahead);
             multiply(now, t);
             if constexpr (FAST && DIRECT) {
 #pragma unroll
                 for (int n = 0; n < TN; ++n) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    if (n < TN / 2) __builtin_amdgcn_sched_group_barrier(0x010, FIRST ? 4 : 2 * N / TM / TN + 1, 0);
+                    if (n < TN / 2) __builtin_amdgcn_sched_group_barrier(0x010, 2 * N / TM / TN, 0);
                     else __builtin_amdgcn_sched_group_barrier(0x100, 8 / TN, 0);
                 }
             }
@@ -320,18 +331,12 @@ __global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring
     };
     Frags even, odd;
     if (a.KB > 0) {
-        load_scales();
-        step();
 #pragma unroll
         for (int i = 0; i < (DIRECT ? 4 : 3); ++i) {
             fetch();
             if (!DIRECT && i < 2) put(i);
             step();
         }
-        take_scales();
-        arrived(std::integral_constant<int, 2 * N>());   // (of both first stages: behind the second there are no scales yet)
-#pragma unroll
-        for (int t = 0; t < TM; ++t) read(even, 0, t);
     }
 #pragma unroll
     for (int t = 0; t < TM; ++t)
@@ -339,22 +344,40 @@ __global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring
         for (int n = 0; n < TN; ++n)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sum[t][n][e] = 0.0f;
-    for (int kb = 0; kb < a.KB; ++kb) {
-        arrived(YOUNGER);
-        multiply_stage(even, odd, std::true_type());
-        arrived(YOUNGER);
-        multiply_stage(odd, even, std::false_type());
+    for (int kb0 = 0; kb0 < a.KB; kb0 += Shape::CHUNK) {
+        if (kb0) __syncthreads();
+        stretch(kb0);
+        if constexpr (DIRECT) loads_left<2 * N>();       // (of the first stage, at the start)
+        __syncthreads();
+        load_scales(0);
         take_scales();
-        // (18 wait states are what the longest product needs: seen in another kernel, the compiler counts too few where a result's first
-        // reader stands behind a loop's exit)
-        step();
-        asm volatile("s_nop 15\n\ts_nop 3");
-        step();
+        if (kb0 == 0) {
+#pragma unroll
+            for (int t = 0; t < TM; ++t) read(even, 0, t);
+        }
+        const int count = min(Shape::CHUNK, a.KB - kb0);
+        for (int k = 0; k < count; ++k) {
+            arrived();
+            multiply_stage(even, odd, min(k + 1, count - 1));
+            arrived();
+            multiply_stage(odd, even, -1);
+            take_scales();
+            // (18 wait states are what the longest product needs: seen in another kernel, the compiler counts too few where a result's first
+            // reader stands behind a loop's exit)
+            step();
+            asm volatile("s_nop 15\n\ts_nop 3");
+            step();
+        }
     }
+    // (stages behind the last have been asked for: none outlives its workgroup's LDS, or meets the results in it)
+    step();
+    if constexpr (DIRECT) loads_left<0>();
+    __syncthreads();
+    step();
     const int out_n = n0 + wn * TN * 32, out_m = m0 + wm * TM * 32;
     // 32 tokens by as many results as 4 KB hold, a row of 16-byte chunks turned by the token
     constexpr int WIDE = Shape::OUT / 32 / (int)sizeof(T) < TN * 32 ? Shape::OUT / 32 / (int)sizeof(T) : TN * 32, E = 16 / (int)sizeof(T), CH = WIDE / E;
-    T* out = (T*)(lds + STAGES * Shape::ROWS * 64 + w * Shape::OUT);
+    T* out = (T*)(lds + w * Shape::OUT);
     const bool whole = a.vec && a.y_m % E == 0;
 #pragma unroll
     for (int t = 0; t < TM; ++t)
@@ -384,7 +407,6 @@ __global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring
             }
             wave_lds_fence();
         }
-    if constexpr (DIRECT) loads_left<0>();               // (of stages behind the last: none outlives its workgroup's LDS)
 }
 
 template <typename T, bool DIRECT, int WM, int WN, int TM, int TN>

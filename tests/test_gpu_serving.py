@@ -226,7 +226,7 @@ def operands(M, N, K, g):
 
 LINEAR = [(1, 1, 1), (1, 16, 128), (2, 17, 129), (16, 1000, 256), (17, 64, 1024), (33, 130, 383), (64, 2048, 2048), (65, 128, 128), (65, 1, 1), (100, 129, 200), (128, 256, 512),
           (200, 1000, 896), (257, 300, 1040), (300, 136, 4096), (1000, 520, 640), (784, 1024, 384), (4100, 4099, 400), (4096, 4096, 256),
-          (2304, 9000, 144), (5000, 4300, 64), (9000, 9000, 80)]
+          (2304, 9000, 144), (5000, 4300, 64), (9000, 9000, 80), (70, 130, 15500), (66, 40, 31000)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
