@@ -1,11 +1,11 @@
 // Product of 8-bit operands with block scales (formula in sconv_serving.h).
 //
-// Few rows (up to 64, single tokens): bound by the weights' read.  A workgroup takes 16 weight rows, its wavefronts share out the blocks of
-// 128, read weights from memory straight into the product's registers and meet in LDS.  The 8-bit values become 16-bit ones, exactly, a
-// block's product is exact to 32 bits and takes its scale as it joins the sum.
-// Many rows: tiles through LDS.  16-bit results take 8-bit products with the scales as operands; the matrix pipe takes eight products at a
-// time and cuts off what lies 2^-13 or more below the largest of them (measured: 1.4e-5 of a result's norm, at any depth), which rounding to
-// 16 bits hides.  32-bit results take 16-bit products of the converted values, as few rows do.
+// Few rows (up to 64, single tokens): bound by the weights' read, and by what every workgroup reads of the tokens.  A workgroup takes 16 or 32 weight
+// rows, its eight wavefronts share out the blocks of 128, read operands from memory straight into the product's registers and meet in LDS.
+// Many rows: tiles through LDS.
+// Up to 16 rows, and in 32-bit results, the 8-bit values become 16-bit ones, exactly, and products are exact to 32 bits.  16-bit results of more
+// rows take 8-bit products with the scales as operands; the matrix pipe takes eight products at a time and cuts off what lies 2^-13 or more
+// below the largest of them (measured: 1.4e-5 of a result's norm, at any depth), which rounding to 16 bits hides.
 //
 // Layout of the products: weights are A, tokens are B, so that a lane's results are neighbours of one token's row.  Which depths of a block a
 // lane holds does not matter, as long as both operands have the same.
@@ -58,68 +58,101 @@ __device__ __forceinline__ void store_row4(T* p, int have, bool vec, const float
     for (int i = 0; i < 4; ++i) if (i < have) p[i] = (T)v[i];
 }
 
-// Few rows: MT tiles of 16 tokens, NW wavefronts.  A lane has 32 bytes (l / 16) * 32.. of row l % 16 of both operands.
-template <typename T, int MT, int NW>
+// Few rows: MT tiles of 16 tokens against NT tiles of 16 weight rows, NW wavefronts.  A lane has 32 bytes (l / 16) * 32.. of row l % 16 of both
+// operands.  FAST: 8-bit products with their scales; otherwise 16-bit ones of the converted values.
+template <typename T, bool FAST, int MT, int NT, int NW>
 __global__ __launch_bounds__(64 * NW) void linear_few(LinArgs a)
 {
-    __shared__ f32x4 part[NW][MT][64];
-    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, h = l >> 4, n0 = blockIdx.x * 16;
-    const uint8_t* wr = a.w + (int64_t)min(n0 + c, a.N - 1) * a.w_n + 32 * h;
-    const uint8_t* ws = a.ws + (int64_t)(n0 >> 7) * a.KB;
+    __shared__ f32x4 part[NW][MT * NT][64];
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, h = l >> 4, n0 = blockIdx.x * 16 * NT;
+    const uint8_t* wr[NT];
+    const uint8_t* ws = a.ws + (int64_t)(n0 >> 7) * a.KB;          // (NT tiles lie within 128 rows)
     const uint8_t* xr[MT];
     const uint8_t* xs[MT];
-    f32x4 sum[MT];
+    f32x4 sum[MT][NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) wr[n] = a.w + (int64_t)min(n0 + 16 * n + c, a.N - 1) * a.w_n + 32 * h;
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         const int m = min(16 * t + c, a.M - 1);
         xr[t] = a.x + m * a.x_m + 32 * h;
         xs[t] = a.xs + (int64_t)m * a.KB;
-        sum[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sum[t][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    i32x4 wv[2], xv[MT][2];
-    int we, xe[MT];
+    union Raw32 { i32x4 q[2]; i32x8 v; };
+    Raw32 wv[NT], xv[MT];
+    int we = 0, xe[MT] = {};
     const auto fetch = [&](int kb) {
         const int k = kb * 128, have = a.K - k - 32 * h;
-        wv[0] = bytes16(wr + k, have);
-        wv[1] = bytes16(wr + k + 16, have - 16);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            wv[n].q[0] = bytes16(wr[n] + k, have);
+            wv[n].q[1] = bytes16(wr[n] + k + 16, have - 16);
+        }
         we = ws[kb];
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-            xv[t][0] = bytes16(xr[t] + k, have);
-            xv[t][1] = bytes16(xr[t] + k + 16, have - 16);
+            xv[t].q[0] = bytes16(xr[t] + k, have);
+            xv[t].q[1] = bytes16(xr[t] + k + 16, have - 16);
             xe[t] = xs[t][kb];
         }
     };
     if (w < a.KB) fetch(w);
     for (int kb = w; kb < a.KB; kb += NW) {
-        bf16x8 wf[4], xf[MT][4];
-        int e[MT];
+        const bool more = kb + NW < a.KB;
+        if constexpr (FAST) {
+            Raw32 wn[NT], xn[MT];
+            int en[MT];
+            const int wen = we;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) wf[s] = widened(wv[s >> 1][2 * (s & 1)], wv[s >> 1][2 * (s & 1) + 1]);
+            for (int n = 0; n < NT; ++n) wn[n] = wv[n];
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            e[t] = we + xe[t] - 254;
+            for (int t = 0; t < MT; ++t) { xn[t] = xv[t]; en[t] = xe[t]; }
+            if (more) fetch(kb + NW);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) xf[t][s] = widened(xv[t][s >> 1][2 * (s & 1)], xv[t][s >> 1][2 * (s & 1) + 1]);
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) sum[t][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wn[n].v, xn[t].v, sum[t][n], 0, 0, 0, wen, 0, en[t]);
+        } else {
+            bf16x8 wf[NT][4], xf[MT][4];
+            int e[MT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) wf[n][s] = widened(wv[n].v[2 * s], wv[n].v[2 * s + 1]);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                e[t] = we + xe[t] - 254;
+#pragma unroll
+                for (int s = 0; s < 4; ++s) xf[t][s] = widened(xv[t].v[2 * s], xv[t].v[2 * s + 1]);
+            }
+            if (more) fetch(kb + NW);
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[n][s], xf[t][s], p, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[t][n][i] += __builtin_ldexpf(p[i], e[t]);
+                }
         }
-        if (kb + NW < a.KB) fetch(kb + NW);
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int s = 0; s < 4; ++s) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[s], xf[t][s], p, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[t][i] += __builtin_ldexpf(p[i], e[t]);
-        }
+        // (18 wait states are what the longest product needs: seen in another kernel, the compiler counts too few where a result's first
+        // reader stands behind a loop's exit)
+        asm volatile("s_nop 15\n\ts_nop 3");
     }
 #pragma unroll
-    for (int t = 0; t < MT; ++t) part[w][t][l] = sum[t];
-    __syncthreads();
-    for (int t = w; t < MT; t += NW) {
-        f32x4 v = part[0][t][l];
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int i = 1; i < NW; ++i) v += part[i][t][l];
-        const int m = 16 * t + c, n = n0 + 4 * h;
+        for (int n = 0; n < NT; ++n) part[w][t * NT + n][l] = sum[t][n];
+    __syncthreads();
+    for (int i = w; i < MT * NT; i += NW) {
+        f32x4 v = part[0][i][l];
+#pragma unroll
+        for (int k = 1; k < NW; ++k) v += part[k][i][l];
+        const int m = 16 * (i / NT) + c, n = n0 + 16 * (i % NT) + 4 * h;
         const float o[4] = {v[0], v[1], v[2], v[3]};
         if (m < a.M) store_row4((T*)a.y + m * a.y_m + n, a.N - n, a.vec, o);
     }
@@ -421,18 +454,26 @@ int ring_launch(const LinArgs& a, hipStream_t stream)
     return launch_status();
 }
 
+template <typename T, bool FAST, int MT, int NT, int NW>
+int few_launch(const LinArgs& a, hipStream_t stream)
+{
+    const int64_t grid = ((int64_t)a.N + 16 * NT - 1) / (16 * NT);
+    if (!grid_fits(grid, 64 * NW)) return SCONV_EUNSUPPORTED;
+    hipLaunchKernelGGL((linear_few<T, FAST, MT, NT, NW>), dim3((unsigned)grid), dim3(64 * NW), 0, stream, a);
+    return launch_status();
+}
+
 template <typename T>
 int linear_run(const LinArgs& a, hipStream_t stream)
 {
-    if (a.M <= 64) {
-        const int64_t grid = ((int64_t)a.N + 15) / 16;
-        if (!grid_fits(grid, 512)) return SCONV_EUNSUPPORTED;
-        const dim3 blocks((unsigned)grid), threads(512);
-        if (a.M <= 16) hipLaunchKernelGGL((linear_few<T, 1, 8>), blocks, threads, 0, stream, a);
-        else if (a.M <= 32) hipLaunchKernelGGL((linear_few<T, 2, 8>), blocks, threads, 0, stream, a);
-        else hipLaunchKernelGGL((linear_few<T, 4, 8>), blocks, threads, 0, stream, a);
-        return launch_status();
-    }
+    constexpr bool FAST = sizeof(T) == 2;
+    // Two weight tiles a workgroup share what it reads of the tokens, where one fills the chip twice (16 tokens, 2048 to 8192: 7.7 -> 6.4 us, 64 tokens
+    // 15.3 -> 9.8); with fewer rows they leave compute units idle (2048 to 2048, 16 tokens: 5.0 -> 5.9).  Tiles through LDS take over where
+    // they are ahead by and large: at 64 tokens 2048 to 8192 11.7 us against 9.8, 1024 to 16384 9.0 against 11.6, 8192 to 8192 47 against 34.
+    const bool two = a.N >= 4096;
+    if (a.M <= 16) return two ? few_launch<T, false, 1, 2, 8>(a, stream) : few_launch<T, false, 1, 1, 8>(a, stream);
+    if (a.M <= 32) return two ? few_launch<T, FAST, 2, 2, 8>(a, stream) : few_launch<T, FAST, 2, 1, 8>(a, stream);
+    if (a.M <= 64) return two ? few_launch<T, FAST, 4, 2, 8>(a, stream) : few_launch<T, FAST, 4, 1, 8>(a, stream);
     // (a tile has to lie within what a buffer's offsets reach)
     const bool direct = (a.K | a.x_m | a.w_n) % 16 == 0 && aligned_to(a.x, 16) && aligned_to(a.w, 16) && a.x_m < (int64_t(1) << 22) && a.w_n < (int64_t(1) << 22);
     const int64_t big = (((int64_t)a.M + 255) / 256) * (((int64_t)a.N + 255) / 256);
