@@ -1,13 +1,14 @@
 // Differential attention of new tokens over a paged cache (formulas in sconv_tokens.h, the cache in sconv_serving.h).
 //
-// Bound by the cache's read.  The keys of all requests, laid end to end in units of 32, are shared out among workgroups by their number, so
-// that workgroups are alike whatever the requests' lengths: a workgroup walks its stretch, request after request; a request that
-// lies within one is answered there, others leave parts, which a second kernel joins.  Where every request begins follows from the lengths, which
-// each workgroup adds up itself.
-// Within a stretch a wavefront walks units of its own, alone: keys go from memory to registers as the product reads them, values
-// through LDS of its own (to be read down the keys), the next unit's on their way under this one's products.  8-bit values become 16-bit ones with
-// their scale as they come, which is exact.  Scores are formed transposed - keys down, queries across -, so a softmax stays within a lane's
-// quarter and the weights never leave the registers.  Weights go as two 16-bit values for their product with V (three pieces in 32 bits).
+// Bound by the cache's read.  The keys of all requests, laid end to end in units of 32, are shared out among wavefronts by their number, so
+// that wavefronts are alike whatever the requests' lengths: each walks its stretch alone, request after request, without barriers; a request
+// that lies within one stretch is answered there, others leave parts, which a second kernel joins.  Where every request begins follows from the
+// lengths, which each wavefront adds up itself.
+// DIRECT (heads as wide as the tile, 16-byte rows, pages of whole 16 slots): keys, values and their scales go from memory to LDS without
+// registers, two units deep.  Otherwise keys go to registers as the product reads them and values through registers to LDS (to be read down
+// the keys), the next unit's on their way under this one's products.  8-bit values become 16-bit ones, exactly, on their way to
+// the products.  Scores are formed transposed - keys down, queries across -, so a softmax stays within a lane's quarter and the weights never
+// leave the registers.  Weights go as two 16-bit values for their product with V (three pieces in 32 bits).
 #include <algorithm>
 
 #include "sconv_diffattn_common.h"
@@ -17,9 +18,9 @@ namespace sconv {
 
 namespace {
 
-constexpr int NW = 4, BN = 32;           // wavefronts of a workgroup, keys of a unit
-constexpr int LEAST = 8;                 // units of a stretch at least: two of every wavefront
-constexpr int MAX_PARTS = 1024;
+constexpr int BN = 32;                   // keys of a unit
+constexpr int LEAST = 2;                 // units of a stretch at least
+constexpr int MAX_PARTS = 2048;
 
 struct PagedArgs {
     const void* q; const void* k; const void* v; const uint8_t* kx; const uint8_t* vx; const int32_t* table; const float* lam;
@@ -181,22 +182,81 @@ template <> struct Weights<float> {
     template <typename V> __device__ __forceinline__ f32x4 times(f32x4 c, const V& v) const { return mma(c, v, p); }
 };
 
-// T: queries and results; P: the pages.  FULL: heads are DT and values whole DVT wide.  ALIGNED: a page is whole 16 slots, so that half a
-// unit lies on one page.  RT: tiles of 16 rows.
-template <typename T, typename P, bool FULL, bool ALIGNED, int DT, int DVT, int RT>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)) void paged_attn(PagedArgs a)
+// Units in LDS (DIRECT).  A key's two rows stand beside each other, RK bytes, a value's RV; their 16-byte chunks stand at chunk ^ turn, so that
+// the lanes that are served together meet different banks: 16 keys' rows of one chunk, and in the transposing read 8 (8 bits: 16) values' rows
+// of one or two.  Behind them the dwords that hold the scales of every key (both maps) and value.
+template <typename P, int DT, int DVT>
+struct Unit {
+    static constexpr int ES = sizeof(P), RK = 2 * DT * ES, RV = DVT * ES, CK = RK / 16, CV = RV / 16;
+    static constexpr int K = BN * RK, V = BN * RV, SCALES = ES == 1 ? 256 : 0;       // bytes; SCALES: twice
+    static constexpr int NK = K / 1024, NV = V / 1024, HK = NK / 2, HV = NV / 2;     // loads of a unit and of half of it
+    static constexpr int KLOADS = NK + (ES == 1), VLOADS = NV + (ES == 1);
+    static constexpr int SIZE = K + V + 2 * SCALES, STAGES = 2, LDS = STAGES * SIZE + (ES == 1 ? 3 * BN * 4 : 0);
+    __device__ __forceinline__ static int turn_k(int key) { return RK >= 256 ? key & 15 : key / (256 / RK) & (CK - 1); }
+    __device__ __forceinline__ static int turn_v(int key)
+    {
+        if (ES == 1) return RV == 128 ? (key >> 1 & 3) | (key >> 4 & 1) << 2 : (key >> 2 & 1) | (key >> 4 & 1) << 1;
+        return RV == 256 ? (key & 7) << 1 : (key >> 1 & 3) << 1;
+    }
+};
+
+// vmcnt(n): all but the n youngest of the wavefront's loads have come
+template <int n>
+__device__ __forceinline__ void loads_left()
+{
+    asm volatile("" ::: "memory");
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (n & 15) | (n >> 4) << 14);
+#endif
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+// Four reads of eight bytes a lane out of LDS, of which 16 lanes each take a tile turned: `b8` eight rows of 16 bytes' columns, else four rows of
+// 16 two-byte columns.  They wait for themselves only: the compiler's would wait for every load to LDS under way.
+template <bool b8, int apart>
+__device__ __forceinline__ void columns(u32x2 (&r)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (b8)
+        asm volatile("ds_read_b64_tr_b8 %0, %4\n\tds_read_b64_tr_b8 %1, %5\n\tds_read_b64_tr_b8 %2, %6\n\tds_read_b64_tr_b8 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]) : "v"(a0), "v"(a1), "v"(a2), "v"(a3) : "memory");
+    else
+        asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %4 offset:%6\n\tds_read_b64_tr_b16 %2, %5\n\tds_read_b64_tr_b16 %3, %5 offset:%6\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]) : "v"(a0), "v"(a2), "n"(apart) : "memory");
+#endif
+}
+__device__ __forceinline__ uint32_t lds_at(const void* p)
+{
+    typedef __attribute__((address_space(3))) const void lds_t;
+    return (uint32_t)(uintptr_t)(lds_t*)p;
+}
+__device__ __forceinline__ void load_to_lds(const void* from, uint8_t* to, bool dword)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef __attribute__((address_space(3))) void lds_t;
+    typedef __attribute__((address_space(1))) const void mem_t;
+    if (dword) __builtin_amdgcn_global_load_lds((mem_t*)from, (lds_t*)to, 4, 0, 0);
+    else __builtin_amdgcn_global_load_lds((mem_t*)from, (lds_t*)to, 16, 0, 0);
+#endif
+}
+
+// T: queries and results; P: the pages.  FULL: heads are DT and values whole DVT wide.  DIRECT: half a unit lies on one page, too.  RT: tiles of
+// 16 rows.
+template <typename T, typename P, bool FULL, bool DIRECT, int DT, int DVT, int RT>
+__global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)) void paged_attn(PagedArgs a)
 {
     typedef typename Kept<P>::type KT;
     typedef Tile<KT, BN, DVT> Values;
-    constexpr int KS = DT / 32, NT = DVT / 16, E = 16 / sizeof(P);
+    typedef Unit<P, DT, DVT> U;
+    static_assert(!DIRECT || (FULL && sizeof(P) <= 2), "whole rows of whole pages");
+    constexpr int KS = DT / 32, NT = DVT / 16, E = 16 / sizeof(P), SC = sizeof(P) == 1;
     constexpr int NV = BN * DVT / E / 64, VPER = DVT / E;        // 16-byte vectors of a lane's and a row's share of the values
     extern __shared__ __attribute__((aligned(16))) char lds[];
 
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, h = l >> 4;
+    const int l = threadIdx.x, c = l & 15, h = l >> 4;
     const int per_head = a.parts ? a.parts : a.B;
     const int at = blockIdx.x % per_head, rest = blockIdx.x / per_head, hk = rest % a.Hkv, first = rest / a.Hkv * 16 * RT;
     const int dv0 = blockIdx.z * DVT, dvn = min(DVT, a.Dv - dv0), wide = (a.Dv + 3) / 4 * 4;
-    bf16* vt = (bf16*)lds + w * Values::SIZE;
 
     int b, begin, end;                                           // the request, the stretch in units from its first
     if (a.parts) {
@@ -214,7 +274,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
     }
 
     for (;; ++b) {
-        const int n = positions(a, b), units = units_of(n);
+        const int n = __builtin_amdgcn_readfirstlane(positions(a, b)), units = units_of(n);
         if (a.parts && units == 0) continue;
         const int u1 = min(end, units);
         int lim[RT];
@@ -246,25 +306,33 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
         const P* vb = (const P*)a.v + (int64_t)hk * a.v_h + dv0;
         const uint8_t* kxb = a.kx + (int64_t)hk * 2 * a.kx_h;
         const uint8_t* vxb = a.vx + (int64_t)hk * a.vx_h;
-        RawKey<P, KS> kr[2][2];                                  // [16 keys][map]
-        uint8_t ke[2][2] = {}, ve[NV] = {};
-        u32x4 vr[NV];
-        uint32_t there = 0, there_next = 0;                      // keys of the unit that are there, as bits
-        // the pages of a unit's halves (ALIGNED) or of key l % 32
-        int page[2], slot[2];
-        const auto look = [&](int u) {
-            const int j0 = u * BN;
+        const int32_t* table = a.table + b * a.table_b;
+        // Where a unit's keys are, in three steps of an iteration each: its pages are asked for, found, read from.  DIRECT: the pages of its two
+        // halves, for the whole wavefront, and rows lie at 32-bit offsets from the halves' first; otherwise the page of key l % 32.
+        typedef __attribute__((address_space(4))) const int32_t scalar_t;
+        int entry[2] = {};
+        int64_t page[2];
+        int slot[2];
+        uint32_t there_next = 0;                                 // keys of the unit that are there, as bits
+        const auto ask = [&](int u) {
+#pragma unroll
+            for (int y = 0; y < (DIRECT ? 2 : 1); ++y) {
+                const int j = DIRECT ? u * BN + 16 * y : u * BN + (l & 31);
+                const int at = min((int)divided((uint32_t)j, a.page), a.width - 1);
+                if constexpr (DIRECT) entry[y] = ((scalar_t*)table)[at];         // (no kernel writes it while this one runs)
+                else entry[y] = table[at];
+            }
+        };
+        const auto find = [&](int u) {
             there_next = 0;
 #pragma unroll
-            for (int y = 0; y < (ALIGNED ? 2 : 1); ++y) {
-                const int j = ALIGNED ? j0 + 16 * y : j0 + (l & 31);
-                const int e = (int)divided((uint32_t)j, a.page);
-                int p = a.table[b * a.table_b + min(e, a.width - 1)];
-                slot[y] = j - e * (int)a.page.d;
+            for (int y = 0; y < (DIRECT ? 2 : 1); ++y) {
+                const int j = DIRECT ? u * BN + 16 * y : u * BN + (l & 31);
+                const int p = entry[y];
                 const bool ok = j < n && p >= 0 && p < a.pages;
-                if (!ok) p = slot[y] = 0;
-                page[y] = p;
-                if constexpr (ALIGNED) {
+                page[y] = ok ? p : 0;
+                slot[y] = ok ? j - (int)(divided((uint32_t)j, a.page) * a.page.d) : 0;
+                if constexpr (DIRECT) {
                     const int left = n - j;
                     if (ok) there_next |= (left >= 16 ? 0xffffu : (1u << left) - 1u) << (16 * y);
                 } else {
@@ -272,69 +340,87 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
                 }
             }
         };
+        // through registers
+        RawKey<P, KS> kr[2][2];                                  // [16 keys][map]
+        uint8_t ke[2][2] = {}, ve[NV] = {};
+        u32x4 vr[NV];
         const auto fetch_keys = [&]() {
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const int p = ALIGNED ? page[y] : __shfl(page[0], 16 * y + c), s = ALIGNED ? slot[y] + c : __shfl(slot[0], 16 * y + c);
-                const P* row = kb + p * a.k_p + s * a.k_s;
+                const int64_t p = __shfl((int)page[0], 16 * y + c), s = __shfl(slot[0], 16 * y + c);
+                const P* row = kb + (p * a.k_p + s * a.k_s);
+                const uint8_t* x = SC ? kxb + (p * a.kx_p + s * a.kx_s) : nullptr;
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
                     load_key<FULL>(kr[y][m], row + m * a.k_h, h, a.D);
-                    if constexpr (sizeof(P) == 1) ke[y][m] = kxb[p * a.kx_p + s * a.kx_s + m * a.kx_h];
+                    if constexpr (SC) ke[y][m] = x[m * a.kx_h];
                 }
             }
         };
         const auto fetch_values = [&]() {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int e = v * 64 + l, row = e / VPER, y = v * (64 / VPER) / 16;
-                const int p = ALIGNED ? page[y] : __shfl(page[0], row), s = ALIGNED ? slot[y] + (row & 15) : __shfl(slot[0], row);
-                if constexpr (sizeof(P) == 1) {
-                    vr[v] = load16_any<FULL>((const uint8_t*)vb + p * a.v_p + s * a.v_s, e % VPER * E, dvn);
+                const int key = v * (64 / VPER) + l / VPER, d = l % VPER * E;
+                const int64_t p = __shfl((int)page[0], key), s = __shfl(slot[0], key);
+                const P* row = vb + (p * a.v_p + s * a.v_s);
+                if constexpr (SC) {
+                    vr[v] = load16_any<FULL>((const uint8_t*)row, d, dvn);
                     ve[v] = vxb[p * a.vx_p + s * a.vx_s];
                 } else {
-                    vr[v] = load16_any<FULL>(vb + p * a.v_p + s * a.v_s, e % VPER * E, dvn);
+                    vr[v] = load16_any<FULL>(row, d, dvn);
                 }
             }
         };
-        int u = begin + w;
-        if (u < u1) { look(u); fetch_keys(); fetch_values(); }
-        for (; u < u1; u += NW) {
-            const int j0 = u * BN;
-            const bool more = u + NW < u1;
-            there = there_next;
-            if (more) look(u + NW);
-            f32x4 s[RT][2][2];                                   // [rows][map][16 keys]
+        // straight to LDS: a load is 1024 bytes in a row; each lane chooses the chunk of memory that belongs where its 16 bytes come to lie
+        uint32_t k_off[DIRECT ? U::HK : 1], v_off[DIRECT ? 2 : 1][DIRECT ? U::HV : 1];
+        float* scales = (float*)(lds + U::STAGES * U::SIZE);     // [2 maps, values][BN]
+        uint32_t there_of[2] = {}, low_k[2] = {}, low_v[2] = {};   // of this unit and the next: what is there, the low bits of its scales' addresses
+        if constexpr (DIRECT) {
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-#pragma unroll
-                    for (int x = 0; x < RT; ++x) s[x][m][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int t = 0; t < KS; ++t) {
-                        const auto kf = key_frag<FULL>(kr[y][m], t, h, a.D, scale_of(ke[y][m]));
-#pragma unroll
-                        for (int x = 0; x < RT; ++x) s[x][m][y] = mma(s[x][m][y], kf, qf[x][m][t]);
-                    }
-                }
-            if (more) fetch_keys();
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int e = v * 64 + l, row = e / VPER, d = e % VPER * E;
-                const bool ok = d < dvn && (there >> row & 1);
-                bf16* to = vt + row * Values::LD + d;
-                if constexpr (sizeof(P) == 1) {
-                    const u32x4 x = shift16<FULL, uint8_t>(vr[v], d, dvn);
-                    const float f = scale_of(ve[v]);
-                    const bf16x8 zero = {}, x0 = widened(x[0], x[1], f), x1 = widened(x[2], x[3], f);
-                    *(bf16x8*)to = ok ? x0 : zero;
-                    *(bf16x8*)(to + 8) = ok ? x1 : zero;
-                } else {
-                    put16<Values::PLANE>(to, shift16<FULL, P>(vr[v], d, dvn), ok, P());
-                }
+            for (int i = 0; i < U::HK; ++i) {
+                const int key = (i * 64 + l) / U::CK, chunk = (l % U::CK) ^ U::turn_k(key), m = chunk / (U::CK / 2);
+                k_off[i] = (uint32_t)(key * a.k_s + m * a.k_h) * U::ES + chunk % (U::CK / 2) * 16;
             }
-            if (more) fetch_values();
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int i = 0; i < U::HV; ++i) {
+                    const int key = (i * 64 + l) / U::CV, chunk = (l % U::CV) ^ U::turn_v(16 * y + key);
+                    v_off[y][i] = (uint32_t)(key * a.v_s) * U::ES + chunk * 16;
+                }
+        }
+        // (a scale's dword: the four aligned bytes that its byte is one of)
+        const auto scale_load = [&](const uint8_t* base, int64_t page_stride, int64_t slot_stride, int64_t map, uint8_t* to, uint32_t& low) {
+            const int y = l >> 4 & 1;
+            const uint64_t at = (uint64_t)(base + (y ? page[1] * page_stride + slot[1] * slot_stride : page[0] * page_stride + slot[0] * slot_stride) + map + c * slot_stride);
+            low = (uint32_t)at & 3;
+            load_to_lds((const void*)(at - low), to, true);
+        };
+        const auto send_keys = [&](int stage, uint32_t& low) {
+            uint8_t* to = (uint8_t*)lds + stage * U::SIZE;
+            if constexpr (SC) scale_load(kxb, a.kx_p, a.kx_s, l >= 32 ? a.kx_h : 0, to + U::K + U::V, low);
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const char* from = (const char*)(kb + (page[y] * a.k_p + slot[y] * a.k_s));
+#pragma unroll
+                for (int i = 0; i < U::HK; ++i) load_to_lds(from + k_off[i], to + (y * U::HK + i) * 1024, false);
+            }
+        };
+        const auto send_values = [&](int stage, uint32_t& low) {
+            uint8_t* to = (uint8_t*)lds + stage * U::SIZE + U::K;
+            if constexpr (SC) scale_load(vxb, a.vx_p, a.vx_s, 0, to + U::V + U::SCALES, low);
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const char* from = (const char*)(vb + (page[y] * a.v_p + slot[y] * a.v_s));
+#pragma unroll
+                for (int i = 0; i < U::HV; ++i) load_to_lds(from + v_off[y][i], to + (y * U::HV + i) * 1024, false);
+            }
+        };
+
+        f32x4 s[RT][2][2];                                       // [rows][map][16 keys]
+        Weights<T> p[RT][2];
+        // scores of the keys that are not there, or not seen, go; then the weights, times their values' scales
+        const auto soften = [&](int j0, uint32_t there, const float (&by)[8]) {
             if (j0 + BN > least || there != ~0u) {
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
@@ -349,7 +435,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
                         }
                     }
             }
-            Weights<T> p[RT][2];
 #pragma unroll
             for (int x = 0; x < RT; ++x)
 #pragma unroll
@@ -371,132 +456,249 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1
                     for (int y = 0; y < 2; ++y)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            v[4 * y + e] = __builtin_amdgcn_exp2f(fmaf(z[y][e], a.scale2, -safe[x][m]));
-                            sum[x][m] += v[4 * y + e];
+                            const float w = __builtin_amdgcn_exp2f(fmaf(z[y][e], a.scale2, -safe[x][m]));
+                            sum[x][m] += w;
+                            v[4 * y + e] = DIRECT && SC ? w * by[4 * y + e] : w;
                         }
                     p[x][m].set(v);
                 }
-            const int vcol = few_col_lane<Values::LD>();
-            wave_lds_fence();
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const auto vf = tile_col<KT, Values::LD, Values::PLANE, 16>(vt + vcol + 16 * t);
-#pragma unroll
-                for (int x = 0; x < RT; ++x) {
-                    o[x][0][t] = p[x][0].times(o[x][0][t], vf);
-                    o[x][1][t] = p[x][1].times(o[x][1][t], vf);
+        };
+        int u = begin;
+        if constexpr (DIRECT) {
+            if (u < u1) {
+                ask(u);
+                find(u);
+                if (u + 1 < u1) ask(u + 1);
+                there_of[0] = there_next;
+                send_keys(0, low_k[0]);
+                send_values(0, low_v[0]);
+                if (u + 1 < u1) {
+                    find(u + 1);
+                    if (u + 2 < u1) ask(u + 2);
+                    there_of[1] = there_next;
+                    send_keys(1, low_k[1]);
+                    send_values(1, low_v[1]);
                 }
             }
-            wave_lds_fence();
-            settle();
+            for (int stage = 0; u < u1; ++u, stage ^= 1) {
+                const int j0 = u * BN;
+                const uint32_t there = there_of[0];
+                uint8_t* kt = (uint8_t*)lds + stage * U::SIZE;
+                uint8_t* vt = kt + U::K;
+                // younger than this unit's keys: its values, the next unit
+                if (u + 1 < u1) loads_left<U::VLOADS + U::KLOADS + U::VLOADS>();
+                else loads_left<U::VLOADS>();
+                float fk[2][2] = {};
+                if constexpr (SC) {
+                    // (lane l: map l / 32 of key l % 32)
+                    const uint32_t d = *(const uint32_t*)(vt + U::V + 4 * l), low = low_k[0];
+                    scales[l] = scale_of((int)(d >> (8 * low) & 255));
+                    wave_lds_fence();
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) fk[y][m] = scales[32 * m + 16 * y + c];
+                }
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                        for (int x = 0; x < RT; ++x) s[x][m][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                        const uint8_t* row = kt + (16 * y + c) * U::RK;
+#pragma unroll
+                        for (int t = 0; t < KS; ++t) {
+                            bf16x8 kf;
+                            if constexpr (!SC) {
+                                kf = *(const bf16x8*)(row + ((m * (U::CK / 2) + 4 * t + h) ^ U::turn_k(c)) * 16);
+                            } else if constexpr (KS == 1) {
+                                const u32x2 x = *(const u32x2*)(row + ((m * (U::CK / 2) + (h >> 1)) ^ U::turn_k(c)) * 16 + 8 * (h & 1));
+                                kf = widened(x[0], x[1], fk[y][m]);
+                            } else {
+                                // (16 bytes are two steps: depth_of)
+                                const u32x4 x = *(const u32x4*)(row + ((m * (U::CK / 2) + 4 * (t / 2) + h) ^ U::turn_k(c)) * 16);
+                                kf = widened(x[2 * (t % 2)], x[2 * (t % 2) + 1], fk[y][m]);
+                            }
+#pragma unroll
+                            for (int x = 0; x < RT; ++x) s[x][m][y] = mma(s[x][m][y], kf, qf[x][m][t]);
+                        }
+                    }
+                const bool more = u + 2 < u1;
+                uint32_t low_k_then = 0, low_v_then = 0;
+                if (more) {
+                    find(u + 2);
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (of the products' reads)
+                    send_keys(stage, low_k_then);
+                    if (u + 3 < u1) ask(u + 3);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                // younger than this unit's values: the next unit, the keys of the one after it
+                if (more) loads_left<U::KLOADS + U::VLOADS + U::KLOADS>();
+                else if (u + 1 < u1) loads_left<U::KLOADS + U::VLOADS>();
+                else loads_left<0>();
+                float fv[8] = {};
+                if constexpr (SC) {
+                    const uint32_t d = *(const uint32_t*)(vt + U::V + U::SCALES + 4 * l), low = low_v[0];
+                    // (what is not there counts as 1: nothing of it may reach a sum)
+                    const float f = there >> (l & 31) & 1 ? scale_of((int)(d >> (8 * low) & 255)) : 1.0f;
+                    if (l < 32) scales[64 + l] = f;
+                    wave_lds_fence();
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const f32x4 g = *(const f32x4*)(scales + 64 + 16 * y + 4 * h);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) fv[4 * y + e] = g[e];
+                    }
+                }
+                if (there != ~0u) {
+                    for (int e = l; e < BN * U::CV; e += 64)
+                        if (!(there >> (e / U::CV) & 1)) *(u32x4*)(vt + e * 16) = u32x4{0, 0, 0, 0};
+                    wave_lds_fence();
+                }
+                soften(j0, there, fv);
+                // 8 bits: 16 lanes take eight keys of 16 columns, lane i the columns' half i % 2 of key i / 2 of {4 h .., 16 + 4 h ..}; 16 bits:
+                // four keys, lane i four columns of key i / 4 of {4 h ..}, then of {16 + 4 h ..}.  (a row's chunks differ in its low bits only)
+                const int r = SC ? (c >> 1 & 3) + 4 * h + (c >> 3) * 16 : 4 * h + (c >> 2);
+                const uint32_t v0 = lds_at(vt) + r * U::RV + (SC ? U::turn_v(r) * 16 + 8 * (c & 1) : (U::turn_v(r) ^ (c >> 1 & 1)) * 16 + 8 * (c & 1));
+                static_assert(U::SIZE % U::RV == 0 && U::K % U::RV == 0, "rows at whole rows' places");
+#pragma unroll
+                for (int t0 = 0; t0 < NT; t0 += SC ? 4 : 2) {
+                    u32x2 x[4];
+                    if constexpr (SC) columns<true, 0>(x, v0 ^ 16 * t0, v0 ^ 16 * (t0 + 1), v0 ^ 16 * (t0 + 2), v0 ^ 16 * (t0 + 3));
+                    else columns<false, 16 * U::RV>(x, v0 ^ 32 * t0, 0, v0 ^ 32 * (t0 + 1), 0);
+#pragma unroll
+                    for (int t = t0; t < t0 + (SC ? 4 : 2); ++t) {
+                        bf16x8 vf;
+                        if constexpr (SC) {
+                            vf = widened(x[t - t0][0], x[t - t0][1], 1.0f);
+                        } else {
+                            union { u32x2 u[2]; bf16x8 v; } y = {{x[2 * (t - t0)], x[2 * (t - t0) + 1]}};
+                            vf = y.v;
+                        }
+#pragma unroll
+                        for (int x = 0; x < RT; ++x) {
+                            o[x][0][t] = p[x][0].times(o[x][0][t], vf);
+                            o[x][1][t] = p[x][1].times(o[x][1][t], vf);
+                        }
+                    }
+                }
+                if (more) {
+                    send_values(stage, low_v_then);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                there_of[0] = there_of[1]; low_k[0] = low_k[1]; low_v[0] = low_v[1];
+                there_of[1] = there_next; low_k[1] = low_k_then; low_v[1] = low_v_then;
+                settle();
+            }
+        } else {
+            bf16* vt = (bf16*)lds;
+            const float none[8] = {};
+            if (u < u1) {
+                ask(u);
+                find(u);
+                if (u + 1 < u1) ask(u + 1);
+                fetch_keys();
+                fetch_values();
+            }
+            for (; u < u1; ++u) {
+                const bool more = u + 1 < u1;
+                const uint32_t there = there_next;
+                if (more) find(u + 1);
+                if (u + 2 < u1) ask(u + 2);
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                        for (int x = 0; x < RT; ++x) s[x][m][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int t = 0; t < KS; ++t) {
+                            const auto kf = key_frag<FULL>(kr[y][m], t, h, a.D, scale_of(ke[y][m]));
+#pragma unroll
+                            for (int x = 0; x < RT; ++x) s[x][m][y] = mma(s[x][m][y], kf, qf[x][m][t]);
+                        }
+                    }
+                if (more) fetch_keys();
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const int e = v * 64 + l, row = e / VPER, d = e % VPER * E;
+                    const bool ok = d < dvn && (there >> row & 1);
+                    bf16* to = vt + row * Values::LD + d;
+                    if constexpr (SC) {
+                        const u32x4 x = shift16<FULL, uint8_t>(vr[v], d, dvn);
+                        const float f = scale_of(ve[v]);
+                        const bf16x8 zero = {}, x0 = widened(x[0], x[1], f), x1 = widened(x[2], x[3], f);
+                        *(bf16x8*)to = ok ? x0 : zero;
+                        *(bf16x8*)(to + 8) = ok ? x1 : zero;
+                    } else {
+                        put16<Values::PLANE>(to, shift16<FULL, P>(vr[v], d, dvn), ok, P());
+                    }
+                }
+                if (more) fetch_values();
+                soften(u * BN, there, none);
+                const int vcol = few_col_lane<Values::LD>();
+                wave_lds_fence();
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const auto vf = tile_col<KT, Values::LD, Values::PLANE, 16>(vt + vcol + 16 * t);
+#pragma unroll
+                    for (int x = 0; x < RT; ++x) {
+                        o[x][0][t] = p[x][0].times(o[x][0][t], vf);
+                        o[x][1][t] = p[x][1].times(o[x][1][t], vf);
+                    }
+                }
+                wave_lds_fence();
+                settle();
+            }
         }
-        // the wavefronts' parts meet in LDS, over the tiles: statistics first, then the sums, halving the wavefronts
-        __syncthreads();
-        float* ml = (float*)lds;                                 // [NW][RT][2][2][16]
-        float* acc = ml + NW * RT * 64;                          // [NW / 2][RT * 2 * NT * 4][64]
+        const bool whole = begin == 0 && u1 == units;
 #pragma unroll
-        for (int x = 0; x < RT; ++x)
+        for (int x = 0; x < RT; ++x) {
+            const int mine = first + 16 * x + c;
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                sum[x][m] = half_sum(quarter_sum(sum[x][m]));
-                if (h == 0) {
-                    float* to = ml + ((w * RT + x) * 2 + m) * 32 + c;
-                    to[0] = top[x][m];
-                    to[16] = sum[x][m];
+            for (int m = 0; m < 2; ++m) sum[x][m] = half_sum(quarter_sum(sum[x][m]));
+            if (mine >= a.rows) continue;
+            if (whole) {
+                const int i = mine / a.G, head = hk * a.G + mine - i * a.G;
+                T* out = (T*)a.out + (((int64_t)b * a.Sq + i) * a.H + head) * a.Dv + dv0;
+                // (a query that sees nothing answers 0, whatever lam is)
+                const bool none = sum[x][1] == 0.0f;
+                const float i0 = none ? 0.0f : 1.0f / sum[x][0], i1 = none ? 0.0f : a.lam[head] / sum[x][1];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    float r[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) r[e] = none ? 0.0f : fmaf(o[x][0][t][e], i0, -o[x][1][t][e] * i1);
+                    store4(out, 16 * t + 4 * h, dvn, a.ovec, r);
                 }
-            }
-        __syncthreads();
+            } else {
+                const int64_t row = (((int64_t)hk * a.parts + at) * 2 + (begin == 0 ? 1 : 0)) * a.rows + mine;
+                if (blockIdx.z == 0 && h == 0) *(f32x4*)(a.part_ml + 4 * row) = f32x4{top[x][0], sum[x][0], top[x][1], sum[x][1]};
 #pragma unroll
-        for (int x = 0; x < RT; ++x)
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                float most = -INFINITY, all = 0.0f;
-#pragma unroll
-                for (int k = 0; k < NW; ++k) most = fmaxf(most, ml[((k * RT + x) * 2 + m) * 32 + c]);
-                const float base = most == -INFINITY ? 0.0f : most;
-#pragma unroll
-                for (int k = 0; k < NW; ++k) {
-                    const float* from = ml + ((k * RT + x) * 2 + m) * 32 + c;
-                    all = fmaf(from[16], __builtin_amdgcn_exp2f(from[0] - base), all);
-                }
-                const float f = __builtin_amdgcn_exp2f(top[x][m] - base);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) o[x][m][t] *= f;
-                top[x][m] = most;
-                sum[x][m] = all;
-            }
-#pragma unroll
-        for (int half = NW / 2; half > 0; half /= 2) {
-            if (w >= half && w < 2 * half) {
-                f32x4* to = (f32x4*)acc + (w - half) * RT * 2 * NT * 64 + l;
-#pragma unroll
-                for (int x = 0; x < RT; ++x)
-#pragma unroll
-                    for (int m = 0; m < 2; ++m)
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) to[((x * 2 + m) * NT + t) * 64] = o[x][m][t];
-            }
-            __syncthreads();
-            if (w < half) {
-                const f32x4* from = (const f32x4*)acc + w * RT * 2 * NT * 64 + l;
-#pragma unroll
-                for (int x = 0; x < RT; ++x)
-#pragma unroll
-                    for (int m = 0; m < 2; ++m)
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) o[x][m][t] += from[((x * 2 + m) * NT + t) * 64];
-            }
-            __syncthreads();
-        }
-        if (w == 0) {
-            const bool whole = begin == 0 && u1 == units;
-#pragma unroll
-            for (int x = 0; x < RT; ++x) {
-                const int mine = first + 16 * x + c;
-                if (mine >= a.rows) continue;
-                if (whole) {
-                    const int i = mine / a.G, head = hk * a.G + mine - i * a.G;
-                    T* out = (T*)a.out + (((int64_t)b * a.Sq + i) * a.H + head) * a.Dv + dv0;
-                    // (a query that sees nothing answers 0, whatever lam is)
-                    const bool none = sum[x][1] == 0.0f;
-                    const float i0 = none ? 0.0f : 1.0f / sum[x][0], i1 = none ? 0.0f : a.lam[head] / sum[x][1];
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        float r[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) r[e] = none ? 0.0f : fmaf(o[x][0][t][e], i0, -o[x][1][t][e] * i1);
-                        store4(out, 16 * t + 4 * h, dvn, a.ovec, r);
+                        const int d = 16 * t + 4 * h;
+                        if (dv0 + d < wide) *(f32x4*)(a.part + (row * 2 + m) * wide + dv0 + d) = o[x][m][t];
                     }
-                } else {
-                    const int64_t row = (((int64_t)hk * a.parts + at) * 2 + (begin == 0 ? 1 : 0)) * a.rows + mine;
-                    if (blockIdx.z == 0 && h == 0) *(f32x4*)(a.part_ml + 4 * row) = f32x4{top[x][0], sum[x][0], top[x][1], sum[x][1]};
-#pragma unroll
-                    for (int m = 0; m < 2; ++m)
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            const int d = 16 * t + 4 * h;
-                            if (dv0 + d < wide) *(f32x4*)(a.part + (row * 2 + m) * wide + dv0 + d) = o[x][m][t];
-                        }
-                }
             }
         }
         if (!a.parts || end <= units) return;
         // the next request, from its first unit on
         end -= units;
         begin = 0;
-        __syncthreads();
     }
 }
 
-// Joins a row's parts: a workgroup a row of (request, query, head), a thread a value of each map.
+// Joins a row's parts: a workgroup a row of (request, query, head); lanes along both maps' values, four at a time, groups of lanes along the parts.
 template <typename T>
 __global__ __launch_bounds__(256) void paged_join(PagedArgs a)
 {
-    __shared__ float f[2][MAX_PARTS];
-    __shared__ float total[2];
+    __shared__ float f[2][MAX_PARTS], total[2];
+    __shared__ f32x4 meet[256];
     const int64_t id = blockIdx.x;
     const int head = (int)(id % a.H), i = (int)(id / a.H % a.Sq), b = (int)(id / a.H / a.Sq);
-    const int hk = head / a.G, r = i * a.G + head % a.G, wide = (a.Dv + 3) / 4 * 4;
+    const int hk = head / a.G, r = i * a.G + head % a.G, quads = (a.Dv + 3) / 4;
     T* out = (T*)a.out + id * a.Dv;
     const int units = units_of(positions(a, b));
     if (units == 0) {
@@ -506,7 +708,9 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a)
     const int per = stretch_of(a, units_before(a, a.B)), before = units_before(a, b);
     const int p0 = before / per, p1 = (before + units - 1) / per, count = p1 - p0 + 1;
     if (count == 1) return;                              // (answered where it was computed)
-    const auto row_of = [&](int p) { return (((int64_t)hk * a.parts + p0 + p) * 2 + (p == 0 ? 1 : 0)) * a.rows + r; };
+    // the first part is its wavefront's last request, the others are their wavefronts' first
+    const int64_t row0 = ((int64_t)hk * a.parts + p0) * 2 * a.rows + r;
+    const auto row_of = [&](int p) { return row0 + (int64_t)(2 * p + (p == 0 ? 1 : 0)) * a.rows; };
     const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
     if (w < 2) {
         float most = -INFINITY, sum = 0.0f;
@@ -524,39 +728,64 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a)
         if (l == 0) total[w] = sum;
     }
     __syncthreads();
+    // 2 * quads lanes a group (at most 128), as many groups as there are lanes for
+    const int wide = 2 * quads, groups = 256 / wide, group = threadIdx.x / wide, q = threadIdx.x - group * wide, m = q >= quads;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (group < groups)
+#pragma unroll 4
+        for (int p = group; p < count; p += groups) {
+            // (a part whose keys were all hidden adds nothing)
+            const float g = f[m][p];
+            const f32x4 x = *(const f32x4*)(a.part + (row_of(p) * wide + q) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += g == 0.0f ? 0.0f : g * x[e];
+        }
+    meet[threadIdx.x] = v;
+    __syncthreads();
+    if (threadIdx.x >= quads) return;
+    f32x4 x = meet[threadIdx.x], y = meet[quads + threadIdx.x];
+    for (int g = 1; g < groups; ++g) { x += meet[g * wide + threadIdx.x]; y += meet[g * wide + quads + threadIdx.x]; }
     const bool none = total[1] == 0.0f;
     const float i0 = none ? 0.0f : 1.0f / total[0], i1 = none ? 0.0f : a.lam[head] / total[1];
-    for (int d = threadIdx.x; d < a.Dv; d += 256) {
-        float x = 0.0f, y = 0.0f;
-#pragma unroll 4
-        for (int p = 0; p < count; ++p) {
-            const float* from = a.part + row_of(p) * 2 * wide + d;
-            // (a part whose keys were all hidden adds nothing)
-            const float g0 = f[0][p], g1 = f[1][p], v0 = from[0], v1 = from[wide];
-            x += g0 == 0.0f ? 0.0f : g0 * v0;
-            y += g1 == 0.0f ? 0.0f : g1 * v1;
-        }
-        out[d] = (T)(none ? 0.0f : fmaf(x, i0, -y * i1));
-    }
+    float o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = none ? 0.0f : fmaf(x[e], i0, -y[e] * i1);
+    store4(out, 4 * (int)threadIdx.x, a.Dv, a.ovec, o);
 }
 
 int dim_tile(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
 
-struct PagedPlan { int rt, row_tiles, chunks, parts; size_t part, ml; };
+struct PagedPlan { bool full, direct; int rt, row_tiles, chunks, parts; size_t part, ml; };
 
-PagedPlan paged_plan(const sconv_paged_desc_t& d, size_t ws_bytes)
+// What a call's operands allow (addresses apart from their low bits do not count: the workspace's size does not know them).
+PagedPlan paged_plan(const sconv_paged_desc_t& d, const sconv_pages_dev_t* at, size_t ws_bytes)
 {
     PagedPlan p = {};
     if (d.B == 0 || d.Sq == 0) return p;
-    const int G = d.H / d.Hkv, rows = d.Sq * G, DVT = dim_tile(d.pages.D) == 32 ? 64 : 128;
-    p.rt = rows > 16 && d.type == SCONV_BF16 ? 2 : 1;
+    const sconv_pages_t& g = d.pages;
+    const int G = d.H / d.Hkv, rows = d.Sq * G, DT = dim_tile(g.D), DVT = DT == 32 ? 64 : 128;
+    p.rt = rows > 16 && d.type == SCONV_BF16 && DT <= 64 ? 2 : 1;      // (two tiles of 128 have no room)
     p.row_tiles = (rows + 16 * p.rt - 1) / (16 * p.rt);
-    p.chunks = (d.pages.Dv + DVT - 1) / DVT;
-    // as many stretches as fill the chip twice over, and no more than the caches can have
-    const int64_t units = (int64_t)d.B * (((int64_t)d.pages.table_width * d.pages.page_size + BN - 1) / BN), base = (int64_t)d.Hkv * p.row_tiles * p.chunks;
+    p.chunks = (g.Dv + DVT - 1) / DVT;
+    // (16 rows of a page, of both maps, within 32-bit offsets)
+    const int64_t far = int64_t(1) << 24;
+    p.full = g.D == DT && g.Dv % DVT == 0;
+    const bool aligned = g.page_size % 16 == 0 && g.k_s < far && g.v_s < far && g.ks_s < far && g.vs_s < far && g.k_h < 8 * far;
+    const int size = serving_type_size(g.type);
+    p.direct = p.full && aligned && size <= 2 && (g.k_p | g.k_s | g.k_h | g.v_p | g.v_s | g.v_h) % (16 / size) == 0;
+    if (size == 1) {
+        // a scale is read with the aligned dword around it: the last byte has to be the last of one
+        const int64_t last_k = (g.pages - 1) * g.ks_p + (g.page_size - 1) * g.ks_s + (g.Hk - 1) * g.ks_h, last_v = (g.pages - 1) * g.vs_p + (g.page_size - 1) * g.vs_s + (g.Hv - 1) * g.vs_h;
+        p.direct = p.direct && last_k % 4 == 3 && last_v % 4 == 3;
+    }
+    if (at) p.direct = p.direct && aligned_to(at->k, 16) && aligned_to(at->v, 16) && aligned_to(at->ks, 4) && aligned_to(at->vs, 4);
+    // As many stretches as there are places for wavefronts, and no more than the caches can have units, or 64 MB hold parts.
+    const int64_t units = (int64_t)d.B * (((int64_t)g.table_width * g.page_size + BN - 1) / BN), base = (int64_t)d.Hkv * p.row_tiles * p.chunks;
     if (units >= (int64_t(1) << 31)) return p;
-    int64_t parts = std::min<int64_t>(std::min<int64_t>((512 + base - 1) / base, (units + LEAST - 1) / LEAST), MAX_PARTS);
-    const int64_t wide = (d.pages.Dv + 3) / 4 * 4, each = (int64_t)d.Hkv * 2 * rows * (2 * wide + 4) * (int64_t)sizeof(float);
+    const int64_t wide = (g.Dv + 3) / 4 * 4, each = (int64_t)d.Hkv * 2 * rows * (2 * wide + 4) * (int64_t)sizeof(float);
+    const int64_t places = (d.type == SCONV_BF16 && p.rt == 1 && DT <= 64 && !(DT == 64 && g.type == SCONV_BF16) ? 8 : 4) * 256;
+    int64_t parts = std::max<int64_t>(std::min<int64_t>(places / base, (int64_t(64) << 20) / each), 1);
+    parts = std::min<int64_t>(std::min<int64_t>(parts, (units + LEAST - 1) / LEAST), MAX_PARTS);
     if ((size_t)(parts * each) > ws_bytes) return p;
     p.parts = (int)parts;
     p.part = (size_t)(parts * d.Hkv * 2 * rows * 2 * wide) * sizeof(float);
@@ -564,39 +793,37 @@ PagedPlan paged_plan(const sconv_paged_desc_t& d, size_t ws_bytes)
     return p;
 }
 
-template <typename T, typename P, bool FULL, bool ALIGNED, int DT, int DVT, int RT>
+template <typename T, typename P, bool FULL, bool DIRECT, int DT, int DVT, int RT>
 int paged_launch(const PagedArgs& a, const PagedPlan& p, hipStream_t stream)
 {
-    constexpr size_t tiles = (size_t)NW * Tile<typename Kept<P>::type, BN, DVT>::SIZE * 2, join = (size_t)(NW * RT * 64 + NW / 2 * RT * 2 * DVT * 16) * 4;
-    constexpr size_t lds = join > tiles ? join : tiles;
-    const auto kern = paged_attn<T, P, FULL, ALIGNED, DT, DVT, RT>;
+    size_t lds = (size_t)Tile<typename Kept<P>::type, BN, DVT>::SIZE * 2;
+    if constexpr (DIRECT) lds = Unit<P, DT, DVT>::LDS;
+    const auto kern = paged_attn<T, P, FULL, DIRECT, DT, DVT, RT>;
     const int rc = allow_lds(kern, lds);
     if (rc) return rc;
     const int64_t grid = (int64_t)(p.parts ? p.parts : a.B) * a.Hkv * p.row_tiles;
-    if (!grid_fits(grid, 256) || !grid_fits((int64_t)a.B * a.Sq * a.H, 256)) return SCONV_EUNSUPPORTED;
-    hipLaunchKernelGGL(kern, dim3((unsigned)grid, 1, (unsigned)p.chunks), dim3(256), lds, stream, a);
+    if (!grid_fits(grid, 64) || !grid_fits((int64_t)a.B * a.Sq * a.H, 256)) return SCONV_EUNSUPPORTED;
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid, 1, (unsigned)p.chunks), dim3(64), lds, stream, a);
     return launch_status();
 }
 
-template <typename T, typename P, bool FULL, bool ALIGNED>
+template <typename T, typename P, bool FULL, bool DIRECT>
 int paged_shape(const PagedArgs& a, const PagedPlan& p, hipStream_t stream)
 {
     const int DT = dim_tile(a.D);
     if constexpr (sizeof(T) == 2)
         if (p.rt == 2)
-            return DT == 32 ? paged_launch<T, P, FULL, ALIGNED, 32, 64, 2>(a, p, stream)
-                 : DT == 64 ? paged_launch<T, P, FULL, ALIGNED, 64, 128, 2>(a, p, stream) : paged_launch<T, P, FULL, ALIGNED, 128, 128, 2>(a, p, stream);
-    return DT == 32 ? paged_launch<T, P, FULL, ALIGNED, 32, 64, 1>(a, p, stream)
-         : DT == 64 ? paged_launch<T, P, FULL, ALIGNED, 64, 128, 1>(a, p, stream) : paged_launch<T, P, FULL, ALIGNED, 128, 128, 1>(a, p, stream);
+            return DT == 32 ? paged_launch<T, P, FULL, DIRECT, 32, 64, 2>(a, p, stream) : paged_launch<T, P, FULL, DIRECT, 64, 128, 2>(a, p, stream);
+    return DT == 32 ? paged_launch<T, P, FULL, DIRECT, 32, 64, 1>(a, p, stream)
+         : DT == 64 ? paged_launch<T, P, FULL, DIRECT, 64, 128, 1>(a, p, stream) : paged_launch<T, P, FULL, DIRECT, 128, 128, 1>(a, p, stream);
 }
 
 template <typename T, typename P>
 int paged_run(const PagedArgs& a, const PagedPlan& p, hipStream_t stream)
 {
-    const int DT = dim_tile(a.D), DVT = DT == 32 ? 64 : 128;
-    const bool full = a.D == DT && a.Dv % DVT == 0, aligned = a.page.d % 16 == 0;
-    const int rc = full ? (aligned ? paged_shape<T, P, true, true>(a, p, stream) : paged_shape<T, P, true, false>(a, p, stream))
-                        : (aligned ? paged_shape<T, P, false, true>(a, p, stream) : paged_shape<T, P, false, false>(a, p, stream));
+    int rc;
+    if constexpr (sizeof(P) <= 2) rc = p.direct ? paged_shape<T, P, true, true>(a, p, stream) : p.full ? paged_shape<T, P, true, false>(a, p, stream) : paged_shape<T, P, false, false>(a, p, stream);
+    else rc = p.full ? paged_shape<T, P, true, false>(a, p, stream) : paged_shape<T, P, false, false>(a, p, stream);
     if (rc || p.parts == 0) return rc;
     hipLaunchKernelGGL((paged_join<T>), dim3((unsigned)((int64_t)a.B * a.Sq * a.H)), dim3(256), 0, stream, a);
     return launch_status();
@@ -606,7 +833,7 @@ int paged_run(const PagedArgs& a, const PagedPlan& p, hipStream_t stream)
 
 size_t paged_workspace(const sconv_paged_desc_t& d)
 {
-    const PagedPlan p = paged_plan(d, ~(size_t)0 >> 1);
+    const PagedPlan p = paged_plan(d, nullptr, ~(size_t)0 >> 1);
     return p.part + p.ml;
 }
 
@@ -614,7 +841,7 @@ int launch_paged(const sconv_paged_desc_t& d, const void* q, const sconv_pages_d
                  void* out, void* ws, size_t ws_bytes, hipStream_t stream)
 {
     const sconv_pages_t& g = d.pages;
-    const PagedPlan p = paged_plan(d, ws_bytes);
+    const PagedPlan p = paged_plan(d, &pages, ws_bytes);
     PagedArgs a = {};
     a.q = q; a.k = pages.k; a.v = pages.v; a.kx = pages.ks; a.vx = pages.vs; a.table = pages.table; a.lam = lam; a.len = lengths; a.out = out;
     a.B = d.B; a.Sq = d.Sq; a.H = d.H; a.Hkv = d.Hkv; a.G = d.H / d.Hkv; a.D = g.D; a.Dv = g.Dv; a.causal = d.causal; a.rows = d.Sq * a.G;
