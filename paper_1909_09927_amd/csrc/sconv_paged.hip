@@ -20,7 +20,8 @@ namespace {
 
 constexpr int BN = 32;                   // keys of a unit
 constexpr int LEAST = 2;                 // units of a stretch at least
-constexpr int MAX_PARTS = 2048;
+constexpr int PLACES = 1024;             // wavefronts: one to a SIMD.  (Two: 64 requests of up to 784 35 -> 38 us, 16 of up to 32768 68 -> 71.)
+constexpr int MAX_PARTS = PLACES;
 
 struct PagedArgs {
     const void* q; const void* k; const void* v; const uint8_t* kx; const uint8_t* vx; const int32_t* table; const float* lam;
@@ -39,6 +40,7 @@ template <> struct Kept<float> { typedef float type; };
 
 // 16-bit values against 32-bit ones in three pieces.
 using sconv::mma;
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 template <typename C>
 __device__ __forceinline__ C mma(C c, const bf16x8& a, const bf16x8x3& b)
 {
@@ -51,42 +53,53 @@ __device__ __forceinline__ int positions(const PagedArgs& a, int b) { return min
 __device__ __forceinline__ int units_of(int n) { return (n + BN - 1) / BN; }
 
 // All requests' units, and those of requests before b: every wavefront adds them up for itself.
-__device__ __forceinline__ int wave_total(int v)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    return __builtin_amdgcn_readfirstlane(v);
-}
 __device__ __forceinline__ int units_before(const PagedArgs& a, int upto)
 {
     const int l = threadIdx.x & 63;
     int v = 0;
     for (int b = l; b < upto; b += 64) v += units_of(positions(a, b));
-    return wave_total(v);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+    return __builtin_amdgcn_readfirstlane(v);
 }
 // Units of a stretch.
 __device__ __forceinline__ int stretch_of(const PagedArgs& a, int units) { return max((units + a.parts - 1) / a.parts, LEAST); }
-// The request that unit u lies in, and the units before it.
-__device__ __forceinline__ void request_of(const PagedArgs& a, int u, int& b, int& before)
+// Of stretch `at`: its first unit, counted from request b's first, and its end, likewise; false: it has none.
+__device__ __forceinline__ bool find_stretch(const PagedArgs& a, int at, int& b, int& begin, int& end)
 {
-    const int l = threadIdx.x & 63;
-    int base = 0;
+    const int l = threadIdx.x & 63, got = l < a.B ? units_of(positions(a, l)) : 0;
+    int all, u = 0, per = 0, base = 0;
+    if (a.B > 64) {
+        all = units_before(a, a.B);
+        per = stretch_of(a, all);
+        u = (int)min((int64_t)at * per, (int64_t)all);
+        if (u == all) return false;
+    }
     for (int b0 = 0;; b0 += 64) {
-        const int mine = b0 + l < a.B ? units_of(positions(a, b0 + l)) : 0;
+        const int mine = b0 == 0 ? got : b0 + l < a.B ? units_of(positions(a, b0 + l)) : 0;
         int upto = mine;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const int t = __shfl_up(upto, d);
             if (l >= d) upto += t;
         }
-        const uint64_t past = __ballot(base + upto > u);
-        if (past || b0 + 64 >= a.B) {
-            const int at = past ? __builtin_ctzll(past) : 63;
-            b = __builtin_amdgcn_readfirstlane(b0 + at);
-            before = __builtin_amdgcn_readfirstlane(base + __shfl(upto - mine, at));
-            return;
+        if (a.B <= 64) {
+            all = __builtin_amdgcn_readlane(upto, 63);
+            per = stretch_of(a, all);
+            u = (int)min((int64_t)at * per, (int64_t)all);
+            if (u == all) return false;
         }
-        base += __shfl(upto, 63);
+        const uint64_t past = __ballot(base + upto > u);
+        if (past) {
+            const int lane = __builtin_ctzll(past);
+            b = b0 + lane;
+            const int before = base + __builtin_amdgcn_readlane(upto - mine, lane);
+            begin = u - before;
+            end = (int)min((int64_t)u + per, (int64_t)all) - before;
+            return true;
+        }
+        base += __builtin_amdgcn_readlane(upto, 63);
+        if (b0 + 64 >= a.B) return false;                // (not reached: the units add up to more than u)
     }
 }
 
@@ -192,7 +205,7 @@ struct Unit {
     static constexpr int NK = K / 1024, NV = V / 1024, HK = NK / 2, HV = NV / 2;     // loads of a unit and of half of it
     static constexpr int KLOADS = NK + (ES == 1), VLOADS = NV + (ES == 1);
     static constexpr int SIZE = K + V + 2 * SCALES, STAGES = 2, LDS = STAGES * SIZE + (ES == 1 ? 3 * BN * 4 : 0);
-    __device__ __forceinline__ static int turn_k(int key) { return RK >= 256 ? key & 15 : key / (256 / RK) & (CK - 1); }
+    __device__ __forceinline__ static int turn_k(int key) { return RK >= 256 ? key & 15 : key / (256 / std::min(RK, 256)) & (CK - 1); }
     __device__ __forceinline__ static int turn_v(int key)
     {
         if (ES == 1) return RV == 128 ? (key >> 1 & 3) | (key >> 4 & 1) << 2 : (key >> 2 & 1) | (key >> 4 & 1) << 1;
@@ -241,32 +254,29 @@ __device__ __forceinline__ void load_to_lds(const void* from, uint8_t* to, bool 
 }
 
 // T: queries and results; P: the pages.  FULL: heads are DT and values whole DVT wide.  DIRECT: half a unit lies on one page, too.  RT: tiles of
-// 16 rows.
+// 16 rows, a lane one of each; 0: up to 8 rows, lanes c < 8 have the first map's, the others the second's, so that softmax and the products with
+// the values are done once for both (M: maps of a lane).
 template <typename T, typename P, bool FULL, bool DIRECT, int DT, int DVT, int RT>
-__global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)) void paged_attn(PagedArgs a)
+__global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)) void paged_attn(PagedArgs a)
 {
     typedef typename Kept<P>::type KT;
     typedef Tile<KT, BN, DVT> Values;
     typedef Unit<P, DT, DVT> U;
     static_assert(!DIRECT || (FULL && sizeof(P) <= 2), "whole rows of whole pages");
+    constexpr bool PAIR = RT == 0;
+    constexpr int R = PAIR ? 1 : RT, M = PAIR ? 1 : 2;
     constexpr int KS = DT / 32, NT = DVT / 16, E = 16 / sizeof(P), SC = sizeof(P) == 1;
     constexpr int NV = BN * DVT / E / 64, VPER = DVT / E;        // 16-byte vectors of a lane's and a row's share of the values
     extern __shared__ __attribute__((aligned(16))) char lds[];
 
-    const int l = threadIdx.x, c = l & 15, h = l >> 4;
+    const int l = threadIdx.x, c = l & 15, h = l >> 4, own_m = PAIR ? c >> 3 : 0, own_c = PAIR ? c & 7 : c;
     const int per_head = a.parts ? a.parts : a.B;
-    const int at = blockIdx.x % per_head, rest = blockIdx.x / per_head, hk = rest % a.Hkv, first = rest / a.Hkv * 16 * RT;
+    const int at = blockIdx.x % per_head, rest = blockIdx.x / per_head, hk = rest % a.Hkv, first = rest / a.Hkv * 16 * R;
     const int dv0 = blockIdx.z * DVT, dvn = min(DVT, a.Dv - dv0), wide = (a.Dv + 3) / 4 * 4;
 
     int b, begin, end;                                           // the request, the stretch in units from its first
     if (a.parts) {
-        const int all = units_before(a, a.B), per = stretch_of(a, all);
-        const int64_t from = (int64_t)at * per;
-        if (from >= all) return;
-        int before;
-        request_of(a, (int)from, b, before);
-        begin = (int)from - before;
-        end = (int)min(from + per, (int64_t)all) - before;
+        if (!find_stretch(a, at, b, begin, end)) return;
     } else {
         b = at;
         begin = 0;
@@ -277,26 +287,26 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)
         const int n = __builtin_amdgcn_readfirstlane(positions(a, b)), units = units_of(n);
         if (a.parts && units == 0) continue;
         const int u1 = min(end, units);
-        int lim[RT];
-        typename Frag<T>::type qf[RT][2][KS];
+        int lim[R];
+        typename Frag<T>::type qf[R][M][KS];
 #pragma unroll
-        for (int x = 0; x < RT; ++x) {
-            const int r = min(first + 16 * x + c, a.rows - 1), i = r / a.G, g = r - i * a.G;
+        for (int x = 0; x < R; ++x) {
+            const int r = min(first + 16 * x + own_c, a.rows - 1), i = r / a.G, g = r - i * a.G;
             lim[x] = limit_of(a, i, n);
-            const T* q = (const T*)a.q + b * a.q_b + i * a.q_s + (int64_t)(hk * a.G + g) * 2 * a.q_h;
+            const T* q = (const T*)a.q + b * a.q_b + i * a.q_s + ((int64_t)(hk * a.G + g) * 2 + own_m) * a.q_h;
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+            for (int m = 0; m < M; ++m)
 #pragma unroll
                 for (int s = 0; s < KS; ++s) qf[x][m][s] = global_frag<false>(q + m * a.q_h, depth_of<P, KS>(s, h), a.D);
         }
         const int least = __builtin_amdgcn_readfirstlane(lim[0]);    // of the first row: limits rise
 
-        f32x4 o[RT][2][NT];
-        float top[RT][2], safe[RT][2], sum[RT][2];
+        f32x4 o[R][M][NT];
+        float top[R][M], safe[R][M], sum[R][M];
 #pragma unroll
-        for (int x = 0; x < RT; ++x)
+        for (int x = 0; x < R; ++x)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
+            for (int m = 0; m < M; ++m) {
                 top[x][m] = -INFINITY; safe[x][m] = 0.0f; sum[x][m] = 0.0f;
 #pragma unroll
                 for (int t = 0; t < NT; ++t) o[x][m][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -311,33 +321,53 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)
         // halves, for the whole wavefront, and rows lie at 32-bit offsets from the halves' first; otherwise the page of key l % 32.
         typedef __attribute__((address_space(4))) const int32_t scalar_t;
         int entry[2] = {};
-        int64_t page[2];
-        int slot[2];
+        int page = 0, slot = 0;
         uint32_t there_next = 0;                                 // keys of the unit that are there, as bits
+        // (DIRECT: units are asked for in turn; of the half that is next: its place in the table, its first slot, the keys from it on)
+        int next_at = 0, next_slot = 0, next_left = n - begin * BN, asked_slot[2], asked_left[2];
+        if constexpr (DIRECT) {
+            next_at = (int)divided((uint32_t)(begin * BN), a.page);
+            next_slot = begin * BN - next_at * (int)a.page.d;
+        }
         const auto ask = [&](int u) {
+            if constexpr (DIRECT) {
 #pragma unroll
-            for (int y = 0; y < (DIRECT ? 2 : 1); ++y) {
-                const int j = DIRECT ? u * BN + 16 * y : u * BN + (l & 31);
-                const int at = min((int)divided((uint32_t)j, a.page), a.width - 1);
-                if constexpr (DIRECT) entry[y] = ((scalar_t*)table)[at];         // (no kernel writes it while this one runs)
-                else entry[y] = table[at];
+                for (int y = 0; y < 2; ++y) {
+                    entry[y] = ((scalar_t*)table)[min(next_at, a.width - 1)];    // (no kernel writes it while this one runs)
+                    asked_slot[y] = next_slot;
+                    asked_left[y] = next_left;
+                    next_left -= 16;
+                    next_slot += 16;
+                    if (next_slot == (int)a.page.d) { next_slot = 0; ++next_at; }
+                }
+            } else {
+                entry[0] = table[min((int)divided((uint32_t)(u * BN + (l & 31)), a.page), a.width - 1)];
             }
         };
+        const char* kp_at[2]; const char* vp_at[2]; const uint8_t* kx_at[2]; const uint8_t* vx_at[2];    // DIRECT: the halves' first rows
         const auto find = [&](int u) {
-            there_next = 0;
+            if constexpr (DIRECT) {
+                there_next = 0;
 #pragma unroll
-            for (int y = 0; y < (DIRECT ? 2 : 1); ++y) {
-                const int j = DIRECT ? u * BN + 16 * y : u * BN + (l & 31);
-                const int p = entry[y];
-                const bool ok = j < n && p >= 0 && p < a.pages;
-                page[y] = ok ? p : 0;
-                slot[y] = ok ? j - (int)(divided((uint32_t)j, a.page) * a.page.d) : 0;
-                if constexpr (DIRECT) {
-                    const int left = n - j;
-                    if (ok) there_next |= (left >= 16 ? 0xffffu : (1u << left) - 1u) << (16 * y);
-                } else {
-                    there_next = (uint32_t)__ballot(ok);
+                for (int y = 0; y < 2; ++y) {
+                    const bool ok = asked_left[y] > 0 && (uint32_t)entry[y] < (uint32_t)a.pages;
+                    const uint32_t p = ok ? entry[y] : 0, s = ok ? asked_slot[y] : 0;
+                    const uint32_t keys = asked_left[y] >= 16 ? 0xffffu : (1u << asked_left[y]) - 1u;
+                    if (ok) there_next |= keys << (16 * y);
+                    const auto from = [&](int64_t page_stride, int64_t slot_stride, int size) { return (uint64_t)p * (uint32_t)(page_stride * size) + (uint64_t)s * (uint32_t)(slot_stride * size); };
+                    kp_at[y] = (const char*)kb + from(a.k_p, a.k_s, sizeof(P));
+                    vp_at[y] = (const char*)vb + from(a.v_p, a.v_s, sizeof(P));
+                    if constexpr (SC) {
+                        kx_at[y] = kxb + from(a.kx_p, a.kx_s, 1);
+                        vx_at[y] = vxb + from(a.vx_p, a.vx_s, 1);
+                    }
                 }
+            } else {
+                const int j = u * BN + (l & 31), p = entry[0];
+                const bool ok = j < n && p >= 0 && p < a.pages;
+                page = ok ? p : 0;
+                slot = ok ? j - (int)(divided((uint32_t)j, a.page) * a.page.d) : 0;
+                there_next = (uint32_t)__ballot(ok);
             }
         };
         // through registers
@@ -347,7 +377,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)
         const auto fetch_keys = [&]() {
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const int64_t p = __shfl((int)page[0], 16 * y + c), s = __shfl(slot[0], 16 * y + c);
+                const int64_t p = __shfl(page, 16 * y + c), s = __shfl(slot, 16 * y + c);
                 const P* row = kb + (p * a.k_p + s * a.k_s);
                 const uint8_t* x = SC ? kxb + (p * a.kx_p + s * a.kx_s) : nullptr;
 #pragma unroll
@@ -361,7 +391,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int key = v * (64 / VPER) + l / VPER, d = l % VPER * E;
-                const int64_t p = __shfl((int)page[0], key), s = __shfl(slot[0], key);
+                const int64_t p = __shfl(page, key), s = __shfl(slot, key);
                 const P* row = vb + (p * a.v_p + s * a.v_s);
                 if constexpr (SC) {
                     vr[v] = load16_any<FULL>((const uint8_t*)row, d, dvn);
@@ -390,35 +420,33 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)
                 }
         }
         // (a scale's dword: the four aligned bytes that its byte is one of)
-        const auto scale_load = [&](const uint8_t* base, int64_t page_stride, int64_t slot_stride, int64_t map, uint8_t* to, uint32_t& low) {
-            const int y = l >> 4 & 1;
-            const uint64_t at = (uint64_t)(base + (y ? page[1] * page_stride + slot[1] * slot_stride : page[0] * page_stride + slot[0] * slot_stride) + map + c * slot_stride);
+        const uint32_t kx_lane = (uint32_t)(c * a.kx_s) + (l >= 32 ? (uint32_t)a.kx_h : 0u), vx_lane = (uint32_t)(c * a.vx_s);
+        const auto scale_load = [&](const uint8_t* half0, const uint8_t* half1, uint32_t lane, uint8_t* to, uint32_t& low) {
+            const uint64_t at = (uint64_t)(l & 16 ? half1 : half0) + lane;
             low = (uint32_t)at & 3;
             load_to_lds((const void*)(at - low), to, true);
         };
         const auto send_keys = [&](int stage, uint32_t& low) {
             uint8_t* to = (uint8_t*)lds + stage * U::SIZE;
-            if constexpr (SC) scale_load(kxb, a.kx_p, a.kx_s, l >= 32 ? a.kx_h : 0, to + U::K + U::V, low);
+            if constexpr (SC) scale_load(kx_at[0], kx_at[1], kx_lane, to + U::K + U::V, low);
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const char* from = (const char*)(kb + (page[y] * a.k_p + slot[y] * a.k_s));
 #pragma unroll
-                for (int i = 0; i < U::HK; ++i) load_to_lds(from + k_off[i], to + (y * U::HK + i) * 1024, false);
+                for (int i = 0; i < U::HK; ++i) load_to_lds(kp_at[y] + k_off[i], to + (y * U::HK + i) * 1024, false);
             }
         };
         const auto send_values = [&](int stage, uint32_t& low) {
             uint8_t* to = (uint8_t*)lds + stage * U::SIZE + U::K;
-            if constexpr (SC) scale_load(vxb, a.vx_p, a.vx_s, 0, to + U::V + U::SCALES, low);
+            if constexpr (SC) scale_load(vx_at[0], vx_at[1], vx_lane, to + U::V + U::SCALES, low);
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const char* from = (const char*)(vb + (page[y] * a.v_p + slot[y] * a.v_s));
 #pragma unroll
-                for (int i = 0; i < U::HV; ++i) load_to_lds(from + v_off[y][i], to + (y * U::HV + i) * 1024, false);
+                for (int i = 0; i < U::HV; ++i) load_to_lds(vp_at[y] + v_off[y][i], to + (y * U::HV + i) * 1024, false);
             }
         };
 
-        f32x4 s[RT][2][2];                                       // [rows][map][16 keys]
-        Weights<T> p[RT][2];
+        f32x4 s[R][M][2];                                       // [rows][map][16 keys]
+        Weights<T> p[R][M];
         // scores of the keys that are not there, or not seen, go; then the weights, times their values' scales
         const auto soften = [&](int j0, uint32_t there, const float (&by)[8]) {
             if (j0 + BN > least || there != ~0u) {
@@ -428,17 +456,17 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)
                     for (int e = 0; e < 4; ++e) {
                         const int j = 16 * y + 4 * h + e;
 #pragma unroll
-                        for (int x = 0; x < RT; ++x) {
+                        for (int x = 0; x < R; ++x) {
                             const bool ok = j0 + j < lim[x] && (there >> j & 1);
-                            s[x][0][y][e] = ok ? s[x][0][y][e] : -INFINITY;
-                            s[x][1][y][e] = ok ? s[x][1][y][e] : -INFINITY;
+#pragma unroll
+                            for (int m = 0; m < M; ++m) s[x][m][y][e] = ok ? s[x][m][y][e] : -INFINITY;
                         }
                     }
             }
 #pragma unroll
-            for (int x = 0; x < RT; ++x)
+            for (int x = 0; x < R; ++x)
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
+                for (int m = 0; m < M; ++m) {
                     f32x4 (&z)[2] = s[x][m];
                     float mx = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
                     mx = half_max(quarter_max(mx)) * a.scale2;
@@ -503,8 +531,9 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
+                        f32x4 z[R];
 #pragma unroll
-                        for (int x = 0; x < RT; ++x) s[x][m][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                        for (int x = 0; x < R; ++x) z[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
                         const uint8_t* row = kt + (16 * y + c) * U::RK;
 #pragma unroll
                         for (int t = 0; t < KS; ++t) {
@@ -520,7 +549,18 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)
                                 kf = widened(x[2 * (t % 2)], x[2 * (t % 2) + 1], fk[y][m]);
                             }
 #pragma unroll
-                            for (int x = 0; x < RT; ++x) s[x][m][y] = mma(s[x][m][y], kf, qf[x][m][t]);
+                            for (int x = 0; x < R; ++x) z[x] = mma(z[x], kf, qf[x][PAIR ? 0 : m][t]);
+                        }
+                        // (both maps' keys meet every lane's query: a lane keeps its own map's)
+#pragma unroll
+                        for (int x = 0; x < R; ++x) {
+                            f32x4& to = s[x][PAIR ? 0 : m][y];
+                            if (PAIR && m == 1) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) to[e] = own_m ? z[x][e] : to[e];
+                            } else {
+                                to = z[x];
+                            }
                         }
                     }
                 const bool more = u + 2 < u1;
@@ -576,10 +616,9 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)
                             vf = y.v;
                         }
 #pragma unroll
-                        for (int x = 0; x < RT; ++x) {
-                            o[x][0][t] = p[x][0].times(o[x][0][t], vf);
-                            o[x][1][t] = p[x][1].times(o[x][1][t], vf);
-                        }
+                        for (int x = 0; x < R; ++x)
+#pragma unroll
+                            for (int m = 0; m < M; ++m) o[x][m][t] = p[x][m].times(o[x][m][t], vf);
                     }
                 }
                 if (more) {
@@ -609,13 +648,25 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
+                        f32x4 z[R];
 #pragma unroll
-                        for (int x = 0; x < RT; ++x) s[x][m][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                        for (int x = 0; x < R; ++x) z[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                         for (int t = 0; t < KS; ++t) {
                             const auto kf = key_frag<FULL>(kr[y][m], t, h, a.D, scale_of(ke[y][m]));
 #pragma unroll
-                            for (int x = 0; x < RT; ++x) s[x][m][y] = mma(s[x][m][y], kf, qf[x][m][t]);
+                            for (int x = 0; x < R; ++x) z[x] = mma(z[x], kf, qf[x][PAIR ? 0 : m][t]);
+                        }
+                        // (both maps' keys meet every lane's query: a lane keeps its own map's)
+#pragma unroll
+                        for (int x = 0; x < R; ++x) {
+                            f32x4& to = s[x][PAIR ? 0 : m][y];
+                            if (PAIR && m == 1) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) to[e] = own_m ? z[x][e] : to[e];
+                            } else {
+                                to = z[x];
+                            }
                         }
                     }
                 if (more) fetch_keys();
@@ -642,10 +693,9 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)
                 for (int t = 0; t < NT; ++t) {
                     const auto vf = tile_col<KT, Values::LD, Values::PLANE, 16>(vt + vcol + 16 * t);
 #pragma unroll
-                    for (int x = 0; x < RT; ++x) {
-                        o[x][0][t] = p[x][0].times(o[x][0][t], vf);
-                        o[x][1][t] = p[x][1].times(o[x][1][t], vf);
-                    }
+                    for (int x = 0; x < R; ++x)
+#pragma unroll
+                        for (int m = 0; m < M; ++m) o[x][m][t] = p[x][m].times(o[x][m][t], vf);
                 }
                 wave_lds_fence();
                 settle();
@@ -653,34 +703,38 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT == 1 ? 2 : 1)
         }
         const bool whole = begin == 0 && u1 == units;
 #pragma unroll
-        for (int x = 0; x < RT; ++x) {
-            const int mine = first + 16 * x + c;
+        for (int x = 0; x < R; ++x) {
+            const int mine = first + 16 * x + own_c;
 #pragma unroll
-            for (int m = 0; m < 2; ++m) sum[x][m] = half_sum(quarter_sum(sum[x][m]));
-            if (mine >= a.rows) continue;
+            for (int m = 0; m < M; ++m) sum[x][m] = half_sum(quarter_sum(sum[x][m]));
             if (whole) {
-                const int i = mine / a.G, head = hk * a.G + mine - i * a.G;
+                const int r = min(mine, a.rows - 1), i = r / a.G, head = hk * a.G + r - i * a.G;
                 T* out = (T*)a.out + (((int64_t)b * a.Sq + i) * a.H + head) * a.Dv + dv0;
                 // (a query that sees nothing answers 0, whatever lam is)
-                const bool none = sum[x][1] == 0.0f;
-                const float i0 = none ? 0.0f : 1.0f / sum[x][0], i1 = none ? 0.0f : a.lam[head] / sum[x][1];
+                const float s0 = sum[x][0], s1 = PAIR ? __shfl_xor(s0, 8) : sum[x][M - 1];
+                const bool none = own_m == 0 ? s1 == 0.0f : s0 == 0.0f;
+                const float by0 = own_m ? a.lam[head] / s0 : 1.0f / s0, by1 = PAIR ? 0.0f : a.lam[head] / s1;
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     float r[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) r[e] = none ? 0.0f : fmaf(o[x][0][t][e], i0, -o[x][1][t][e] * i1);
-                    store4(out, 16 * t + 4 * h, dvn, a.ovec, r);
+                    for (int e = 0; e < 4; ++e) {
+                        const float other = PAIR ? __shfl_xor(o[x][0][t][e] * by0, 8) : o[x][M - 1][t][e] * by1;
+                        r[e] = none ? 0.0f : fmaf(o[x][0][t][e], by0, -other);
+                    }
+                    if (own_m == 0 && mine < a.rows) store4(out, 16 * t + 4 * h, dvn, a.ovec, r);
                 }
-            } else {
+            } else if (mine < a.rows) {
                 const int64_t row = (((int64_t)hk * a.parts + at) * 2 + (begin == 0 ? 1 : 0)) * a.rows + mine;
-                if (blockIdx.z == 0 && h == 0) *(f32x4*)(a.part_ml + 4 * row) = f32x4{top[x][0], sum[x][0], top[x][1], sum[x][1]};
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+                for (int m = 0; m < M; ++m) {
+                    if (blockIdx.z == 0 && h == 0) *(f32x2*)(a.part_ml + 4 * row + 2 * (m + own_m)) = f32x2{top[x][m], sum[x][m]};
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         const int d = 16 * t + 4 * h;
-                        if (dv0 + d < wide) *(f32x4*)(a.part + (row * 2 + m) * wide + dv0 + d) = o[x][m][t];
+                        if (dv0 + d < wide) *(f32x4*)(a.part + (row * 2 + m + own_m) * wide + dv0 + d) = o[x][m][t];
                     }
+                }
             }
         }
         if (!a.parts || end <= units) return;
@@ -700,17 +754,30 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a)
     const int head = (int)(id % a.H), i = (int)(id / a.H % a.Sq), b = (int)(id / a.H / a.Sq);
     const int hk = head / a.G, r = i * a.G + head % a.G, quads = (a.Dv + 3) / 4;
     T* out = (T*)a.out + id * a.Dv;
-    const int units = units_of(positions(a, b));
+    int all = 0, before = 0, units = 0;
+    for (int r = threadIdx.x & 63; r < a.B; r += 64) {
+        const int n = units_of(positions(a, r));
+        all += n;
+        before += r < b ? n : 0;
+        units += r == b ? n : 0;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) { all += __shfl_xor(all, d); before += __shfl_xor(before, d); units += __shfl_xor(units, d); }
     if (units == 0) {
         for (int d = threadIdx.x; d < a.Dv; d += 256) out[d] = (T)0.0f;
         return;
     }
-    const int per = stretch_of(a, units_before(a, a.B)), before = units_before(a, b);
-    const int p0 = before / per, p1 = (before + units - 1) / per, count = p1 - p0 + 1;
+    const int per = stretch_of(a, all), p0 = before / per, p1 = (before + units - 1) / per, count = p1 - p0 + 1;
     if (count == 1) return;                              // (answered where it was computed)
     // the first part is its wavefront's last request, the others are their wavefronts' first
     const int64_t row0 = ((int64_t)hk * a.parts + p0) * 2 * a.rows + r;
     const auto row_of = [&](int p) { return row0 + (int64_t)(2 * p + (p == 0 ? 1 : 0)) * a.rows; };
+    // 2 * quads lanes a group (at most 128), as many groups as there are lanes for; a group's first parts are asked for at once
+    constexpr int AHEAD = 4;
+    const int wide = 2 * quads, groups = 256 / wide, group = threadIdx.x / wide, q = threadIdx.x - group * wide, m = q >= quads;
+    f32x4 part[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) part[i] = *(const f32x4*)(a.part + (row_of(min(group + i * groups, count - 1)) * wide + q) * 4);
     const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
     if (w < 2) {
         float most = -INFINITY, sum = 0.0f;
@@ -728,18 +795,19 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a)
         if (l == 0) total[w] = sum;
     }
     __syncthreads();
-    // 2 * quads lanes a group (at most 128), as many groups as there are lanes for
-    const int wide = 2 * quads, groups = 256 / wide, group = threadIdx.x / wide, q = threadIdx.x - group * wide, m = q >= quads;
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (group < groups)
-#pragma unroll 4
-        for (int p = group; p < count; p += groups) {
-            // (a part whose keys were all hidden adds nothing)
-            const float g = f[m][p];
-            const f32x4 x = *(const f32x4*)(a.part + (row_of(p) * wide + q) * 4);
+    // (a part whose keys were all hidden adds nothing)
+    const auto add = [&](int p, const f32x4& x) {
+        const float g = f[m][p];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += g == 0.0f ? 0.0f : g * x[e];
-        }
+        for (int e = 0; e < 4; ++e) v[e] += g == 0.0f ? 0.0f : g * x[e];
+    };
+    if (group < groups) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) if (group + i * groups < count) add(group + i * groups, part[i]);
+#pragma unroll 4
+        for (int p = group + AHEAD * groups; p < count; p += groups) add(p, *(const f32x4*)(a.part + (row_of(p) * wide + q) * 4));
+    }
     meet[threadIdx.x] = v;
     __syncthreads();
     if (threadIdx.x >= quads) return;
@@ -764,13 +832,13 @@ PagedPlan paged_plan(const sconv_paged_desc_t& d, const sconv_pages_dev_t* at, s
     if (d.B == 0 || d.Sq == 0) return p;
     const sconv_pages_t& g = d.pages;
     const int G = d.H / d.Hkv, rows = d.Sq * G, DT = dim_tile(g.D), DVT = DT == 32 ? 64 : 128;
-    p.rt = rows > 16 && d.type == SCONV_BF16 && DT <= 64 ? 2 : 1;      // (two tiles of 128 have no room)
-    p.row_tiles = (rows + 16 * p.rt - 1) / (16 * p.rt);
+    p.rt = rows <= 8 ? 0 : rows > 16 && d.type == SCONV_BF16 && DT <= 64 ? 2 : 1;      // (two tiles of 128 have no room)
+    p.row_tiles = (rows + 16 * std::max(p.rt, 1) - 1) / (16 * std::max(p.rt, 1));
     p.chunks = (g.Dv + DVT - 1) / DVT;
-    // (16 rows of a page, of both maps, within 32-bit offsets)
+    // (16 rows of both maps within 32-bit offsets, strides of 32 bits)
     const int64_t far = int64_t(1) << 24;
     p.full = g.D == DT && g.Dv % DVT == 0;
-    const bool aligned = g.page_size % 16 == 0 && g.k_s < far && g.v_s < far && g.ks_s < far && g.vs_s < far && g.k_h < 8 * far;
+    const bool aligned = g.page_size % 16 == 0 && std::max({g.k_s, g.v_s, g.ks_s, g.vs_s}) < far && std::max(g.k_h, g.ks_h) < 8 * far && std::max({g.k_p, g.v_p, g.ks_p, g.vs_p}) < 128 * far;
     const int size = serving_type_size(g.type);
     p.direct = p.full && aligned && size <= 2 && (g.k_p | g.k_s | g.k_h | g.v_p | g.v_s | g.v_h) % (16 / size) == 0;
     if (size == 1) {
@@ -779,12 +847,11 @@ PagedPlan paged_plan(const sconv_paged_desc_t& d, const sconv_pages_dev_t* at, s
         p.direct = p.direct && last_k % 4 == 3 && last_v % 4 == 3;
     }
     if (at) p.direct = p.direct && aligned_to(at->k, 16) && aligned_to(at->v, 16) && aligned_to(at->ks, 4) && aligned_to(at->vs, 4);
-    // As many stretches as there are places for wavefronts, and no more than the caches can have units, or 64 MB hold parts.
+    // No more stretches than the caches can have units, or 64 MB hold parts.
     const int64_t units = (int64_t)d.B * (((int64_t)g.table_width * g.page_size + BN - 1) / BN), base = (int64_t)d.Hkv * p.row_tiles * p.chunks;
     if (units >= (int64_t(1) << 31)) return p;
     const int64_t wide = (g.Dv + 3) / 4 * 4, each = (int64_t)d.Hkv * 2 * rows * (2 * wide + 4) * (int64_t)sizeof(float);
-    const int64_t places = (d.type == SCONV_BF16 && p.rt == 1 && DT <= 64 && !(DT == 64 && g.type == SCONV_BF16) ? 8 : 4) * 256;
-    int64_t parts = std::max<int64_t>(std::min<int64_t>(places / base, (int64_t(64) << 20) / each), 1);
+    int64_t parts = std::max<int64_t>(std::min<int64_t>(PLACES / base, (int64_t(64) << 20) / each), 1);
     parts = std::min<int64_t>(std::min<int64_t>(parts, (units + LEAST - 1) / LEAST), MAX_PARTS);
     if ((size_t)(parts * each) > ws_bytes) return p;
     p.parts = (int)parts;
@@ -814,6 +881,9 @@ int paged_shape(const PagedArgs& a, const PagedPlan& p, hipStream_t stream)
     if constexpr (sizeof(T) == 2)
         if (p.rt == 2)
             return DT == 32 ? paged_launch<T, P, FULL, DIRECT, 32, 64, 2>(a, p, stream) : paged_launch<T, P, FULL, DIRECT, 64, 128, 2>(a, p, stream);
+    if (p.rt == 0)
+        return DT == 32 ? paged_launch<T, P, FULL, DIRECT, 32, 64, 0>(a, p, stream)
+             : DT == 64 ? paged_launch<T, P, FULL, DIRECT, 64, 128, 0>(a, p, stream) : paged_launch<T, P, FULL, DIRECT, 128, 128, 0>(a, p, stream);
     return DT == 32 ? paged_launch<T, P, FULL, DIRECT, 32, 64, 1>(a, p, stream)
          : DT == 64 ? paged_launch<T, P, FULL, DIRECT, 64, 128, 1>(a, p, stream) : paged_launch<T, P, FULL, DIRECT, 128, 128, 1>(a, p, stream);
 }
