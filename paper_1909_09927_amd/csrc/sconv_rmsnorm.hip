@@ -104,33 +104,53 @@ __global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void rms_bwd(RmsArgs a)
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[j][i] = 0.0f;
-    int turn = 0;
-    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB, turn ^= 1) {
-        const int64_t row = r0 + group;
+    float w[NV][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * LPR + lane) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[j][i] = 1.0f;
+        if (a.w && c < a.C) load8_typed(a.w, a.w_type, c, a.C - c, w[j]);
+    }
+    // AHEAD: a row is read while the one before it is worked on (two chunks of it a lane have no room for that).
+    constexpr bool AHEAD = NV == 1;
+    float next_u[NV][8], next_g[NV][8], next_d[NV][8], next_rstd = 0.0f;
+    const auto read = [&](int64_t row) __attribute__((always_inline)) {
         const bool live = row < a.rows;
-        const float rstd = live ? a.rstd_in[row] : 0.0f;
-        float u[NV][8], g[NV][8];
-        float sum = 0.0f;
+        next_rstd = live ? a.rstd_in[row] : 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * LPR + lane) * 8, have = live ? a.C - c : 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[j][i] = g[j][i] = 0.0f;
+            for (int i = 0; i < 8; ++i) next_u[j][i] = next_g[j][i] = next_d[j][i] = 0.0f;
             if (have <= 0) continue;
-            load8((const TR*)a.t + row * a.t_r + c, have, u[j]);
-            load8((const TG*)a.dy + row * a.y_r + c, have, g[j]);
-            float w[8];
+            load8((const TR*)a.t + row * a.t_r + c, have, next_u[j]);
+            load8((const TG*)a.dy + row * a.y_r + c, have, next_g[j]);
+            if (a.dt) load8((const TR*)a.dt + row * a.res_r + c, have, next_d[j]);
+        }
+    };
+    int turn = 0;
+    int64_t row = (int64_t)blockIdx.x * RPB + group;
+    const int64_t step = (int64_t)gridDim.x * RPB;
+    if (AHEAD) read(row);
+    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step, row += step, turn ^= 1) {
+        const bool live = row < a.rows;
+        if (!AHEAD) read(row);
+        const float rstd = next_rstd;
+        float u[NV][8], g[NV][8], d[NV][8];
+        float sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = 1.0f;
-            if (a.w) load8_typed(a.w, a.w_type, c, have, w);
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                u[j][i] *= rstd;
+                u[j][i] = next_u[j][i] * rstd;
+                g[j][i] = next_g[j][i];
+                d[j][i] = next_d[j][i];
                 dw[j][i] = fmaf(g[j][i], u[j][i], dw[j][i]);
-                g[j][i] *= w[i];
+                g[j][i] *= w[j][i];
                 sum = fmaf(g[j][i], u[j][i], sum);
             }
-        }
+        if (AHEAD && r0 + step < a.rows) read(row + step);
         if (!a.dx && !a.dres) continue;
         const float mean = row_sum<LPR>(sum, red[turn]) * a.inv_c;
         if (!live) continue;
@@ -138,14 +158,10 @@ __global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void rms_bwd(RmsArgs a)
         for (int j = 0; j < NV; ++j) {
             const int c = (j * LPR + lane) * 8, have = a.C - c;
             if (have <= 0) continue;
-            float d[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = 0.0f;
-            if (a.dt) load8((const TR*)a.dt + row * a.res_r + c, have, d);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = fmaf(rstd, fmaf(-u[j][i], mean, g[j][i]), d[i]);
-            if (a.dx) store8((TX*)a.dx + row * a.C + c, have, d);
-            if (a.dres) store8((TR*)a.dres + row * a.C + c, have, d);
+            for (int i = 0; i < 8; ++i) d[j][i] = fmaf(rstd, fmaf(-u[j][i], mean, g[j][i]), d[j][i]);
+            if (a.dx) store8((TX*)a.dx + row * a.C + c, have, d[j]);
+            if (a.dres) store8((TR*)a.dres + row * a.C + c, have, d[j]);
         }
     }
     if (!a.part) return;
@@ -172,14 +188,15 @@ __global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void rms_bwd(RmsArgs a)
     }
 }
 
-// dw: 32 groups of lanes add every 32nd row of the partial sums of 32 columns, then the groups are added in their order.
+// dw: 32 groups of lanes add every 32nd row of the partial sums of 32 columns, then the groups are added in their order.  Bound by latency: many
+// rows are asked for at once.
 __global__ __launch_bounds__(1024) void rms_dw_sum(const float* part, int blocks, int C, void* dw, int type)
 {
     __shared__ float sums[32][33];
     const int l = threadIdx.x & 31, g = threadIdx.x >> 5, c = blockIdx.x * 32 + l;
     float v = 0.0f;
     if (c < C)
-#pragma unroll 4
+#pragma unroll 16
         for (int b = g; b < blocks; b += 32) v += part[(int64_t)b * C + c];
     sums[g][l] = v;
     __syncthreads();
