@@ -191,22 +191,14 @@ __device__ __forceinline__ void bare_barrier()
     asm volatile("" ::: "memory");
 }
 
+// The tile of which (m0, n0) is the first token and weight row.
 template <typename T, bool FAST, bool DIRECT, int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring(LinArgs a, int tiles_m, int tiles_n)
+__device__ __forceinline__ void ring_tile(const LinArgs& a, uint8_t* lds, int m0, int n0)
 {
     typedef RingShape<WM, WN, TM, TN> Shape;
     constexpr int N = Shape::N, WAVES = Shape::WAVES, NWL = Shape::BN / 16 / WAVES, STAGES = Shape::STAGES;
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 31, h = l >> 5;
-    const int wm = w / WN, wn = w - wm * WN, total = tiles_m * tiles_n;
-    // blocks go round the chiplets: each gets a stretch of tiles, in groups of eight tiles of tokens that share their weights
-    const auto place = [&](int id, int& n0, int& m0) {
-        const int each = total / 8, more = total % 8, chip = id % 8;
-        const int lin = chip * each + min(chip, more) + id / 8, width = 8 * tiles_n, group = lin / width, in = lin - group * width;
-        const int high = min(8, tiles_m - 8 * group), tn = in / high, tm = 8 * group + in - tn * high;
-        n0 = tn * Shape::BN;
-        m0 = tm * Shape::BM;
-    };
+    const int wm = w / WN, wn = w - wm * WN;
 
     // a load is 16 rows of four chunks; lane l writes chunk l % 4 of row l / 4
     const auto row_of = [&](int i) { return ((i < NWL ? i : i - NWL) * WAVES + w) * 16 + (l >> 2); };
@@ -220,8 +212,6 @@ __global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring
     const auto slot = [&](int i, int buffer) {           // in bytes, of a load's first row
         return (buffer * Shape::ROWS + (i < NWL ? 0 : Shape::BN) + ((i < NWL ? i : i - NWL) * WAVES + w) * 16) * 64;
     };
-    int n0, m0;
-    place(blockIdx.x, n0, m0);
     int f_buffer = 0, left = a.K;                        // of the stage to be loaded: its buffer, the depth from it on
     [[maybe_unused]] const uint32_t size_w = (uint32_t)((min(a.N - n0, Shape::BN) - 1) * a.w_n), size_x = (uint32_t)((min(a.M - m0, Shape::BM) - 1) * a.x_m);
     const uint8_t* from_w = a.w + n0 * a.w_n;
@@ -442,15 +432,39 @@ __global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring
         }
 }
 
+// rest: the last so many tiles come in quarters, of 32 TM / 2 tokens and 32 TN / 2 weight rows a wavefront.
+template <typename T, bool FAST, bool DIRECT, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring(LinArgs a, int tiles_m, int tiles_n, int rest)
+{
+    typedef RingShape<WM, WN, TM, TN> Shape;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const int total = tiles_m * tiles_n, whole = total - rest, id = blockIdx.x;
+    // blocks go round the chiplets: each gets a stretch of tiles, in groups of eight tiles of tokens that share their weights
+    const int each = whole / 8, more = whole % 8, chip = id % 8;
+    const int lin = id < whole ? chip * each + min(chip, more) + id / 8 : whole + (id - whole) / 4;
+    const int width = 8 * tiles_n, group = lin / width, in = lin - group * width, high = min(8, tiles_m - 8 * group), tn = in / high, tm = 8 * group + in - tn * high;
+    const int m0 = tm * Shape::BM, n0 = tn * Shape::BN;
+    if constexpr (TM * TN > 8) {
+        if (id >= whole) {
+            const int quarter = (id - whole) % 4, m = m0 + quarter / 2 * (Shape::BM / 2), n = n0 + quarter % 2 * (Shape::BN / 2);
+            if (m < a.M && n < a.N) ring_tile<T, FAST, DIRECT, WM, WN, TM / 2, TN / 2>(a, lds, m, n);
+            return;
+        }
+    }
+    ring_tile<T, FAST, DIRECT, WM, WN, TM, TN>(a, lds, m0, n0);
+}
+
 template <typename T, bool DIRECT, int WM, int WN, int TM, int TN>
 int ring_launch(const LinArgs& a, hipStream_t stream)
 {
     typedef RingShape<WM, WN, TM, TN> Shape;
     const int64_t tiles_m = ((int64_t)a.M + Shape::BM - 1) / Shape::BM, tiles_n = ((int64_t)a.N + Shape::BN - 1) / Shape::BN;
-    if (!grid_fits(tiles_m * tiles_n, Shape::THREADS)) return SCONV_EUNSUPPORTED;
+    // A last round of tiles that would leave half of the compute units or more without work goes in quarters.
+    const int64_t last = tiles_m * tiles_n % 256, rest = TM * TN > 8 && last <= 128 ? last : 0, grid = tiles_m * tiles_n + 3 * rest;
+    if (!grid_fits(grid, Shape::THREADS)) return SCONV_EUNSUPPORTED;
     const auto kern = linear_ring<T, sizeof(T) == 2, DIRECT, WM, WN, TM, TN>;
     if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::LDS) != hipSuccess) return SCONV_ELAUNCH;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n)), dim3(Shape::THREADS), Shape::LDS, stream, a, (int)tiles_m, (int)tiles_n);
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(Shape::THREADS), Shape::LDS, stream, a, (int)tiles_m, (int)tiles_n, (int)rest);
     return launch_status();
 }
 
