@@ -64,10 +64,10 @@ __device__ __forceinline__ int units_before(const PagedArgs& a, int upto)
 }
 // Units of a stretch.
 __device__ __forceinline__ int stretch_of(const PagedArgs& a, int units) { return max((units + a.parts - 1) / a.parts, LEAST); }
-// Of stretch `at`: its first unit, counted from request b's first, and its end, likewise; false: it has none.
-__device__ __forceinline__ bool find_stretch(const PagedArgs& a, int at, int& b, int& begin, int& end)
+// Of stretch `at`: its first unit, counted from request b's first, and its end, likewise, and b's positions; false: it has none.
+__device__ __forceinline__ bool find_stretch(const PagedArgs& a, int at, int& b, int& begin, int& end, int& n)
 {
-    const int l = threadIdx.x & 63, got = l < a.B ? units_of(positions(a, l)) : 0;
+    const int l = threadIdx.x & 63;
     int all, u = 0, per = 0, base = 0;
     if (a.B > 64) {
         all = units_before(a, a.B);
@@ -76,7 +76,7 @@ __device__ __forceinline__ bool find_stretch(const PagedArgs& a, int at, int& b,
         if (u == all) return false;
     }
     for (int b0 = 0;; b0 += 64) {
-        const int mine = b0 == 0 ? got : b0 + l < a.B ? units_of(positions(a, b0 + l)) : 0;
+        const int length = b0 + l < a.B ? positions(a, b0 + l) : 0, mine = units_of(length);
         int upto = mine;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -96,6 +96,7 @@ __device__ __forceinline__ bool find_stretch(const PagedArgs& a, int at, int& b,
             const int before = base + __builtin_amdgcn_readlane(upto - mine, lane);
             begin = u - before;
             end = (int)min((int64_t)u + per, (int64_t)all) - before;
+            n = __builtin_amdgcn_readlane(length, lane);
             return true;
         }
         base += __builtin_amdgcn_readlane(upto, 63);
@@ -274,17 +275,19 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
     const int at = blockIdx.x % per_head, rest = blockIdx.x / per_head, hk = rest % a.Hkv, first = rest / a.Hkv * 16 * R;
     const int dv0 = blockIdx.z * DVT, dvn = min(DVT, a.Dv - dv0), wide = (a.Dv + 3) / 4 * 4;
 
-    int b, begin, end;                                           // the request, the stretch in units from its first
+    int b, begin, end, n;                                        // the request, the stretch in units from its first, the request's positions
     if (a.parts) {
-        if (!find_stretch(a, at, b, begin, end)) return;
+        if (!find_stretch(a, at, b, begin, end, n)) return;
     } else {
         b = at;
         begin = 0;
-        end = units_of(positions(a, b));
+        n = __builtin_amdgcn_readfirstlane(positions(a, b));
+        end = units_of(n);
     }
 
-    for (;; ++b) {
-        const int n = __builtin_amdgcn_readfirstlane(positions(a, b)), units = units_of(n);
+    for (int next_n;; ++b, n = __builtin_amdgcn_readfirstlane(next_n)) {
+        const int units = units_of(n);
+        next_n = b + 1 < a.B ? positions(a, b + 1) : 0;
         if (a.parts && units == 0) continue;
         const int u1 = min(end, units);
         int lim[R];
