@@ -186,23 +186,22 @@ def sconv_rmsnorm_forward(x, weight=None, residual=None, eps: float = 1e-6, out_
     plan = _plans.get(key)
     if plan is None:
         plan = _keep(key, _rmsnorm_plan(x, weight, residual, total, eps, out_dtype))
-    _, ref, dtype, lead, device = plan
+    _, ref, dtype, shape, blocks, device = plan
     _current(device)
     scales = sp = None
     if dtype is E4M3:
-        shape = (*lead, _blocks(x.shape[-1]))
         if out is None:
-            y, scales = torch.empty(x.shape, dtype=E4M3, device=device), torch.empty(shape, dtype=torch.uint8, device=device)
+            y, scales = x.new_empty(shape, dtype=E4M3), x.new_empty(blocks, dtype=torch.uint8)
         else:
-            y, scales = _given(out[0], x.shape, E4M3, device, "out[0]"), _given(out[1], shape, torch.uint8, device, "out[1]")
+            y, scales = _given(out[0], shape, E4M3, device, "out[0]"), _given(out[1], blocks, torch.uint8, device, "out[1]")
         sp = scales.data_ptr()
     elif out is None:
-        y = torch.empty(x.shape, dtype=dtype, device=device)
+        y = x.new_empty(shape, dtype=dtype)
     else:
-        y = _given(out, x.shape, dtype, device, "out")
+        y = _given(out, shape, dtype, device, "out")
     if residual is not None and total is None:
-        total = torch.empty(x.shape, dtype=residual.dtype, device=device)
-    rstd = torch.empty(lead, dtype=torch.float32, device=device) if stats else None
+        total = residual.new_empty(shape)
+    rstd = x.new_empty(shape[:-1], dtype=torch.float32) if stats else None
     rc = _serving_lib().sconv_rmsnorm_forward(ref, x.data_ptr(), _opt(residual), _opt(weight), y.data_ptr(), sp, _opt(total), _opt(rstd),
                                               _raw_stream(torch))
     if rc:
@@ -211,7 +210,7 @@ def sconv_rmsnorm_forward(x, weight=None, residual=None, eps: float = 1e-6, out_
 
 
 def _rmsnorm_plan(x, weight, residual, total, eps, out_dtype):
-    """(descriptor, reference to it, y's type, the rows' shape, device)"""
+    """(descriptor, reference to it, y's type, its shape and its scales', device)"""
     xt = _check(x, "x", _TYPES)
     rows, xr = _rows(x, "x")
     C = x.shape[-1]
@@ -237,7 +236,7 @@ def _rmsnorm_plan(x, weight, residual, total, eps, out_dtype):
     dtype = x.dtype if out_dtype is None else out_dtype
     yt = _KINDS.get(dtype, -1)
     desc = RmsNormDesc(rows, C, xt, tt, yt, wt, eps, xr, res_r, t_r, C)
-    return desc, ctypes.byref(desc), dtype, tuple(x.shape[:-1]), x.device
+    return desc, ctypes.byref(desc), dtype, tuple(x.shape), (*x.shape[:-1], _blocks(C)), x.device
 
 
 def sconv_rmsnorm_backward(dy, total, rstd, weight=None, dtotal=None, x_dtype=None, param_grads: bool = True, ws=None):
@@ -251,15 +250,15 @@ def sconv_rmsnorm_backward(dy, total, rstd, weight=None, dtotal=None, x_dtype=No
     plan = _plans.get(key)
     if plan is None:
         plan = _keep(key, _rmsnorm_grad_plan(dy, total, rstd, weight, dtotal, x_dtype))
-    _, ref, C, need, device = plan
+    _, ref, shape, need, device = plan
     _current(device)
-    dres = torch.empty(total.shape, dtype=total.dtype, device=device)
+    dres = total.new_empty(shape)
     narrow = x_dtype is not None and x_dtype != total.dtype
-    dx = torch.empty(total.shape, dtype=x_dtype, device=device) if narrow else None
+    dx = total.new_empty(shape, dtype=x_dtype) if narrow else None
     dw = ptr = None
     nbytes = 0
     if param_grads:
-        dw = torch.empty(C, dtype=torch.float32 if weight is None else weight.dtype, device=device)
+        dw = total.new_empty(shape[-1:], dtype=torch.float32 if weight is None else weight.dtype)
         ws, ptr, nbytes = _ws(ws, need, device)
     rc = _serving_lib().sconv_rmsnorm_backward(ref, dy.data_ptr(), total.data_ptr(), rstd.data_ptr(), _opt(weight), _opt(dtotal), _opt(dx),
                                                dres.data_ptr(), _opt(dw), ptr, nbytes, _raw_stream(torch))
@@ -269,7 +268,7 @@ def sconv_rmsnorm_backward(dy, total, rstd, weight=None, dtotal=None, x_dtype=No
 
 
 def _rmsnorm_grad_plan(dy, total, rstd, weight, dtotal, x_dtype):
-    """(descriptor, reference to it, channels, bytes of scratch, device)"""
+    """(descriptor, reference to it, the gradients' shape, bytes of scratch, device)"""
     tt = _check(total, "total", _TYPES)
     yt = _check(dy, "dy", _TYPES, None, total.device)
     if dy.shape != total.shape:
@@ -295,7 +294,7 @@ def _rmsnorm_grad_plan(dy, total, rstd, weight, dtotal, x_dtype):
     rc = _serving_lib().sconv_rmsnorm_workspace_size(ctypes.byref(desc), ctypes.byref(need))
     if rc:
         raise SconvError(rc, "sconv_rmsnorm_backward")
-    return desc, ctypes.byref(desc), C, need.value, total.device
+    return desc, ctypes.byref(desc), tuple(total.shape), need.value, total.device
 
 
 # ---- 8-bit operands and their product
@@ -307,12 +306,12 @@ def sconv_quant8(x, block_rows: int = 1, out=None):
     plan = _plans.get(key)
     if plan is None:
         plan = _keep(key, _quant8_plan(x, block_rows))
-    _, ref, shape, device = plan
+    _, ref, shape, blocks, device = plan
     _current(device)
     if out is None:
-        q, s = torch.empty(x.shape, dtype=E4M3, device=device), torch.empty(shape, dtype=torch.uint8, device=device)
+        q, s = x.new_empty(shape, dtype=E4M3), x.new_empty(blocks, dtype=torch.uint8)
     else:
-        q, s = _given(out[0], x.shape, E4M3, device, "out[0]"), _given(out[1], shape, torch.uint8, device, "out[1]")
+        q, s = _given(out[0], shape, E4M3, device, "out[0]"), _given(out[1], blocks, torch.uint8, device, "out[1]")
     rc = _serving_lib().sconv_quant8(ref, x.data_ptr(), q.data_ptr(), s.data_ptr(), _raw_stream(torch))
     if rc:
         raise SconvError(rc, "sconv_quant8")
@@ -320,13 +319,13 @@ def sconv_quant8(x, block_rows: int = 1, out=None):
 
 
 def _quant8_plan(x, block_rows):
-    """(descriptor, reference to it, the scales' shape, device)"""
+    """(descriptor, reference to it, the values' shape and the scales', device)"""
     xt = _check(x, "x", _TYPES, 2 if block_rows != 1 else None)
     M, x_m = _rows(x, "x")
     K = x.shape[-1]
     desc = Quant8Desc(M, K, xt, block_rows, x_m, K)
-    shape = (*x.shape[:-1], _blocks(K)) if block_rows == 1 else (_blocks(M), _blocks(K))
-    return desc, ctypes.byref(desc), shape, x.device
+    blocks = (*x.shape[:-1], _blocks(K)) if block_rows == 1 else (_blocks(M), _blocks(K))
+    return desc, ctypes.byref(desc), tuple(x.shape), blocks, x.device
 
 
 def sconv_linear8(x, w, out_dtype=torch.bfloat16, out=None):
@@ -341,7 +340,7 @@ def sconv_linear8(x, w, out_dtype=torch.bfloat16, out=None):
         plan = _keep(key, _linear8_plan(xv, xs, wv, wsc, out_dtype))
     _, ref, shape, device = plan
     _current(device)
-    y = torch.empty(shape, dtype=out_dtype, device=device) if out is None else _given(out, shape, out_dtype, device, "out")
+    y = xv.new_empty(shape, dtype=out_dtype) if out is None else _given(out, shape, out_dtype, device, "out")
     rc = _serving_lib().sconv_linear8(ref, xv.data_ptr(), xs.data_ptr(), wv.data_ptr(), wsc.data_ptr(), y.data_ptr(), _raw_stream(torch))
     if rc:
         raise SconvError(rc, "sconv_linear8")
@@ -452,10 +451,18 @@ def sconv_cache_read(cache: PagedCache, S: int, starts, counts=None, out_dtype=N
     heads, Dv]), contiguous; rows that are not there are zeros.  out_dtype: the cache's type; of an 8-bit cache bf16 (default, exact) or fp32."""
     k, v = cache.k, cache.v
     if out is None:
-        dtype = out_dtype or (torch.bfloat16 if k.dtype == E4M3 else k.dtype)
-        B = starts.shape[0]
-        out = (torch.empty((B, S, *k.shape[2:]), dtype=dtype, device=k.device), torch.empty((B, S, *v.shape[2:]), dtype=dtype, device=k.device))
-    _, ref, device = _cache_plan(cache, out[0], out[1], starts, counts)
+        key = (16, _cache_sig(cache), S, _sig(starts), _sig(counts), out_dtype)
+        plan = _plans.get(key)
+        if plan is None:
+            dtype = out_dtype or (torch.bfloat16 if k.dtype == E4M3 else k.dtype)
+            B = starts.shape[0]
+            out = k.new_empty((B, S, *k.shape[2:]), dtype=dtype), v.new_empty((B, S, *v.shape[2:]), dtype=dtype)
+            plan = _keep(key, (*_cache_plan(cache, *out, starts, counts), tuple(out[0].shape), tuple(out[1].shape), dtype))
+        else:
+            out = k.new_empty(plan[3], dtype=plan[5]), v.new_empty(plan[4], dtype=plan[5])
+    else:
+        plan = _cache_plan(cache, out[0], out[1], starts, counts)
+    ref, device = plan[1:3]
     _current(device)
     rc = _serving_lib().sconv_cache_read(ref, _pages_dev(cache), starts.data_ptr(), _opt(counts), out[0].data_ptr(), out[1].data_ptr(),
                                          _raw_stream(torch))
@@ -508,7 +515,7 @@ def sconv_diffattn_paged(q, cache: PagedCache, lam, lengths, scale: Optional[flo
     allocator is asked)."""
     _, ref, shape, need, device = _paged_plan(q, cache, lam, lengths, scale, causal)
     _current(device)
-    out = torch.empty(shape, dtype=q.dtype, device=device) if out is None else _given(out, shape, q.dtype, device, "out")
+    out = q.new_empty(shape) if out is None else _given(out, shape, q.dtype, device, "out")
     ws, ptr, nbytes = _ws(ws, need, device)
     rc = _serving_lib().sconv_diffattn_paged(ref, q.data_ptr(), _pages_dev(cache), lam.data_ptr(), lengths.data_ptr(), out.data_ptr(), ptr, nbytes,
                                              _raw_stream(torch))
