@@ -579,12 +579,16 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                 if (more) loads_left<U::KLOADS + U::VLOADS + U::KLOADS>();
                 else if (u + 1 < u1) loads_left<U::KLOADS + U::VLOADS>();
                 else loads_left<0>();
-                float fv[8] = {};
+                float fv[8] = {}, apart = 1.0f;
                 if constexpr (SC) {
                     const uint32_t d = *(const uint32_t*)(vt + U::V + U::SCALES + 4 * l), low = low_v[0];
                     // (what is not there counts as 1: nothing of it may reach a sum)
-                    const float f = there >> (l & 31) & 1 ? scale_of((int)(d >> (8 * low) & 255)) : 1.0f;
-                    if (l < 32) scales[64 + l] = f;
+                    const bool has = there >> (l & 31) & 1;
+                    const int byte = (int)(d >> (8 * low) & 255);
+                    // (the weights take the scales: 2^32 goes between them and the values, so that neither leaves the range of 32 bits)
+                    const bool far = __any(has && byte > 200);
+                    apart = far ? 0x1p32f : 0x1p-32f;
+                    if (l < 32) scales[64 + l] = has ? scale_of(byte) * (far ? 0x1p-32f : 0x1p32f) : 1.0f;
                     wave_lds_fence();
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
@@ -613,7 +617,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                     for (int t = t0; t < t0 + (SC ? 4 : 2); ++t) {
                         bf16x8 vf;
                         if constexpr (SC) {
-                            vf = widened(x[t - t0][0], x[t - t0][1], 1.0f);
+                            vf = widened(x[t - t0][0], x[t - t0][1], apart);
                         } else {
                             union { u32x2 u[2]; bf16x8 v; } y = {{x[2 * (t - t0)], x[2 * (t - t0) + 1]}};
                             vf = y.v;

@@ -513,6 +513,72 @@ def test_paged_scale_and_large_scores(device):
         within(got, want, bound, "out")
 
 
+#       lengths, Sq, H, Hkv, D, Dv, page: up to eight rows of a key head, pages of whole 16 slots
+FEW = [([700, 16, 0, 17], 1, 2, 2, 128, 256, 16), ([130, 1000], 2, 8, 2, 128, 128, 32), ([333, 64, 1], 1, 8, 1, 32, 64, 48), ([40] * 70, 1, 4, 4, 64, 128, 16), ([2000, 5], 8, 1, 1, 64, 256, 64)]
+
+
+@pytest.mark.parametrize("heads_first", [True, False], ids=["heads-first", "slots-first"])
+@pytest.mark.parametrize("dtype,kept", [(F32, E4M3), (BF16, E4M3), (F32, F32), (BF16, BF16)], ids=["fp32-e4m3", "bf16-e4m3", "fp32", "bf16"])
+@pytest.mark.parametrize("case", FEW, ids=lambda c: "-".join(map(str, c[1:])) + "-n" + "_".join(map(str, c[0][:4])))
+def test_paged_few_rows(device, case, dtype, kept, heads_first):
+    lengths, Sq, H, Hkv, D, Dv, page = case
+    g = gen(*case[1:])
+    cache = filled(device, g, lengths, page, Hkv, D, Dv, dtype, kept, heads_first=heads_first)
+    q = torch.randn(len(lengths), Sq, 2 * H, D, generator=g).to(dtype).to(device)
+    lam = 0.3 + 0.2 * torch.randn(H, generator=g).to(device)
+    n = torch.tensor(lengths, dtype=torch.int32, device=device)
+    for causal in (True, False):
+        want, bound = attend(q, cache, lam, lengths, None, causal)
+        within(sconv.sconv_diffattn_paged(q, cache, lam, n, causal=causal), want, bound, f"out, causal {causal}")
+
+
+@pytest.mark.parametrize("kept", [BF16, E4M3], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("off", [1, 4, 8])
+def test_paged_pages_at_odd_addresses(device, off, kept):
+    """Pools and scales that begin inside an allocation: the same results from any address."""
+    g = gen(13, off)
+    cache = filled(device, g, [300, 33], 16, 2, 64, 128, BF16, kept, True)
+    q, lam = torch.randn(2, 1, 8, 64, generator=g).to(BF16).to(device), torch.full((4,), 0.5, device=device)
+    n = torch.tensor([300, 33], dtype=torch.int32, device=device)
+
+    def moved(t, by):
+        if t is None:
+            return None
+        buf = torch.empty(t.numel() + 32, dtype=t.dtype, device=device)
+        to = buf[by:by + t.numel()].as_strided(t.shape, t.stride())
+        to.copy_(t)
+        return to
+
+    want, bound = attend(q, cache, lam, [300, 33], None, True)
+    for which in ("k", "v", "k_scales", "v_scales"):
+        got = sconv.sconv_diffattn_paged(q, cache._replace(**{which: moved(getattr(cache, which), off)}), lam, n, causal=True)
+        within(got, want, bound, which)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("page", [16, 12])
+def test_paged_of_far_scales(device, page, dtype):
+    """Values near both ends of 32 bits, and both in one request.  Scores near 0: weights near 1, whose sum of products stays in range."""
+    g = gen(14, page)
+    lengths = [100, 70, 90]
+    cache = filled(device, g, lengths, page, 2, 64, 128, dtype, E4M3, True)
+    v, vs = cache.v, cache.v_scales.clone()
+    small = torch.randint(1, 3, v.shape, generator=g) + 128 * torch.randint(0, 2, v.shape, generator=g)           # 2^-9, 2^-8, either sign
+    large = torch.randint(0x70, 0x7f, v.shape, generator=g) + 128 * torch.randint(0, 2, v.shape, generator=g)     # 128 .. 448
+    own = torch.full_like(v.view(torch.uint8), 127)
+    table = cache.table.cpu()
+    for b, (bytes_, scale) in enumerate(((small, 254), (large, 1), (small, 0))):
+        for p in table[b][:-(-lengths[b] // page)].tolist():
+            own[p] = bytes_[p].to(torch.uint8).to(device)
+            vs[p] = scale or torch.tensor([254, 1], dtype=torch.uint8).repeat(page)[:page, None].to(device)
+    cache = cache._replace(v=own.view(E4M3), v_scales=vs)
+    q, lam = (0.01 * torch.randn(3, 1, 8, 64, generator=g)).to(dtype).to(device), torch.full((4,), 0.5, device=device)
+    want, bound = attend(q, cache, lam, lengths, None, True)
+    # an addition of the matrix pipe may take what is below the smallest normal number, 2^-126, as 0: three pieces, a term a key
+    bound = bound + 3 * 100 * 1.5 * 2.0 ** -126
+    within(sconv.sconv_diffattn_paged(q, cache, lam, torch.tensor(lengths, dtype=torch.int32, device=device), causal=True), want, bound, "out")
+
+
 @pytest.mark.parametrize("kept", [BF16, E4M3], ids=["bf16", "e4m3"])
 def test_paged_offsets_past_32_bits(device, kept):
     """A pool of more than 2^32 elements whose last pages are used, by every call on a cache."""
