@@ -285,6 +285,150 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
         end = units_of(n);
     }
 
+    const P* kb = (const P*)a.k + (int64_t)hk * 2 * a.k_h;
+    const P* vb = (const P*)a.v + (int64_t)hk * a.v_h + dv0;
+    const uint8_t* kxb = a.kx + (int64_t)hk * 2 * a.kx_h;
+    const uint8_t* vxb = a.vx + (int64_t)hk * a.vx_h;
+    const int32_t* table = a.table + b * a.table_b;              // DIRECT: of the request whose units are asked for
+    // Where a unit's keys are, in three steps of an iteration each: its pages are asked for, found, read from.  DIRECT: the pages of its two
+    // halves, for the whole wavefront, and rows lie at 32-bit offsets from the halves' first; otherwise the page of key l % 32.
+    typedef __attribute__((address_space(4))) const int32_t scalar_t;
+    int entry[2] = {};
+    int page = 0, slot = 0;
+    uint32_t there_next = 0;                                 // keys of the unit that are there, as bits
+    // (DIRECT: units are asked for in turn, from one request to the next.  Of the half that is next: its place in the table, its first slot, the
+    // keys from it on; of its request: its units that have not been asked for)
+    int asked_b = b, units_left = units_of(n) - begin, next_at = 0, next_slot = 0, next_left = n - begin * BN, asked_slot[2], asked_left[2];
+    if constexpr (DIRECT) {
+        next_at = (int)divided((uint32_t)(begin * BN), a.page);
+        next_slot = begin * BN - next_at * (int)a.page.d;
+    }
+    const auto ask = [&](int u) {
+        if constexpr (DIRECT) {
+            while (units_left == 0 && asked_b + 1 < a.B) {
+                ++asked_b;
+                next_left = min(max(((scalar_t*)a.len)[asked_b], 0), a.capacity);
+                units_left = units_of(next_left);
+                table = a.table + asked_b * a.table_b;
+                next_at = next_slot = 0;
+            }
+            --units_left;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                entry[y] = ((scalar_t*)table)[min(next_at, a.width - 1)];        // (no kernel writes it while this one runs)
+                asked_slot[y] = next_slot;
+                asked_left[y] = next_left;
+                next_left -= 16;
+                next_slot += 16;
+                if (next_slot == (int)a.page.d) { next_slot = 0; ++next_at; }
+            }
+        } else {
+            entry[0] = table[min((int)divided((uint32_t)(u * BN + (l & 31)), a.page), a.width - 1)];
+        }
+    };
+    const char* kp_at[2]; const char* vp_at[2]; const uint8_t* kx_at[2]; const uint8_t* vx_at[2];    // DIRECT: the halves' first rows
+    const auto find = [&](int u) {
+        if constexpr (DIRECT) {
+            there_next = 0;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const bool ok = asked_left[y] > 0 && (uint32_t)entry[y] < (uint32_t)a.pages;
+                const uint32_t p = ok ? entry[y] : 0, s = ok ? asked_slot[y] : 0;
+                const uint32_t keys = asked_left[y] >= 16 ? 0xffffu : (1u << asked_left[y]) - 1u;
+                if (ok) there_next |= keys << (16 * y);
+                const auto from = [&](int64_t page_stride, int64_t slot_stride, int size) { return (uint64_t)p * (uint32_t)(page_stride * size) + (uint64_t)s * (uint32_t)(slot_stride * size); };
+                kp_at[y] = (const char*)kb + from(a.k_p, a.k_s, sizeof(P));
+                vp_at[y] = (const char*)vb + from(a.v_p, a.v_s, sizeof(P));
+                if constexpr (SC) {
+                    kx_at[y] = kxb + from(a.kx_p, a.kx_s, 1);
+                    vx_at[y] = vxb + from(a.vx_p, a.vx_s, 1);
+                }
+            }
+        } else {
+            const int j = u * BN + (l & 31), p = entry[0];
+            const bool ok = j < n && p >= 0 && p < a.pages;
+            page = ok ? p : 0;
+            slot = ok ? j - (int)(divided((uint32_t)j, a.page) * a.page.d) : 0;
+            there_next = (uint32_t)__ballot(ok);
+        }
+    };
+    // through registers
+    RawKey<P, KS> kr[2][2];                                  // [16 keys][map]
+    uint8_t ke[2][2] = {}, ve[NV] = {};
+    u32x4 vr[NV];
+    const auto fetch_keys = [&]() {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const int64_t p = __shfl(page, 16 * y + c), s = __shfl(slot, 16 * y + c);
+            const P* row = kb + (p * a.k_p + s * a.k_s);
+            const uint8_t* x = SC ? kxb + (p * a.kx_p + s * a.kx_s) : nullptr;
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                load_key<FULL>(kr[y][m], row + m * a.k_h, h, a.D);
+                if constexpr (SC) ke[y][m] = x[m * a.kx_h];
+            }
+        }
+    };
+    const auto fetch_values = [&]() {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int key = v * (64 / VPER) + l / VPER, d = l % VPER * E;
+            const int64_t p = __shfl(page, key), s = __shfl(slot, key);
+            const P* row = vb + (p * a.v_p + s * a.v_s);
+            if constexpr (SC) {
+                vr[v] = load16_any<FULL>((const uint8_t*)row, d, dvn);
+                ve[v] = vxb[p * a.vx_p + s * a.vx_s];
+            } else {
+                vr[v] = load16_any<FULL>(row, d, dvn);
+            }
+        }
+    };
+    // straight to LDS: a load is 1024 bytes in a row; each lane chooses the chunk of memory that belongs where its 16 bytes come to lie
+    uint32_t k_off[DIRECT ? U::HK : 1], v_off[DIRECT ? 2 : 1][DIRECT ? U::HV : 1];
+    float* scales = (float*)(lds + U::STAGES * U::SIZE);     // [2 maps, values][BN]
+    uint32_t there_of[2] = {}, low_k[2] = {}, low_v[2] = {};   // of this unit and the next: what is there, the low bits of its scales' addresses
+    if constexpr (DIRECT) {
+#pragma unroll
+        for (int i = 0; i < U::HK; ++i) {
+            const int key = (i * 64 + l) / U::CK, chunk = (l % U::CK) ^ U::turn_k(key), m = chunk / (U::CK / 2);
+            k_off[i] = (uint32_t)(key * a.k_s + m * a.k_h) * U::ES + chunk % (U::CK / 2) * 16;
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int i = 0; i < U::HV; ++i) {
+                const int key = (i * 64 + l) / U::CV, chunk = (l % U::CV) ^ U::turn_v(16 * y + key);
+                v_off[y][i] = (uint32_t)(key * a.v_s) * U::ES + chunk * 16;
+            }
+    }
+    // (a scale's dword: the four aligned bytes that its byte is one of)
+    const uint32_t kx_lane = (uint32_t)(c * a.kx_s) + (l >= 32 ? (uint32_t)a.kx_h : 0u), vx_lane = (uint32_t)(c * a.vx_s);
+    const auto scale_load = [&](const uint8_t* half0, const uint8_t* half1, uint32_t lane, uint8_t* to, uint32_t& low) {
+        const uint64_t at = (uint64_t)(l & 16 ? half1 : half0) + lane;
+        low = (uint32_t)at & 3;
+        load_to_lds((const void*)(at - low), to, true);
+    };
+    const auto send_keys = [&](int stage, uint32_t& low) {
+        uint8_t* to = (uint8_t*)lds + stage * U::SIZE;
+        if constexpr (SC) scale_load(kx_at[0], kx_at[1], kx_lane, to + U::K + U::V, low);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+#pragma unroll
+            for (int i = 0; i < U::HK; ++i) load_to_lds(kp_at[y] + k_off[i], to + (y * U::HK + i) * 1024, false);
+        }
+    };
+    const auto send_values = [&](int stage, uint32_t& low) {
+        uint8_t* to = (uint8_t*)lds + stage * U::SIZE + U::K;
+        if constexpr (SC) scale_load(vx_at[0], vx_at[1], vx_lane, to + U::V + U::SCALES, low);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+#pragma unroll
+            for (int i = 0; i < U::HV; ++i) load_to_lds(vp_at[y] + v_off[y][i], to + (y * U::HV + i) * 1024, false);
+        }
+    };
+
+    int left = end - begin, stage = 0;                           // DIRECT: the stretch's units that are not multiplied yet; where this one's are
+    bool first_request = true;
     for (int next_n;; ++b, n = __builtin_amdgcn_readfirstlane(next_n)) {
         const int units = units_of(n);
         next_n = b + 1 < a.B ? positions(a, b + 1) : 0;
@@ -314,139 +458,6 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
 #pragma unroll
                 for (int t = 0; t < NT; ++t) o[x][m][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             }
-
-        const P* kb = (const P*)a.k + (int64_t)hk * 2 * a.k_h;
-        const P* vb = (const P*)a.v + (int64_t)hk * a.v_h + dv0;
-        const uint8_t* kxb = a.kx + (int64_t)hk * 2 * a.kx_h;
-        const uint8_t* vxb = a.vx + (int64_t)hk * a.vx_h;
-        const int32_t* table = a.table + b * a.table_b;
-        // Where a unit's keys are, in three steps of an iteration each: its pages are asked for, found, read from.  DIRECT: the pages of its two
-        // halves, for the whole wavefront, and rows lie at 32-bit offsets from the halves' first; otherwise the page of key l % 32.
-        typedef __attribute__((address_space(4))) const int32_t scalar_t;
-        int entry[2] = {};
-        int page = 0, slot = 0;
-        uint32_t there_next = 0;                                 // keys of the unit that are there, as bits
-        // (DIRECT: units are asked for in turn; of the half that is next: its place in the table, its first slot, the keys from it on)
-        int next_at = 0, next_slot = 0, next_left = n - begin * BN, asked_slot[2], asked_left[2];
-        if constexpr (DIRECT) {
-            next_at = (int)divided((uint32_t)(begin * BN), a.page);
-            next_slot = begin * BN - next_at * (int)a.page.d;
-        }
-        const auto ask = [&](int u) {
-            if constexpr (DIRECT) {
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    entry[y] = ((scalar_t*)table)[min(next_at, a.width - 1)];    // (no kernel writes it while this one runs)
-                    asked_slot[y] = next_slot;
-                    asked_left[y] = next_left;
-                    next_left -= 16;
-                    next_slot += 16;
-                    if (next_slot == (int)a.page.d) { next_slot = 0; ++next_at; }
-                }
-            } else {
-                entry[0] = table[min((int)divided((uint32_t)(u * BN + (l & 31)), a.page), a.width - 1)];
-            }
-        };
-        const char* kp_at[2]; const char* vp_at[2]; const uint8_t* kx_at[2]; const uint8_t* vx_at[2];    // DIRECT: the halves' first rows
-        const auto find = [&](int u) {
-            if constexpr (DIRECT) {
-                there_next = 0;
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const bool ok = asked_left[y] > 0 && (uint32_t)entry[y] < (uint32_t)a.pages;
-                    const uint32_t p = ok ? entry[y] : 0, s = ok ? asked_slot[y] : 0;
-                    const uint32_t keys = asked_left[y] >= 16 ? 0xffffu : (1u << asked_left[y]) - 1u;
-                    if (ok) there_next |= keys << (16 * y);
-                    const auto from = [&](int64_t page_stride, int64_t slot_stride, int size) { return (uint64_t)p * (uint32_t)(page_stride * size) + (uint64_t)s * (uint32_t)(slot_stride * size); };
-                    kp_at[y] = (const char*)kb + from(a.k_p, a.k_s, sizeof(P));
-                    vp_at[y] = (const char*)vb + from(a.v_p, a.v_s, sizeof(P));
-                    if constexpr (SC) {
-                        kx_at[y] = kxb + from(a.kx_p, a.kx_s, 1);
-                        vx_at[y] = vxb + from(a.vx_p, a.vx_s, 1);
-                    }
-                }
-            } else {
-                const int j = u * BN + (l & 31), p = entry[0];
-                const bool ok = j < n && p >= 0 && p < a.pages;
-                page = ok ? p : 0;
-                slot = ok ? j - (int)(divided((uint32_t)j, a.page) * a.page.d) : 0;
-                there_next = (uint32_t)__ballot(ok);
-            }
-        };
-        // through registers
-        RawKey<P, KS> kr[2][2];                                  // [16 keys][map]
-        uint8_t ke[2][2] = {}, ve[NV] = {};
-        u32x4 vr[NV];
-        const auto fetch_keys = [&]() {
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                const int64_t p = __shfl(page, 16 * y + c), s = __shfl(slot, 16 * y + c);
-                const P* row = kb + (p * a.k_p + s * a.k_s);
-                const uint8_t* x = SC ? kxb + (p * a.kx_p + s * a.kx_s) : nullptr;
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    load_key<FULL>(kr[y][m], row + m * a.k_h, h, a.D);
-                    if constexpr (SC) ke[y][m] = x[m * a.kx_h];
-                }
-            }
-        };
-        const auto fetch_values = [&]() {
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int key = v * (64 / VPER) + l / VPER, d = l % VPER * E;
-                const int64_t p = __shfl(page, key), s = __shfl(slot, key);
-                const P* row = vb + (p * a.v_p + s * a.v_s);
-                if constexpr (SC) {
-                    vr[v] = load16_any<FULL>((const uint8_t*)row, d, dvn);
-                    ve[v] = vxb[p * a.vx_p + s * a.vx_s];
-                } else {
-                    vr[v] = load16_any<FULL>(row, d, dvn);
-                }
-            }
-        };
-        // straight to LDS: a load is 1024 bytes in a row; each lane chooses the chunk of memory that belongs where its 16 bytes come to lie
-        uint32_t k_off[DIRECT ? U::HK : 1], v_off[DIRECT ? 2 : 1][DIRECT ? U::HV : 1];
-        float* scales = (float*)(lds + U::STAGES * U::SIZE);     // [2 maps, values][BN]
-        uint32_t there_of[2] = {}, low_k[2] = {}, low_v[2] = {};   // of this unit and the next: what is there, the low bits of its scales' addresses
-        if constexpr (DIRECT) {
-#pragma unroll
-            for (int i = 0; i < U::HK; ++i) {
-                const int key = (i * 64 + l) / U::CK, chunk = (l % U::CK) ^ U::turn_k(key), m = chunk / (U::CK / 2);
-                k_off[i] = (uint32_t)(key * a.k_s + m * a.k_h) * U::ES + chunk % (U::CK / 2) * 16;
-            }
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-#pragma unroll
-                for (int i = 0; i < U::HV; ++i) {
-                    const int key = (i * 64 + l) / U::CV, chunk = (l % U::CV) ^ U::turn_v(16 * y + key);
-                    v_off[y][i] = (uint32_t)(key * a.v_s) * U::ES + chunk * 16;
-                }
-        }
-        // (a scale's dword: the four aligned bytes that its byte is one of)
-        const uint32_t kx_lane = (uint32_t)(c * a.kx_s) + (l >= 32 ? (uint32_t)a.kx_h : 0u), vx_lane = (uint32_t)(c * a.vx_s);
-        const auto scale_load = [&](const uint8_t* half0, const uint8_t* half1, uint32_t lane, uint8_t* to, uint32_t& low) {
-            const uint64_t at = (uint64_t)(l & 16 ? half1 : half0) + lane;
-            low = (uint32_t)at & 3;
-            load_to_lds((const void*)(at - low), to, true);
-        };
-        const auto send_keys = [&](int stage, uint32_t& low) {
-            uint8_t* to = (uint8_t*)lds + stage * U::SIZE;
-            if constexpr (SC) scale_load(kx_at[0], kx_at[1], kx_lane, to + U::K + U::V, low);
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-#pragma unroll
-                for (int i = 0; i < U::HK; ++i) load_to_lds(kp_at[y] + k_off[i], to + (y * U::HK + i) * 1024, false);
-            }
-        };
-        const auto send_values = [&](int stage, uint32_t& low) {
-            uint8_t* to = (uint8_t*)lds + stage * U::SIZE + U::K;
-            if constexpr (SC) scale_load(vx_at[0], vx_at[1], vx_lane, to + U::V + U::SCALES, low);
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-#pragma unroll
-                for (int i = 0; i < U::HV; ++i) load_to_lds(vp_at[y] + v_off[y][i], to + (y * U::HV + i) * 1024, false);
-            }
-        };
 
         f32x4 s[R][M][2];                                       // [rows][map][16 keys]
         Weights<T> p[R][M];
@@ -496,28 +507,30 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
         };
         int u = begin;
         if constexpr (DIRECT) {
-            if (u < u1) {
+            // the first two units' loads; those of later requests go out under the products of the ones before
+            if (first_request && left > 0) {
                 ask(u);
                 find(u);
-                if (u + 1 < u1) ask(u + 1);
+                if (left > 1) ask(u + 1);
                 there_of[0] = there_next;
                 send_keys(0, low_k[0]);
                 send_values(0, low_v[0]);
-                if (u + 1 < u1) {
+                if (left > 1) {
                     find(u + 1);
-                    if (u + 2 < u1) ask(u + 2);
+                    if (left > 2) ask(u + 2);
                     there_of[1] = there_next;
                     send_keys(1, low_k[1]);
                     send_values(1, low_v[1]);
                 }
             }
-            for (int stage = 0; u < u1; ++u, stage ^= 1) {
+            first_request = false;
+            for (; u < u1; ++u, --left, stage ^= 1) {
                 const int j0 = u * BN;
                 const uint32_t there = there_of[0];
                 uint8_t* kt = (uint8_t*)lds + stage * U::SIZE;
                 uint8_t* vt = kt + U::K;
                 // younger than this unit's keys: its values, the next unit
-                if (u + 1 < u1) loads_left<U::VLOADS + U::KLOADS + U::VLOADS>();
+                if (left > 1) loads_left<U::VLOADS + U::KLOADS + U::VLOADS>();
                 else loads_left<U::VLOADS>();
                 float fk[2][2] = {};
                 if constexpr (SC) {
@@ -566,18 +579,18 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                             }
                         }
                     }
-                const bool more = u + 2 < u1;
+                const bool more = left > 2;
                 uint32_t low_k_then = 0, low_v_then = 0;
                 if (more) {
                     find(u + 2);
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (of the products' reads)
                     send_keys(stage, low_k_then);
-                    if (u + 3 < u1) ask(u + 3);
+                    if (left > 3) ask(u + 3);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 // younger than this unit's values: the next unit, the keys of the one after it
                 if (more) loads_left<U::KLOADS + U::VLOADS + U::KLOADS>();
-                else if (u + 1 < u1) loads_left<U::KLOADS + U::VLOADS>();
+                else if (left > 1) loads_left<U::KLOADS + U::VLOADS>();
                 else loads_left<0>();
                 float fv[8] = {}, apart = 1.0f;
                 if constexpr (SC) {
@@ -639,6 +652,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
         } else {
             bf16* vt = (bf16*)lds;
             const float none[8] = {};
+            table = a.table + b * a.table_b;
             if (u < u1) {
                 ask(u);
                 find(u);
