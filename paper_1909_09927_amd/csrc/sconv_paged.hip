@@ -19,7 +19,7 @@ namespace sconv {
 namespace {
 
 constexpr int BN = 32;                   // keys of a unit
-constexpr int LEAST = 2;                 // units of a stretch at least
+constexpr int LEAST = 1;                 // units of a stretch at least
 constexpr int PLACES = 1024;             // wavefronts: one to a SIMD.  (Two: 64 requests of up to 784 35 -> 38 us, 16 of up to 32768 68 -> 71.)
 constexpr int MAX_PARTS = PLACES;
 
@@ -104,11 +104,25 @@ __device__ __forceinline__ bool find_stretch(const PagedArgs& a, int at, int& b,
     }
 }
 
-// How many of a request's n positions query i sees.
-__device__ __forceinline__ int limit_of(const PagedArgs& a, int i, int n)
+// The arguments once more, from where the kernel got them: what is wanted between requests only need not lie in scalar registers, of which the
+// loop over units has too few.
+typedef __attribute__((address_space(4))) const PagedArgs* ArgsAgain;
+__device__ __forceinline__ ArgsAgain again()
 {
-    if (!a.causal) return n;
-    const int64_t lim = (int64_t)i + n - a.Sq + 1;
+#if defined(__HIP_DEVICE_COMPILE__)
+    ArgsAgain p = (ArgsAgain)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return p;
+#else
+    return nullptr;
+#endif
+}
+
+// How many of a request's n positions query i of Sq sees.
+__device__ __forceinline__ int limit_of(int causal, int Sq, int i, int n)
+{
+    if (!causal) return n;
+    const int64_t lim = (int64_t)i + n - Sq + 1;
     return (int)(lim < 0 ? 0 : lim > n ? n : lim);
 }
 
@@ -273,7 +287,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
     const int l = threadIdx.x, c = l & 15, h = l >> 4, own_m = PAIR ? c >> 3 : 0, own_c = PAIR ? c & 7 : c;
     const int per_head = a.parts ? a.parts : a.B;
     const int at = blockIdx.x % per_head, rest = blockIdx.x / per_head, hk = rest % a.Hkv, first = rest / a.Hkv * 16 * R;
-    const int dv0 = blockIdx.z * DVT, dvn = min(DVT, a.Dv - dv0), wide = (a.Dv + 3) / 4 * 4;
+    const int dv0 = blockIdx.z * DVT, dvn = min(DVT, a.Dv - dv0);
 
     int b, begin, end, n;                                        // the request, the stretch in units from its first, the request's positions
     if (a.parts) {
@@ -305,11 +319,14 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
     }
     const auto ask = [&](int u) {
         if constexpr (DIRECT) {
-            while (units_left == 0 && asked_b + 1 < a.B) {
-                ++asked_b;
-                next_left = min(max(((scalar_t*)a.len)[asked_b], 0), a.capacity);
-                units_left = units_of(next_left);
-                table = a.table + asked_b * a.table_b;
+            if (__builtin_expect(units_left == 0, 0)) {
+                const ArgsAgain z = again();
+                do {
+                    if (++asked_b >= z->B) break;        // (not reached: there are units to ask for)
+                    next_left = min(max(((scalar_t*)z->len)[asked_b], 0), z->capacity);
+                    units_left = units_of(next_left);
+                } while (units_left == 0);
+                table = z->table + asked_b * z->table_b;
                 next_at = next_slot = 0;
             }
             --units_left;
@@ -326,23 +343,17 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
             entry[0] = table[min((int)divided((uint32_t)(u * BN + (l & 31)), a.page), a.width - 1)];
         }
     };
-    const char* kp_at[2]; const char* vp_at[2]; const uint8_t* kx_at[2]; const uint8_t* vx_at[2];    // DIRECT: the halves' first rows
+    uint32_t page_of[2], slot_of[2];                             // DIRECT: the halves' pages and first slots
     const auto find = [&](int u) {
         if constexpr (DIRECT) {
             there_next = 0;
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 const bool ok = asked_left[y] > 0 && (uint32_t)entry[y] < (uint32_t)a.pages;
-                const uint32_t p = ok ? entry[y] : 0, s = ok ? asked_slot[y] : 0;
+                page_of[y] = ok ? entry[y] : 0;
+                slot_of[y] = ok ? asked_slot[y] : 0;
                 const uint32_t keys = asked_left[y] >= 16 ? 0xffffu : (1u << asked_left[y]) - 1u;
                 if (ok) there_next |= keys << (16 * y);
-                const auto from = [&](int64_t page_stride, int64_t slot_stride, int size) { return (uint64_t)p * (uint32_t)(page_stride * size) + (uint64_t)s * (uint32_t)(slot_stride * size); };
-                kp_at[y] = (const char*)kb + from(a.k_p, a.k_s, sizeof(P));
-                vp_at[y] = (const char*)vb + from(a.v_p, a.v_s, sizeof(P));
-                if constexpr (SC) {
-                    kx_at[y] = kxb + from(a.kx_p, a.kx_s, 1);
-                    vx_at[y] = vxb + from(a.vx_p, a.vx_s, 1);
-                }
             }
         } else {
             const int j = u * BN + (l & 31), p = entry[0];
@@ -408,43 +419,73 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
         low = (uint32_t)at & 3;
         load_to_lds((const void*)(at - low), to, true);
     };
+    const auto half = [&](int y, int64_t page_stride, int64_t slot_stride, int size) {
+        return (uint64_t)page_of[y] * (uint32_t)(page_stride * size) + (uint64_t)slot_of[y] * (uint32_t)(slot_stride * size);
+    };
     const auto send_keys = [&](int stage, uint32_t& low) {
         uint8_t* to = (uint8_t*)lds + stage * U::SIZE;
-        if constexpr (SC) scale_load(kx_at[0], kx_at[1], kx_lane, to + U::K + U::V, low);
+        if constexpr (SC) scale_load(kxb + half(0, a.kx_p, a.kx_s, 1), kxb + half(1, a.kx_p, a.kx_s, 1), kx_lane, to + U::K + U::V, low);
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
+            const char* from = (const char*)kb + half(y, a.k_p, a.k_s, sizeof(P));
 #pragma unroll
-            for (int i = 0; i < U::HK; ++i) load_to_lds(kp_at[y] + k_off[i], to + (y * U::HK + i) * 1024, false);
+            for (int i = 0; i < U::HK; ++i) load_to_lds(from + k_off[i], to + (y * U::HK + i) * 1024, false);
         }
     };
     const auto send_values = [&](int stage, uint32_t& low) {
         uint8_t* to = (uint8_t*)lds + stage * U::SIZE + U::K;
-        if constexpr (SC) scale_load(vx_at[0], vx_at[1], vx_lane, to + U::V + U::SCALES, low);
+        if constexpr (SC) scale_load(vxb + half(0, a.vx_p, a.vx_s, 1), vxb + half(1, a.vx_p, a.vx_s, 1), vx_lane, to + U::V + U::SCALES, low);
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
+            const char* from = (const char*)vb + half(y, a.v_p, a.v_s, sizeof(P));
 #pragma unroll
-            for (int i = 0; i < U::HV; ++i) load_to_lds(vp_at[y] + v_off[y][i], to + (y * U::HV + i) * 1024, false);
+            for (int i = 0; i < U::HV; ++i) load_to_lds(from + v_off[y][i], to + (y * U::HV + i) * 1024, false);
         }
     };
 
     int left = end - begin, stage = 0;                           // DIRECT: the stretch's units that are not multiplied yet; where this one's are
     bool first_request = true;
+    // a lane's rows: the same in every request.  DIRECT: a request's queries are read a request ahead.
+    float lam[R];
+    const T* q_row[R];
+    int token[R];
+    typename Frag<T>::type next_q[R][M][KS];
+    const auto read_q = [&](int r) {
+        const ArgsAgain z = again();
+#pragma unroll
+        for (int x = 0; x < R; ++x)
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) next_q[x][m][s] = global_frag<false>(q_row[x] + r * z->q_b + m * z->q_h, depth_of<P, KS>(s, h), z->D);
+    };
+#pragma unroll
+    for (int x = 0; x < R; ++x) {
+        const int r = min(first + 16 * x + own_c, a.rows - 1), head = hk * a.G + r % a.G;
+        token[x] = r / a.G;
+        lam[x] = a.lam[head];
+        q_row[x] = (const T*)a.q + token[x] * a.q_s + ((int64_t)head * 2 + own_m) * a.q_h;
+    }
+    if (DIRECT) read_q(b);
     for (int next_n;; ++b, n = __builtin_amdgcn_readfirstlane(next_n)) {
         const int units = units_of(n);
-        next_n = b + 1 < a.B ? positions(a, b + 1) : 0;
-        if (a.parts && units == 0) continue;
+        const ArgsAgain z = again();
+        next_n = b + 1 < z->B ? min(max(((scalar_t*)z->len)[b + 1], 0), z->capacity) : 0;
+        if (z->parts && units == 0) {
+            if (DIRECT) read_q(b + 1);                           // (there is one: the stretch goes on)
+            continue;
+        }
         const int u1 = min(end, units);
+        if (!DIRECT) read_q(b);
         int lim[R];
         typename Frag<T>::type qf[R][M][KS];
 #pragma unroll
         for (int x = 0; x < R; ++x) {
-            const int r = min(first + 16 * x + own_c, a.rows - 1), i = r / a.G, g = r - i * a.G;
-            lim[x] = limit_of(a, i, n);
-            const T* q = (const T*)a.q + b * a.q_b + i * a.q_s + ((int64_t)(hk * a.G + g) * 2 + own_m) * a.q_h;
+            lim[x] = limit_of(z->causal, z->Sq, token[x], n);
 #pragma unroll
             for (int m = 0; m < M; ++m)
 #pragma unroll
-                for (int s = 0; s < KS; ++s) qf[x][m][s] = global_frag<false>(q + m * a.q_h, depth_of<P, KS>(s, h), a.D);
+                for (int s = 0; s < KS; ++s) qf[x][m][s] = next_q[x][m][s];
         }
         const int least = __builtin_amdgcn_readfirstlane(lim[0]);    // of the first row: limits rise
 
@@ -463,7 +504,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
         Weights<T> p[R][M];
         // scores of the keys that are not there, or not seen, go; then the weights, times their values' scales
         const auto soften = [&](int j0, uint32_t there, const float (&by)[8]) {
-            if (j0 + BN > least || there != ~0u) {
+            if (__builtin_expect(j0 + BN > least || there != ~0u, 0)) {
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -484,7 +525,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                     f32x4 (&z)[2] = s[x][m];
                     float mx = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
                     mx = half_max(quarter_max(mx)) * a.scale2;
-                    if (__any(mx > top[x][m] + 8.0f)) {
+                    if (__builtin_expect(__any(mx > top[x][m] + 8.0f), 0)) {
                         const float grown = fmaxf(top[x][m], mx);
                         safe[x][m] = grown == -INFINITY ? 0.0f : grown;
                         const float f = __builtin_amdgcn_exp2f(top[x][m] - safe[x][m]);
@@ -524,6 +565,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                 }
             }
             first_request = false;
+            if (z->parts && end > units) read_q(b + 1);          // (there is one: the stretch goes on)
             for (; u < u1; ++u, --left, stage ^= 1) {
                 const int j0 = u * BN;
                 const uint32_t there = there_of[0];
@@ -610,7 +652,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                         for (int e = 0; e < 4; ++e) fv[4 * y + e] = g[e];
                     }
                 }
-                if (there != ~0u) {
+                if (__builtin_expect(there != ~0u, 0)) {
                     for (int e = l; e < BN * U::CV; e += 64)
                         if (!(there >> (e / U::CV) & 1)) *(u32x4*)(vt + e * 16) = u32x4{0, 0, 0, 0};
                     wave_lds_fence();
@@ -722,6 +764,8 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                 settle();
             }
         }
+        const ArgsAgain f = again();
+        const int wide = (f->Dv + 3) / 4 * 4;
         const bool whole = begin == 0 && u1 == units;
 #pragma unroll
         for (int x = 0; x < R; ++x) {
@@ -729,12 +773,11 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
 #pragma unroll
             for (int m = 0; m < M; ++m) sum[x][m] = half_sum(quarter_sum(sum[x][m]));
             if (whole) {
-                const int r = min(mine, a.rows - 1), i = r / a.G, head = hk * a.G + r - i * a.G;
-                T* out = (T*)a.out + (((int64_t)b * a.Sq + i) * a.H + head) * a.Dv + dv0;
+                T* out = (T*)f->out + (((int64_t)b * f->Sq + token[x]) * f->H + hk * f->G + min(mine, f->rows - 1) % f->G) * f->Dv + dv0;
                 // (a query that sees nothing answers 0, whatever lam is)
                 const float s0 = sum[x][0], s1 = PAIR ? __shfl_xor(s0, 8) : sum[x][M - 1];
                 const bool none = own_m == 0 ? s1 == 0.0f : s0 == 0.0f;
-                const float by0 = own_m ? a.lam[head] / s0 : 1.0f / s0, by1 = PAIR ? 0.0f : a.lam[head] / s1;
+                const float by0 = own_m ? lam[x] / s0 : 1.0f / s0, by1 = PAIR ? 0.0f : lam[x] / s1;
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     float r[4];
@@ -743,22 +786,22 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                         const float other = PAIR ? __shfl_xor(o[x][0][t][e] * by0, 8) : o[x][M - 1][t][e] * by1;
                         r[e] = none ? 0.0f : fmaf(o[x][0][t][e], by0, -other);
                     }
-                    if (own_m == 0 && mine < a.rows) store4(out, 16 * t + 4 * h, dvn, a.ovec, r);
+                    if (own_m == 0 && mine < f->rows) store4(out, 16 * t + 4 * h, dvn, f->ovec, r);
                 }
-            } else if (mine < a.rows) {
-                const int64_t row = (((int64_t)hk * a.parts + at) * 2 + (begin == 0 ? 1 : 0)) * a.rows + mine;
+            } else if (mine < f->rows) {
+                const int64_t row = (((int64_t)hk * f->parts + at) * 2 + (begin == 0 ? 1 : 0)) * f->rows + mine;
 #pragma unroll
                 for (int m = 0; m < M; ++m) {
-                    if (blockIdx.z == 0 && h == 0) *(f32x2*)(a.part_ml + 4 * row + 2 * (m + own_m)) = f32x2{top[x][m], sum[x][m]};
+                    if (blockIdx.z == 0 && h == 0) *(f32x2*)(f->part_ml + 4 * row + 2 * (m + own_m)) = f32x2{top[x][m], sum[x][m]};
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         const int d = 16 * t + 4 * h;
-                        if (dv0 + d < wide) *(f32x4*)(a.part + (row * 2 + m + own_m) * wide + dv0 + d) = o[x][m][t];
+                        if (dv0 + d < wide) *(f32x4*)(f->part + (row * 2 + m + own_m) * wide + dv0 + d) = o[x][m][t];
                     }
                 }
             }
         }
-        if (!a.parts || end <= units) return;
+        if (!f->parts || end <= units) return;
         // the next request, from its first unit on
         end -= units;
         begin = 0;
