@@ -873,11 +873,13 @@ PagedPlan paged_plan(const sconv_paged_desc_t& d, const sconv_pages_dev_t* at, s
         p.direct = p.direct && last_k % 4 == 3 && last_v % 4 == 3;
     }
     if (at) p.direct = p.direct && aligned_to(at->k, 16) && aligned_to(at->v, 16) && aligned_to(at->ks, 4) && aligned_to(at->vs, 4);
-    // No more stretches than the caches can have units, or 64 MB hold parts.
+    // As many stretches as there are places for wavefronts (16-bit heads of more than 64 fill LDS with three: 16 requests over 16384, heads of 128
+    // (256), 276 -> 190 us), no more than the caches can have units, or 64 MB hold parts.
     const int64_t units = (int64_t)d.B * (((int64_t)g.table_width * g.page_size + BN - 1) / BN), base = (int64_t)d.Hkv * p.row_tiles * p.chunks;
     if (units >= (int64_t(1) << 31)) return p;
+    const int64_t places = DT == 128 && g.type == SCONV_BF16 ? PLACES * 3 / 4 : PLACES;
     const int64_t wide = (g.Dv + 3) / 4 * 4, each = (int64_t)d.Hkv * 2 * rows * (2 * wide + 4) * (int64_t)sizeof(float);
-    int64_t parts = std::max<int64_t>(std::min<int64_t>(PLACES / base, (int64_t(64) << 20) / each), 1);
+    int64_t parts = std::max<int64_t>(std::min<int64_t>(places / base, (int64_t(64) << 20) / each), 1);
     parts = std::min<int64_t>(std::min<int64_t>(parts, (units + LEAST - 1) / LEAST), MAX_PARTS);
     if ((size_t)(parts * each) > ws_bytes) return p;
     p.parts = (int)parts;
