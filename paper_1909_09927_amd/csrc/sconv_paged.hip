@@ -50,7 +50,7 @@ __device__ __forceinline__ C mma(C c, const bf16x8& a, const bf16x8x3& b)
 }
 
 __device__ __forceinline__ int positions(const PagedArgs& a, int b) { return min(max(a.len[b], 0), a.capacity); }
-__device__ __forceinline__ int units_of(int n) { return (n + BN - 1) / BN; }
+__device__ __forceinline__ int units_of(int n) { return (int)(((uint32_t)n + BN - 1) / BN); }      // (n up to 2^31 - 1)
 
 // All requests' units, and those of requests before b: every wavefront adds them up for itself.
 __device__ __forceinline__ int units_before(const PagedArgs& a, int upto)
@@ -490,7 +490,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 ? 2 : 1)) void page
         Weights<T> p[M];
         // scores of the keys that are not there, or not seen, go; then the weights, times their values' scales
         const auto soften = [&](int j0, uint32_t there, const float (&by)[8]) {
-            if (__builtin_expect(j0 + BN > least || there != ~0u, 0)) {
+            if (__builtin_expect(j0 > least - BN || there != ~0u, 0)) {
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -881,7 +881,8 @@ PagedPlan paged_plan(const sconv_paged_desc_t& d, const sconv_pages_dev_t* at, s
     const int64_t wide = (g.Dv + 3) / 4 * 4, each = (int64_t)d.Hkv * 2 * rows * (2 * wide + 4) * (int64_t)sizeof(float);
     int64_t parts = std::max<int64_t>(std::min<int64_t>(places / base, (int64_t(64) << 20) / each), 1);
     parts = std::min<int64_t>(std::min<int64_t>(parts, (units + LEAST - 1) / LEAST), MAX_PARTS);
-    if ((size_t)(parts * each) > ws_bytes) return p;
+    // (one stretch: every request is a wavefront's, as without scratch)
+    if (parts == 1 || (size_t)(parts * each) > ws_bytes) return p;
     p.parts = (int)parts;
     p.part = (size_t)(parts * d.Hkv * 2 * rows * 2 * wide) * sizeof(float);
     p.ml = (size_t)(parts * d.Hkv * 2 * rows * 4) * sizeof(float);

@@ -606,6 +606,29 @@ def test_paged_offsets_past_32_bits(device, kept):
     torch.cuda.empty_cache()
 
 
+def test_paged_the_longest_length(device):
+    """2^31 - 1 positions in one page: equal scores, so a head's answer is the mean of its values, sums of 2^31 - 1 terms."""
+    n = (1 << 31) - 1
+    k, v = torch.zeros(1, n, 2, 1, dtype=BF16, device=device), torch.ones(1, n, 1, 1, dtype=BF16, device=device)
+    table = torch.zeros(1, 1, dtype=torch.int32, device=device)
+    cache = sconv.PagedCache(k, v, table)
+    q, lam = torch.ones(1, 2, 2, 1, dtype=BF16, device=device), torch.tensor([0.25], device=device)
+    length = torch.tensor([n], dtype=torch.int32, device=device)
+    got = sconv.sconv_diffattn_paged(q, cache, lam, length, causal=True)
+    # (1 - 0.25, which 16 bits hold; sums of ones are whole numbers below 2^24 a lane, their quotients and join within 2^-20)
+    assert got.shape == (1, 2, 1, 1) and ((got.double() - 0.75).abs() <= 0.75 * U[BF16]).all()
+    # the last position, seen by the last query alone
+    v[0, -1] = float("inf")
+    got = sconv.sconv_diffattn_paged(q[:, 1:], cache, lam, length, causal=True)
+    assert not torch.isfinite(got).any()
+    got = sconv.sconv_diffattn_paged(q[:, 1:], cache, lam, length - 1, causal=True)
+    assert ((got.double() - 0.75).abs() <= 0.75 * U[BF16]).all()
+    rk, rv = sconv.sconv_cache_read(cache, 3, length - 3)
+    assert torch.isinf(rv[0, 2]).all() and (rv[0, :2] == 1).all() and (rk == 0).all()
+    del k, v, cache
+    torch.cuda.empty_cache()
+
+
 # ---- together
 
 def step(x, res, w, w_in, w_out, cache, lens, lam, freq, axes, H, Hkv, D, Dv):

@@ -160,6 +160,8 @@ def test_paged_refusals():
     for empty in (dict(Sq=0), dict(B=0), dict(Sq=0, B=0), dict(pages=_pages(table_width=0)), dict(pages=_pages(pages=0, table_width=0))):
         assert size(BY(S.PagedDesc(**{**dict(B=2, Sq=1, H=4, Hkv=2, type=0, scale=1.0, pages=_pages()), **empty})), BY(n)) == 0 and n.value == 0, empty
     assert size(BY(S.PagedDesc(B=2, Sq=1, H=4, Hkv=2, type=0, scale=1.0, pages=_pages())), None) == EINVAL
+    # many rows: as many wavefronts as the chip has places for without parts, which would take 272 MB
+    assert size(BY(S.PagedDesc(B=2, Sq=1024, H=128, Hkv=2, type=0, scale=1.0, pages=_pages(table_width=300))), BY(n)) == 0 and n.value == 0
 
 
 def test_device_tensors_are_asked_for():
