@@ -464,7 +464,8 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 ? 2 : 1)) void page
         const ArgsAgain z = again();
         next_n = b + 1 < z->B ? min(max(((scalar_t*)z->len)[b + 1], 0), z->capacity) : 0;
         if (z->parts && units == 0) {
-            if (DIRECT) read_q(b + 1);                           // (there is one: the stretch goes on)
+            if (b + 1 >= z->B) return;                           // (not reached: the stretch goes on)
+            if (DIRECT) read_q(b + 1);
             continue;
         }
         const int u1 = min(end, units);
@@ -546,7 +547,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 ? 2 : 1)) void page
                 }
             }
             first_request = false;
-            if (z->parts && end > units) read_q(b + 1);          // (there is one: the stretch goes on)
+            if (z->parts && end > units && b + 1 < z->B) read_q(b + 1);
             for (; u < u1; ++u, --left, stage ^= 1) {
                 const int j0 = u * BN;
                 const uint32_t there = there_of[0];
@@ -763,7 +764,7 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 ? 2 : 1)) void page
                 }
             }
         }
-        if (!f->parts || end <= units) return;
+        if (!f->parts || end <= units || b + 1 >= f->B) return;
         // the next request, from its first unit on
         end -= units;
         begin = 0;
@@ -793,7 +794,7 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a)
         for (int d = threadIdx.x; d < a.Dv; d += 256) out[d] = (T)0.0f;
         return;
     }
-    const int per = stretch_of(a, all), p0 = before / per, p1 = (before + units - 1) / per, count = p1 - p0 + 1;
+    const int per = stretch_of(a, all), p0 = min(before / per, a.parts - 1), p1 = min((before + units - 1) / per, a.parts - 1), count = p1 - p0 + 1;
     if (count == 1) return;                              // (answered where it was computed)
     // the first part is its wavefront's last request, the others are their wavefronts' first
     const int64_t row0 = ((int64_t)hk * a.parts + p0) * 2 * a.rows + r;
