@@ -274,7 +274,7 @@ __device__ __forceinline__ void load_to_lds(const void* from, uint8_t* to, bool 
 // 77; 27.1, 30.2).  More than 16 rows read the cache once for every 16 (two tiles of rows a wavefront: 32 rows, 8 requests over 8192, 16 bits
 // 42 -> 57 us, two requests 27 -> 34).
 template <typename T, typename P, bool FULL, bool DIRECT, int DT, int DVT, bool PAIR>
-__global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 ? 2 : 1)) void paged_attn(PagedArgs a)
+__global__ __launch_bounds__(64, (DIRECT && sizeof(T) == 2 && DT <= 64 ? 2 : 1)) void paged_attn(PagedArgs a)
 {
     typedef typename Kept<P>::type KT;
     typedef Tile<KT, BN, DVT> Values;
@@ -362,37 +362,6 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 ? 2 : 1)) void page
             page = ok ? p : 0;
             slot = ok ? j - (int)(divided((uint32_t)j, a.page) * a.page.d) : 0;
             there_next = (uint32_t)__ballot(ok);
-        }
-    };
-    // through registers
-    RawKey<P, KS> kr[2][2];                                  // [16 keys][map]
-    uint8_t ke[2][2] = {}, ve[NV] = {};
-    u32x4 vr[NV];
-    const auto fetch_keys = [&]() {
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const int64_t p = __shfl(page, 16 * y + c), s = __shfl(slot, 16 * y + c);
-            const P* row = kb + (p * a.k_p + s * a.k_s);
-            const uint8_t* x = SC ? kxb + (p * a.kx_p + s * a.kx_s) : nullptr;
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                load_key<FULL>(kr[y][m], row + m * a.k_h, h, a.D);
-                if constexpr (SC) ke[y][m] = x[m * a.kx_h];
-            }
-        }
-    };
-    const auto fetch_values = [&]() {
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int key = v * (64 / VPER) + l / VPER, d = l % VPER * E;
-            const int64_t p = __shfl(page, key), s = __shfl(slot, key);
-            const P* row = vb + (p * a.v_p + s * a.v_s);
-            if constexpr (SC) {
-                vr[v] = load16_any<FULL>((const uint8_t*)row, d, dvn);
-                ve[v] = vxb[p * a.vx_p + s * a.vx_s];
-            } else {
-                vr[v] = load16_any<FULL>(row, d, dvn);
-            }
         }
     };
     // straight to LDS: a load is 1024 bytes in a row; each lane chooses the chunk of memory that belongs where its 16 bytes come to lie
@@ -666,6 +635,36 @@ __global__ __launch_bounds__(64, (sizeof(T) == 2 && DT <= 64 ? 2 : 1)) void page
                 settle();
             }
         } else {
+            RawKey<P, KS> kr[2][2];                                  // [16 keys][map]
+            uint8_t ke[2][2] = {}, ve[NV] = {};
+            u32x4 vr[NV];
+            const auto fetch_keys = [&]() {
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int64_t p = __shfl(page, 16 * y + c), s = __shfl(slot, 16 * y + c);
+                    const P* row = kb + (p * a.k_p + s * a.k_s);
+                    const uint8_t* x = SC ? kxb + (p * a.kx_p + s * a.kx_s) : nullptr;
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        load_key<FULL>(kr[y][m], row + m * a.k_h, h, a.D);
+                        if constexpr (SC) ke[y][m] = x[m * a.kx_h];
+                    }
+                }
+            };
+            const auto fetch_values = [&]() {
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const int key = v * (64 / VPER) + l / VPER, d = l % VPER * E;
+                    const int64_t p = __shfl(page, key), s = __shfl(slot, key);
+                    const P* row = vb + (p * a.v_p + s * a.v_s);
+                    if constexpr (SC) {
+                        vr[v] = load16_any<FULL>((const uint8_t*)row, d, dvn);
+                        ve[v] = vxb[p * a.vx_p + s * a.vx_s];
+                    } else {
+                        vr[v] = load16_any<FULL>(row, d, dvn);
+                    }
+                }
+            };
             bf16* vt = (bf16*)lds;
             const float none[8] = {};
             table = a.table + b * a.table_b;
