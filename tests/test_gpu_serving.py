@@ -606,6 +606,38 @@ def test_paged_offsets_past_32_bits(device, kept):
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("H", [4, 24])
+@pytest.mark.parametrize("page", [16, 12])
+def test_paged_infinities_and_nan_stay_where_they_are(device, page, H):
+    """A query of NaN makes its own row NaN and no other; a key of -Inf in one map loses its weight in that map alone."""
+    g = gen(15, page, H)
+    lengths = [200, 40]
+    cache = filled(device, g, lengths, page, 2, 64, 128, BF16, BF16, True)
+    q, lam = torch.randn(2, 1, 2 * H, 64, generator=g).abs().to(BF16).to(device), torch.full((H,), 0.5, device=device)
+    n = torch.tensor(lengths, dtype=torch.int32, device=device)
+    want, bound = attend(q, cache, lam, lengths, None, True)
+    bad = q.clone()
+    bad[0, 0, 2 * 1 + 1, 5] = float("nan")
+    got = sconv.sconv_diffattn_paged(bad, cache, lam, n, causal=True).cpu()
+    assert torch.isnan(got[0, 0, 1]).all()
+    keep = torch.ones(2, 1, H, dtype=torch.bool)
+    keep[0, 0, 1] = False
+    within(got[keep], want[keep], bound[keep], "rows beside a NaN")
+    # position 37 of request 0: the first map's key of key head 1 (queries are positive, so its scores are -Inf)
+    at = int(cache.table[0, 37 // page])
+    cache.k[at, 37 % page, 2, 7] = -float("inf")
+    got = sconv.sconv_diffattn_paged(q, cache, lam, n, causal=True).cpu().double()
+    within(got[1], want[1], bound[1], "the other request")
+    k, v, _ = ref.gathered(cache, lengths, 0)
+    G, qd = H // 2, q[0, 0].cpu().double()
+    for h in range(H):
+        w = [torch.softmax((k[:, 2 * (h // G) + m] @ qd[2 * h + m]) / 8.0, 0) for m in (0, 1)]
+        exact = (w[0] - 0.5 * w[1]) @ v[:, h // G]
+        # the result's rounding, and 2^-16 of every weight (two 16-bit values; scores and sums in 32 bits are far closer)
+        err = exact.abs() * U[BF16] + (w[0] + 0.5 * w[1]) @ v[:, h // G].abs() * 2.0 ** -14
+        assert torch.isfinite(exact).all() and ((got[0, 0, h] - exact).abs() <= err).all(), h
+
+
 def test_paged_the_longest_length(device):
     """2^31 - 1 positions in one page: equal scores, so a head's answer is the mean of its values, sums of 2^31 - 1 terms."""
     n = (1 << 31) - 1
