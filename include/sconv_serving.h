@@ -129,7 +129,8 @@ int sconv_cache_read(const sconv_cache_desc_t* desc, const sconv_pages_dev_t* pa
  * 2g + 1) and Hv = Hkv values a slot.  Request b has lengths[b] positions (taken as 0 below 0, and as table_width * page_size above); causal:
  * the last query stands at the last of them.  A query that sees nothing gives zeros.  Keys and values behind the length, or on
  * pages that are not there, are never part of a sum; one that causal alone hides has to be finite.  Inf, and NaN as 8-bit values hold it, go
- * through the formulas.  The keys of all requests are shared out among wavefronts by their number, whose parts a second kernel joins.
+ * through the formulas.  The keys of all requests are shared out among wavefronts by their number, whose parts a second kernel joins; in short
+ * caches every request is one wavefront's.
  * For single tokens and a few (a prompt's own attention is sconv_diffattn_forward's: 16 (query, head) rows of a key head are
  * the most that one read of the cache serves).
  */

@@ -877,6 +877,10 @@ PagedPlan paged_plan(const sconv_paged_desc_t& d, const sconv_pages_dev_t* at, s
     // (256), 276 -> 190 us), no more than the caches can have units, or 64 MB hold parts.
     const int64_t units = (int64_t)d.B * (((int64_t)g.table_width * g.page_size + BN - 1) / BN), base = (int64_t)d.Hkv * p.row_tiles * p.chunks;
     if (units >= (int64_t(1) << 31)) return p;
+    // Short caches, and more of them the more requests fill the chip: a wavefront a request, without parts or a second kernel (equal lengths, split
+    // and so: one request of 128 positions 14 and 10 us, 64 with 8 heads 13.9 and 9.8, of 512 29 and 25; 512 with 8 heads, 8 bits, of 1024 253 and 215,
+    // one of 1024 among others a quarter of it at most 80 and 75, 128 such 29 and 46).
+    if ((int64_t)g.table_width * g.page_size <= 256 * std::max<int64_t>(1, d.B * base / PLACES)) return p;
     const int64_t places = DT == 128 && g.type == SCONV_BF16 ? PLACES * 3 / 4 : PLACES;
     const int64_t wide = (g.Dv + 3) / 4 * 4, each = (int64_t)d.Hkv * 2 * rows * (2 * wide + 4) * (int64_t)sizeof(float);
     int64_t parts = std::max<int64_t>(std::min<int64_t>(places / base, (int64_t(64) << 20) / each), 1);

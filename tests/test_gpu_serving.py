@@ -502,6 +502,27 @@ def test_paged_many_requests_and_spare_capacity(device):
     within(got, want, bound, "out")
 
 
+@pytest.mark.parametrize("page", [16, 20])
+def test_paged_many_short_requests(device, page):
+    """So many that no request is split: the same answers with scratch and without."""
+    g = gen(16, page)
+    lengths = [int(n) for n in torch.randint(0, 120, (300,), generator=g)]
+    lengths[5], lengths[6] = 400, 0
+    cache = filled(device, g, lengths, page, 8, 32, 64, BF16, E4M3, True)
+    q, lam = torch.randn(300, 1, 16, 32, generator=g).to(BF16).to(device), torch.full((8,), 0.4, device=device)
+    n = torch.tensor(lengths, dtype=torch.int32, device=device)
+    got = sconv.sconv_diffattn_paged(q, cache, lam, n, causal=True)
+    want, bound = attend(q, cache, lam, lengths, None, True)
+    within(got, want, bound, "out")
+    assert sconv.sconv_diffattn_paged_workspace_size(q, cache, lam, n) == 0
+    # a wider table of the same positions: split
+    wide = torch.full((300, 2000), -1, dtype=torch.int32, device=device)
+    wide[:, :cache.table.shape[1]] = cache.table
+    split = cache._replace(table=wide)
+    assert sconv.sconv_diffattn_paged_workspace_size(q, split, lam, n) > 0
+    within(sconv.sconv_diffattn_paged(q, split, lam, n, causal=True), want, bound, "out, split")
+
+
 def test_paged_scale_and_large_scores(device):
     g = gen(11)
     cache = filled(device, g, [300, 77], 16, 2, 64, 128, F32, F32, False)
