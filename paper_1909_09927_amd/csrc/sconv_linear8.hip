@@ -12,6 +12,7 @@
 // Layout of the products: weights are A, tokens are B, so that a lane's results are neighbours of one token's row.  Which depths of a block a
 // lane holds does not matter, as long as both operands have the same.
 #include <algorithm>
+#include <type_traits>
 
 #include "sconv_serving_common.h"
 
@@ -174,7 +175,7 @@ struct RingShape {
     static constexpr int OUT = 4096;                                     // of a wavefront's results on their way out, in the ring
     static constexpr int RING = STAGES * ROWS * 64, CHUNK = 120;         // blocks whose scales are in LDS: of the tokens, then of the weights
     static_assert(WAVES * OUT <= RING, "results go out through the ring");
-    static constexpr size_t LDS = (size_t)RING + CHUNK * (BM + BN / 128);
+    static constexpr size_t LDS = (size_t)RING + CHUNK * (BM + BN / 128) + WAVES;
 };
 
 // vmcnt(n) lgkmcnt(0): all loads but the n youngest have come, and all reads of LDS
@@ -193,10 +194,19 @@ __device__ __forceinline__ void bare_barrier()
     asm volatile("" ::: "memory");
 }
 
-// The tile of which (m0, n0) is the first token and weight row.
-template <typename T, bool FAST, bool DIRECT, int WM, int WN, int TM, int TN>
-__device__ __forceinline__ void ring_tile(const LinArgs& a, uint8_t* lds, int m0, int n0)
+// What a tile's scales may be.  PIPE: anything, 8-bit products take them as operands.  16-bit products: tokens take both operands' scales, 2^by.  Values
+// are 2^-9 to 448, so with 2^-108 to 2^100 no token leaves the range of 16 bits, and no product or sum of products, a multiple of
+// 2^(by - 18), that of normal numbers.  NEAR: scales of 2^-54 to 2^50, of which any two are such.  ZEROS: others too, but two that are beyond these
+// ends belong to zeros (whose blocks have the smallest scale).  FAR: anything, a stage's sums take the scales.
+// (4096 x 8192 to 8192, every other token zeros, 32-bit results: 388 us in ZEROS, which looks at the values, 365 where nobody does.  Looked for in
+// every call: 411 us for ordinary scales, 400 this way.)
+enum { PIPE, NEAR, ZEROS, FAR };
+
+// The tile of which (m0, n0) is the first token and weight row.  false: nothing is written, its scales are others.
+template <typename T, int SCALES, bool DIRECT, int WM, int WN, int TM, int TN>
+__device__ __forceinline__ bool ring_tile(const LinArgs& a, uint8_t* lds, int m0, int n0)
 {
+    constexpr bool FAST = SCALES == PIPE;
     typedef RingShape<WM, WN, TM, TN> Shape;
     constexpr int N = Shape::N, WAVES = Shape::WAVES, NWL = Shape::BN / 16 / WAVES, STAGES = Shape::STAGES;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 31, h = l >> 5;
@@ -251,21 +261,42 @@ __device__ __forceinline__ void ring_tile(const LinArgs& a, uint8_t* lds, int m0
     // token and block, they cost more than the operands (4096 x 8192 to 8192 284 us, without them 219).
     uint8_t* x_scales = lds + Shape::RING;
     uint8_t* w_scales = x_scales + Shape::CHUNK * Shape::BM;
+    // what a wavefront has to tell the others, behind a barrier
+    uint8_t* told = w_scales + Shape::BN / 128 * Shape::CHUNK;
+    const auto say = [&](bool yes) {
+        if (l == 0) told[w] = yes;
+    };
+    const auto met = [&]() {
+        int any = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) any |= told[i];
+        return any != 0;
+    };
     const auto stretch = [&](int kb0) {
         const int count = min(Shape::CHUNK, a.KB - kb0);
+        [[maybe_unused]] bool odd = false;               // outside 2^-54 .. 2^50, of which any two make no sum that is far
+        const auto look = [&](int byte) {
+            if constexpr (SCALES == NEAR) odd = odd || (uint32_t)(byte - 73) > 177u - 73u;
+        };
         for (int r = threadIdx.x; r < Shape::BM; r += Shape::THREADS) {
             const uint8_t* from = a.xs + (int64_t)min(m0 + r, a.M - 1) * a.KB + kb0;
             for (int k = 0; k < count; k += 16) {
                 const i32x4 v = bytes16(from + k, count - k);
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (k + i < count) x_scales[(k + i) * Shape::BM + r] = (uint8_t)(v[i >> 2] >> (8 * (i & 3)));
+                    if (k + i < count) {
+                        const int byte = v[i >> 2] >> (8 * (i & 3)) & 255;
+                        x_scales[(k + i) * Shape::BM + r] = (uint8_t)byte;
+                        look(byte);
+                    }
             }
         }
         for (int e = threadIdx.x; e < Shape::BN / 128 * count; e += Shape::THREADS) {
-            const int n = e / count, k = e - n * count;
-            w_scales[n * Shape::CHUNK + k] = a.ws[(int64_t)min((n0 >> 7) + n, (a.N - 1) >> 7) * a.KB + kb0 + k];
+            const int n = e / count, k = e - n * count, byte = a.ws[(int64_t)min((n0 >> 7) + n, (a.N - 1) >> 7) * a.KB + kb0 + k];
+            w_scales[n * Shape::CHUNK + k] = (uint8_t)byte;
+            look(byte);
         }
+        if constexpr (SCALES == NEAR) say(__any(odd));
     };
     int we = 0, xe[TM] = {}, we_next = 0, xe_next[TM] = {};
     const auto load_scales = [&](int k) {                // of block k of the stretch
@@ -296,13 +327,37 @@ __device__ __forceinline__ void ring_tile(const LinArgs& a, uint8_t* lds, int m0
         f.w[t] = frag(first + (wn * TN + t) * 32);
         f.x[t] = frag(first + Shape::BN + (wm * TM + t) * 32);
     };
+    [[maybe_unused]] int far = 0;
     const auto multiply = [&](const Frags& f, int t) {
         if constexpr (FAST) {
 #pragma unroll
             for (int n = 0; n < TN; ++n) sum[t][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.w[n], f.x[t], sum[t][n], 0, 0, 0, we, 0, xe[t]);
+        } else if constexpr (SCALES == FAR) {
+#pragma unroll
+            for (int n = 0; n < TN; ++n) {
+                f32x16 p = {};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widened(f.w[n][2 * i], f.w[n][2 * i + 1]), widened(f.x[t][2 * i], f.x[t][2 * i + 1]), p, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[t][n][e] += __builtin_ldexpf(p[e], we + xe[t] - 254);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         } else {
-            // (the tokens take both scales: a product whose scale passes 2^119 is out of their range)
-            const float e = __builtin_ldexpf(1.0f, we + xe[t] - 254);
+            int by = we + xe[t] - 254;
+            if constexpr (SCALES == ZEROS) {
+                const int said = by;
+                uint32_t xb = 0, wb = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    xb |= (uint32_t)f.x[t][i];
+#pragma unroll
+                    for (int n = 0; n < TN; ++n) wb |= (uint32_t)f.w[n][i];
+                }
+                by = min(max(said, -108), 100);
+                far |= (int)(__ballot(by != said && (xb & 0x7f7f7f7fu)) != 0) & (int)(__ballot((wb & 0x7f7f7f7fu) != 0) != 0);
+            }
+            const float e = __builtin_ldexpf(1.0f, by);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bf16x8 xv = widened(f.x[t][2 * i], f.x[t][2 * i + 1], e);
@@ -374,6 +429,12 @@ __device__ __forceinline__ void ring_tile(const LinArgs& a, uint8_t* lds, int m0
         stretch(kb0);
         if constexpr (DIRECT) loads_left<2 * N>();       // (of the first stage, at the start)
         __syncthreads();
+        if constexpr (SCALES == NEAR) {
+            if (met()) {
+                far = 1;
+                break;
+            }
+        }
         load_scales(0);
         take_scales();
         if (kb0 == 0) {
@@ -399,6 +460,14 @@ __device__ __forceinline__ void ring_tile(const LinArgs& a, uint8_t* lds, int m0
     if constexpr (DIRECT) loads_left<0>();
     __syncthreads();
     step();
+    if constexpr (SCALES == NEAR || SCALES == ZEROS) {
+        say(far);
+        __syncthreads();
+        if (met()) {
+            __syncthreads();
+            return false;
+        }
+    }
     const int out_n = n0 + wn * TN * 32, out_m = m0 + wm * TM * 32;
     // 32 tokens by as many results as 4 KB hold, a row of 16-byte chunks turned by the token
     constexpr int WIDE = Shape::OUT / 32 / (int)sizeof(T) < TN * 32 ? Shape::OUT / 32 / (int)sizeof(T) : TN * 32, E = 16 / (int)sizeof(T), CH = WIDE / E;
@@ -432,6 +501,7 @@ __device__ __forceinline__ void ring_tile(const LinArgs& a, uint8_t* lds, int m0
             }
             wave_lds_fence();
         }
+    return true;
 }
 
 // rest: so many tiles, the last, come in quarters, of 32 TM / 2 tokens and 32 TN / 2 weight rows a wavefront; they go first, which also keeps the
@@ -447,14 +517,29 @@ __global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring
     const int lin = id >= 0 ? chip * each + min(chip, more) + id / 8 : whole + (int)blockIdx.x / 4;
     const int width = 8 * tiles_n, group = lin / width, in = lin - group * width, high = min(8, tiles_m - 8 * group), tn = in / high, tm = 8 * group + in - tn * high;
     const int m0 = tm * Shape::BM, n0 = tn * Shape::BN;
+    constexpr int FIRST = FAST ? PIPE : NEAR;
+    constexpr int SM = TM > 2 ? TM / 2 : TM, SN = TN > 2 ? TN / 2 : TN;      // FAR holds a stage's sums, too, for which larger tiles have no room
+    const auto small = [&](int m, int n) __attribute__((always_inline)) {
+        if (m >= a.M || n >= a.N || ring_tile<T, FIRST, DIRECT, WM, WN, SM, SN>(a, lds, m, n)) return;
+        if constexpr (!FAST)
+            if (!ring_tile<T, ZEROS, DIRECT, WM, WN, SM, SN>(a, lds, m, n)) ring_tile<T, FAR, DIRECT, WM, WN, SM, SN>(a, lds, m, n);
+    };
     if constexpr (TM * TN > 8) {
-        if (id < 0) {
-            const int quarter = blockIdx.x % 4, m = m0 + quarter / 2 * (Shape::BM / 2), n = n0 + quarter % 2 * (Shape::BN / 2);
-            if (m < a.M && n < a.N) ring_tile<T, FAST, DIRECT, WM, WN, TM / 2, TN / 2>(a, lds, m, n);
-            return;
+        int part = (int)blockIdx.x % 4, parts = 1;
+        if (id >= 0) {
+            if (ring_tile<T, FIRST, DIRECT, WM, WN, TM, TN>(a, lds, m0, n0)) return;
+            if constexpr (!FAST)
+                if (ring_tile<T, ZEROS, DIRECT, WM, WN, TM, TN>(a, lds, m0, n0)) return;
+            part = 0;
+            parts = 4;
         }
+        for (; parts > 0; --parts, ++part) {
+            small(m0 + part / 2 * (Shape::BM / 2), n0 + part % 2 * (Shape::BN / 2));
+            __syncthreads();
+        }
+    } else {
+        small(m0, n0);
     }
-    ring_tile<T, FAST, DIRECT, WM, WN, TM, TN>(a, lds, m0, n0);
 }
 
 template <typename T, bool DIRECT, int WM, int WN, int TM, int TN>
