@@ -3,11 +3,13 @@
 // Few rows (up to 64, single tokens): bound by the weights' read, and by what every workgroup reads of the tokens.  A workgroup takes 16 or 32 weight
 // rows, its eight wavefronts share out the blocks of 128, read operands from memory straight into the product's registers and meet in LDS.
 // Many rows: tiles through LDS, bound by the matrix pipe, or by the results' write where the depth is small.
-// Measured, 16-bit results: 16 x 2048 to 8192 6.7 us (2.6 TB/s), 64 x 8192 to 8192 34; 12544 x 2048 to 8192 210 (2004 TFLOP/s),
+// Measured, 16-bit results: 16 x 2048 to 8192 6.7 us (2.6 TB/s), 64 x 8192 to 8192 36; 12544 x 2048 to 8192 210 (2004 TFLOP/s),
 // 4096 x 8192 to 8192 222 (2481), 25088 x 512 to 2048 48 (1087), 6272 x 896 to 1000 15.  A tile of 256 x 256 costs 4.3 us beside its depth, 13 us for 1000.
-// Up to 16 rows, and in 32-bit results, the 8-bit values become 16-bit ones, exactly, and products are exact to 32 bits.  16-bit results of more
-// rows take 8-bit products with the scales as operands; the matrix pipe takes eight products at a time and cuts off what lies 2^-13 or more
-// below the largest of them (measured: 1.4e-5 of a result's norm, at any depth), which rounding to 16 bits hides.
+// Up to 64 rows, in 32-bit results and with `exact` the 8-bit values become 16-bit ones, exactly, and products are exact to 32 bits.  Other 16-bit
+// results take 8-bit products with the scales as operands, at nearly twice the rate (12544 x 2048 to 8192 207 to 217 us, with `exact` 353;
+// 784 x 2048 to 2048 12.3 and 19.1).  The matrix pipe takes eight products at a time and cuts off what lies 2^-13 or more below the largest of
+// them: of normal values 1.4e-5 of a result's norm at any depth, which rounding to 16 bits (1.7e-3) hides; where the largest products cancel it
+// shows (two channels of 1000 times the rest with opposite signs, depth 256: 1.1e-2), so it is the caller's choice.
 //
 // Layout of the products: weights are A, tokens are B, so that a lane's results are neighbours of one token's row.  Which depths of a block a
 // lane holds does not matter, as long as both operands have the same.
@@ -62,8 +64,9 @@ __device__ __forceinline__ void store_row4(T* p, int have, bool vec, const float
 }
 
 // Few rows: MT tiles of 16 tokens against NT tiles of 16 weight rows, NW wavefronts.  A lane has 32 bytes (l / 16) * 32.. of row l % 16 of both
-// operands.  FAST: 8-bit products with their scales; otherwise 16-bit ones of the converted values.
-template <typename T, bool FAST, int MT, int NT, int NW>
+// operands.  Products are 16-bit ones of the converted values, whatever the result's type: the memory is what they wait for (64 x 8192 to 8192
+// 36.3 us, by 8-bit products 34.2; 64 x 2048 to 8192 11.0 and 10.1).
+template <typename T, int MT, int NT, int NW>
 __global__ __launch_bounds__(64 * NW) void linear_few(LinArgs a)
 {
     __shared__ f32x4 part[NW][MT * NT][64];
@@ -104,44 +107,29 @@ __global__ __launch_bounds__(64 * NW) void linear_few(LinArgs a)
     if (w < a.KB) fetch(w);
     for (int kb = w; kb < a.KB; kb += NW) {
         const bool more = kb + NW < a.KB;
-        if constexpr (FAST) {
-            Raw32 wn[NT], xn[MT];
-            int en[MT];
-            const int wen = we;
+        bf16x8 wf[NT][4], xf[MT][4];
+        int e[MT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) wn[n] = wv[n];
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int t = 0; t < MT; ++t) { xn[t] = xv[t]; en[t] = xe[t]; }
-            if (more) fetch(kb + NW);
+            for (int s = 0; s < 4; ++s) wf[n][s] = widened(wv[n].v[2 * s], wv[n].v[2 * s + 1]);
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
+        for (int t = 0; t < MT; ++t) {
+            e[t] = we + xe[t] - 254;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) sum[t][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wn[n].v, xn[t].v, sum[t][n], 0, 0, 0, wen, 0, en[t]);
-        } else {
-            bf16x8 wf[NT][4], xf[MT][4];
-            int e[MT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int s = 0; s < 4; ++s) wf[n][s] = widened(wv[n].v[2 * s], wv[n].v[2 * s + 1]);
-#pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                e[t] = we + xe[t] - 254;
-#pragma unroll
-                for (int s = 0; s < 4; ++s) xf[t][s] = widened(xv[t].v[2 * s], xv[t].v[2 * s + 1]);
-            }
-            if (more) fetch(kb + NW);
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[n][s], xf[t][s], p, 0, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[t][n][i] += __builtin_ldexpf(p[i], e[t]);
-                }
+            for (int s = 0; s < 4; ++s) xf[t][s] = widened(xv[t].v[2 * s], xv[t].v[2 * s + 1]);
         }
+        if (more) fetch(kb + NW);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = 0; s < 4; ++s) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[n][s], xf[t][s], p, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[t][n][i] += __builtin_ldexpf(p[i], e[t]);
+            }
         // (18 wait states are what the longest product needs: seen in another kernel, the compiler counts too few where a result's first
         // reader stands behind a loop's exit)
         asm volatile("s_nop 15\n\ts_nop 3");
@@ -542,7 +530,7 @@ __global__ __launch_bounds__(64 * WM * WN, TM * TN > 8 ? 1 : 2) void linear_ring
     }
 }
 
-template <typename T, bool DIRECT, int WM, int WN, int TM, int TN>
+template <typename T, bool FAST, bool DIRECT, int WM, int WN, int TM, int TN>
 int ring_launch(const LinArgs& a, hipStream_t stream)
 {
     typedef RingShape<WM, WN, TM, TN> Shape;
@@ -550,37 +538,36 @@ int ring_launch(const LinArgs& a, hipStream_t stream)
     // Where whole tiles would leave half of the compute units or more without one in their last round, so many go in quarters.
     const int64_t last = tiles_m * tiles_n % 256, rest = TM * TN > 8 && last <= 128 ? last : 0, grid = tiles_m * tiles_n + 3 * rest;
     if (!grid_fits(grid, Shape::THREADS)) return SCONV_EUNSUPPORTED;
-    const auto kern = linear_ring<T, sizeof(T) == 2, DIRECT, WM, WN, TM, TN>;
+    const auto kern = linear_ring<T, FAST, DIRECT, WM, WN, TM, TN>;
     if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::LDS) != hipSuccess) return SCONV_ELAUNCH;
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(Shape::THREADS), Shape::LDS, stream, a, (int)tiles_m, (int)tiles_n, (int)rest);
     return launch_status();
 }
 
-template <typename T, bool FAST, int MT, int NT, int NW>
+template <typename T, int MT, int NT, int NW>
 int few_launch(const LinArgs& a, hipStream_t stream)
 {
     const int64_t grid = ((int64_t)a.N + 16 * NT - 1) / (16 * NT);
     if (!grid_fits(grid, 64 * NW)) return SCONV_EUNSUPPORTED;
-    hipLaunchKernelGGL((linear_few<T, FAST, MT, NT, NW>), dim3((unsigned)grid), dim3(64 * NW), 0, stream, a);
+    hipLaunchKernelGGL((linear_few<T, MT, NT, NW>), dim3((unsigned)grid), dim3(64 * NW), 0, stream, a);
     return launch_status();
 }
 
-template <typename T>
+template <typename T, bool FAST>
 int linear_run(const LinArgs& a, hipStream_t stream)
 {
-    constexpr bool FAST = sizeof(T) == 2;
     // Two weight tiles a workgroup share what it reads of the tokens, where one fills the chip twice (16 tokens, 2048 to 8192: 7.7 -> 6.4 us, 64 tokens
     // 15.3 -> 9.8); with fewer rows they leave compute units idle (2048 to 2048, 16 tokens: 5.0 -> 5.9).  Tiles through LDS take over where
-    // they are ahead by and large: at 64 tokens 2048 to 8192 11.7 us against 9.8, 1024 to 16384 9.0 against 11.6, 8192 to 8192 47 against 34.
+    // they are ahead by and large (8-bit products: at 64 tokens 2048 to 8192 11.7 us against 9.8, 1024 to 16384 9.0 against 11.6, 8192 to 8192 47 against 34).
     const bool two = a.N >= 4096;
-    if (a.M <= 16) return two ? few_launch<T, false, 1, 2, 8>(a, stream) : few_launch<T, false, 1, 1, 8>(a, stream);
-    if (a.M <= 32) return two ? few_launch<T, FAST, 2, 2, 8>(a, stream) : few_launch<T, FAST, 2, 1, 8>(a, stream);
-    if (a.M <= 64) return two ? few_launch<T, FAST, 4, 2, 8>(a, stream) : few_launch<T, FAST, 4, 1, 8>(a, stream);
+    if (a.M <= 16) return two ? few_launch<T, 1, 2, 8>(a, stream) : few_launch<T, 1, 1, 8>(a, stream);
+    if (a.M <= 32) return two ? few_launch<T, 2, 2, 8>(a, stream) : few_launch<T, 2, 1, 8>(a, stream);
+    if (a.M <= 64) return two ? few_launch<T, 4, 2, 8>(a, stream) : few_launch<T, 4, 1, 8>(a, stream);
     // (a tile has to lie within what a buffer's offsets reach)
     const bool direct = (a.K | a.x_m | a.w_n) % 16 == 0 && aligned_to(a.x, 16) && aligned_to(a.w, 16) && a.x_m < (int64_t(1) << 22) && a.w_n < (int64_t(1) << 22);
     const int64_t big = (((int64_t)a.M + 255) / 256) * (((int64_t)a.N + 255) / 256);
-    if (direct && big >= 256) return ring_launch<T, true, 2, 2, 4, 4>(a, stream);
-    return direct ? ring_launch<T, true, 2, 2, 2, 2>(a, stream) : ring_launch<T, false, 2, 2, 2, 2>(a, stream);
+    if (direct && big >= 256) return ring_launch<T, FAST, true, 2, 2, 4, 4>(a, stream);
+    return direct ? ring_launch<T, FAST, true, 2, 2, 2, 2>(a, stream) : ring_launch<T, FAST, false, 2, 2, 2, 2>(a, stream);
 }
 
 }  // namespace
@@ -592,7 +579,8 @@ int launch_linear8(const sconv_linear8_desc_t& d, const void* x, const uint8_t* 
     a.M = d.M; a.N = d.N; a.K = d.K; a.KB = (int)(((int64_t)d.K + 127) / 128);
     a.x_m = d.x_m; a.w_n = d.w_n; a.y_m = d.y_m;
     a.vec = d.y_m % 4 == 0 && aligned_to(y, 16);
-    return d.y_type == SCONV_BF16 ? linear_run<bf16>(a, stream) : linear_run<float>(a, stream);
+    if (d.y_type != SCONV_BF16) return linear_run<float, false>(a, stream);
+    return d.exact ? linear_run<bf16, false>(a, stream) : linear_run<bf16, true>(a, stream);
 }
 
 }  // namespace sconv

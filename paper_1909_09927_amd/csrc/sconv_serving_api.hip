@@ -28,6 +28,7 @@ int check_quant8(const sconv_quant8_desc_t* d)
 int check_linear8(const sconv_linear8_desc_t* d)
 {
     if (!d || d->M < 0 || d->N < 0 || d->K < 0 || !type_known(d->y_type) || d->x_m < 0 || d->w_n < 0 || d->y_m < 0) return SCONV_EINVAL;
+    if (d->exact != 0 && d->exact != 1) return SCONV_EINVAL;
     return d->M > 1 << 30 || d->N > 1 << 30 || d->K > 1 << 30 ? SCONV_EUNSUPPORTED : SCONV_OK;
 }
 

@@ -39,7 +39,7 @@ class Quant8Desc(ctypes.Structure):
 
 class Linear8Desc(ctypes.Structure):
     """sconv_linear8_desc_t"""
-    _fields_ = [(n, _i32) for n in ("M", "N", "K", "y_type")] + [(n, _i64) for n in ("x_m", "w_n", "y_m")]
+    _fields_ = [(n, _i32) for n in ("M", "N", "K", "y_type")] + [(n, _i64) for n in ("x_m", "w_n", "y_m")] + [("exact", _i32)]
 
 
 class PagesDesc(ctypes.Structure):
@@ -328,16 +328,18 @@ def _quant8_plan(x, block_rows):
     return desc, ctypes.byref(desc), tuple(x.shape), blocks, x.device
 
 
-def sconv_linear8(x, w, out_dtype=torch.bfloat16, out=None):
+def sconv_linear8(x, w, out_dtype=torch.bfloat16, out=None, exact: bool = False):
     """Product of 8-bit operands: y[..., n] = sum_k x[..., k] w[n, k], both as the values that they stand for.
 
     x: (values [..., K], scales [..., ceil(K / 128)]), as sconv_quant8(x) and sconv_rmsnorm_forward give them; w: (values [N, K], scales
-    [ceil(N / 128), ceil(K / 128)]), sconv_quant8(weights, 128) once.  out_dtype: bf16 or fp32."""
+    [ceil(N / 128), ceil(K / 128)]), sconv_quant8(weights, 128) once.  out_dtype: bf16 or fp32.  exact: exact products for bf16 results of more
+    than 64 rows, too (fp32 ones always have them); without it the matrix pipe cuts off what is far below the largest of eight."""
     (xv, xs), (wv, wsc) = x, w
-    key = (13, _sig(xv), _sig(xs), _sig(wv), _sig(wsc), out_dtype)
+    exact = bool(exact)
+    key = (13, _sig(xv), _sig(xs), _sig(wv), _sig(wsc), out_dtype, exact)
     plan = _plans.get(key)
     if plan is None:
-        plan = _keep(key, _linear8_plan(xv, xs, wv, wsc, out_dtype))
+        plan = _keep(key, _linear8_plan(xv, xs, wv, wsc, out_dtype, exact))
     _, ref, shape, device = plan
     _current(device)
     y = xv.new_empty(shape, dtype=out_dtype) if out is None else _given(out, shape, out_dtype, device, "out")
@@ -347,7 +349,7 @@ def sconv_linear8(x, w, out_dtype=torch.bfloat16, out=None):
     return y
 
 
-def _linear8_plan(xv, xs, wv, wsc, out_dtype):
+def _linear8_plan(xv, xs, wv, wsc, out_dtype, exact):
     """(descriptor, reference to it, y's shape, device)"""
     _check(xv, "x's values", (E4M3,))
     _check(wv, "w's values", (E4M3,), 2, xv.device)
@@ -359,7 +361,7 @@ def _linear8_plan(xv, xs, wv, wsc, out_dtype):
         _check(s, what, (torch.uint8,), None, xv.device)
         if s.shape != torch.Size(shape) or not s.is_contiguous():
             raise ValueError(f"{what} must be contiguous, of shape {shape}")
-    desc = Linear8Desc(M, N, K, _TYPES.get(out_dtype, -1), x_m, w_n, N)
+    desc = Linear8Desc(M, N, K, _TYPES.get(out_dtype, -1), x_m, w_n, N, exact)
     return desc, ctypes.byref(desc), (*xv.shape[:-1], N), xv.device
 
 

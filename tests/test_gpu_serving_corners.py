@@ -53,7 +53,9 @@ def test_linear8_of_products_at_both_ends(device, M, N, K):
         want, bound = _product(x, w, F32)
         assert (want != 0).any() and want.abs().max() < 3e38
         for xd, wd in _both(x, w, device):
-            within(sconv.sconv_linear8(xd, wd, out_dtype=F32), want, bound, f"scales {a}, {b}")
+            y = sconv.sconv_linear8(xd, wd, out_dtype=F32)
+            within(y, want, bound, f"scales {a}, {b}")
+            assert torch.equal(sconv.sconv_linear8(xd, wd, exact=True), y.to(BF16)), f"scales {a}, {b}, rounded"
 
 
 @pytest.mark.parametrize("M,N,K", FAR)
@@ -91,3 +93,66 @@ def test_linear8_of_a_far_block_behind_ordinary_ones(device, M, N):
     want, bound = _product((xq, xs), (wq, ws), F32)
     for xd, wd in _both((xq, xs), (wq, ws), device):
         within(sconv.sconv_linear8(xd, wd, out_dtype=F32), want, bound, "y")
+
+
+# ---- the product: 16-bit results by exact products, and by the matrix pipe's 8-bit ones
+
+def _cancelling(M, N, K, g):
+    """Two channels of 1000 times the rest, whose products take each other away but for their rounding to 8 bits."""
+    x, w = torch.randn(M, K, generator=g), torch.randn(N, K, generator=g)
+    x[:, 5], x[:, K - 9], w[:, K - 9] = 1000.0, -1000.0, w[:, 5]
+    return [(torch.from_numpy(q).view(E4M3), torch.from_numpy(s)) for q, s in (ref.quant8(x), ref.quant8(w, 128))]
+
+
+SHAPES = [(3, 40, 256), (17, 300, 256), (64, 300, 256), (33, 4200, 130), (65, 300, 256), (300, 300, 2048), (4096, 4096, 256)]
+
+
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_linear8_exact(device, M, N, K):
+    """16-bit results that are the 32-bit ones rounded once, where products cancel and where they do not; of up to 64 rows always."""
+    for x, w in (_cancelling(M, N, K, gen(23, M)), operands(M, N, K, gen(24, M))):
+        want, bound = _product(x, w, BF16)
+        for xd, wd in _both(x, w, device):
+            y = sconv.sconv_linear8(xd, wd, exact=True)
+            assert y.dtype == BF16
+            within(y, want, bound, "y")
+            assert torch.equal(y, sconv.sconv_linear8(xd, wd, out_dtype=F32).to(BF16))
+            assert torch.equal(y, sconv.sconv_linear8(xd, wd, exact=torch.ones(1, device=device)))
+            if M <= 64:
+                assert torch.equal(y, sconv.sconv_linear8(xd, wd))
+
+
+@pytest.mark.parametrize("M,N,K", [(65, 1024, 512), (100, 4200, 512), (1024, 1024, 2048), (4096, 4096, 512)])
+def test_linear8_cuts_off_no_more_than_is_said(device, M, N, K):
+    """The matrix pipe's products of normal values against the 64-bit result rounded once, as a whole and in every row and column.  An error d moves a
+    rounding to its neighbour, one step away, with a chance of |d| / step, so the squares of what moves add up to |d| * step each, and a step
+    is at most 2^-7 of a value: d of 1.4e-5 of the norm moves sqrt(2^-7 * 1.4e-5) = 3.4e-4 of it.  A row has at least 1024 values, of which a
+    dozen move: three times as much by chance."""
+    g = gen(25, M, K)
+    x, w = torch.randn(M, K, generator=g), torch.randn(N, K, generator=g)
+    x, w = [(torch.from_numpy(q).view(E4M3), torch.from_numpy(s)) for q, s in (ref.quant8(x), ref.quant8(w, 128))]
+    want = ref.held(*x) @ ref.held(*w, 128).t()
+    for xd, wd in _both(x, w, device):
+        off = sconv.sconv_linear8(xd, wd).cpu().double() - want.to(BF16).double()
+        said = 3.4e-4
+        assert off.norm() <= said * want.norm()
+        assert (off.norm(dim=1) <= 3 * said * want.norm(dim=1)).all()
+        if M >= 1024:
+            assert (off.norm(dim=0) <= 3 * said * want.norm(dim=0)).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(65, 150, 300), (300, 300, 400), (4096, 4096, 256)])
+def test_linear8_by_the_pipe_at_far_scales_and_outliers(device, M, N, K):
+    """Each result within the bound that the format's cut gives: less than 2^-10 of the product of the largest magnitudes of every eight depths, of which
+    those without a leading one (2^-6 of the scale) may count as 2^-6; what is below the smallest normal number may be taken as 0."""
+    g = gen(26, M, K)
+    (xq, xs), (wq, ws) = operands(M, N, K, g)
+    tiny = _small_bytes(wq.shape, g)
+    k = torch.arange(K) // 128
+    cases = [((xq, xs.clone().fill_(a)), (tiny if small else wq, ws.clone().fill_(b))) for a, b, small in (ENDS if M < 4096 else ENDS[:1])]
+    for x, w in cases + [_cancelling(M, N, K, g)]:
+        want, bound = _product(x, w, BF16)
+        tops = [ref._tops_of_eight(ref.held(q, s, rows), 2.0 ** (s.double() - 133.0)[torch.arange(q.shape[0]) // rows][:, k]) for (q, s), rows in ((x, 1), (w, 128))]
+        bound = bound + 2.0 ** -10 * (tops[0] @ tops[1].t()) + (K // 8 + 1) * 2.0 ** -126
+        for xd, wd in _both(x, w, device):
+            within(sconv.sconv_linear8(xd, wd), want, bound, f"scales {int(x[1][0, 0])}, {int(w[1][0, 0])}")
