@@ -5,7 +5,7 @@ import torch
 import paper_1909_09927_amd as sconv
 import serving_ref as ref
 from serving_ref import E, E4M3, U, within
-from test_gpu_serving import gen, operands, spread_rows
+from test_gpu_serving import gen, new_cache, operands, spread_rows
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
@@ -156,3 +156,62 @@ def test_linear8_by_the_pipe_at_far_scales_and_outliers(device, M, N, K):
         bound = bound + 2.0 ** -10 * (tops[0] @ tops[1].t()) + (K // 8 + 1) * 2.0 ** -126
         for xd, wd in _both(x, w, device):
             within(sconv.sconv_linear8(xd, wd), want, bound, f"scales {int(x[1][0, 0])}, {int(w[1][0, 0])}")
+
+
+# ---- attention: weights of 32 bits
+
+def _written(device, k, v, page, kept):
+    """A cache that holds keys [B, n, 2Hkv, D] and values [B, n, Hkv, Dv], and its lengths."""
+    B, n = k.shape[:2]
+    cache = new_cache(device, gen(27, page), B, [-(-n // page)] * B, page, k.shape[2], k.shape[3], v.shape[2], v.shape[3], kept, True)
+    lengths = torch.full((B,), n, dtype=torch.int32, device=device)
+    sconv.sconv_cache_write(cache, k.to(device), v.to(device), torch.zeros_like(lengths))
+    return cache, lengths
+
+
+@pytest.mark.parametrize("H", [4, 24], ids=["few-rows", "rows"])
+@pytest.mark.parametrize("kept", [BF16, E4M3], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("page", [16, 12])
+@pytest.mark.parametrize("D,Dv", [(64, 128), (32, 64), (40, 72)])
+def test_paged_weights_of_two_keys_that_cancel(device, D, Dv, page, kept, H):
+    """Two keys of nearly equal weights whose values are 1 and -1: what is left is 2^-8 and less, and shows what weights are rounded to.
+
+    A weight's argument: the score is one exact product of at most 2^-8, its factor is rounded twice, the difference with the largest once: below E.  Its
+    exponential: 2 E.  The sum of two, their quotient and the products' sums of two: 2 E, 2 E, 4 E, and the two maps' difference 2 E: 12 E of either map."""
+    B, Hkv = 64, 2
+    g = gen(28, D, H)
+    k, v = torch.zeros(B, 2, 2 * Hkv, D), torch.ones(B, 2, Hkv, Dv)
+    k[:, 0, :, 0], k[:, 1, :, 0], v[:, 1] = 1.0, -1.0, -1.0
+    q = torch.zeros(B, 1, 2 * H, D)
+    q[..., 0] = 2.0 ** -8 * (2.0 * torch.rand(B, 1, 2 * H, generator=g) - 1.0)
+    q, lam = q.to(BF16), -torch.rand(H, generator=g)
+    cache, n = _written(device, k.to(BF16), v.to(BF16), page, kept)
+    got = sconv.sconv_diffattn_paged(q.to(device), cache, lam.to(device), n, scale=1.0).cpu().double()
+    left = torch.tanh(q[..., 0].double()).view(B, 1, H, 2)             # (e^s - e^-s) / (e^s + e^-s)
+    l = lam.double()
+    want = (left[..., 0] - l * left[..., 1]).unsqueeze(-1).expand(B, 1, H, Dv)
+    within(got, want, 12 * E * (1.0 + l.abs())[:, None] + 1.01 * U[BF16] * want.abs(), "out")
+
+
+@pytest.mark.parametrize("H", [4, 24], ids=["few-rows", "rows"])
+@pytest.mark.parametrize("page", [16, 12])
+def test_paged_values_of_infinity(device, page, H):
+    """An Inf among the values is its column's answer whatever its weight, 1 and other powers of two among them; other columns do not see it."""
+    B, n, Hkv, D, Dv = 3, 32, 2, 64, 128
+    g = gen(29, H)
+    k, v = torch.zeros(B, n, 2 * Hkv, D), torch.randn(B, n, Hkv, Dv, generator=g)
+    k[1, :, :, 0] = -torch.arange(n)[:, None].float()
+    k[2] = torch.randn(n, 2 * Hkv, D, generator=g)
+    v = v.to(BF16)
+    v[:, 5, 1, 7], v[:, 0, 1, 9], v[:, 20, 0, 100] = float("inf"), float("inf"), -float("inf")
+    q = torch.randn(B, 1, 2 * H, D, generator=g)
+    q[1] = 0.0
+    q[1, :, :, 0] = 1.0
+    cache, lengths = _written(device, k.to(BF16), v, page, BF16)
+    lam = torch.full((H,), -0.5, device=device)
+    got = sconv.sconv_diffattn_paged(q.to(BF16).to(device), cache, lam, lengths, scale=0.6931471805599453).cpu()
+    G = H // Hkv
+    assert (got[:, 0, G:, 7] == float("inf")).all() and (got[:, 0, G:, 9] == float("inf")).all() and (got[:, 0, :G, 100] == -float("inf")).all()
+    keep = torch.ones(H, Dv, dtype=torch.bool)
+    keep[G:, 7] = keep[G:, 9] = keep[:G, 100] = False
+    assert torch.isfinite(got[:, 0][:, keep]).all()
