@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+from operator import index
 from typing import NamedTuple, Optional
 
 import torch
@@ -302,6 +303,7 @@ def _rmsnorm_grad_plan(dy, total, rstd, weight, dtotal, x_dtype):
 def sconv_quant8(x, block_rows: int = 1, out=None):
     """Rows [..., K] into 8 bits: (values, scales), a scale for every 128 of a row ([..., ceil(K / 128)]), or with block_rows 128 for
     128 x 128 of weights [N, K] ([ceil(N / 128), ceil(K / 128)]).  out: a pair (optional)."""
+    block_rows = index(block_rows)
     key = (12, _sig(x), block_rows)
     plan = _plans.get(key)
     if plan is None:
@@ -452,6 +454,7 @@ def sconv_cache_read(cache: PagedCache, S: int, starts, counts=None, out_dtype=N
     """Positions starts[b] + i, i < counts[b] (S by default), of every request out of its pages: (k [B, S, key heads, D], v [B, S, value
     heads, Dv]), contiguous; rows that are not there are zeros.  out_dtype: the cache's type; of an 8-bit cache bf16 (default, exact) or fp32."""
     k, v = cache.k, cache.v
+    S = index(S)
     if out is None:
         key = (16, _cache_sig(cache), S, _sig(starts), _sig(counts), out_dtype)
         plan = _plans.get(key)

@@ -215,3 +215,26 @@ def test_paged_values_of_infinity(device, page, H):
     keep = torch.ones(H, Dv, dtype=torch.bool)
     keep[G:, 7] = keep[G:, 9] = keep[:G, 100] = False
     assert torch.isfinite(got[:, 0][:, keep]).all()
+
+
+# ---- numbers given as tensors: every call takes what they hold then
+
+@pytest.mark.parametrize("where", ["cpu", "cuda"])
+def test_whole_numbers_in_tensors_are_read_at_every_call(device, where):
+    cache = sconv.sconv_cache_new(2, 4, 8, 16, 2, 8, 1, 8, dtype=F32, device=device)
+    cache.table.copy_(torch.arange(8, dtype=torch.int32).view(2, 4))
+    k, v = torch.randn(2, 40, 2, 8, generator=gen(30)).to(device), torch.randn(2, 40, 1, 8, generator=gen(31)).to(device)
+    starts = torch.zeros(2, dtype=torch.int32, device=device)
+    sconv.sconv_cache_write(cache, k, v, starts)
+    x = torch.randn(130, 200, generator=gen(32)).to(device)
+    S, rows = torch.tensor(3, device=where), torch.tensor(1, device=where)
+    for n, block in ((3, 1), (40, 128), (1, 1), (40, 128)):
+        S.fill_(n)
+        rows.fill_(block)
+        rk, rv = sconv.sconv_cache_read(cache, S, starts)
+        assert torch.equal(rk, k[:, :n]) and torch.equal(rv, v[:, :n])
+        for got, want in zip(sconv.sconv_quant8(x, rows), sconv.sconv_quant8(x, block)):
+            assert torch.equal(got.view(torch.uint8), want.view(torch.uint8))
+    for bad in (2.0, "3", None):
+        with pytest.raises(TypeError):
+            sconv.sconv_cache_read(cache, bad, starts)
