@@ -50,7 +50,7 @@ int sconv_rmsnorm_forward(const sconv_rmsnorm_desc_t* desc, const void* x_dev, c
  * Its gradient.  With u = t * rstd and g = dy * w:
  *   d = dt + rstd * (g - u * mean_c(g * u)),  dw[c] = sum over rows of dy * u;
  * d is the gradient of x and of residual alike, dt (optional) the one that reaches the sum along the stream.
- *   dy_dev   device, in, of y_type (SCONV_F32 or SCONV_BF16; the rounding to 8 bits has no gradient of its own)
+ *   dy_dev   device, in, of y_type (x_type or SCONV_BF16; the rounding to 8 bits has no gradient of its own)
  *   total_dev, dt_dev  device, in, of t_type: the sum as it was stored (without residual: x)
  *   dx_dev, dres_dev   device, out, contiguous, optional: d in x_type and in t_type
  *   dw_dev   device, out, [C] of w_type, optional

@@ -243,9 +243,9 @@ def _rmsnorm_plan(x, weight, residual, total, eps, out_dtype):
 def sconv_rmsnorm_backward(dy, total, rstd, weight=None, dtotal=None, x_dtype=None, param_grads: bool = True, ws=None):
     """Gradient of sconv_rmsnorm_forward: (dx, dresidual, dweight).
 
-    dy: bf16 or fp32, of total's shape; total: the sum that the forward call returned (without a residual: x); dtotal: the gradient that
-    reaches the sum along the stream, in total's type (optional).  x and residual have one gradient, in total's type; x_dtype: x's
-    type where it is bf16 under an fp32 stream (dx is then its rounding).  dweight: weight's type (fp32 without one; None
+    dy: of total's shape, in y's type as the forward call gives it: bf16, or fp32 where x is fp32; total: the sum that the forward call
+    returned (without a residual: x); dtotal: the gradient that reaches the sum along the stream, in total's type (optional).  x and residual have
+    one gradient, in total's type; x_dtype: x's type where it is bf16 under an fp32 stream (dx is then its rounding, dy is bf16).  dweight: weight's type (fp32 without one; None
     with param_grads False).  ws: a device tensor as scratch (optional)."""
     key = (11, _sig(dy), _sig(total), _sig(rstd), _sig(weight), _sig(dtotal), x_dtype)
     plan = _plans.get(key)

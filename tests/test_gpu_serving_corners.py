@@ -238,3 +238,21 @@ def test_whole_numbers_in_tensors_are_read_at_every_call(device, where):
     for bad in (2.0, "3", None):
         with pytest.raises(TypeError):
             sconv.sconv_cache_read(cache, bad, starts)
+
+
+# ---- refusals
+
+def test_rmsnorm_backward_takes_what_the_forward_call_gives(device):
+    """dy of y's types: bf16 anywhere, fp32 where x is fp32."""
+    t = torch.randn(3, 40, generator=gen(33)).to(device)
+    rstd = torch.ones(3, device=device)
+    for total, dy, x_dtype, goes in ((F32, F32, None, True), (F32, F32, F32, True), (F32, BF16, None, True), (F32, BF16, BF16, True), (BF16, BF16, None, True), (BF16, BF16, BF16, True),
+                                     (F32, F32, BF16, False), (BF16, F32, None, False), (BF16, F32, BF16, False), (BF16, BF16, F32, False)):
+        def call():
+            return sconv.sconv_rmsnorm_backward(t.to(dy), t.to(total), rstd, x_dtype=x_dtype)
+
+        if goes:
+            assert call()[0].dtype == (total if x_dtype is None else x_dtype)
+        else:
+            with pytest.raises(sconv.SconvError):
+                call()
