@@ -129,6 +129,8 @@ def _ws(ws, need, device):
         ws = torch.empty(need, dtype=torch.uint8, device=device)
     elif not (isinstance(ws, torch.Tensor) and ws.is_cuda and ws.is_contiguous()):
         raise TypeError("ws must be a contiguous tensor in device memory")
+    elif ws.device != device:
+        raise ValueError("ws is on another device")
     return ws, (ws.data_ptr() if ws.numel() else None), ws.numel() * ws.element_size()
 
 

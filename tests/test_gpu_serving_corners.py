@@ -256,3 +256,12 @@ def test_rmsnorm_backward_takes_what_the_forward_call_gives(device):
         else:
             with pytest.raises(sconv.SconvError):
                 call()
+
+
+def test_scratch_on_another_device_is_refused(device):
+    """(asked as the calls ask: of scratch on this device for tensors that are on the next)"""
+    from paper_1909_09927_amd.tokens import _ws
+    ws = torch.empty(64, dtype=torch.uint8, device=device)
+    assert _ws(ws, 16, ws.device)[2] == 64
+    with pytest.raises(ValueError):
+        _ws(ws, 16, torch.device("cuda", ws.device.index + 1))
