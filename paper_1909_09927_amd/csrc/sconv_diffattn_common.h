@@ -143,8 +143,6 @@ __device__ __forceinline__ int few_col_lane()
     const int l = threadIdx.x & 63;
     return (4 * (l >> 4) + ((l & 15) >> 2)) * LD + (l & 3) * 4;
 }
-// Between a wavefront's own writes and reads of LDS: they are carried out in order; the compiler is told to leave them so.
-__device__ __forceinline__ void wave_lds_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
 
 // Registers 8s..8s+7 of a result as the next product's B.
 __device__ __forceinline__ void to_frag(const float (&v)[8], bf16x8& f)

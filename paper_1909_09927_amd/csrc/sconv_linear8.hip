@@ -24,16 +24,12 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 struct LinArgs {
     const uint8_t* x; const uint8_t* xs; const uint8_t* w; const uint8_t* ws; void* y;
     int M, N, K, KB, vec;
     int64_t x_m, w_n, y_m;
 };
-
-// Between a wavefront's own writes and reads of LDS: they are carried out in order; the compiler is told to leave them so.
-__device__ __forceinline__ void wave_lds_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
 
 // 16 bytes of a row of which `have` are there, from any address.
 __device__ __forceinline__ i32x4 bytes16(const uint8_t* p, int have)
@@ -45,14 +41,6 @@ __device__ __forceinline__ i32x4 bytes16(const uint8_t* p, int have)
 #pragma unroll
     for (int i = 0; i < 16; ++i) if (i < have) r.u[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
     return r.v;
-}
-
-// Eight bytes as 16-bit values.
-__device__ __forceinline__ bf16x8 widened(int lo, int hi, float scale = 1.0f)
-{
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
 template <typename T>
@@ -168,7 +156,7 @@ struct RingShape {
 
 // vmcnt(n) lgkmcnt(0): all loads but the n youngest have come, and all reads of LDS
 template <int n>
-__device__ __forceinline__ void loads_left()
+__device__ __forceinline__ void loads_and_reads()
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     __builtin_amdgcn_s_waitcnt(0x0070 | (n & 15) | (n >> 4) << 14);
@@ -365,7 +353,7 @@ __device__ __forceinline__ bool ring_tile(const LinArgs& a, uint8_t* lds, int m0
     const auto arrived = [&]() {
         step();
         if constexpr (DIRECT) {
-            loads_left<2 * N>();
+            loads_and_reads<2 * N>();
             bare_barrier();
         } else {
             __syncthreads();
@@ -415,7 +403,7 @@ __device__ __forceinline__ bool ring_tile(const LinArgs& a, uint8_t* lds, int m0
     for (int kb0 = 0; kb0 < a.KB; kb0 += Shape::CHUNK) {
         if (kb0) __syncthreads();
         stretch(kb0);
-        if constexpr (DIRECT) loads_left<2 * N>();       // (of the first stage, at the start)
+        if constexpr (DIRECT) loads_and_reads<2 * N>();       // (of the first stage, at the start)
         __syncthreads();
         if constexpr (SCALES == NEAR) {
             if (met()) {
@@ -445,7 +433,7 @@ __device__ __forceinline__ bool ring_tile(const LinArgs& a, uint8_t* lds, int m0
     }
     // (stages behind the last have been asked for: none outlives its workgroup's LDS, or meets the results in it)
     step();
-    if constexpr (DIRECT) loads_left<0>();
+    if constexpr (DIRECT) loads_and_reads<0>();
     __syncthreads();
     step();
     if constexpr (SCALES == NEAR || SCALES == ZEROS) {

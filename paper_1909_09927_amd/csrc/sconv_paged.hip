@@ -19,7 +19,6 @@ namespace sconv {
 namespace {
 
 constexpr int BN = 32;                   // keys of a unit
-constexpr int LEAST = 1;                 // units of a stretch at least
 constexpr int PLACES = 1024;             // wavefronts: one to a SIMD.  (Two: 64 requests of up to 784 35 -> 38 us, 16 of up to 32768 68 -> 71.)
 constexpr int MAX_PARTS = PLACES;
 
@@ -63,7 +62,7 @@ __device__ __forceinline__ int units_before(const PagedArgs& a, int upto)
     return __builtin_amdgcn_readfirstlane(v);
 }
 // Units of a stretch.
-__device__ __forceinline__ int stretch_of(const PagedArgs& a, int units) { return max((units + a.parts - 1) / a.parts, LEAST); }
+__device__ __forceinline__ int stretch_of(const PagedArgs& a, int units) { return max((units + a.parts - 1) / a.parts, 1); }
 // Of stretch `at`: its first unit, counted from request b's first, and its end, likewise, and b's positions; false: it has none.
 __device__ __forceinline__ bool find_stretch(const PagedArgs& a, int at, int& b, int& begin, int& end, int& n)
 {
@@ -144,14 +143,6 @@ __device__ __forceinline__ u32x4 load16_any(const T* row, int d, int have)
     typedef u32x4 any __attribute__((aligned(2)));
     if constexpr (FULL) return *(const any*)(row + d);
     return load16<false>(row, d, have);
-}
-
-__device__ __forceinline__ bf16x8 widened(uint32_t lo, uint32_t hi, float scale)
-{
-    typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
 // A key's row of one map as it lies in memory: the fragments of KS steps of 32.  In 8 bits a lane reads 16 bytes at once, which are eight
@@ -914,7 +905,7 @@ PagedPlan paged_plan(const sconv_paged_desc_t& d, const sconv_pages_dev_t* at, s
     const int64_t places = DT == 128 && g.type == SCONV_BF16 ? PLACES * 3 / 4 : PLACES;
     const int64_t wide = (g.Dv + 3) / 4 * 4, each = (int64_t)d.Hkv * 2 * rows * (2 * wide + 4) * (int64_t)sizeof(float);
     int64_t parts = std::max<int64_t>(std::min<int64_t>(places / base, (int64_t(64) << 20) / each), 1);
-    parts = std::min<int64_t>(std::min<int64_t>(parts, (units + LEAST - 1) / LEAST), MAX_PARTS);
+    parts = std::min<int64_t>(std::min<int64_t>(parts, units), MAX_PARTS);
     // (one stretch: every request is a wavefront's, as without scratch)
     if (parts == 1 || (size_t)(parts * each) > ws_bytes) return p;
     p.parts = (int)parts;

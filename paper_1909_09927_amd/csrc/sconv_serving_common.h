@@ -137,6 +137,15 @@ __device__ __forceinline__ void from_e4m3(u32x2 q, float scale, float* v)
     }
 }
 
+// Eight values in 8 bits as 16-bit ones, which hold them exactly, times a power of two.
+__device__ __forceinline__ bf16x8 widened(uint32_t lo, uint32_t hi, float scale = 1.0f)
+{
+    typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
 // Division of 0 .. 2^31 - 1 by a number of the same range by multiplication: m = ceil(2^(31 + l) / d) with 2^(l - 1) < d <= 2^l passes
 // 2^(31 + l) / d by less than 2^l / d, so n * m / 2^(31 + l) stays below the next whole number.
 struct Divide { uint32_t d, m; int l; };

@@ -123,6 +123,9 @@ inline bool grid_fits(int64_t blocks, int threads) { return blocks * threads < (
 
 inline bool aligned_to(const void* p, int bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
+// Between a wavefront's own writes and reads of LDS: they are carried out in order; the compiler is told to leave them so.
+__device__ __forceinline__ void wave_lds_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
+
 int launch_layernorm_forward(const sconv_layernorm_desc_t& d, const void* x, const void* w, const void* b, void* y,
                              float* mean, float* rstd, hipStream_t stream);
 size_t layernorm_workspace(const sconv_layernorm_desc_t& d);
