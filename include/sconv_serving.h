@@ -28,7 +28,8 @@ enum { SCONV_E4M3 = 2, SCONV_SCALE_BLOCK = 128 };
 /*
  * Root-mean-square norm of rows of C channels, a residual stream's addition in front of it:
  *   t = x + residual (or x);  rstd = 1 / sqrt(sum_c t^2 / C + eps);  y = t * rstd * w[c].
- * The sum is formed in 32 bits; y comes from it as it is, and it is rounded to the stream's type where it is stored.
+ * The sum is formed in 32 bits; y comes from it as it is, and it is rounded to the stream's type where it is stored.  Its squares are added in 32
+ * bits: rows have to lie below 2^63 / sqrt(C), and above 2^-63 where eps is 0.
  */
 typedef struct {
     int32_t rows, C;           /* rows >= 0; 1 <= C <= 16384                                                      */
@@ -132,8 +133,9 @@ int sconv_cache_read(const sconv_cache_desc_t* desc, const sconv_pages_dev_t* pa
  * 2g + 1) and Hv = Hkv values a slot.  Request b has lengths[b] positions (taken as 0 below 0, and as table_width * page_size above); causal:
  * the last query stands at the last of them.  A query that sees nothing gives zeros.  Keys and values behind the length, or on
  * pages that are not there, are never part of a sum; one that causal alone hides has to be finite.  Inf, and NaN as 8-bit values hold it, go
- * through the formulas.  The keys of all requests are shared out among wavefronts by their number, whose parts a second kernel joins; in short
- * caches every request is one wavefront's.
+ * through the formulas.  Products of values and weights (of up to 2^8) are added in 32 bits before the division by the weights' sum.  The keys of
+ * all requests are shared out among wavefronts by their number, whose parts a second kernel joins; in short caches every request is one
+ * wavefront's.
  * For single tokens and a few (a prompt's own attention is sconv_diffattn_forward's: 16 (query, head) rows of a key head are
  * the most that one read of the cache serves).
  */

@@ -4,8 +4,8 @@
 // with eight elements each, whose largest value comes by rotation; a group finds its token's slot by itself: one division by the page size, by
 // multiplication, and one read of the table.  A workgroup has a stretch of tokens of a head, then of the next: a page's lines, of which a slot
 // of a head is half a line or less, and a slot's scale a byte, are written from one place, whichever of heads and slots lie beside each other.
-// (Heads side by side, tokens apart: 8 x 3136 tokens of 8 key heads of 64 and 4 value heads of 128, 16 to 8 bits, 28.3 us written, 23.1 read; this
-// way 20.3 and 16.9, 3.8 and 4.6 TB/s.)
+// (Medians of 8 x 3136 tokens of 8 key heads of 64 and 4 value heads of 128, 16 to 8 bits: 21.8 us written, 21.4 read, 3.5 and 3.6 TB/s; of up to
+// 3136, ragged, 14.9 and 14.9.  Heads side by side, tokens apart, the same 8 x 3136 took two fifths longer.)
 #include <algorithm>
 
 #include "sconv_serving_common.h"

@@ -3,10 +3,12 @@
 // Few rows (up to 64, single tokens): bound by the weights' read, and by what every workgroup reads of the tokens.  A workgroup takes 16 or 32 weight
 // rows, its eight wavefronts share out the blocks of 128, read operands from memory straight into the product's registers and meet in LDS.
 // Many rows: tiles through LDS, bound by the matrix pipe, or by the results' write where the depth is small.
-// Measured, 16-bit results: 16 x 2048 to 8192 6.7 us (2.6 TB/s), 64 x 8192 to 8192 36; 12544 x 2048 to 8192 210 (2004 TFLOP/s),
-// 4096 x 8192 to 8192 222 (2481), 25088 x 512 to 2048 48 (1087), 6272 x 896 to 1000 15.  A tile of 256 x 256 costs 4.3 us beside its depth, 13 us for 1000.
+// Measured, 16-bit results, medians: 16 x 2048 to 8192 6.5 us (2.6 TB/s), 64 x 8192 to 8192 36; 12544 x 2048 to 8192 209 (2014 TFLOP/s; 201 cold, 221 to
+// 278 where call follows call for milliseconds and the clock falls), 4096 x 8192 to 8192 220 (2495), 25088 x 512 to 2048 47 (1115), 6272 x 896 to 1000 14.9.
+// A tile of 256 x 256 costs 4.3 us beside its depth, 13 us for 1000.  Depths of no whole 16 go through registers, in tiles of 128 x 128: 4096 x 1000 to
+// 4096 53 us, x 1008 26; 4096 x 8200 to 8192 450.
 // Up to 64 rows, in 32-bit results and with `exact` the 8-bit values become 16-bit ones, exactly, and products are exact to 32 bits.  Other 16-bit
-// results take 8-bit products with the scales as operands, at nearly twice the rate (12544 x 2048 to 8192 207 to 217 us, with `exact` 353;
+// results take 8-bit products with the scales as operands, at nearly twice the rate (12544 x 2048 to 8192 209 us, with `exact` 341;
 // 784 x 2048 to 2048 12.3 and 19.1).  The matrix pipe takes eight products at a time and cuts off what lies 2^-13 or more below the largest of
 // them: of normal values 1.4e-5 of a result's norm at any depth, which rounding to 16 bits (1.7e-3) hides; where the largest products cancel it
 // shows (two channels of 1000 times the rest with opposite signs, depth 256: 1.1e-2), so it is the caller's choice.

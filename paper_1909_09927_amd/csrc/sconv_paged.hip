@@ -190,7 +190,7 @@ __device__ __forceinline__ typename Frag<typename Kept<P>::type>::type key_frag(
 
 // A row's weights for their product with the values: three 16-bit values that make up the weight's 32 bits.  16-bit values of the cache meet them as they
 // are, an Inf among them, too, so each is positive where the weight is: the largest 16-bit value below the weight, the largest below what is left, and what is
-// left then, which 16 bits hold.  (Two would leave 2^-16 of a weight out: where two keys cancel to 2^-8 that is 1 % of the answer.  16 requests of up to
+// left then, which 16 bits hold.  (Two would leave 2^-16 of a weight out: where two keys cancel to 2^-11 that is 1 % of the answer.  16 requests of up to
 // 32768, 8 bits 70.8 us with two, 70.1 with three; 64 of up to 784, 16 bits 34.7 and 35.0; 2048 short ones with 8 heads 91 and 97.)
 template <typename T> struct Weights;
 template <> struct Weights<bf16> {

@@ -1,8 +1,9 @@
 // Rows into 8 bits with block scales (format in sconv_serving.h).
 //
 // Bound by memory: x is read once, a byte a value and a byte a block are written.  A block of 128 of a row is 16 lanes with eight values
-// each; a block of 128 x 128 is a workgroup, which holds it in registers between its largest value and its bytes.  6272 x 896 of 16 bits: 5.6 us
-// (3.0 TB/s), 2.5 of it the launch.
+// each; a block of 128 x 128 is a workgroup, which holds it in registers between its largest value and its bytes.  Medians, 16 bits: rows 6272 x 896
+// 5.2 us (3.2 TB/s; 2.5 of it the launch), 7.3 behind another kernel's work, 25088 x 2048 30 (5.1 TB/s); blocks 2048 x 2048 6.9 us, 8192 x 2048 11.8
+// (4.3 TB/s), 8192 x 8192 41 (4.9).
 #include <algorithm>
 
 #include "sconv_serving_common.h"

@@ -5,8 +5,8 @@
 // each, from any address.  A block of 128 channels that shares a scale is 16 neighbouring lanes, whose largest value comes
 // by rotation.  The weight's gradient sums over all rows: a workgroup walks many rows, keeps its sums in registers and writes one row of partial
 // sums, which a second kernel adds in a fixed order.
-// Measured, 16 bits: forward 25088 x 512 with a residual 16.9 us (6.1 TB/s, in part from the caches); 64 x 2048 3.3 us, one latency chain.
-// Gradient 25088 x 512 20.7 + 3.8 us (4.2 TB/s both), 25088 x 1024 38.0 (5.4 TB/s), 1568 x 16384 64 (3.2 TB/s: one row a workgroup, nothing ahead).
+// Measured, 16 bits, medians: forward 25088 x 512 with a residual 17.4 us (5.9 TB/s, in part from the caches); 64 x 2048 3.3 us, one latency chain.
+// Gradient 25088 x 512 21.4 + 3.8 us (4.1 TB/s both), 25088 x 1024 39.9 (5.2 TB/s), 1568 x 16384 60 (3.4 TB/s: one row a workgroup, nothing ahead).
 #include <algorithm>
 
 #include "sconv_serving_common.h"
