@@ -16,7 +16,6 @@
 // Layout of the products: weights are A, tokens are B, so that a lane's results are neighbours of one token's row.  Which depths of a block a
 // lane holds does not matter, as long as both operands have the same.
 #include <algorithm>
-#include <type_traits>
 
 #include "sconv_serving_common.h"
 
@@ -547,7 +546,7 @@ template <typename T, bool FAST>
 int linear_run(const LinArgs& a, hipStream_t stream)
 {
     // Two weight tiles a workgroup share what it reads of the tokens, where one fills the chip twice (16 tokens, 2048 to 8192: 7.7 -> 6.4 us, 64 tokens
-    // 15.3 -> 9.8); with fewer rows they leave compute units idle (2048 to 2048, 16 tokens: 5.0 -> 5.9).  Tiles through LDS take over where
+    // by 8-bit products 15.3 -> 9.8); with fewer rows they leave compute units idle (2048 to 2048, 16 tokens: 5.0 -> 5.9).  Tiles through LDS take over where
     // they are ahead by and large (8-bit products: at 64 tokens 2048 to 8192 11.7 us against 9.8, 1024 to 16384 9.0 against 11.6, 8192 to 8192 47 against 34).
     const bool two = a.N >= 4096;
     if (a.M <= 16) return two ? few_launch<T, 1, 2, 8>(a, stream) : few_launch<T, 1, 1, 8>(a, stream);
